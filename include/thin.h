@@ -383,6 +383,165 @@ int thin_express_prefill(int32_t dtype, int64_t B, int64_t H, int64_t n, int64_t
                          void* stream);
 
 /*
+ * Rotary positions: every row of X (and of Y in the same launch, nullable) is
+ * turned by its position.  A pair of channels (x_i, x_j), j = i + rot/2 or
+ * (2i, 2i+1), turns by the angle a = 2 pi pos turns[i]:
+ *   x_i' = amp (x_i cos a - x_j sin a),   x_j' = amp (x_j cos a + x_i sin a).
+ * The channels from rot on are copied.  inverse turns by -a (same amp): applied
+ * to a gradient, the gradient of the turn.
+ *   X, Y      (device) [B, heads, T, d] of `dtype`; X_out, Y_out likewise.  An
+ *             output may be its input itself (same pointer and strides), else
+ *             outputs overlap nothing.
+ *   *_strides (host, nullable) three element strides (batch, head, row); NULL =
+ *             contiguous.  Channels are contiguous; pointers and the strides of
+ *             dimensions longer than one are multiples of 16 bytes; an output's
+ *             are not 0.
+ *   rot       multiple of 16, 16 <= rot <= d (d in {32, 64, 128}).
+ *   layout    THIN_ROTARY_HALF or THIN_ROTARY_INTERLEAVED.
+ *   pos       (device) int32: the rows' positions [B, T] (pos_per_token != 0),
+ *             or [B], the first row's, the others following it.
+ *   turns     (device) float64 [rot/2]: turns per position of every pair.
+ *   amp       finite.
+ * Angles are formed in float64 and reduced to one turn before cos and sin; rows
+ * are turned in float32 and rounded once.  B * T <= 2^27.
+ * Errors: THIN_EINVAL, THIN_EDTYPE, THIN_EHIP.
+ */
+typedef enum { THIN_ROTARY_HALF = 0, THIN_ROTARY_INTERLEAVED = 1 } thin_rotary_layout_t;
+int thin_rotary(const void* X, const int64_t* x_strides, int64_t x_heads, void* X_out,
+                const int64_t* x_out_strides, const void* Y, const int64_t* y_strides,
+                int64_t y_heads, void* Y_out, const int64_t* y_out_strides, int32_t dtype,
+                int64_t B, int64_t T, int64_t d, int64_t rot, int32_t layout, const int32_t* pos,
+                int32_t pos_per_token, const double* turns, double amp, int32_t inverse,
+                void* stream);
+
+/*
+ * The table of thin_rotary: turns[i] = base^(-2i/rot) / (2 pi), i < rot/2, for
+ * contexts `factor` times as long as `length` positions by one of these rules,
+ *   THIN_ROTARY_PLAIN   no change (factor and length are ignored),
+ *   THIN_ROTARY_LINEAR  every frequency divided by factor,
+ *   THIN_ROTARY_BASE    base * factor^(rot / (rot - 2)) for base: the slowest
+ *                       pair's frequency divided by factor, the fastest kept,
+ *   THIN_ROTARY_BANDS   pairs that turn at least `fast` times in `length`
+ *                       positions keep their frequency, those that turn at most
+ *                       `slow` times have it divided by factor, a linear mix
+ *                       between; *amp = 0.1 ln(factor) + 1 (else 1).
+ * Host-only.  turns (host) float64 [rot/2], amp (host).  THIN_EINVAL: null
+ * pointers, rot not an even number >= 2 (>= 4 for BASE), base <= 1, factor < 1,
+ * and for BANDS length <= 0 or slow >= fast.
+ */
+typedef enum {
+  THIN_ROTARY_PLAIN = 0,
+  THIN_ROTARY_LINEAR = 1,
+  THIN_ROTARY_BASE = 2,
+  THIN_ROTARY_BANDS = 3
+} thin_rotary_scaling_t;
+int thin_rotary_turns(int64_t rot, double base, int32_t scaling, double factor, double length,
+                      double slow, double fast, double* turns, double* amp);
+
+/*
+ * A key/value cache held in 4 bits (the caller's device buffers; this struct is
+ * host memory, read during a call only).  A row's d channels are d/32 groups of
+ * 32; a group is 32 codes of 4 bits (channel 2i in the low half of byte i: sign,
+ * two exponent bits, one mantissa bit, i.e. +-{0, .5, 1, 1.5, 2, 3, 4, 6}) and one
+ * scale byte s that stands for 2^(s-127).  Rows of keys and values are stored
+ * after any rotary turn.
+ *   bounds  the least, then the largest stored key value of every channel over
+ *           each block of THIN_Q4_BLOCK rows (the rows stored so far).
+ * B * H <= 65535, 1 <= n_max <= THIN_Q4_MAX_ROWS, d in {32, 64, 128}; all five
+ * buffers 16-byte aligned.
+ */
+#define THIN_Q4_BLOCK 64
+#define THIN_Q4_MAX_ROWS ((int64_t)1 << 21)
+typedef struct {
+  void* k_codes;  /* uint8 [B, H, n_max, d/2]                   */
+  void* k_scales; /* uint8 [B, H, n_max, d/32]                  */
+  void* v_codes;  /* uint8 [B, H, n_max, d/2]                   */
+  void* v_scales; /* uint8 [B, H, n_max, d/32]                  */
+  void* bounds;   /* bf16  [B, H, ceil(n_max/64), 2, d]         */
+  int64_t B, H, n_max, d;
+} thin_q4_cache_t;
+
+/*
+ * The tokens of a call (thin_q4_store, _select, _attention): T per batch entry,
+ * token t of entry b at position at[b] + t.
+ *   at      (device) int32 [B].
+ *   count   (device, nullable) int32 [B]: tokens t >= count[b] are padding; NULL =
+ *           none is.
+ * Padding and positions outside [0, n_max) are legal: such a token is not stored,
+ * selects nothing and has an output row of zeros (a position past the cache sees
+ * the whole cache).  T <= 2^20.  Strides as in thin_rotary.
+ */
+
+/*
+ * Encode key and value rows K, V (device) [B, H, T, d] of `dtype` into the rows
+ * at[b] + t of the cache.  A group whose largest magnitude is amax gets e = the
+ * least integer in [-125, 125] with amax <= 7 * 2^e (s = e + 127) and the codes of
+ * x / 2^e rounded to nearest, ties to the even code, saturating at 6; NaN is
+ * stored as 0.  The bounds of every block that holds a new row are formed anew
+ * over the block's rows up to the last new one (rows before at[b] must have been
+ * stored; what the block holds behind the new rows no longer counts).  Other rows
+ * and bounds keep their contents.
+ * Errors: THIN_EINVAL, THIN_EDTYPE, THIN_EHIP.
+ */
+int thin_q4_store(const thin_q4_cache_t* cache, const void* K, const int64_t* k_strides,
+                  const void* V, const int64_t* v_strides, int32_t dtype, int64_t T,
+                  const int32_t* at, const int32_t* count, void* stream);
+
+/*
+ * The values that cached rows at[b] .. at[b] + T - 1 stand for (exact in either
+ * type): K, V (device) contiguous [B, H, T, d] of `dtype`, 16-byte aligned.  Rows
+ * outside the cache give zeros.  Errors: THIN_EINVAL, THIN_EDTYPE, THIN_EHIP.
+ */
+int thin_q4_load(const thin_q4_cache_t* cache, int64_t T, const int32_t* at, void* K, void* V,
+                 int32_t dtype, void* stream);
+
+/*
+ * The blocks of cached rows that every token attends to.  Query heads g of key
+ * head h are h * (q_heads / H) + g; the score of block k for a token and key head is
+ *   sum_g sum_c max(q_gc lo_kc, q_gc hi_kc),
+ * the most that <q_g, key> can be over the block's bounds, summed over the group,
+ * in float64.  Of the blocks up to the token's own, the first n_sinks, the last
+ * n_window and those of the largest scores are taken, n_sel in all (ties: the
+ * lowest; a NaN score is the smallest), or every one if they are at most n_sel.
+ *   Q       (device) [B, q_heads, T, d] of `dtype`, q_heads a multiple of H.
+ *   blocks  (device) int32 [B, H, T, n_sel]: ascending, -1 behind the last one.
+ *   n_sinks >= 0, n_window >= 1, n_sinks + n_window <= n_sel <= 32768.
+ *   workspace (device) at least *workspace_bytes of thin_q4_select_plan, 16-byte
+ *           aligned; contents on entry are irrelevant.  Calls that may run at the
+ *           same time need workspaces of their own.
+ * Errors: THIN_EINVAL, THIN_EDTYPE, THIN_EWORKSPACE, THIN_EHIP.
+ */
+int thin_q4_select_plan(int64_t B, int64_t H, int64_t n_max, int64_t T, size_t* workspace_bytes);
+int thin_q4_select(const thin_q4_cache_t* cache, const void* Q, const int64_t* q_strides,
+                   int64_t q_heads, int32_t dtype, int64_t T, const int32_t* at,
+                   const int32_t* count, int64_t n_sel, int64_t n_sinks, int64_t n_window,
+                   int32_t* blocks, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Causal attention over the cache: token t of entry b attends to the cached rows
+ * 0 .. at[b] + t (its own row stored before the call), or to those of them in its
+ * listed blocks,
+ *   O = sum_j exp(<q, k_j> / sqrt(d)) v_j / sum_j exp(<q, k_j> / sqrt(d)),
+ * k_j and v_j the values that the cache stands for.
+ *   Q, O    (device) [B, q_heads, T, d] of `dtype` (O's strides as an output's in
+ *           thin_rotary; O overlaps no input), heads grouped as in thin_q4_select.
+ *   blocks  (device, nullable) int32 [B, H, T, n_sel] in any order; entries that
+ *           are no block of the cache, or lie behind the token, count for nothing,
+ *           a block listed twice counts twice.  NULL with n_sel = 0: every row.
+ * A row that sees nothing is zeros.  float32 queries: products and weights to
+ * float32 accuracy; bf16: weights rounded to bf16, sums in float32.
+ *   workspace as for thin_q4_select (may be NULL where the plan asks for 0 bytes).
+ * Errors: THIN_EINVAL, THIN_EDTYPE, THIN_EWORKSPACE, THIN_EHIP.
+ */
+int thin_q4_attention_plan(int64_t B, int64_t H, int64_t q_heads, int64_t n_max, int64_t d,
+                           int64_t T, int64_t n_sel, size_t* workspace_bytes);
+int thin_q4_attention(const thin_q4_cache_t* cache, const void* Q, const int64_t* q_strides,
+                      int64_t q_heads, int32_t dtype, int64_t T, const int32_t* at,
+                      const int32_t* count, const int32_t* blocks, int64_t n_sel, void* O,
+                      const int64_t* o_strides, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/*
  * Diagnostic: out[m*16 + n] = <rows[m], rows[16 + n]> for m, n < 16, computed
  * through the MFMA row-fragment path the pair-score kernel uses.
  *   rows (device) [32, d] of `dtype`;  out (device) float32 [16, 16].
@@ -406,8 +565,8 @@ int thin_workspace_status(const void* workspace, int32_t* status, void* stream);
  * of the compute contract; the library keeps no state between calls apart
  * from it).  While a hook is set,
  * every kernel launch made by thin_compress, thin_compress_traced,
- * thin_compress_ex, thin_attention, thin_attention_ex and thin_express_step
- * is bracketed by two calls on the
+ * thin_compress_ex, thin_attention, thin_attention_ex, thin_express_step,
+ * thin_rotary and the thin_q4_* calls is bracketed by two calls on the
  * calling thread:
  * hook(ctx, kernel, round, 0, stream) right before the launch is enqueued and
  * hook(ctx, kernel, round, 1, stream) right after.  The hook may enqueue
@@ -436,7 +595,12 @@ typedef enum {
   THIN_KERNEL_UNIFORM = 8,     /* uniform halving (all rounds, or one)    */
   THIN_KERNEL_ASSEMBLE = 9,    /* sinks + coreset + window, log-weights   */
   THIN_KERNEL_EXPRESS = 10,    /* Express cache moves, per-call v_max, keys */
-  THIN_KERNEL_STATUS = 11      /* clearing of the device status word      */
+  THIN_KERNEL_STATUS = 11,     /* clearing of the device status word      */
+  THIN_KERNEL_ROTARY = 12,     /* rotary positions                        */
+  THIN_KERNEL_Q4_STORE = 13,   /* rows into the 4-bit cache               */
+  THIN_KERNEL_Q4_LOAD = 14,    /* rows of the 4-bit cache                 */
+  THIN_KERNEL_Q4_SELECT = 15,  /* block scores and choice                 */
+  THIN_KERNEL_Q4_ATTENTION = 16 /* attention over the 4-bit cache, joins  */
 } thin_kernel_t;
 typedef void (*thin_launch_hook_t)(void* ctx, int32_t kernel, int32_t round, int32_t phase,
                                    void* stream);

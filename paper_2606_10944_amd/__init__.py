@@ -9,3 +9,5 @@ from ._lib import (THIN_BF16, THIN_EDTYPE, THIN_EHIP, THIN_EINVAL, THIN_EUNIFORM
                    thin_attention, thin_compress, thin_express_plan, thin_express_prefill,
                    thin_express_prefill_plan, thin_plan,
                    thin_selftest_gram16, thin_status_str, workspace_status)
+from .q4 import (Q4Cache, thin_q4_attention, thin_q4_load, thin_q4_select,  # noqa: F401
+                 thin_q4_store, thin_rotary, thin_rotary_turns)

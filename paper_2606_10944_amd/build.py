@@ -7,7 +7,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SO = os.path.join(HERE, "libthin.so")
 SOURCES = ["csrc/compress.hip", "csrc/attention.hip", "csrc/express.hip", "csrc/api.cpp",
-           "csrc/noalloc.hip"]
+           "csrc/noalloc.hip", "csrc/rotary.hip", "csrc/q4_cache.hip", "csrc/q4_attention.hip",
+           "csrc/api_q4.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # no packed fp32 instructions in device code

@@ -13,6 +13,14 @@
 
 #include "../../include/thin.h"
 #include "launch.hpp"
+#include "observe.hpp"
+
+namespace thin {
+thread_local thin_launch_hook_t g_hook = nullptr;
+thread_local void* g_hook_ctx = nullptr;
+}  // namespace thin
+
+using thin::observed;
 
 namespace {
 
@@ -177,20 +185,6 @@ Workspace carve(void* base, int64_t S, int64_t d, const Levels& lv, size_t cap =
 size_t workspace_size(int64_t S, int64_t d, const Levels& lv, size_t cap = kScoreCap,
                       bool spread = false) {
   return carve(nullptr, S, d, lv, cap, spread).bytes;
-}
-
-// The launch observer is a diagnostic of the calling thread (thread-local):
-// calls from other threads never see it.
-thread_local thin_launch_hook_t g_hook = nullptr;
-thread_local void* g_hook_ctx = nullptr;
-
-// Enqueue one launch between the observer's two calls.
-template <typename F>
-hipError_t observed(int32_t kernel, int32_t round, hipStream_t st, F&& launch) {
-  if (g_hook) g_hook(g_hook_ctx, kernel, round, 0, st);
-  const hipError_t e = launch();
-  if (g_hook) g_hook(g_hook_ctx, kernel, round, 1, st);
-  return e;
 }
 
 // One KH round over the S*G buckets described by `a`: one local launch for
@@ -796,8 +790,8 @@ int thin_workspace_status(const void* workspace, int32_t* status, void* stream) 
 }
 
 int thin_set_launch_hook(thin_launch_hook_t hook, void* ctx) {
-  g_hook = hook;
-  g_hook_ctx = ctx;
+  thin::g_hook = hook;
+  thin::g_hook_ctx = ctx;
   return THIN_OK;
 }
 

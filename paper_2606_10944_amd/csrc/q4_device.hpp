@@ -1,0 +1,68 @@
+// Device-side pieces of the 4-bit cache's kernels.
+#pragma once
+
+#include "common.hpp"
+#include "q4.hpp"
+
+namespace thin {
+
+// 2^(byte - 127)
+__device__ __forceinline__ float q4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Eight codes as bf16 pairs (exact: a code times a power of two).
+__device__ __forceinline__ void decode8(uint32_t c, float scale, uint32_t* w) {
+  w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0));
+  w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1));
+  w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2));
+  w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3));
+}
+
+template <typename T>
+__device__ __forceinline__ float elem(const T* p, int64_t i);
+template <>
+__device__ __forceinline__ float elem<float>(const float* p, int64_t i) {
+  return p[i];
+}
+template <>
+__device__ __forceinline__ float elem<bf16_t>(const bf16_t* p, int64_t i) {
+  return bf16_to_float(p[i].bits);
+}
+
+// Eight elements from a 16-byte aligned place.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float* f);
+template <>
+__device__ __forceinline__ void load8<float>(const float* p, float* f) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+  f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+template <>
+__device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float* f) {
+  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(w[i] << 16);
+    f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+
+// The last cached row that token t of batch entry b sees (its own); -1 for a
+// token that is not there or stands before row 0.
+__device__ __forceinline__ int64_t q4_last_row(const Q4Tokens& tok, int64_t b, int64_t t,
+                                               int64_t n_max) {
+  if (tok.count && t >= tok.count[b]) return -1;
+  const int64_t r = (int64_t)tok.at[b] + t;
+  return r < 0 ? -1 : (r < n_max ? r : n_max - 1);
+}
+
+// Instance F<element type, head dimension> of a launch.
+#define Q4_BY_D(F, ...)                                                                      \
+  return dtype == 0 ? (d == 32   ? F<float, 32>(__VA_ARGS__)                                 \
+                       : d == 64 ? F<float, 64>(__VA_ARGS__)                                 \
+                                 : F<float, 128>(__VA_ARGS__))                               \
+                    : (d == 32   ? F<bf16_t, 32>(__VA_ARGS__)                                \
+                       : d == 64 ? F<bf16_t, 64>(__VA_ARGS__)                                \
+                                 : F<bf16_t, 128>(__VA_ARGS__))
+
+}  // namespace thin
