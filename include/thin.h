@@ -503,7 +503,8 @@ int thin_q4_load(const thin_q4_cache_t* cache, int64_t T, const int32_t* at, voi
  * in float64.  Of the blocks up to the token's own, the first n_sinks, the last
  * n_window and those of the largest scores are taken, n_sel in all (ties: the
  * lowest; a NaN score is the smallest), or every one if they are at most n_sel.
- *   Q       (device) [B, q_heads, T, d] of `dtype`, q_heads a multiple of H.
+ *   Q       (device) [B, q_heads, T, d] of `dtype`, q_heads a multiple of H, at
+ *           most 1024 H.
  *   blocks  (device) int32 [B, H, T, n_sel]: ascending, -1 behind the last one.
  *   n_sinks >= 0, n_window >= 1, n_sinks + n_window <= n_sel <= 32768.
  *   workspace (device) at least *workspace_bytes of thin_q4_select_plan, 16-byte

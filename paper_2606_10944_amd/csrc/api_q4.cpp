@@ -11,7 +11,7 @@ using thin::observed;
 namespace {
 
 constexpr int64_t kMaxSlices = 65535;  // grid y
-constexpr int64_t kMaxTokens = (int64_t)1 << 20;
+constexpr int64_t kMaxTokens = thin::kQ4MaxTokens;
 // workgroups of a grid row: the runtime takes fewer than 2^32 threads
 constexpr int64_t kMaxGroups = ((int64_t)1 << 24) - 1;
 
@@ -54,7 +54,7 @@ int cache_view(const thin_q4_cache_t* c, thin::Q4View* v) {
     if (!p || !aligned16(p)) return THIN_EINVAL;
   *v = {static_cast<uint8_t*>(c->k_codes), static_cast<uint8_t*>(c->k_scales),
         static_cast<uint8_t*>(c->v_codes), static_cast<uint8_t*>(c->v_scales),
-        static_cast<uint16_t*>(c->bounds), c->B, c->H, c->n_max};
+        static_cast<uint16_t*>(c->bounds), (int32_t)c->B, (int32_t)c->H, (int32_t)c->n_max};
   return THIN_OK;
 }
 
@@ -65,21 +65,25 @@ bool valid_sizes(int64_t B, int64_t H, int64_t n_max, int64_t T) {
 
 int64_t blocks_of(int64_t n_max) { return (n_max + THIN_Q4_BLOCK - 1) / THIN_Q4_BLOCK; }
 
+// Query heads per key head, 0 if there is no such grouping.
+int64_t group_of(int64_t q_heads, int64_t H) {
+  return q_heads >= H && q_heads % H == 0 && q_heads / H <= thin::kQ4MaxGroup ? q_heads / H : 0;
+}
+
 struct AttnPlan {
-  int64_t splits;
+  thin::Q4AttnShape shape;
   size_t bytes;
 };
 
 bool plan_attention(int64_t B, int64_t H, int64_t q_heads, int64_t n_max, int64_t d, int64_t T,
                     int64_t n_sel, AttnPlan* p) {
-  if (!valid_sizes(B, H, n_max, T) || !supported_d(d) || q_heads < H || q_heads % H != 0 ||
-      q_heads / H > kMaxSlices || n_sel < 0 || n_sel > 32768)
+  if (!valid_sizes(B, H, n_max, T) || !supported_d(d) || !group_of(q_heads, H) || n_sel < 0 ||
+      n_sel > 32768)
     return false;
   const int64_t tiles = thin::q4_row_tiles(q_heads / H, T, n_sel > 0);
-  const int64_t keys = n_sel > 0 ? n_sel * THIN_Q4_BLOCK : n_max;
-  p->splits = thin::q4_splits(B * H, tiles, keys);
-  p->bytes = thin::q4_attention_bytes(B * H, tiles, p->splits, d);
-  return tiles * p->splits <= kMaxGroups;
+  p->shape = thin::q4_attention_shape(B, H, tiles, n_sel > 0 ? n_sel * THIN_Q4_BLOCK : n_max);
+  p->bytes = thin::q4_attention_bytes(B * H, tiles, p->shape.splits, d);
+  return tiles <= kMaxGroups;  // (B * tiles * splits is at most 2048 where splits > 1)
 }
 
 }  // namespace
@@ -162,7 +166,7 @@ int thin_q4_store(const thin_q4_cache_t* cache, const void* K, const int64_t* k_
   if (rc) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = observed(THIN_KERNEL_Q4_STORE, -1, st, [&] {
-    return thin::launch_q4_store(dtype, cache->d, c, k, v, {at, count, T}, st);
+    return thin::launch_q4_store(dtype, cache->d, c, k, v, {at, count, (int32_t)T}, st);
   });
   return e == hipSuccess ? THIN_OK : THIN_EHIP;
 }
@@ -200,7 +204,7 @@ int thin_q4_select(const thin_q4_cache_t* cache, const void* Q, const int64_t* q
   size_t need = 0;
   if (thin_q4_select_plan(c.B, c.H, c.n_max, T, &need) != THIN_OK || !at || !blocks)
     return THIN_EINVAL;
-  if (q_heads < c.H || q_heads % c.H != 0 || q_heads / c.H > kMaxSlices) return THIN_EINVAL;
+  if (!group_of(q_heads, c.H)) return THIN_EINVAL;
   if (n_sel < 1 || n_sel > 32768 || n_sinks < 0 || n_window < 1 || n_sinks > n_sel ||
       n_window > n_sel || n_sinks + n_window > n_sel)
     return THIN_EINVAL;
@@ -208,18 +212,19 @@ int thin_q4_select(const thin_q4_cache_t* cache, const void* Q, const int64_t* q
   rc = rows_view(Q, q_strides, c.B, q_heads, T, cache->d, dtype, false, &a.q);
   if (rc) return rc;
   if (!workspace || workspace_bytes < need || !aligned16(workspace)) return THIN_EWORKSPACE;
-  a.G = q_heads / c.H;
-  a.tok = {at, count, T};
-  a.n_sel = n_sel;
-  a.n_sinks = n_sinks;
-  a.n_window = n_window;
+  a.G = (int32_t)group_of(q_heads, c.H);
+  a.tok = {at, count, (int32_t)T};
+  a.n_sel = (int32_t)n_sel;
+  a.n_sinks = (int32_t)n_sinks;
+  a.n_window = (int32_t)n_window;
   a.blocks = blocks;
   a.scores = static_cast<uint64_t*>(workspace);
-  const int64_t step = thin::q4_select_tokens(c.B * c.H, blocks_of(c.n_max), T);
+  const int64_t step = thin::q4_select_tokens((int64_t)c.B * c.H, blocks_of(c.n_max), T);
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
-  for (a.t0 = 0; a.t0 < T && e == hipSuccess; a.t0 += step) {
-    a.tn = T - a.t0 < step ? T - a.t0 : step;
+  for (int64_t t0 = 0; t0 < T && e == hipSuccess; t0 += step) {
+    a.t0 = (int32_t)t0;
+    a.tn = (int32_t)(T - t0 < step ? T - t0 : step);
     e = observed(THIN_KERNEL_Q4_SELECT, -1, st,
                  [&] { return thin::launch_q4_scores(dtype, cache->d, c, a, st); });
     if (e == hipSuccess)
@@ -256,16 +261,16 @@ int thin_q4_attention(const thin_q4_cache_t* cache, const void* Q, const int64_t
   if (rc) return rc;
   if (p.bytes && (!workspace || workspace_bytes < p.bytes || !aligned16(workspace)))
     return THIN_EWORKSPACE;
-  a.G = q_heads / c.H;
-  a.tok = {at, count, T};
+  a.G = (int32_t)group_of(q_heads, c.H);
+  a.tok = {at, count, (int32_t)T};
   a.blocks = blocks;
-  a.n_sel = n_sel;
-  a.splits = p.splits;
+  a.n_sel = (int32_t)n_sel;
+  a.shape = p.shape;
   a.part = static_cast<float*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = observed(THIN_KERNEL_Q4_ATTENTION, -1, st,
                           [&] { return thin::launch_q4_attention(dtype, cache->d, c, a, st); });
-  if (e == hipSuccess && p.splits > 1)
+  if (e == hipSuccess && p.shape.splits > 1)
     e = observed(THIN_KERNEL_Q4_ATTENTION, -1, st,
                  [&] { return thin::launch_q4_join(dtype, cache->d, c, a, st); });
   return e == hipSuccess ? THIN_OK : THIN_EHIP;

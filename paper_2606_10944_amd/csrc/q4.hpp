@@ -18,7 +18,7 @@ struct Q4View {
   uint8_t* v_codes;
   uint8_t* v_scales;
   uint16_t* bounds;   // bf16 [B, H, ceil(n_max / 64), 2, d]: least and largest key values
-  int64_t B, H, n_max;
+  int32_t B, H, n_max;
 };
 
 // Rows [B, heads, T, d] of any strides (elements; channels are contiguous).
@@ -32,7 +32,7 @@ struct RowsView {
 struct Q4Tokens {
   const int32_t* at;
   const int32_t* count;
-  int64_t T;
+  int32_t T;
 };
 
 struct RotaryArgs {
@@ -53,11 +53,11 @@ hipError_t launch_q4_load(int dtype, int64_t d, const Q4View& c, const int32_t* 
 
 struct Q4SelectArgs {
   RowsView q;
-  int64_t G;  // query heads per key head
+  int32_t G;  // query heads per key head
   Q4Tokens tok;
-  int64_t n_sel, n_sinks, n_window;
+  int32_t n_sel, n_sinks, n_window;
   int32_t* blocks;   // [B, H, T, n_sel]
-  int64_t t0, tn;    // the launch's tokens: t0 .. t0 + tn - 1
+  int32_t t0, tn;    // the launch's tokens: t0 .. t0 + tn - 1
   uint64_t* scores;  // [B, H, tn, ceil(n_max / 64)]
 };
 hipError_t launch_q4_scores(int dtype, int64_t d, const Q4View& c, const Q4SelectArgs& a,
@@ -66,12 +66,12 @@ hipError_t launch_q4_pick(const Q4View& c, const Q4SelectArgs& a, hipStream_t st
 
 struct Q4AttnArgs {
   RowsView q, o;
-  int64_t G;
+  int32_t G;
   Q4Tokens tok;
   const int32_t* blocks;  // null: every cached row
-  int64_t n_sel;
-  int64_t splits;  // workgroups that share the keys of a tile of rows
-  float* part;     // splits > 1: [tile, split, 16, d] sums, then [tile, split, 2, 16] max and sum
+  int32_t n_sel;
+  Q4AttnShape shape;
+  float* part;  // shape.splits > 1: [slot, 16, d] sums, then [slot, 2, 16] maxima and sums
 };
 hipError_t launch_q4_attention(int dtype, int64_t d, const Q4View& c, const Q4AttnArgs& a,
                                hipStream_t st);

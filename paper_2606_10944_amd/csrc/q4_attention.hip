@@ -3,15 +3,13 @@
 //
 // o = sum_j p_j v_j / sum_j p_j,  p_j = exp(<q, k_j> / sqrt(d) - max).
 //
-// A code times its power of two is exactly a bf16, so keys and values enter the
-// bf16 matrix instructions without loss, for float32 queries too: those split
-// into three bf16 parts (24 bits), and so do their weights p.  bf16 queries use
-// one bf16 weight: its rounding (2^-9 of a term) is that of the output.
+// A code times its power of two is exactly a bf16, so values (and, for float32
+// queries, keys) enter the bf16 matrix instructions without loss.  float32 weights p
+// split into three bf16 parts; bf16 queries use one bf16 weight: its rounding (2^-8 of
+// a term at most) is that of the output.
 //
-// Lane layout of the 16x16x32 instruction: lane l = 16 g + m.  Scores S^T = K Q^T
-// (keys x query rows): lane (m, g) feeds key row m's channels of quarter g of the
-// head, as they lie in memory (d / 8 bytes of codes, one scale), and of query row
-// m the same channels.  Lane (m, g) then holds the scores of keys 4 g .. 4 g + 3
+// Lanes are l = 16 g + m.  Scores S^T = K Q^T (keys x query rows): lane (m, g) feeds
+// key row m's share of the channels (Codes), and query row m's.  It then holds the scores of keys 4 g .. 4 g + 3
 // for query row m, which is what the product O^T = V^T P^T wants as its second
 // operand.  Its first, V^T, is read from LDS by the transposing read: a wave keeps
 // 32 decoded value rows there.
@@ -27,11 +25,14 @@ namespace thin {
 
 namespace {
 
-constexpr int WAVES = 4;
-constexpr int CH = 32;  // keys per step of a wave
+constexpr int CH = kQ4Step;
 constexpr float kLowest = -3.0e38f;
+constexpr float kSlack = 8.0f;
 constexpr double kLog2e = 1.44269504088896340736;
 
+// Buffers of codes of a wave: the step in work and the next (three cost registers: 8
+// sequences of up to 65536 rows 66.6 -> 68.0 us, a prompt's 1497 -> 1668).
+constexpr int PF = 2;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // bf16 parts of eight float32 values: 1 (rounded) or 3 (their sum is the value).
@@ -56,9 +57,12 @@ __device__ __forceinline__ void split8(const float* f, bf16x8_t* out) {
 }
 
 // One wave's step: the codes of 32 keys and values.
-template <int D>
+template <typename T, int D>
 struct Codes {
-  static constexpr int KB = D / 8;  // bytes of a lane's quarter of a key row
+  // bytes of a key row that a lane holds: a group of 32 channels (bf16 queries, see
+  // Queries), else a quarter of the row
+  static constexpr bool MX = Elem<T>::bytes == 2;
+  static constexpr int KB = MX ? 16 : D / 8;
   static constexpr int KW = KB / 4;
   uint32_t k[2][KW];
   uint32_t ks[2];
@@ -85,199 +89,460 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
   }
 }
 
-// Rows row0 .. row0 + 31 of a slice; rows past `last` stand for `last`.
+// A slice's rows: offsets within it fit 32 bits (n_max * d / 2 <= 2^27 bytes).
+struct Slice {
+  const uint8_t *kc, *ks, *vc, *vs;
+};
 template <int D>
-__device__ __forceinline__ void load_codes(const Q4View& c, int64_t s, int64_t row0, int64_t last,
-                                           int lane, Codes<D>& x) {
-  using C = Codes<D>;
-  const int m = lane & 15, g = lane >> 4;
+__device__ __forceinline__ Slice slice_of(const Q4View& c, int64_t s) {
+  const int64_t row = s * c.n_max;
+  return {c.k_codes + row * (D / 2), c.k_scales + row * (D / 32), c.v_codes + row * (D / 2),
+          c.v_scales + row * (D / 32)};
+}
+
+// Rows row0 .. row0 + 31; rows past `last` stand for `last`.
+template <typename T, int D>
+__device__ __forceinline__ void load_codes(const Slice& c, int row0, int last, int lane,
+                                           Codes<T, D>& x) {
+  using C = Codes<T, D>;
+  const int m = lane & 15, g = (lane >> 4) % (D / 2 / C::KB);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    int64_t r = row0 + t * 16 + m;
-    r = s * c.n_max + (r < last ? r : last);
-    load_words<C::KW>(c.k_codes + r * (D / 2) + g * C::KB, x.k[t]);
-    x.ks[t] = c.k_scales[r * (D / 32) + g * C::KB * 2 / 32];
+    const uint32_t r = std::min(row0 + t * 16 + m, last);
+    load_words<C::KW>(c.kc + (r * (D / 2) + g * C::KB), x.k[t]);
+    x.ks[t] = c.ks[r * (D / 32) + g * C::KB * 2 / 32];
   }
 #pragma unroll
   for (int i = 0; i < C::VI; ++i) {
     const int item = i * 64 + lane;
-    int64_t r = row0 + item / C::VR;
-    r = s * c.n_max + (r < last ? r : last);
-    load_words<C::VL / 4>(c.v_codes + r * (D / 2) + item % C::VR * C::VL, x.v[i]);
-    x.vs[i] = c.v_scales[r * (D / 32) + item % C::VR * C::VL * 2 / 32];
+    const uint32_t r = std::min(row0 + item / C::VR, last);
+    load_words<C::VL / 4>(c.vc + (r * (D / 2) + item % C::VR * C::VL), x.v[i]);
+    x.vs[i] = c.vs[r * (D / 32) + item % C::VR * C::VL * 2 / 32];
   }
 }
+
+// A tile's 16 query rows as the second operand of the scores, and the scores of 16 keys.
+//
+// float32: three bf16 parts (24 bits), the keys decoded to bf16.
+template <typename T, int D>
+struct Queries {
+  static constexpr int KS = D / 32;
+  bf16x8_t q[3][KS];
+  // row: this lane's query row (null: zeros); g: lane / 16
+  __device__ __forceinline__ void load(const T* row, int g) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (row) load8<T>(row + g * (D / 4) + k * 8, f);
+      bf16x8_t part[3];
+      split8<3>(f, part);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) q[p][k] = part[p];
+    }
+  }
+  __device__ __forceinline__ floatx4_t scores(const uint32_t* codes, uint32_t byte) const {
+    floatx4_t z = {0.f, 0.f, 0.f, 0.f};
+    const float ks = q4_scale(byte);
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      uint32_t w[4];
+      decode8(codes[k], ks, w);
+      const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, (u32x4){w[0], w[1], w[2], w[3]});
+#pragma unroll
+      for (int p = 2; p >= 0; --p)
+        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[p][k], z, 0, 0, 0);
+    }
+    return z;
+  }
+};
+
+// bf16: the scaled 16x16x128 instruction takes the codes and their scales as they are
+// stored, 128 channels at a time, beside fp8 queries.  A bf16 is the sum of two e4m3
+// numbers (four significant bits each) under one power of two per row, exactly for
+// values down to 2^-9 of the row's largest, within 2^-18 of that below.  (The
+// instruction cuts products below about 2^-15 of its largest one: 1e-6 of the sum of
+// magnitudes for normal values.)  Against decoding the keys to bf16 it saves 32 of 64
+// conversions per step of 32 keys and takes two thirds of the matrix cores' time.
+//
+// Channels of k-slot 16 g + i and 64 + 16 g + i in lane (m, g) of the fp8 operand; the
+// fp4 operand's lane (m, g) holds k-slots 32 g .. 32 g + 31, all under its own scale.
+// d = 128: an instruction for each part; d = 64: k-slots 0 .. 63 take the first part,
+// the others the second, beside the same keys; d = 32: 0 .. 31 and 32 .. 63.
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+template <int D>
+struct Queries<bf16_t, D> {
+  static constexpr int NI = D == 128 ? 2 : 1;  // instructions
+  i32x8 q[NI];
+  int scale;
+  __device__ __forceinline__ void load(const bf16_t* row, int g) {
+    // this lane's 16 channels (d = 128: 32) and the part that it holds
+    constexpr int N = D == 128 ? 32 : 16;
+    float f[N];
+    const int c0 = D == 32 ? g % 2 * 16 : g * 16;
+    float amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; i += 8) {
+      if (row)
+        load8<bf16_t>(row + c0 + i / 16 * 64 + i % 16, f + i);
+      else
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[i + j] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) amax = fmaxf(amax, fabsf(f[i]));
+    amax = fmaxf(amax, __shfl_xor(amax, 16));
+    amax = fmaxf(amax, __shfl_xor(amax, 32));
+    // the largest value lands in [2^7, 2^8)
+    int byte = (int)(__float_as_uint(amax) >> 23) - 7;
+    byte = byte < 1 ? 1 : byte;
+    scale = byte;
+    const float up = __uint_as_float((uint32_t)(254 - byte) << 23);
+    int part[2][N / 4];
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        float* x = f + 4 * i;
+        if (p == 0)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] *= up;
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], w, true);
+        part[p][i] = w;
+        x[0] -= __builtin_amdgcn_cvt_f32_fp8(w, 0);
+        x[1] -= __builtin_amdgcn_cvt_f32_fp8(w, 1);
+        x[2] -= __builtin_amdgcn_cvt_f32_fp8(w, 2);
+        x[3] -= __builtin_amdgcn_cvt_f32_fp8(w, 3);
+      }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (D == 128) {
+        q[0][i] = part[0][i];
+        q[NI - 1][i] = part[1][i];
+      } else if (D == 64) {
+        q[0][i] = part[i / 4][i % 4];
+      } else {
+        q[0][i] = i < 4 ? part[g / 2][i % 4] : 0;
+      }
+    }
+  }
+  __device__ __forceinline__ floatx4_t scores(const uint32_t* codes, uint32_t byte) const {
+    floatx4_t z = {0.f, 0.f, 0.f, 0.f};
+    const i32x8 k = {(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3], 0, 0, 0, 0};
+#pragma unroll
+    for (int i = NI - 1; i >= 0; --i)
+      z = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q[i], z, 4, 0, 0, (int)byte, 0, scale);
+    return z;
+  }
+};
 
 // Bytes per value row in LDS: 32 past the row put the four rows that 16 lanes read
 // together on different banks.
 template <int D>
 constexpr int kVStride = 2 * D + 32;
 
-// Channels ch .. ch + 3 of query row r of a tile, if there is such a row.
+// Channels ch .. ch + 3 of query row r (there is one) of a tile.
 template <typename T, bool LIST>
-__device__ __forceinline__ void store_row4(const Q4AttnArgs& a, int64_t b, int64_t h, int64_t tile,
-                                           int r, int ch, floatx4_t o) {
-  int64_t t, head;
+__device__ __forceinline__ void store_row4(const Q4AttnArgs& a, int b, int h, int tile, int r,
+                                           int ch, floatx4_t o) {
+  int t, head;
   if (LIST) {
-    const int64_t gt = (a.G + 15) / 16;
+    const int gt = (a.G + 15) / 16;
     t = tile / gt;
     head = tile % gt * 16 + r;
-    if (head >= a.G) return;
   } else {
-    const int64_t row = tile * 16 + r;
-    if (row >= a.tok.T * a.G) return;
-    t = row / a.G;
-    head = row % a.G;
+    t = (tile * 16 + r) / a.G;
+    head = (tile * 16 + r) % a.G;
   }
-  T* p = static_cast<T*>(const_cast<void*>(a.o.p)) + b * a.o.sb + (h * a.G + head) * a.o.sh +
-         t * a.o.sr + ch;
+  T* p = static_cast<T*>(const_cast<void*>(a.o.p)) + b * a.o.sb +
+         ((int64_t)h * a.G + head) * a.o.sh + t * a.o.sr + ch;
   if constexpr (Elem<T>::bytes == 2)
     *reinterpret_cast<uint2*>(p) = make_uint2(cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]));
   else
     *reinterpret_cast<floatx4_t*>(p) = o;
 }
 
-template <typename T, int D, bool LIST>
-__global__ __launch_bounds__(64 * WAVES) void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
-  constexpr int NP = Elem<T>::bytes == 2 ? 1 : 3;
-  constexpr int KS = D / 32;  // k-steps of the scores
-  using C = Codes<D>;
-  __shared__ __align__(16) unsigned char lds[WAVES * CH * kVStride<D>];
-  __shared__ float sm[WAVES][16], sl[WAVES][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int m = lane & 15, g = lane >> 4;
-  const int64_t s = blockIdx.y, b = s / c.H, h = s % c.H;
-  const int64_t split = blockIdx.x % a.splits, tile = blockIdx.x / a.splits;
-  // the tile's 16 query rows: heads of one token (LIST), or tokens x heads in a row
-  const int64_t gt = (a.G + 15) / 16;
-  int64_t t, head, tl;  // this lane's token and head, the tile's last token
-  bool there;
-  if (LIST) {
-    t = tl = tile / gt;
-    head = tile % gt * 16 + m;
-    there = head < a.G;
-  } else {
-    const int64_t row = tile * 16 + m, rows = a.tok.T * a.G;
-    const int64_t end = std::min(tile * 16 + 15, rows - 1);
-    there = row < rows;
-    t = there ? row / a.G : 0;
-    head = there ? row % a.G : 0;
-    tl = end / a.G;
-  }
-  const int64_t qlast = there ? q4_last_row(a.tok, b, t, c.n_max) : -1;
-  // the last row that any of the tile's queries sees
-  int64_t last = -1;
-  if (LIST) {
-    last = q4_last_row(a.tok, b, tl, c.n_max);
-  } else {
-    const int64_t cnt = a.tok.count ? (int64_t)a.tok.count[b] : a.tok.T;
-    if (tl >= cnt) tl = cnt - 1;
-    if (tl >= 0 && tl * a.G + a.G > tile * 16) last = q4_last_row(a.tok, b, tl, c.n_max);
+// The tokens of which tile `tile` (tokens x heads in a row) holds a head.
+struct TileTokens {
+  int first, last;
+};
+__device__ __forceinline__ TileTokens tile_tokens(const Q4AttnArgs& a, int tile) {
+  const int rows = a.tok.T * a.G;
+  return {tile * 16 / a.G, (tile * 16 + 16 < rows ? tile * 16 + 15 : rows - 1) / a.G};
+}
+
+// The last cached row that any of a tile's tokens of sequence b sees, -1 if none.
+__device__ __forceinline__ int tile_row(const Q4View& c, const Q4AttnArgs& a, int b, TileTokens tt) {
+  const int cnt = a.tok.count ? a.tok.count[b] : a.tok.T;
+  return cnt <= tt.first ? -1 : q4_last_row(a.tok, b, tt.last < cnt ? tt.last : cnt - 1, c.n_max);
+}
+
+// Steps of 32 keys up to there.
+__device__ __forceinline__ int steps_of(const Q4View& c, const Q4AttnArgs& a, int b, TileTokens tt) {
+  return (tile_row(c, a, b, tt) + CH) / CH;
+}
+
+// How the workgroups of a key head and tile share the sequences' steps.  Every
+// sequence gets workgroups by its length: a share is what a workgroup takes of one
+// sequence, the least for which the workgroups are enough.  Lane l holds sequences
+// l, l + 64, ..
+struct Shares {
+  static constexpr int N = kQ4SharedEntries / 64;
+  int steps[N];  // of this lane's sequences
+  int upto[N];   // shares of the sequences up to each of them
+  uint32_t share;
+
+  __device__ __forceinline__ uint32_t count(int i) const {
+    return ((uint32_t)steps[i] + share - 1) / share;
   }
 
-  bf16x8_t q[NP][KS];
-  {
-    const T* qp = static_cast<const T*>(a.q.p) + b * a.q.sb + (h * a.G + head) * a.q.sh +
-                  t * a.q.sr + g * (D / 4);
+  __device__ __forceinline__ Shares(const Q4View& c, const Q4AttnArgs& a, int tile, int lane) {
+    const TileTokens tt = tile_tokens(a, tile);
+    int sum = 0;  // (at most 2^24: 256 sequences, 2^16 steps each)
 #pragma unroll
-    for (int i = 0; i < KS; ++i) {
-      float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (there) load8<T>(qp + i * 8, f);
-      bf16x8_t part[NP];
-      split8<NP>(f, part);
+    for (int i = 0; i < N; ++i) {
+      steps[i] = 0;
+      if (i * 64 < c.B && i * 64 + lane < c.B) steps[i] = steps_of(c, a, i * 64 + lane, tt);
+      sum += steps[i];
+    }
 #pragma unroll
-      for (int p = 0; p < NP; ++p) q[p][i] = part[p];
+    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
+    // rounded up per sequence, the shares are at most B more than the sum's
+    const int groups = c.B * a.shape.splits, spare = groups - c.B;
+    const int least = (int)((uint32_t)(sum + spare - 1) / (uint32_t)spare);
+    share = (uint32_t)__builtin_amdgcn_readfirstlane(least < a.shape.least ? a.shape.least : least);
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      upto[i] = before;
+      if (i * 64 >= c.B) continue;
+      int x = (int)count(i);
+#pragma unroll
+      for (int m = 1; m < 64; m *= 2) {
+        const int y = __shfl_up(x, m);
+        if (lane >= m) x += y;
+      }
+      upto[i] += x;
+      before = __shfl(upto[i], 63);
     }
   }
 
-  // steps of 32 keys: the split's share, the waves in turn
-  const int64_t steps = LIST ? a.n_sel * (kQ4Block / CH) : (last + CH) / CH;
-  const int64_t share = (steps + a.splits - 1) / a.splits;
-  const int64_t i1 = std::min(steps, (split + 1) * share);
-  const int32_t* list = LIST ? a.blocks + (s * a.tok.T + tl) * a.n_sel : nullptr;
-  const int64_t nb = (c.n_max + kQ4Block - 1) / kQ4Block;
-  auto row_of = [&](int64_t i) -> int64_t {  // first row of step i, or past `last`
-    if (!LIST) return i * CH;
-    const int64_t k = list[i / (kQ4Block / CH)];
-    return k < 0 || k >= nb ? c.n_max : k * kQ4Block + i % (kQ4Block / CH) * CH;
-  };
+  // Workgroup j's sequence (-1: none is left for it) and steps i0 .. i1 - 1.
+  __device__ __forceinline__ int find(const Q4View& c, int j, int* i0, int* i1) const {
+    int b = -1;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (i * 64 >= c.B || b >= 0) continue;
+      const uint64_t past = __ballot(upto[i] > j);
+      if (!past) continue;
+      const int l = __ffsll((unsigned long long)past) - 1;
+      const int first = __shfl(upto[i] - (int)count(i), l);
+      *i0 = __builtin_amdgcn_readfirstlane((j - first) * (int)share);
+      const int end = __builtin_amdgcn_readfirstlane(__shfl(steps[i], l));
+      *i1 = *i0 + (int)share < end ? *i0 + (int)share : end;
+      b = i * 64 + l;
+    }
+    return b;
+  }
 
+  // The first of sequence b's workgroups and how many there are.
+  __device__ __forceinline__ void of(const Q4View& c, int b, int* first, int* n) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (i != b / 64) continue;
+      const int x = (int)count(i);
+      *n = __shfl(x, b % 64);
+      *first = __shfl(upto[i] - x, b % 64);
+    }
+  }
+};
+
+// WV waves.  Without splits a workgroup takes a tile's whole keys; with them
+// workgroups share the keys and leave sums in a.part, one slot of existing rows each.
+template <typename T, int D, bool LIST, int WV>
+__global__ __launch_bounds__(64 * WV, 2) void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
+  constexpr int NP = Elem<T>::bytes == 2 ? 1 : 3;  // bf16 parts of the weights
+  using C = Codes<T, D>;
+  __shared__ __align__(16) unsigned char lds[WV * CH * kVStride<D>];
+  __shared__ float sm[WV][16], sl[WV][16];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = lane & 15, g = lane >> 4;
+  // the workgroup's slice, tile and share of the steps
+  const int splits = a.shape.splits;
+  const int64_t slot = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  int b, h, tile, i0, i1;
+  if (LIST || splits == 1) {
+    b = blockIdx.y / c.H;
+    h = blockIdx.y % c.H;
+    tile = blockIdx.x / splits;
+    const int steps = LIST ? a.n_sel * (kQ4Block / CH) : steps_of(c, a, b, tile_tokens(a, tile));
+    const int share = (steps + splits - 1) / splits;
+    i0 = blockIdx.x % splits * share;
+    i1 = i0 + share < steps ? i0 + share : steps;
+  } else {
+    const int groups = c.B * splits;
+    h = blockIdx.y;
+    tile = blockIdx.x / groups;
+    b = Shares(c, a, tile, lane).find(c, blockIdx.x % groups, &i0, &i1);
+    if (b < 0) return;
+  }
+  const int64_t s = (int64_t)b * c.H + h;
+  const Slice rows = slice_of<D>(c, s);
+  // the tile's query rows: heads of one token (LIST), or tokens x heads in a row
+  int t, head, nrows;  // this lane's
+  if (LIST) {
+    const int gt = (a.G + 15) / 16;
+    t = tile / gt;
+    head = tile % gt * 16 + m;
+    nrows = std::min(16, a.G - tile % gt * 16);
+  } else {
+    nrows = std::min(16, a.tok.T * a.G - tile * 16);
+    t = (tile * 16 + m) / a.G;
+    head = (tile * 16 + m) % a.G;
+  }
+  const bool there = m < nrows;
+  const int qlast = there ? q4_last_row(a.tok, b, t, c.n_max) : -1;
+  // the last row that any of them sees
+  const int last = __builtin_amdgcn_readfirstlane(
+      LIST ? q4_last_row(a.tok, b, t, c.n_max) : tile_row(c, a, b, tile_tokens(a, tile)));
+
+  // a wave's steps are i0 + wave + WV n.  LIST: lane n % 64 holds the listed block
+  // of step n, for 64 steps at a time.
+  const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  const int32_t* list = LIST ? a.blocks + (s * a.tok.T + t) * a.n_sel : nullptr;
+  int entry = -1;
+  // the wave's first step with rows to read from step n on; past i1 there is none, and
+  // *row0 keeps its value
+  auto next = [&](int n, int* row0) {
+    for (;; ++n) {
+      const int i = i0 + wave + WV * n;
+      if (i >= i1) break;
+      if (!LIST) {
+        *row0 = i * CH;
+        break;
+      }
+      if ((n & 63) == 0) {
+        const int k = i + WV * lane;
+        entry = k < i1 ? list[k / (kQ4Block / CH)] : -1;
+      }
+      const int k = __builtin_amdgcn_readlane(entry, n & 63);
+      if (k < 0 || k >= nb) continue;
+      const int r = k * kQ4Block + i % (kQ4Block / CH) * CH;
+      if (r > last) continue;
+      *row0 = r;
+      break;
+    }
+    return n;
+  };
+  auto more = [&](int n) { return i0 + wave + WV * n < i1; };
+  if (last < 0) i1 = i0;
+  // the codes of this step and of the next one, which are on their way.  (Past the end
+  // the last row is loaded again: a load that is sometimes not made would have every
+  // use wait for all loads.)
+  C buf[PF];
+  int row0[PF], n = -1;
+  bool go[PF];
+  auto fetch = [&](int k) __attribute__((always_inline)) {
+    row0[k] = c.n_max;
+    n = next(n + 1, &row0[k]);
+    go[k] = more(n);
+    load_codes<T, D>(rows, row0[k], std::max(last, 0), lane, buf[k]);
+  };
+#pragma unroll
+  for (int k = 0; k + 1 < PF; ++k) fetch(k);
+
+  Queries<T, D> q;
+  q.load(there ? static_cast<const T*>(a.q.p) + b * a.q.sb + ((int64_t)h * a.G + head) * a.q.sh +
+                     t * a.q.sr
+               : nullptr,
+         g);
+
+  // Scores to base 2: exp(z / sqrt d - max) = 2^(z c2 - mrun).  mrun moves only when a
+  // score passes it by more than kSlack: until then weights up to 2^kSlack are as
+  // exact as weights up to 1, and neither maxima nor sums pass between lanes.
   const float c2 = (float)(kLog2e / sqrt((double)D));
   float mrun = kLowest, lrun = 0.0f;
   floatx4_t acc[D / 16];
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) acc[i] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+  for (int dt = 0; dt < D / 16; ++dt) acc[dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
   unsigned char* sv = lds + wave * CH * kVStride<D>;
+  // rows that every query of the tile sees need no mask
+  int all = there ? qlast : 0x7fffffff;
+#pragma unroll
+  for (int x = 1; x < 16; x *= 2) all = std::min(all, __shfl_xor(all, x));
+  all = __builtin_amdgcn_readfirstlane(all);
 
-  if (last >= 0) {
-    for (int64_t i = split * share + wave; i < i1; i += WAVES) {
-      const int64_t row0 = row_of(i);
-      if (row0 > last) continue;
-      C x;
-      load_codes<D>(c, s, row0, last, lane, x);
-      float sc[8];
+  auto step = [&](const C& x, int row0) __attribute__((always_inline)) {
+    float sc[8];
 #pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2) {
-        floatx4_t z = {0.f, 0.f, 0.f, 0.f};
-        const float ks = q4_scale(x.ks[t2]);
+    for (int t2 = 0; t2 < 2; ++t2) {
+      const floatx4_t z = q.scores(x.k[t2], x.ks[t2]);
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          uint32_t w[4];
-          decode8(x.k[t2][k], ks, w);
-          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, (u32x4){w[0], w[1], w[2], w[3]});
+      for (int j = 0; j < 4; ++j) sc[t2 * 4 + j] = z[j];
+    }
+    // values to LDS
 #pragma unroll
-          for (int p = NP - 1; p >= 0; --p)
-            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[p][k], z, 0, 0, 0);
-        }
+    for (int n2 = 0; n2 < C::VI; ++n2) {
+      const int item = n2 * 64 + lane;
+      unsigned char* to = sv + item / C::VR * kVStride<D> + item % C::VR * C::VL * 4;
+      const float vs = q4_scale(x.vs[n2]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          sc[t2 * 4 + j] = row0 + t2 * 16 + 4 * g + j <= qlast ? z[j] : -INFINITY;
+      for (int w8 = 0; w8 < C::VL / 4; ++w8) {
+        uint32_t w[4];
+        decode8(x.v[n2][w8], vs, w);
+        *reinterpret_cast<u32x4*>(to + w8 * 16) = (u32x4){w[0], w[1], w[2], w[3]};
       }
-      float mx = sc[0];
+    }
+    if (row0 + CH - 1 > all) {
 #pragma unroll
-      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[j]);
+      for (int j = 0; j < 8; ++j)
+        if (row0 + j / 4 * 16 + 4 * g + j % 4 > qlast) sc[j] = -INFINITY;
+    }
+    float mx = sc[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[j]);
+    mx *= c2;
+    if (__any(mx > mrun + kSlack)) {
       mx = fmaxf(mx, __shfl_xor(mx, 16));
       mx = fmaxf(mx, __shfl_xor(mx, 32));
       const float mnew = fmaxf(mrun, mx);
-      const float scale = __builtin_amdgcn_exp2f((mrun - mnew) * c2);
+      const float scale = __builtin_amdgcn_exp2f(mrun - mnew);
       mrun = mnew;
-      float sum = 0.0f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        sc[j] = __builtin_amdgcn_exp2f((sc[j] - mnew) * c2);
-        sum += sc[j];
-      }
-      lrun = lrun * scale + sum;
+      lrun *= scale;
 #pragma unroll
       for (int dt = 0; dt < D / 16; ++dt) acc[dt] *= scale;
-      bf16x8_t pp[NP];
-      split8<NP>(sc, pp);
-      // values to LDS
+    }
 #pragma unroll
-      for (int n = 0; n < C::VI; ++n) {
-        const int item = n * 64 + lane;
-        unsigned char* to = sv + item / C::VR * kVStride<D> + item % C::VR * C::VL * 4;
-        const float vs = q4_scale(x.vs[n]);
+    for (int j = 0; j < 8; ++j) {
+      sc[j] = __builtin_amdgcn_exp2f(fmaf(sc[j], c2, -mrun));
+      lrun += sc[j];
+    }
+    bf16x8_t pp[NP];
+    split8<NP>(sc, pp);
 #pragma unroll
-        for (int w8 = 0; w8 < C::VL / 4; ++w8) {
-          uint32_t w[4];
-          decode8(x.v[n][w8], vs, w);
-          *reinterpret_cast<u32x4*>(to + w8 * 16) = (u32x4){w[0], w[1], w[2], w[3]};
-        }
+    for (int dt = 0; dt < D / 16; ++dt) {
+      typedef __attribute__((address_space(3))) s16x4 lds_t;
+      unsigned char* from = sv + (4 * g + m / 4) * kVStride<D> + dt * 32 + m % 4 * 8;
+      const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)from);
+      const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)(from + 16 * kVStride<D>));
+      typedef short s16x8 __attribute__((ext_vector_type(8)));
+      const bf16x8_t vf = __builtin_bit_cast(
+          bf16x8_t, (s16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int p = NP - 1; p >= 0; --p)
+        acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[p], acc[dt], 0, 0, 0);
+    }
+  };
+  for (bool done = false; !done;) {
+#pragma unroll
+    for (int k = 0; k < PF; ++k) {
+      if (!go[k]) {
+        done = true;
+        break;
       }
-#pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt) {
-        typedef __attribute__((address_space(3))) s16x4 lds_t;
-        unsigned char* from = sv + (4 * g + m / 4) * kVStride<D> + dt * 32 + m % 4 * 8;
-        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)from);
-        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)(from + 16 * kVStride<D>));
-        typedef short s16x8 __attribute__((ext_vector_type(8)));
-        const bf16x8_t vf = __builtin_bit_cast(
-            bf16x8_t, (s16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-        for (int p = NP - 1; p >= 0; --p)
-          acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[p], acc[dt], 0, 0, 0);
-      }
+      fetch((k + PF - 1) % PF);
+      step(buf[k], row0[k]);
     }
   }
   lrun += __shfl_xor(lrun, 16);
@@ -291,21 +556,20 @@ __global__ __launch_bounds__(64 * WAVES) void q4_attn_kernel(Q4View c, Q4AttnArg
   __syncthreads();  // (also: every wave is done with its value rows)
   float mall = sm[0][m], lall = 0.0f;
 #pragma unroll
-  for (int w = 1; w < WAVES; ++w) mall = fmaxf(mall, sm[w][m]);
+  for (int w = 1; w < WV; ++w) mall = fmaxf(mall, sm[w][m]);
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) lall += sl[w][m] * __builtin_amdgcn_exp2f((sm[w][m] - mall) * c2);
+  for (int w = 0; w < WV; ++w) lall += sl[w][m] * __builtin_amdgcn_exp2f(sm[w][m] - mall);
   constexpr int OS = D + 4;  // floats per row of a wave's sums
-  static_assert(WAVES * 16 * OS * 4 <= (int)sizeof(lds), "the waves' sums fit the value rows");
+  static_assert(WV * 16 * OS * 4 <= (int)sizeof(lds), "the waves' sums fit the value rows");
   float* so = reinterpret_cast<float*>(lds);
-  {
-    const float scale = __builtin_amdgcn_exp2f((mrun - mall) * c2);
+  if (there) {
+    const float scale = __builtin_amdgcn_exp2f(mrun - mall);
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) {
       const floatx4_t r = acc[dt] * scale;
       *reinterpret_cast<floatx4_t*>(so + (wave * 16 + m) * OS + dt * 16 + 4 * g) = r;
     }
   }
-  // sl and sm of all rows for the threads that write them
   __syncthreads();
   if (wave == 0 && g == 0) {
     sm[0][m] = mall;
@@ -313,14 +577,13 @@ __global__ __launch_bounds__(64 * WAVES) void q4_attn_kernel(Q4View c, Q4AttnArg
   }
   __syncthreads();
   constexpr int V = D / 4;  // threads per row, four channels each
-  for (int i = threadIdx.x; i < 16 * V; i += 64 * WAVES) {
-    const int r = i / V, ch = i % V * 4;
+  for (int k = threadIdx.x; k < nrows * V; k += 64 * WV) {
+    const int r = k / V, ch = k % V * 4;
     floatx4_t o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w)
+    for (int w = 0; w < WV; ++w)
       o += *reinterpret_cast<const floatx4_t*>(so + (w * 16 + r) * OS + ch);
-    if (a.splits > 1) {
-      const int64_t slot = (s * (gridDim.x / a.splits) + tile) * a.splits + split;
+    if (splits > 1) {
       *reinterpret_cast<floatx4_t*>(a.part + (slot * 16 + r) * D + ch) = o;
       float* ml = a.part + (int64_t)gridDim.y * gridDim.x * 16 * D + slot * 32;
       if (ch == 0) {
@@ -333,38 +596,109 @@ __global__ __launch_bounds__(64 * WAVES) void q4_attn_kernel(Q4View c, Q4AttnArg
   }
 }
 
-// The splits' sums of a tile of rows under one maximum.
+// The splits' sums of a tile of rows under one maximum.  A workgroup per tile: its
+// threads take rows x four channels, and share the splits where that leaves threads.
+constexpr int JT = 512;  // threads
 template <typename T, int D, bool LIST>
-__global__ __launch_bounds__(64 * WAVES) void q4_join_kernel(Q4View c, Q4AttnArgs a) {
-  const int64_t s = blockIdx.y, b = s / c.H, h = s % c.H, tile = blockIdx.x;
-  const int64_t slot0 = (s * gridDim.x + tile) * a.splits;
-  const float* ml = a.part + (int64_t)gridDim.y * gridDim.x * a.splits * 16 * D + slot0 * 32;
-  const float c2 = (float)(kLog2e / sqrt((double)D));
+__global__ __launch_bounds__(JT) void q4_join_kernel(Q4View c, Q4AttnArgs a) {
   constexpr int V = D / 4;
-  for (int i = threadIdx.x; i < 16 * V; i += 64 * WAVES) {
-    const int r = i / V, ch = i % V * 4;
-    float mall = kLowest;
-    for (int64_t p = 0; p < a.splits; ++p) mall = fmaxf(mall, ml[p * 32 + r]);
-    floatx4_t o = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.0f;
-    for (int64_t p = 0; p < a.splits; ++p) {
-      const float w = __builtin_amdgcn_exp2f((ml[p * 32 + r] - mall) * c2);
-      o += *reinterpret_cast<const floatx4_t*>(a.part + ((slot0 + p) * 16 + r) * D + ch) * w;
-      l += ml[p * 32 + 16 + r] * w;
-    }
-    store_row4<T, LIST>(a, b, h, tile, r, ch, o * (l > 0.0f ? 1.0f / l : 0.0f));
+  __shared__ float w[kQ4MaxSplits][16];  // the splits' factors
+  __shared__ float inv[16];
+  __shared__ floatx4_t part[JT];
+  const int b = blockIdx.y / c.H, h = blockIdx.y % c.H, tile = blockIdx.x;
+  const int splits = a.shape.splits;
+  int nrows, n;
+  int64_t slot0;
+  if (LIST) {
+    const int gt = (a.G + 15) / 16;
+    nrows = std::min(16, a.G - tile % gt * 16);
+    slot0 = ((int64_t)blockIdx.y * gridDim.x + tile) * splits;
+    n = splits;
+  } else {
+    nrows = std::min(16, a.tok.T * a.G - tile * 16);
+    int first;
+    Shares(c, a, tile, threadIdx.x & 63).of(c, b, &first, &n);
+    slot0 = ((int64_t)h * gridDim.x + tile) * c.B * splits + first;
   }
+  const int64_t slots = (int64_t)gridDim.y * gridDim.x * splits;
+  const float* ml = a.part + slots * 16 * D + slot0 * 32;
+  // rows x four channels: `ways` threads per item, split way, way + ways, ..; the first
+  // of them are on their way while the factors are formed
+  const int items = nrows * V;
+  const int ways = items >= JT ? 1 : JT / items;
+  const int span = JT / ways;
+  const int way = (int)threadIdx.x / span;
+  constexpr int EARLY = 4;
+  floatx4_t early[EARLY];
+#pragma unroll
+  for (int e = 0; e < EARLY; ++e) {
+    const int k = (int)threadIdx.x % span, p = way + e * ways;
+    early[e] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+    if (k < items && way < ways && p < n)
+      early[e] = *reinterpret_cast<const floatx4_t*>(a.part + ((slot0 + p) * 16 + k / V) * D +
+                                                     k % V * 4);
+  }
+  {
+    // JT / 16 threads per row
+    constexpr int RT = JT / 16;
+    const int r = threadIdx.x / RT, k = threadIdx.x % RT;
+    float mall = kLowest, l = 0.0f;
+    if (r < nrows) {
+      for (int p = k; p < n; p += RT) mall = fmaxf(mall, ml[p * 32 + r]);
+#pragma unroll
+      for (int x = 1; x < RT; x *= 2) mall = fmaxf(mall, __shfl_xor(mall, x));
+      for (int p = k; p < n; p += RT) {
+        const float f = __builtin_amdgcn_exp2f(ml[p * 32 + r] - mall);
+        w[p][r] = f;
+        l += ml[p * 32 + 16 + r] * f;
+      }
+#pragma unroll
+      for (int x = 1; x < RT; x *= 2) l += __shfl_xor(l, x);
+      if (k == 0) inv[r] = l > 0.0f ? 1.0f / l : 0.0f;
+    }
+  }
+  __syncthreads();
+  for (int k0 = 0; k0 < items; k0 += span) {
+    const int k = k0 + (int)threadIdx.x % span;
+    const int r = k / V, ch = k % V * 4;
+    floatx4_t o = {0.f, 0.f, 0.f, 0.f};
+    if (k < items && way < ways) {
+      int p = way;
+      if (k0 == 0)
+#pragma unroll
+        for (int e = 0; e < EARLY; ++e, p += ways)
+          if (p < n) o += early[e] * w[p][r];
+      const float* p0 = a.part + (slot0 * 16 + r) * D + ch;
+#pragma unroll 4
+      for (; p < n; p += ways)
+        o += *reinterpret_cast<const floatx4_t*>(p0 + (int64_t)p * 16 * D) * w[p][r];
+    }
+    if (ways > 1) {
+      part[threadIdx.x] = o;
+      __syncthreads();
+      if (way == 0 && k < items)
+        for (int x = 1; x < ways; ++x) o += part[threadIdx.x + x * span];
+    }
+    if (way == 0 && k < items) store_row4<T, LIST>(a, b, h, tile, r, ch, o * inv[r]);
+  }
+}
+
+template <typename T, int D, bool LIST, int WV>
+hipError_t attn(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
+  const int64_t tiles = q4_row_tiles(a.G, a.tok.T, LIST);
+  const int64_t splits = a.shape.splits;
+  const dim3 grid = LIST || splits == 1
+                        ? dim3((uint32_t)(tiles * splits), (uint32_t)(c.B * c.H))
+                        : dim3((uint32_t)(tiles * splits * c.B), (uint32_t)c.H);
+  q4_attn_kernel<T, D, LIST, WV><<<grid, 64 * WV, 0, st>>>(c, a);
+  return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t attn_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
-  const int64_t tiles = q4_row_tiles(a.G, a.tok.T, a.blocks != nullptr);
-  const dim3 grid((uint32_t)(tiles * a.splits), (uint32_t)(c.B * c.H));
-  if (a.blocks)
-    q4_attn_kernel<T, D, true><<<grid, 64 * WAVES, 0, st>>>(c, a);
-  else
-    q4_attn_kernel<T, D, false><<<grid, 64 * WAVES, 0, st>>>(c, a);
-  return hipGetLastError();
+  if (a.shape.waves == 8)
+    return a.blocks ? attn<T, D, true, 8>(c, a, st) : attn<T, D, false, 8>(c, a, st);
+  return a.blocks ? attn<T, D, true, 4>(c, a, st) : attn<T, D, false, 4>(c, a, st);
 }
 
 template <typename T, int D>
@@ -372,9 +706,9 @@ hipError_t join_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
   const dim3 grid((uint32_t)q4_row_tiles(a.G, a.tok.T, a.blocks != nullptr),
                   (uint32_t)(c.B * c.H));
   if (a.blocks)
-    q4_join_kernel<T, D, true><<<grid, 64 * WAVES, 0, st>>>(c, a);
+    q4_join_kernel<T, D, true><<<grid, JT, 0, st>>>(c, a);
   else
-    q4_join_kernel<T, D, false><<<grid, 64 * WAVES, 0, st>>>(c, a);
+    q4_join_kernel<T, D, false><<<grid, JT, 0, st>>>(c, a);
   return hipGetLastError();
 }
 

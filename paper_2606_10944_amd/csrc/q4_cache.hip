@@ -53,7 +53,8 @@ __global__ __launch_bounds__(THREADS) void q4_store_kernel(Q4View c, RowsView k,
                                                            Q4Tokens tok) {
   constexpr int LR = D / 8;           // lanes per row
   constexpr int RPP = THREADS / LR;   // rows per pass
-  const int64_t s = blockIdx.y, b = s / c.H, h = s % c.H;
+  const int64_t s = blockIdx.y;
+  const int b = blockIdx.y / c.H, h = blockIdx.y % c.H;
   const int64_t at = tok.at[b];
   int64_t cnt = tok.count ? tok.count[b] : tok.T;
   cnt = cnt < 0 ? 0 : (cnt > tok.T ? tok.T : cnt);
@@ -137,7 +138,7 @@ __global__ __launch_bounds__(THREADS) void q4_load_kernel(Q4View c, const int32_
   const int64_t s = blockIdx.y, t = blockIdx.x * (int64_t)(THREADS / LR) + threadIdx.x / LR;
   const int l = threadIdx.x % LR;
   if (t >= T_) return;
-  const int64_t r = (int64_t)at[s / c.H] + t;
+  const int64_t r = (int64_t)at[blockIdx.y / c.H] + t;
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
     uint32_t w[4] = {0, 0, 0, 0};
@@ -181,17 +182,18 @@ constexpr int SLANES = 8;  // lanes per block's bounds
 
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS) void q4_scores_kernel(Q4View c, Q4SelectArgs a) {
-  const int64_t s = blockIdx.y, b = s / c.H, h = s % c.H;
-  const int64_t t = a.t0 + blockIdx.x % a.tn, part = blockIdx.x / a.tn;
-  const int64_t nb = (c.n_max + kQ4Block - 1) / kQ4Block;
-  const int64_t last_row = q4_last_row(a.tok, b, t, c.n_max);
+  const int64_t s = blockIdx.y;
+  const int b = blockIdx.y / c.H, h = blockIdx.y % c.H;
+  const int t = a.t0 + blockIdx.x % a.tn, part = blockIdx.x / a.tn;
+  const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  const int last_row = q4_last_row(a.tok, b, t, c.n_max);
   if (last_row < 0) return;
-  const int64_t last = last_row / kQ4Block;
+  const int last = last_row / kQ4Block;
   __shared__ double sq[2 * D];  // q- beside lo, then q+ beside hi
   if (threadIdx.x < D) {
-    const T* q = static_cast<const T*>(a.q.p) + b * a.q.sb + h * a.G * a.q.sh + t * a.q.sr;
+    const T* q = static_cast<const T*>(a.q.p) + b * a.q.sb + (int64_t)h * a.G * a.q.sh + t * a.q.sr;
     double neg = 0.0, pos = 0.0;
-    for (int64_t g = 0; g < a.G; ++g) {
+    for (int g = 0; g < a.G; ++g) {
       const double x = (double)elem<T>(q + g * a.q.sh, threadIdx.x);
       if (!(x >= 0.0)) neg += x;  // (NaN here, and so in the score)
       if (x > 0.0) pos += x;
@@ -207,8 +209,8 @@ __global__ __launch_bounds__(THREADS) void q4_scores_kernel(Q4View c, Q4SelectAr
   for (int w = 0; w < W; ++w)
 #pragma unroll
     for (int i = 0; i < 8; ++i) q[w][i] = sq[(w * SLANES + j) * 8 + i];
-  const int64_t step = (int64_t)(gridDim.x / a.tn) * (THREADS / SLANES);
-  for (int64_t k = part * (THREADS / SLANES) + threadIdx.x / SLANES; k <= last; k += step) {
+  const int step = (int)(gridDim.x / a.tn) * (THREADS / SLANES);
+  for (int k = part * (THREADS / SLANES) + threadIdx.x / SLANES; k <= last; k += step) {
     const u32x4* p = reinterpret_cast<const u32x4*>(c.bounds + (s * nb + k) * 2 * D);
     double sum = 0.0;
 #pragma unroll
@@ -233,20 +235,21 @@ __global__ __launch_bounds__(THREADS) void q4_scores_kernel(Q4View c, Q4SelectAr
 // blocks.
 template <int W, int KPL>
 __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs a) {
-  const int64_t s = blockIdx.y, b = s / c.H, t = a.t0 + blockIdx.x;
-  const int64_t nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  const int64_t s = blockIdx.y;
+  const int b = blockIdx.y / c.H, t = a.t0 + blockIdx.x;
+  const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
   int32_t* out = a.blocks + (s * a.tok.T + t) * a.n_sel;
   const uint64_t* keys = a.scores + (s * a.tn + blockIdx.x) * nb;
-  const int64_t lr = q4_last_row(a.tok, b, t, c.n_max);
-  const int64_t n = lr < 0 ? 0 : lr / kQ4Block + 1;  // blocks that are there
+  const int lr = q4_last_row(a.tok, b, t, c.n_max);
+  const int n = lr < 0 ? 0 : lr / kQ4Block + 1;  // blocks that are there
   __shared__ int cnt[2][W];
   // a wave's keys are its KPL runs of 64 blocks
   uint64_t key[KPL];
-  const int64_t base = (int64_t)wave * KPL * 64;
+  const int base = wave * KPL * 64;
 #pragma unroll
   for (int i = 0; i < KPL; ++i) {
-    const int64_t k = base + i * 64 + lane;
+    const int k = base + i * 64 + lane;
     key[i] = 0;
     if (k < n) key[i] = k < a.n_sinks || k >= n - a.n_window ? ~0ull : keys[k];
   }
@@ -269,7 +272,7 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
   // least x with count(x) <= n_sel: the keys at least x stay, and of those equal
   // to x - 1 the lowest blocks as far as they fit
   uint64_t x = 1;
-  int above = (int)(n < a.n_sel ? n : a.n_sel);
+  int above = n < a.n_sel ? n : a.n_sel;
   if (n > a.n_sel) {
     uint64_t lo = 1, hi = ~0ull;  // count(lo) > n_sel >= count(hi): sinks and window fit
     above = count(hi);
@@ -286,7 +289,7 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
     }
     x = hi;
   }
-  int ties = (int)((n < a.n_sel ? n : a.n_sel) - above);  // keys equal to x - 1 that stay
+  const int ties = (n < a.n_sel ? n : a.n_sel) - above;  // keys equal to x - 1 that stay
   // places in order: waves, then runs of 64
   const uint64_t below = (1ull << lane) - 1;
   int nabove = 0, nties = 0;
@@ -315,12 +318,12 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
     const int before = pt + __popcll(mt & below);
     // ties that stay before this one: min(before, ties)
     const int place = pa + __popcll(mi & below) + (before < ties ? before : ties);
-    if (in || (tie && before < ties)) out[place] = (int32_t)(base + i * 64 + lane);
+    if (in || (tie && before < ties)) out[place] = base + i * 64 + lane;
     pa += __popcll(mi);
     pt += __popcll(mt);
   }
-  const int64_t used = n < a.n_sel ? n : a.n_sel;
-  for (int64_t i = used + threadIdx.x; i < a.n_sel; i += 64 * W) out[i] = -1;
+  const int used = n < a.n_sel ? n : a.n_sel;
+  for (int i = used + (int)threadIdx.x; i < a.n_sel; i += 64 * W) out[i] = -1;
 }
 
 template <typename T, int D>
@@ -342,7 +345,7 @@ hipError_t load_d(const Q4View& c, const int32_t* at, int64_t T_, void* k, void*
 template <typename T, int D>
 hipError_t scores_d(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
   const int64_t nb = (c.n_max + kQ4Block - 1) / kQ4Block;
-  const int64_t rows = c.B * c.H * a.tn, per = THREADS / SLANES;
+  const int64_t rows = (int64_t)c.B * c.H * a.tn, per = THREADS / SLANES;
   int64_t x = (nb + per - 1) / per;
   const int64_t most = (4096 + rows - 1) / rows;  // workgroups enough to fill the device
   if (x > most) x = most;

@@ -49,10 +49,11 @@ __device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float* f) {
 
 // The last cached row that token t of batch entry b sees (its own); -1 for a
 // token that is not there or stands before row 0.
-__device__ __forceinline__ int64_t q4_last_row(const Q4Tokens& tok, int64_t b, int64_t t,
-                                               int64_t n_max) {
+__device__ __forceinline__ int q4_last_row(const Q4Tokens& tok, int b, int t, int n_max) {
   if (tok.count && t >= tok.count[b]) return -1;
-  const int64_t r = (int64_t)tok.at[b] + t;
+  int at = tok.at[b];
+  at = at > n_max ? n_max : (at < -kQ4MaxTokens ? -kQ4MaxTokens : at);  // t < kQ4MaxTokens
+  const int r = at + t;
   return r < 0 ? -1 : (r < n_max ? r : n_max - 1);
 }
 
