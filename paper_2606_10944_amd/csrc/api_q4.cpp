@@ -72,17 +72,19 @@ int64_t group_of(int64_t q_heads, int64_t H) {
 
 struct AttnPlan {
   thin::Q4AttnShape shape;
-  size_t bytes;
+  size_t bytes, sums;
 };
 
 bool plan_attention(int64_t B, int64_t H, int64_t q_heads, int64_t n_max, int64_t d, int64_t T,
-                    int64_t n_sel, AttnPlan* p) {
+                    int64_t n_sel, bool bf16, AttnPlan* p) {
   if (!valid_sizes(B, H, n_max, T) || !supported_d(d) || !group_of(q_heads, H) || n_sel < 0 ||
       n_sel > 32768)
     return false;
   const int64_t tiles = thin::q4_row_tiles(q_heads / H, T, n_sel > 0);
-  p->shape = thin::q4_attention_shape(B, H, tiles, n_sel > 0 ? n_sel * THIN_Q4_BLOCK : n_max);
-  p->bytes = thin::q4_attention_bytes(B * H, tiles, p->shape.splits, d);
+  p->shape = thin::q4_attention_shape(B, H, q_heads / H, T, n_sel > 0,
+                                      n_sel > 0 ? n_sel * THIN_Q4_BLOCK : n_max, bf16);
+  p->bytes = thin::q4_attention_bytes(B, H, tiles, p->shape.splits, d);
+  p->sums = thin::q4_sums_bytes(B, H, tiles, p->shape.splits, d);
   return tiles <= kMaxGroups;  // (B * tiles * splits is at most 2048 where splits > 1)
 }
 
@@ -236,9 +238,12 @@ int thin_q4_select(const thin_q4_cache_t* cache, const void* Q, const int64_t* q
 int thin_q4_attention_plan(int64_t B, int64_t H, int64_t q_heads, int64_t n_max, int64_t d,
                            int64_t T, int64_t n_sel, size_t* workspace_bytes) {
   AttnPlan p;
-  if (!workspace_bytes || !plan_attention(B, H, q_heads, n_max, d, T, n_sel, &p))
-    return THIN_EINVAL;
-  *workspace_bytes = p.bytes;
+  if (!workspace_bytes) return THIN_EINVAL;
+  *workspace_bytes = 0;
+  for (const bool bf16 : {false, true}) {  // the larger of the two types'
+    if (!plan_attention(B, H, q_heads, n_max, d, T, n_sel, bf16, &p)) return THIN_EINVAL;
+    if (p.bytes > *workspace_bytes) *workspace_bytes = p.bytes;
+  }
   return THIN_OK;
 }
 
@@ -253,7 +258,7 @@ int thin_q4_attention(const thin_q4_cache_t* cache, const void* Q, const int64_t
   if (!known_dtype(dtype)) return THIN_EDTYPE;
   AttnPlan p;
   if (!at || (blocks != nullptr) != (n_sel > 0) ||
-      !plan_attention(c.B, c.H, q_heads, c.n_max, cache->d, T, n_sel, &p))
+      !plan_attention(c.B, c.H, q_heads, c.n_max, cache->d, T, n_sel, dtype == THIN_BF16, &p))
     return THIN_EINVAL;
   thin::Q4AttnArgs a{};
   rc = rows_view(Q, q_strides, c.B, q_heads, T, cache->d, dtype, false, &a.q);
@@ -266,10 +271,15 @@ int thin_q4_attention(const thin_q4_cache_t* cache, const void* Q, const int64_t
   a.blocks = blocks;
   a.n_sel = (int32_t)n_sel;
   a.shape = p.shape;
-  a.part = static_cast<float*>(workspace);
+  if (p.bytes) {
+    a.part = static_cast<float*>(workspace);
+    a.table = reinterpret_cast<int2*>(static_cast<char*>(workspace) + p.sums);
+  }
   hipStream_t st = static_cast<hipStream_t>(stream);
-  hipError_t e = observed(THIN_KERNEL_Q4_ATTENTION, -1, st,
-                          [&] { return thin::launch_q4_attention(dtype, cache->d, c, a, st); });
+  hipError_t e = observed(THIN_KERNEL_Q4_ATTENTION, -1, st, [&] {
+    return p.shape.waves == 0 ? thin::launch_q4_prompt(dtype, cache->d, c, a, st)
+                              : thin::launch_q4_attention(dtype, cache->d, c, a, st);
+  });
   if (e == hipSuccess && p.shape.splits > 1)
     e = observed(THIN_KERNEL_Q4_ATTENTION, -1, st,
                  [&] { return thin::launch_q4_join(dtype, cache->d, c, a, st); });

@@ -71,10 +71,16 @@ struct Q4AttnArgs {
   const int32_t* blocks;  // null: every cached row
   int32_t n_sel;
   Q4AttnShape shape;
-  float* part;  // shape.splits > 1: [slot, 16, d] sums, then [slot, 2, 16] maxima and sums
+  // shape.splits > 1: [slot, 16, d] sums, then [slot, 2, 16] maxima and sums; where the
+  // slots follow the sequences' lengths, the first and the number of each sequence's
+  // ([tile, B], the same for every head)
+  float* part;
+  int2* table;
 };
 hipError_t launch_q4_attention(int dtype, int64_t d, const Q4View& c, const Q4AttnArgs& a,
                                hipStream_t st);
+hipError_t launch_q4_prompt(int dtype, int64_t d, const Q4View& c, const Q4AttnArgs& a,
+                            hipStream_t st);
 hipError_t launch_q4_join(int dtype, int64_t d, const Q4View& c, const Q4AttnArgs& a,
                           hipStream_t st);
 

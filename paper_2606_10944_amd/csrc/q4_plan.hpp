@@ -17,9 +17,12 @@ inline int64_t q4_row_tiles(int64_t G, int64_t T, bool list) {
   return list ? T * ((G + 15) / 16) : (T * G + 15) / 16;
 }
 
+// Query rows of a workgroup of the kernel for many of them.
+constexpr int64_t q4_prompt_rows(bool bf16) { return bf16 ? 128 : 64; }
+
 // Workgroups of an attention launch.
 struct Q4AttnShape {
-  int32_t waves;   // per workgroup
+  int32_t waves;   // per workgroup; 0: the kernel for many query rows
   int32_t splits;  // workgroups per tile (list), or per tile on average over the sequences
   int32_t least;   // steps of 32 keys that a workgroup takes at least
 };
@@ -29,8 +32,11 @@ struct Q4AttnShape {
 // last of them run alone).  Up to 2048 keys one workgroup of eight waves takes them all:
 // no second launch to join sums.  Long caches of more slices are shared out in two, so
 // that one long sequence among short ones is not left to one workgroup per head.
-inline Q4AttnShape q4_attention_shape(int64_t B, int64_t H, int64_t tiles, int64_t keys) {
-  const int64_t groups = B * H * tiles;
+inline Q4AttnShape q4_attention_shape(int64_t B, int64_t H, int64_t G, int64_t T, bool list,
+                                      int64_t keys, bool bf16) {
+  const int64_t per = q4_prompt_rows(bf16), prompt = B * H * ((T * G + per - 1) / per);
+  if (!list && prompt >= 256) return {0, 1, 1};
+  const int64_t groups = B * H * q4_row_tiles(G, T, list);
   if (keys <= 2048 || groups > 1024 || B > kQ4SharedEntries) return {groups > 511 ? 4 : 8, 1, 1};
   const int64_t steps = (keys + kQ4Step - 1) / kQ4Step;
   int64_t splits = 512 / groups;
@@ -42,9 +48,13 @@ inline Q4AttnShape q4_attention_shape(int64_t B, int64_t H, int64_t tiles, int64
   return {4, (int32_t)splits, (int32_t)least};
 }
 
-// Bytes of the splits' sums: a slot of [16, d] float32, maxima and sums of 16 rows.
-inline size_t q4_attention_bytes(int64_t slices, int64_t tiles, int64_t splits, int64_t d) {
-  return splits > 1 ? (size_t)(slices * tiles * splits) * (16 * d + 32) * 4 : 0;
+// Bytes of the splits' sums (a slot of [16, d] float32, maxima and sums of 16 rows), and of
+// them with the table of slots behind.
+inline size_t q4_sums_bytes(int64_t B, int64_t H, int64_t tiles, int64_t splits, int64_t d) {
+  return (size_t)(B * H * tiles * splits) * (16 * d + 32) * 4;
+}
+inline size_t q4_attention_bytes(int64_t B, int64_t H, int64_t tiles, int64_t splits, int64_t d) {
+  return splits > 1 ? q4_sums_bytes(B, H, tiles, splits, d) + (size_t)(tiles * B) * 8 : 0;
 }
 
 // Tokens whose block scores a selection holds at a time: 64 MiB of them, at least one

@@ -1,0 +1,237 @@
+// Attention over the 4-bit key/value cache on gfx950 for many query rows of a slice (a
+// prompt or a chunk of one): causal over every cached row.
+//
+// A workgroup of four waves takes 64 RT query rows, RT tiles of 16 per wave, and walks
+// the cached rows 64 at a time.  Its threads bring codes to LDS once for all of them:
+// keys as stored, values decoded, one 16-byte word of each per thread, while the
+// tile before is worked on.  Against the kernel for few rows, a value row is decoded
+// once per 64 RT query rows instead of once per 16, and each operand read from LDS
+// serves RT products.
+#include "q4_attn_device.hpp"
+
+namespace thin {
+
+namespace {
+
+constexpr int PW = 4;    // waves
+constexpr int PK = 64;   // cached rows per tile
+
+template <typename T, int D, int RT>
+__global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnArgs a) {
+  constexpr bool MX = Elem<T>::bytes == 2;
+  constexpr int NP = MX ? 1 : 3;                  // bf16 parts of the weights
+  constexpr int GR = D / 32;                      // groups per row
+  constexpr int KW = (MX ? 16 : D / 8) / 4;       // words of a key row that a lane feeds
+  constexpr int ROWS = 16 * RT;                   // query rows of a wave
+  struct Stage {
+    unsigned char v[PK * kVStride<D>];
+    uint32_t k[PK * D / 8];
+    uint8_t ks[PK * GR];
+  };
+  __shared__ __align__(16) Stage stage[2];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = lane & 15, g = lane >> 4;
+
+  // Every XCD takes a contiguous eighth of the tiles, slice by slice, so that its L2
+  // holds few slices; a slice's last tiles, which see the most rows, come first.
+  const int tiles = gridDim.x;
+  int b, h, tile;
+  {
+    const uint32_t l = blockIdx.y * gridDim.x + blockIdx.x, n = gridDim.x * gridDim.y;
+    const uint32_t x = l % 8, i = x * (n / 8) + (x < n % 8 ? x : n % 8) + l / 8;
+    const int s = i / tiles;
+    b = s / c.H;
+    h = s % c.H;
+    tile = tiles - 1 - (int)(i % tiles);
+  }
+  const int nrows = a.tok.T * a.G;
+  const int r0 = tile * (ROWS * PW);  // the workgroup's first query row
+  const int cnt = a.tok.count ? std::min(a.tok.count[b], a.tok.T) : a.tok.T;
+  // the last cached row that query rows up to r see
+  auto seen = [&](int r) {
+    const int t = std::min(std::min(r, nrows - 1) / a.G, cnt - 1);
+    return t < 0 ? -1 : q4_last_row(a.tok, b, t, c.n_max);
+  };
+  const int last = __builtin_amdgcn_readfirstlane(r0 / a.G < cnt ? seen(r0 + ROWS * PW - 1) : -1);
+  const int w0 = r0 + wave * ROWS;
+  const int wlast =
+      __builtin_amdgcn_readfirstlane(w0 < nrows && w0 / a.G < cnt ? seen(w0 + ROWS - 1) : -1);
+
+  int qlast[RT];
+  int all = 0x7fffffff;  // rows up to here are seen by every query of the wave
+  Queries<T, D> q[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = w0 + rt * 16 + m;
+    const bool there = r < nrows;
+    const int t = there ? r / a.G : 0, head = there ? r % a.G : 0;
+    qlast[rt] = there ? q4_last_row(a.tok, b, t, c.n_max) : -1;
+    if (there) all = std::min(all, qlast[rt]);
+    q[rt].load(there ? static_cast<const T*>(a.q.p) + b * a.q.sb +
+                           ((int64_t)h * a.G + head) * a.q.sh + t * a.q.sr
+                     : nullptr,
+               g);
+  }
+#pragma unroll
+  for (int x = 1; x < 16; x *= 2) all = std::min(all, __shfl_xor(all, x));
+  all = __builtin_amdgcn_readfirstlane(all);
+
+  // this thread's word of a tile: row and group
+  const int srow = threadIdx.x / GR, sgr = threadIdx.x % GR;
+  const bool stages = srow < PK;
+  const Slice rows = slice_of<D>(c, (int64_t)b * c.H + h);
+  u32x4 kw, vw;
+  uint32_t kb, vb;
+  auto load = [&](int row0) __attribute__((always_inline)) {
+    const uint32_t r = std::min(row0 + srow, last);
+    kw = *reinterpret_cast<const u32x4*>(rows.kc + (r * (D / 2) + sgr * 16));
+    kb = rows.ks[r * GR + sgr];
+    vw = *reinterpret_cast<const u32x4*>(rows.vc + (r * (D / 2) + sgr * 16));
+    vb = rows.vs[r * GR + sgr];
+  };
+  auto put = [&](Stage& to) __attribute__((always_inline)) {
+    if (!stages) return;
+    *reinterpret_cast<u32x4*>(to.k + (srow * GR + sgr) * 4) = kw;
+    to.ks[srow * GR + sgr] = (uint8_t)kb;
+    const float scale = q4_scale(vb);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t w[4];
+      decode8(vw[i], scale, w);
+      *reinterpret_cast<u32x4*>(to.v + srow * kVStride<D> + sgr * 64 + i * 16) =
+          (u32x4){w[0], w[1], w[2], w[3]};
+    }
+  };
+
+  const float c2 = (float)(kQ4Log2e / sqrt((double)D));
+  float mrun[RT], lrun[RT];
+  floatx4_t acc[RT][D / 16];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    mrun[rt] = kLowest;
+    lrun[rt] = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) acc[rt][dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+  }
+
+  if (last >= 0) {
+    load(0);
+    put(stage[0]);
+    load(PK);
+    __syncthreads();
+  }
+  for (int row0 = 0, i = 0; row0 <= last; row0 += PK, i ^= 1) {
+    Stage& now = stage[i];
+    put(stage[i ^ 1]);  // (the tile before, which lay there, is behind the barrier)
+    load(row0 + 2 * PK);
+    if (row0 <= wlast) {
+      float sc[RT][PK / 4];
+#pragma unroll
+      for (int kt = 0; kt < PK / 16; ++kt) {
+        const int key = kt * 16 + m;
+        uint32_t kc[KW], byte;
+        if constexpr (MX) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(now.k + (key * GR + g % GR) * 4);
+          kc[0] = w[0]; kc[1] = w[1]; kc[2] = w[2]; kc[3] = w[3];
+          byte = now.ks[key * GR + g % GR];
+        } else {
+#pragma unroll
+          for (int w = 0; w < KW; ++w) kc[w] = now.k[key * (D / 8) + g * KW + w];
+          byte = now.ks[key * GR + g * GR / 4];
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const floatx4_t z = q[rt].scores(kc, byte);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sc[rt][kt * 4 + j] = z[j];
+        }
+      }
+      if (row0 + PK - 1 > all) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int j = 0; j < PK / 4; ++j)
+            if (row0 + j / 4 * 16 + 4 * g + j % 4 > qlast[rt]) sc[rt][j] = -INFINITY;
+      }
+      bf16x8_t pp[RT][PK / 32][NP];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float mx = sc[rt][0];
+#pragma unroll
+        for (int j = 1; j < PK / 4; ++j) mx = fmaxf(mx, sc[rt][j]);
+        mx *= c2;
+        if (__any(mx > mrun[rt] + kSlack)) {
+          mx = fmaxf(mx, __shfl_xor(mx, 16));
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          const float mnew = fmaxf(mrun[rt], mx);
+          const float scale = __builtin_amdgcn_exp2f(mrun[rt] - mnew);
+          mrun[rt] = mnew;
+          lrun[rt] *= scale;
+#pragma unroll
+          for (int dt = 0; dt < D / 16; ++dt) acc[rt][dt] *= scale;
+        }
+#pragma unroll
+        for (int j = 0; j < PK / 4; ++j) {
+          sc[rt][j] = __builtin_amdgcn_exp2f(fmaf(sc[rt][j], c2, -mrun[rt]));
+          lrun[rt] += sc[rt][j];
+        }
+#pragma unroll
+        for (int ch = 0; ch < PK / 32; ++ch) split8<NP>(sc[rt] + ch * 8, pp[rt][ch]);
+      }
+#pragma unroll
+      for (int ch = 0; ch < PK / 32; ++ch)
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) {
+          const bf16x8_t vf = value_columns<D>(now.v + ch * 32 * kVStride<D>, dt, m, g);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int p = NP - 1; p >= 0; --p)
+              acc[rt][dt] =
+                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[rt][ch][p], acc[rt][dt], 0, 0, 0);
+        }
+    }
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    float l = lrun[rt];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const int r = w0 + rt * 16 + m;
+    if (r >= nrows) continue;
+    T* p = static_cast<T*>(const_cast<void*>(a.o.p)) + b * a.o.sb +
+           ((int64_t)h * a.G + r % a.G) * a.o.sh + r / a.G * a.o.sr + 4 * g;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) {
+      const floatx4_t o = acc[rt][dt] * inv;
+      if constexpr (MX)
+        *reinterpret_cast<uint2*>(p + dt * 16) =
+            make_uint2(cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]));
+      else
+        *reinterpret_cast<floatx4_t*>(p + dt * 16) = o;
+    }
+  }
+}
+
+template <typename T, int D>
+hipError_t prompt_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
+  constexpr int RT = Elem<T>::bytes == 2 ? 2 : 1;
+  static_assert(16 * RT * PW == q4_prompt_rows(Elem<T>::bytes == 2), "rows of a workgroup");
+  const int64_t tiles = ((int64_t)a.tok.T * a.G + 16 * RT * PW - 1) / (16 * RT * PW);
+  const dim3 grid((uint32_t)tiles, (uint32_t)(c.B * c.H));
+  q4_prompt_kernel<T, D, RT><<<grid, 64 * PW, 0, st>>>(c, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_q4_prompt(int dtype, int64_t d, const Q4View& c, const Q4AttnArgs& a,
+                            hipStream_t st) {
+  Q4_BY_D(prompt_d, c, a, st);
+}
+
+}  // namespace thin

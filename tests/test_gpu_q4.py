@@ -339,6 +339,55 @@ def check_attention(c, q, at, count, blocks, got, dtype, tokens=None):
                 assert ((o - want).abs() <= attention_bound(want, A, S, dtype)).all(), (b, h, t)
 
 
+def check_dense(c, q, at, count, got, dtype):
+    """check_attention without lists, a slice at a time."""
+    B, Hq, T, d = q.shape
+    G = Hq // c.H
+    got = got.cpu().double()
+    for b in range(B):
+        last = torch.arange(T) + at[b]
+        last = torch.where(torch.arange(T) < (T if count is None else count[b]),
+                           last.clamp(max=c.n_max - 1), -1)
+        n = max(0, int(last.max()) + 1)
+        w = (torch.arange(n) <= last.unsqueeze(1)).double().repeat(G, 1)  # [G * T, n]
+        for h in range(c.H):
+            o = got[b, h * G:(h + 1) * G].reshape(G * T, d)
+            if n == 0:
+                assert (o == 0).all()
+                continue
+            want, A, S = ref.attention(q[b, h * G:(h + 1) * G].reshape(G * T, d),
+                                       ref.cached(c.k_codes[b, h, :n], c.k_scales[b, h, :n]),
+                                       ref.cached(c.v_codes[b, h, :n], c.v_scales[b, h, :n]), w)
+            ok = (o - want).abs() <= attention_bound(want, A, S, dtype)
+            assert ok.all(), (b, h, (~ok).nonzero()[:3].tolist())
+
+
+# Enough query rows for the kernel that shares decoded rows: 256 workgroups of 128 (64
+# float32) rows, the last one of a slice partly filled.
+PROMPT = [
+    (128, 4, 16, 4, 130, 700, [0, 300, 570, 650], None),
+    (64, 8, 8, 1, 513, 600, [0, 5, 87, -20, 60, 300, 1, 80], [513, 500, 0, 400, 1, 300, 129, 64]),
+    (32, 16, 16, 16, 9, 300, list(range(0, 288, 18)), None),
+    (128, 2, 50, 3, 171, 171, [0, 0], [171, 100]),
+    (64, 43, 2, 7, 55, 200, [3 * b for b in range(43)], None),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d,B,H,G,T,n_max,at,count", PROMPT)
+def test_attention_of_prompts(dtype, d, B, H, G, T, n_max, at, count):
+    g = gen(20)
+    rows = [max(0, min(n_max, a + T)) for a in at]
+    c = filled(g, B, H, n_max, d, rows)
+    q = randn(g, B, H * G, T, d, dtype=dtype)
+    o = strided(torch.zeros_like(q))
+    got = thin_q4_attention(strided(q), c, i32(at), count=None if count is None else i32(count),
+                            O=o)
+    check_dense(c, q, at, count, got, dtype)
+    again = thin_q4_attention(q.to(DEV), c, i32(at), count=None if count is None else i32(count))
+    assert torch.equal(again, got)
+
+
 ATT = [
     # d, B, H, G, T, n_max, at, count
     (128, 1, 1, 1, 1, 1, [0], None),
