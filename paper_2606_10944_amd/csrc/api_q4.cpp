@@ -191,7 +191,9 @@ int thin_q4_load(const thin_q4_cache_t* cache, int64_t T, const int32_t* at, voi
 int thin_q4_select_plan(int64_t B, int64_t H, int64_t n_max, int64_t T, size_t* workspace_bytes) {
   if (!workspace_bytes || !valid_sizes(B, H, n_max, T)) return THIN_EINVAL;
   const int64_t nb = blocks_of(n_max);
-  *workspace_bytes = (size_t)(B * H * nb * thin::q4_select_tokens(B * H, nb, T)) * 8;
+  *workspace_bytes = thin::q4_select_fused(B * H, nb, T)
+                         ? 0
+                         : (size_t)(B * H * nb * thin::q4_select_tokens(B * H, nb, T)) * 8;
   return THIN_OK;
 }
 
@@ -213,7 +215,8 @@ int thin_q4_select(const thin_q4_cache_t* cache, const void* Q, const int64_t* q
   thin::Q4SelectArgs a{};
   rc = rows_view(Q, q_strides, c.B, q_heads, T, cache->d, dtype, false, &a.q);
   if (rc) return rc;
-  if (!workspace || workspace_bytes < need || !aligned16(workspace)) return THIN_EWORKSPACE;
+  if (need && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+    return THIN_EWORKSPACE;
   a.G = (int32_t)group_of(q_heads, c.H);
   a.tok = {at, count, (int32_t)T};
   a.n_sel = (int32_t)n_sel;
@@ -221,9 +224,14 @@ int thin_q4_select(const thin_q4_cache_t* cache, const void* Q, const int64_t* q
   a.n_window = (int32_t)n_window;
   a.blocks = blocks;
   a.scores = static_cast<uint64_t*>(workspace);
-  const int64_t step = thin::q4_select_tokens((int64_t)c.B * c.H, blocks_of(c.n_max), T);
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
+  if (thin::q4_select_fused((int64_t)c.B * c.H, blocks_of(c.n_max), T)) {
+    e = observed(THIN_KERNEL_Q4_SELECT, -1, st,
+                 [&] { return thin::launch_q4_select(dtype, cache->d, c, a, st); });
+    return e == hipSuccess ? THIN_OK : THIN_EHIP;
+  }
+  const int64_t step = thin::q4_select_tokens((int64_t)c.B * c.H, blocks_of(c.n_max), T);
   for (int64_t t0 = 0; t0 < T && e == hipSuccess; t0 += step) {
     a.t0 = (int32_t)t0;
     a.tn = (int32_t)(T - t0 < step ? T - t0 : step);

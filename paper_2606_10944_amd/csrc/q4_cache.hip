@@ -9,6 +9,7 @@
 #include "common.hpp"
 #include "q4.hpp"
 #include "q4_device.hpp"
+#include "q4_attn_device.hpp"
 
 namespace thin {
 
@@ -326,6 +327,261 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
   for (int i = used + (int)threadIdx.x; i < a.n_sel; i += 64 * W) out[i] = -1;
 }
 
+// Selection for several tokens of a slice in one launch.  A workgroup takes 16 tokens:
+// their scores of every block come from the bf16 matrix instructions, the queries'
+// float64 sums split into three bf16 parts (24 bits; bounds are bf16), and stay in LDS.
+// Such a score is off by less than eps = 2^-16 qsum bmax (qsum = sum_gc |q_gc|, bmax the
+// largest bound: 24 sums of 32 products, each within 2^-21.6 of the sum of magnitudes,
+// and 2^-27 of the split).  So a block more than 2 eps above the last one that fits is
+// in, one more than 2 eps below it is out, whatever the rounding; the others between
+// (mostly that one alone) are scored again in float64.
+//
+// 2047 tokens x 8 key heads over up to 512 blocks, d = 128: 8e6 scores of 256 products,
+// 62 us in float64 at the rate of a large float64 matrix product.
+
+// A float's key: integers of the same order, NaN below everything, 0 left free.
+__device__ __forceinline__ uint32_t float_key(float f) {
+  if (f != f) return 1;
+  const uint32_t u = __float_as_uint(f + 0.0f);
+  const uint32_t k = (u >> 31) ? ~u : u | 0x80000000u;
+  return k < 2 ? 2 : k;
+}
+__device__ __forceinline__ float key_float(uint32_t k) {
+  return __uint_as_float((k >> 31) ? k & 0x7fffffffu : ~k);
+}
+
+// Of the keys of a wave (key i of lane l stands at place 64 i + l) the largest `want`,
+// ties to the lowest places: bit i of the result says whether this lane's key i is one.
+// Keys of 0 are none; there are at least `want` others.
+template <typename K, int KPL>
+__device__ __forceinline__ uint32_t largest(const K* key, int want, int lane) {
+  K lo = ~(K)0, hi = 0;
+#pragma unroll
+  for (int i = 0; i < KPL; ++i) {
+    if (key[i] != 0 && key[i] < lo) lo = key[i];
+    if (key[i] > hi) hi = key[i];
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    const K a = __shfl_xor(lo, m), b = __shfl_xor(hi, m);
+    lo = a < lo ? a : lo;
+    hi = b > hi ? b : hi;
+  }
+  auto count = [&](K x) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) n += __popcll(__ballot(key[i] >= x));
+    return n;
+  };
+  // least x in (lo, hi + 1] with count(x) <= want; hi + 1 overflows at most to 0: a key of
+  // all ones does not occur
+  int above = 0;
+  hi += 1;
+  if (count(lo) <= want) {
+    hi = lo;
+    above = want;
+  }
+  while (hi - lo > 1) {
+    const K mid = lo + (hi - lo) / 2;
+    const int n = count(mid);
+    if (n > want) {
+      lo = mid;
+    } else {
+      hi = mid;
+      above = n;
+      if (n == want) break;
+    }
+  }
+  int ties = want - above;  // keys equal to lo that are in
+  uint32_t in = 0;
+#pragma unroll
+  for (int i = 0; i < KPL; ++i) {
+    const bool tie = key[i] == lo && lo < hi;
+    const uint64_t t = __ballot(tie);
+    const int before = __popcll(t & ((1ull << lane) - 1));
+    if (key[i] != 0 && (key[i] >= hi || (tie && before < ties))) in |= 1u << i;
+    const int taken = __popcll(t);
+    ties -= taken < ties ? taken : ties;
+  }
+  return in;
+}
+
+template <typename T, int D, int KPL>
+__global__ __launch_bounds__(THREADS) void q4_select_kernel(Q4View c, Q4SelectArgs a, int stride) {
+  constexpr int KS = 2 * D / 32;  // k-steps: q- beside lo, then q+ beside hi
+  extern __shared__ __align__(16) float score[];  // [16, stride]
+  __shared__ uint32_t smax[4];
+  const int64_t s = blockIdx.y;
+  const int b = blockIdx.y / c.H, h = blockIdx.y % c.H, t0 = blockIdx.x * 16;
+  const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const T* qh = static_cast<const T*>(a.q.p) + b * a.q.sb + (int64_t)h * a.G * a.q.sh;
+  const uint16_t* bounds = c.bounds + s * nb * 2 * D;
+
+  // the last block that any of the tokens sees
+  int most = t0 + m < a.tok.T ? q4_last_row(a.tok, b, t0 + m, c.n_max) : -1;
+#pragma unroll
+  for (int x = 1; x < 16; x *= 2) most = std::max(most, __shfl_xor(most, x));
+  const int blocks = most < 0 ? 0 : most / kQ4Block + 1;
+
+  // lane (m, g): token m's channels of words 4 i + g
+  bf16x8_t q[KS][3];
+  float qsum = 0.0f;
+  const bool there = t0 + m < a.tok.T;
+#pragma unroll
+  for (int i = 0; i < KS / 2; ++i) {
+    double neg[8], pos[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) neg[j] = pos[j] = 0.0;
+    if (there)
+      for (int x = 0; x < a.G; ++x) {
+        float f[8];
+        load8<T>(qh + x * a.q.sh + (int64_t)(t0 + m) * a.q.sr + (4 * i + g) * 8, f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (!(f[j] >= 0.0f)) neg[j] += (double)f[j];
+          if (f[j] > 0.0f) pos[j] += (double)f[j];
+          qsum += fabsf(f[j]);
+        }
+      }
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      float fn[8], fp[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        fn[j] = (float)(__bf16)(float)neg[j];
+        fp[j] = (float)(__bf16)(float)pos[j];
+        neg[j] -= (double)fn[j];
+        pos[j] -= (double)fp[j];
+      }
+      split8<1>(fn, &q[i][p]);
+      split8<1>(fp, &q[i + KS / 2][p]);
+    }
+  }
+  qsum += __shfl_xor(qsum, 16);
+  qsum += __shfl_xor(qsum, 32);
+
+  uint32_t bmax = 0;  // largest magnitude of a bound, as bf16 bits
+  for (int k0 = wave * 16; k0 < blocks; k0 += 64) {
+    const int k = std::min(k0 + m, nb - 1);
+    const u32x4* row = reinterpret_cast<const u32x4*>(bounds + (int64_t)k * 2 * D);
+    floatx4_t z = {0.f, 0.f, 0.f, 0.f};
+    u32x4 w[KS];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) w[i] = row[4 * i + g];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = w[i][j] & 0x7fffu, hi = (w[i][j] >> 16) & 0x7fffu;
+        if (k0 + m < blocks) bmax = std::max(bmax, std::max(lo, hi));
+      }
+#pragma unroll
+      for (int p = 2; p >= 0; --p)
+        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w[i]), q[i][p], z,
+                                                    0, 0, 0);
+    }
+    *reinterpret_cast<floatx4_t*>(score + m * stride + k0 + 4 * g) = z;
+  }
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) bmax = std::max(bmax, (uint32_t)__shfl_xor((int)bmax, x));
+  if (lane == 0) smax[wave] = bmax;
+  __syncthreads();
+  bmax = std::max(std::max(smax[0], smax[1]), std::max(smax[2], smax[3]));
+
+  for (int r = wave; r < 16; r += 4) {
+    const int t = t0 + r;
+    if (t >= a.tok.T) break;
+    int32_t* out = a.blocks + (s * a.tok.T + t) * a.n_sel;
+    const int lr = q4_last_row(a.tok, b, t, c.n_max);
+    const int n = lr < 0 ? 0 : lr / kQ4Block + 1;  // blocks that are there
+    const int want = n < a.n_sel ? n : a.n_sel;
+    uint32_t in = 0;  // bit i: block 64 i + lane is taken
+    if (n <= a.n_sel) {
+#pragma unroll
+      for (int i = 0; i < KPL; ++i)
+        if (i * 64 + lane < n) in |= 1u << i;
+    } else {
+      uint32_t key[KPL];
+      int forced = 0;  // sinks and window
+#pragma unroll
+      for (int i = 0; i < KPL; ++i) {
+        const int k = i * 64 + lane;
+        const bool f = k < n && (k < a.n_sinks || k >= n - a.n_window);
+        if (f) in |= 1u << i;
+        forced += __popcll(__ballot(f));
+        key[i] = k < n && !f ? float_key(score[r * stride + k]) : 0;
+      }
+      const int free = want - forced;
+      if (free > 0) {
+        uint32_t best = largest<uint32_t, KPL>(key, free, lane);
+        uint32_t least = ~0u;  // of the chosen keys
+#pragma unroll
+        for (int i = 0; i < KPL; ++i)
+          if ((best >> i & 1) && key[i] < least) least = key[i];
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) least = std::min(least, (uint32_t)__shfl_xor((int)least, x));
+        // 2 eps (at least what products below the normal numbers can make); not a number or
+        // infinite: every block is scored again
+        const float size = __shfl(qsum, r) * __uint_as_float(bmax << 16);
+        const float eps = fmaxf(0x1p-15f * size, 0x1p-110f);
+        const float mid = key_float(least), up = mid + eps, down = mid - eps;
+        const bool wild = !(size < INFINITY) || !(fabsf(mid) < INFINITY);
+        int sure = 0, open = 0;
+        uint32_t maybe = 0;
+#pragma unroll
+        for (int i = 0; i < KPL; ++i) {
+          const float f = key_float(key[i]);
+          const bool x = key[i] != 0 && (wild || (f <= up && f >= down));
+          if (x) maybe |= 1u << i;
+          open += __popcll(__ballot(x));
+          sure += __popcll(__ballot((best >> i & 1) && !x));
+        }
+        // (all scores 0: the lowest blocks are chosen already)
+        if (open > free - sure && !(size == 0.0f)) {
+          constexpr int N = 2 * D / 64;  // products per lane
+          double qd[N];
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            const int e = lane * N + j;
+            qd[j] = 0.0;
+            for (int x = 0; x < a.G; ++x) {
+              const float f = elem<T>(qh + x * a.q.sh + (int64_t)t * a.q.sr, e % D);
+              if (e < D ? !(f >= 0.0f) : f > 0.0f) qd[j] += (double)f;
+            }
+          }
+          uint64_t wide[KPL];
+#pragma unroll
+          for (int i = 0; i < KPL; ++i) {
+            wide[i] = 0;
+            for (uint64_t todo = __ballot(maybe >> i & 1); todo; todo &= todo - 1) {
+              const int l = __ffsll((unsigned long long)todo) - 1;
+              const uint16_t* p = bounds + (int64_t)(i * 64 + l) * 2 * D + lane * N;
+              double sum = 0.0;
+#pragma unroll
+              for (int j = 0; j < N; ++j) sum += qd[j] * (double)bf16_to_float(p[j]);
+#pragma unroll
+              for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+              if (lane == l) wide[i] = score_key(sum);
+            }
+          }
+          best = (best & ~maybe) | largest<uint64_t, KPL>(wide, free - sure, lane);
+        }
+        in |= best;
+      }
+    }
+    int place = 0;
+#pragma unroll
+    for (int i = 0; i < KPL; ++i) {
+      const uint64_t mask = __ballot(in >> i & 1);
+      if (in >> i & 1) out[place + __popcll(mask & ((1ull << lane) - 1))] = i * 64 + lane;
+      place += __popcll(mask);
+    }
+    for (int i = want + lane; i < a.n_sel; i += 64) out[i] = -1;
+  }
+}
+
 template <typename T, int D>
 hipError_t store_d(const Q4View& c, const RowsView& k, const RowsView& v, const Q4Tokens& tok,
                    hipStream_t st) {
@@ -361,6 +617,31 @@ hipError_t pick(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <typename T, int D, int KPL>
+hipError_t select_k(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
+  const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  const int stride = (nb + 15) / 16 * 16 + 4;
+  const dim3 grid((uint32_t)((a.tok.T + 15) / 16), (uint32_t)(c.B * c.H));
+  const size_t lds = (size_t)16 * stride * 4;
+  if (lds > 64 * 1024) {
+    const hipError_t e =
+        hipFuncSetAttribute(reinterpret_cast<const void*>(&q4_select_kernel<T, D, KPL>),
+                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  q4_select_kernel<T, D, KPL><<<grid, THREADS, lds, st>>>(c, a, stride);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t select_d(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
+  const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  if (nb <= 128) return select_k<T, D, 2>(c, a, st);
+  if (nb <= 512) return select_k<T, D, 8>(c, a, st);
+  if (nb <= 1024) return select_k<T, D, 16>(c, a, st);
+  return select_k<T, D, 32>(c, a, st);
+}
+
 }  // namespace
 
 hipError_t launch_q4_store(int dtype, int64_t d, const Q4View& c, const RowsView& k,
@@ -376,6 +657,11 @@ hipError_t launch_q4_load(int dtype, int64_t d, const Q4View& c, const int32_t* 
 hipError_t launch_q4_scores(int dtype, int64_t d, const Q4View& c, const Q4SelectArgs& a,
                             hipStream_t st) {
   Q4_BY_D(scores_d, c, a, st);
+}
+
+hipError_t launch_q4_select(int dtype, int64_t d, const Q4View& c, const Q4SelectArgs& a,
+                            hipStream_t st) {
+  Q4_BY_D(select_d, c, a, st);
 }
 
 hipError_t launch_q4_pick(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {

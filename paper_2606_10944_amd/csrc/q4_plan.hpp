@@ -57,6 +57,12 @@ inline size_t q4_attention_bytes(int64_t B, int64_t H, int64_t tiles, int64_t sp
   return splits > 1 ? q4_sums_bytes(B, H, tiles, splits, d) + (size_t)(tiles * B) * 8 : 0;
 }
 
+// Whether a selection runs as one launch with its scores in LDS.
+constexpr int64_t kQ4SelectBlocks = 2048;  // 16 tokens' float32 scores: 128 KiB
+inline bool q4_select_fused(int64_t slices, int64_t blocks, int64_t T) {
+  return blocks <= kQ4SelectBlocks && T > 1 && slices * ((T + 15) / 16) >= 64;
+}
+
 // Tokens whose block scores a selection holds at a time: 64 MiB of them, at least one
 // token's.
 inline int64_t q4_select_tokens(int64_t slices, int64_t blocks, int64_t T) {

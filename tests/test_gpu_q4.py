@@ -284,14 +284,74 @@ def test_select_ties_and_nan():
     assert got.flatten().tolist() == list(range(19)) + [299]
 
 
+# Enough tokens for the launch that scores 16 of them at a time (64 workgroups).
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d,B,H,G,T,n_max,at,count,sel", [
+    (128, 4, 4, 4, 67, 9000, [0, 8900, 4000, 700], [67, 67, 30, 0], (9, 1, 2)),
+    (64, 1, 32, 3, 33, 2000, [1990], None, (5, 0, 1)),
+    (32, 2, 40, 1, 9, 30000, [-4, 29000], None, (40, 2, 3)),
+    (128, 1, 33, 17, 20, 300, [200], None, (1, 0, 1))])
+def test_select_of_prompts(dtype, d, B, H, G, T, n_max, at, count, sel):
+    g = gen(21)
+    rows = [max(0, min(n_max, a + T)) for a in at]
+    c = filled(g, B, H, n_max, d, rows)
+    q = randn(g, B, H * G, T, d, dtype=dtype)
+    got = thin_q4_select(strided(q), c, i32(at), sel[0], n_sinks=sel[1], n_window=sel[2],
+                         count=None if count is None else i32(count))
+    check_select(c, q, at, count, *sel, got)
+
+
+@pytest.mark.parametrize("kind", ["equal", "near", "nan", "inf", "zero", "tiny", "nan query"])
+@pytest.mark.parametrize("nb,n_sel", [(100, 20), (600, 70), (1500, 9)])
+def test_select_of_prompts_at_borders(kind, nb, n_sel):
+    """Scores that float32 sums cannot tell apart, and values that are none."""
+    g = gen(22)
+    H, T, d = 64, 3, 64
+    c = fresh(1, H, 64 * nb, d)
+    x = torch.randn(1, 1, 1, 2, d, generator=g).bfloat16().expand(1, H, nb, 2, d).clone()
+    if kind == "near":
+        # differences of 2^-20 of a channel and less, both ways
+        step = torch.randint(-3, 4, (1, H, nb, 2), generator=g).float() * 2.0 ** -20
+        x[..., 5] = step.bfloat16()
+    if kind == "nan":
+        x[:, :, nb // 3:nb // 2] = math.nan
+    if kind == "inf":
+        x[:, ::2, nb // 3:nb // 2, 1, 4] = math.inf
+    if kind == "zero":
+        x.zero_()
+    if kind == "tiny":
+        x = (torch.randn(1, H, nb, 2, d, generator=g) * 2.0 ** -124).bfloat16()
+    # (least, then largest)
+    c.bounds.copy_(torch.stack((torch.minimum(x[..., 0, :], x[..., 1, :]),
+                                torch.maximum(x[..., 0, :], x[..., 1, :])), -2))
+    q = randn(g, 1, 2 * H, T, d, dtype="bf16")
+    if kind == "tiny":
+        q = (q.float() * 2.0 ** -20).bfloat16()
+    if kind == "nan query":
+        q[:, ::3, 1] = math.nan
+    at = 64 * nb - T
+    got = thin_q4_select(q.to(DEV), c, i32([at]), n_sel, n_sinks=1, n_window=2).cpu()
+    for h in range(0, H, 7):
+        check_select_head(c, q, at, n_sel, 1, 2, got, h)
+
+
+def check_select_head(c, q, at, n_sel, n_sinks, n_window, got, h):
+    G = q.shape[1] // c.H
+    for t in range(q.shape[2]):
+        sc = ref.block_scores(q[0, h * G:(h + 1) * G, t], c.bounds[0, h].cpu()).tolist()
+        want = ref.select(sc, at + t, n_sel, n_sinks, n_window)
+        assert got[0, h, t].tolist() == want, (h, t)
+
+
 def test_select_in_pieces():
-    """More tokens than the scores held at a time: 8 slices x 2048 blocks."""
+    """More tokens than the scores held at a time: 8 slices x 2049 blocks."""
     g = gen(9)
-    c = filled(g, 1, 8, 131072, 32, [131072])
+    n = 131073
+    c = filled(g, 1, 8, n, 32, [n])
     q = randn(g, 1, 8, 600, 32, dtype="bf16").to(DEV)
-    got = thin_q4_select(q, c, i32([131072 - 600]), 9)
-    for t in (0, 511, 512, 599):
-        one = thin_q4_select(q[:, :, t:t + 1], c, i32([131072 - 600 + t]), 9)
+    got = thin_q4_select(q, c, i32([n - 600]), 9)
+    for t in (0, 510, 511, 512, 599):
+        one = thin_q4_select(q[:, :, t:t + 1], c, i32([n - 600 + t]), 9)
         assert torch.equal(got[:, :, t:t + 1], one)
 
 
