@@ -187,6 +187,18 @@ __global__ __launch_bounds__(THREADS) void q4_scores_kernel(Q4View c, Q4SelectAr
   const int b = blockIdx.y / c.H, h = blockIdx.y % c.H;
   const int t = a.t0 + blockIdx.x % a.tn, part = blockIdx.x / a.tn;
   const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  constexpr int W = 2 * D / 8 / SLANES;  // 16-byte words of bounds per lane
+  const int j = threadIdx.x % SLANES;
+  const int step = (int)(gridDim.x / a.tn) * (THREADS / SLANES);
+  int k = part * (THREADS / SLANES) + threadIdx.x / SLANES;
+  u32x4 x[W];
+  auto fetch = [&](int block) __attribute__((always_inline)) {
+    const u32x4* p = reinterpret_cast<const u32x4*>(
+        c.bounds + (s * nb + (block < nb ? block : nb - 1)) * 2 * D);
+#pragma unroll
+    for (int w = 0; w < W; ++w) x[w] = p[w * SLANES + j];
+  };
+  fetch(k);  // (on its way while the queries are summed)
   const int last_row = q4_last_row(a.tok, b, t, c.n_max);
   if (last_row < 0) return;
   const int last = last_row / kQ4Block;
@@ -195,37 +207,32 @@ __global__ __launch_bounds__(THREADS) void q4_scores_kernel(Q4View c, Q4SelectAr
     const T* q = static_cast<const T*>(a.q.p) + b * a.q.sb + (int64_t)h * a.G * a.q.sh + t * a.q.sr;
     double neg = 0.0, pos = 0.0;
     for (int g = 0; g < a.G; ++g) {
-      const double x = (double)elem<T>(q + g * a.q.sh, threadIdx.x);
-      if (!(x >= 0.0)) neg += x;  // (NaN here, and so in the score)
-      if (x > 0.0) pos += x;
+      const double v = (double)elem<T>(q + g * a.q.sh, threadIdx.x);
+      if (!(v >= 0.0)) neg += v;  // (NaN here, and so in the score)
+      if (v > 0.0) pos += v;
     }
     sq[threadIdx.x] = neg;
     sq[D + threadIdx.x] = pos;
   }
   __syncthreads();
-  const int j = threadIdx.x % SLANES;
-  constexpr int W = 2 * D / 8 / SLANES;  // 16-byte words of bounds per lane
   double q[W][8];
 #pragma unroll
   for (int w = 0; w < W; ++w)
 #pragma unroll
     for (int i = 0; i < 8; ++i) q[w][i] = sq[(w * SLANES + j) * 8 + i];
-  const int step = (int)(gridDim.x / a.tn) * (THREADS / SLANES);
-  for (int k = part * (THREADS / SLANES) + threadIdx.x / SLANES; k <= last; k += step) {
-    const u32x4* p = reinterpret_cast<const u32x4*>(c.bounds + (s * nb + k) * 2 * D);
+  for (; k <= last; k += step) {
     double sum = 0.0;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      const u32x4 x = p[w * SLANES + j];
+    for (int w = 0; w < W; ++w)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        sum += q[w][2 * i] * (double)__uint_as_float(x[i] << 16);
-        sum += q[w][2 * i + 1] * (double)__uint_as_float(x[i] & 0xffff0000u);
+        sum += q[w][2 * i] * (double)__uint_as_float(x[w][i] << 16);
+        sum += q[w][2 * i + 1] * (double)__uint_as_float(x[w][i] & 0xffff0000u);
       }
-    }
 #pragma unroll
     for (int m = 1; m < SLANES; m *= 2) sum += __shfl_xor(sum, m);
     if (j == 0) a.scores[(s * a.tn + t - a.t0) * nb + k] = score_key(sum);
+    fetch(k + step);
   }
 }
 
@@ -245,14 +252,37 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
   const int lr = q4_last_row(a.tok, b, t, c.n_max);
   const int n = lr < 0 ? 0 : lr / kQ4Block + 1;  // blocks that are there
   __shared__ int cnt[2][W];
+  __shared__ uint64_t ends[2][W];
   // a wave's keys are its KPL runs of 64 blocks
   uint64_t key[KPL];
   const int base = wave * KPL * 64;
+  uint64_t lo = ~0ull, hi = 0;  // least and largest score
 #pragma unroll
   for (int i = 0; i < KPL; ++i) {
     const int k = base + i * 64 + lane;
     key[i] = 0;
-    if (k < n) key[i] = k < a.n_sinks || k >= n - a.n_window ? ~0ull : keys[k];
+    if (k >= n) continue;
+    if (k < a.n_sinks || k >= n - a.n_window) {
+      key[i] = ~0ull;
+    } else {
+      key[i] = keys[k];
+      lo = key[i] < lo ? key[i] : lo;
+      hi = key[i] > hi ? key[i] : hi;
+    }
+  }
+  lo = wave_min(lo);
+  hi = wave_max(hi);
+  if (W > 1) {
+    if (lane == 0) {
+      ends[0][wave] = lo;
+      ends[1][wave] = hi;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      lo = ends[0][w] < lo ? ends[0][w] : lo;
+      hi = ends[1][w] > hi ? ends[1][w] : hi;
+    }
   }
   // how many of the workgroup's keys are at least x
   int parity = 0;
@@ -275,7 +305,9 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
   uint64_t x = 1;
   int above = n < a.n_sel ? n : a.n_sel;
   if (n > a.n_sel) {
-    uint64_t lo = 1, hi = ~0ull;  // count(lo) > n_sel >= count(hi): sinks and window fit
+    // count(lo) = n > n_sel >= count(hi): what is above every score are sinks and window,
+    // which fit.  (Some block is neither: lo <= hi.)
+    hi += 1;
     above = count(hi);
     while (hi - lo > 1) {
       const uint64_t mid = lo + (hi - lo) / 2;
@@ -329,15 +361,16 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
 
 // Selection for several tokens of a slice in one launch.  A workgroup takes 16 tokens:
 // their scores of every block come from the bf16 matrix instructions, the queries'
-// float64 sums split into three bf16 parts (24 bits; bounds are bf16), and stay in LDS.
-// Such a score is off by less than eps = 2^-16 qsum bmax (qsum = sum_gc |q_gc|, bmax the
-// largest bound: 24 sums of 32 products, each within 2^-21.6 of the sum of magnitudes,
-// and 2^-27 of the split).  So a block more than 2 eps above the last one that fits is
-// in, one more than 2 eps below it is out, whatever the rounding; the others between
-// (mostly that one alone) are scored again in float64.
+// float64 sums split into two bf16 parts (bounds are bf16), and stay in LDS.  Such a
+// score is off by less than eps = 1.25 * 2^-14 size, size = the token's largest sum of
+// the products' magnitudes: 4 d additions that lose at most 2^-23 of it each make 2^-14
+// for d = 128, the split leaves 2^-17 of each query sum.  So a block more than 2 eps
+// above the last one that fits is in, one more than 2 eps below it is out, whatever the
+// rounding; the others between (mostly that one alone) are scored again in float64.
 //
 // 2047 tokens x 8 key heads over up to 512 blocks, d = 128: 8e6 scores of 256 products,
 // 62 us in float64 at the rate of a large float64 matrix product.
+constexpr int SW = 8;  // waves
 
 // A float's key: integers of the same order, NaN below everything, 0 left free.
 __device__ __forceinline__ uint32_t float_key(float f) {
@@ -361,12 +394,8 @@ __device__ __forceinline__ uint32_t largest(const K* key, int want, int lane) {
     if (key[i] != 0 && key[i] < lo) lo = key[i];
     if (key[i] > hi) hi = key[i];
   }
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    const K a = __shfl_xor(lo, m), b = __shfl_xor(hi, m);
-    lo = a < lo ? a : lo;
-    hi = b > hi ? b : hi;
-  }
+  lo = wave_min(lo);
+  hi = wave_max(hi);
   auto count = [&](K x) {
     int n = 0;
 #pragma unroll
@@ -407,10 +436,10 @@ __device__ __forceinline__ uint32_t largest(const K* key, int want, int lane) {
 }
 
 template <typename T, int D, int KPL>
-__global__ __launch_bounds__(THREADS) void q4_select_kernel(Q4View c, Q4SelectArgs a, int stride) {
+__global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectArgs a, int stride) {
   constexpr int KS = 2 * D / 32;  // k-steps: q- beside lo, then q+ beside hi
-  extern __shared__ __align__(16) float score[];  // [16, stride]
-  __shared__ uint32_t smax[4];
+  extern __shared__ __align__(16) float score[];  // [16, stride], then the queries' parts
+  __shared__ uint32_t ssize[SW][16];
   const int64_t s = blockIdx.y;
   const int b = blockIdx.y / c.H, h = blockIdx.y % c.H, t0 = blockIdx.x * 16;
   const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
@@ -419,78 +448,90 @@ __global__ __launch_bounds__(THREADS) void q4_select_kernel(Q4View c, Q4SelectAr
   const T* qh = static_cast<const T*>(a.q.p) + b * a.q.sb + (int64_t)h * a.G * a.q.sh;
   const uint16_t* bounds = c.bounds + s * nb * 2 * D;
 
-  // the last block that any of the tokens sees
-  int most = t0 + m < a.tok.T ? q4_last_row(a.tok, b, t0 + m, c.n_max) : -1;
+  // the first bounds of this wave are on their way while the queries are summed
+  u32x4 w[KS];
+  auto fetch = [&](int k0, u32x4* to) __attribute__((always_inline)) {
+    const u32x4* row =
+        reinterpret_cast<const u32x4*>(bounds + (int64_t)std::min(k0 + m, nb - 1) * 2 * D);
 #pragma unroll
-  for (int x = 1; x < 16; x *= 2) most = std::max(most, __shfl_xor(most, x));
-  const int blocks = most < 0 ? 0 : most / kQ4Block + 1;
+    for (int i = 0; i < KS; ++i) to[i] = row[4 * i + g];
+  };
+  fetch(wave * 16, w);
 
-  // lane (m, g): token m's channels of words 4 i + g
-  bf16x8_t q[KS][3];
-  float qsum = 0.0f;
+  // the last block that any of the tokens sees
   const bool there = t0 + m < a.tok.T;
-#pragma unroll
-  for (int i = 0; i < KS / 2; ++i) {
+  const int most = (int)wave_max((uint32_t)(
+      (there ? q4_last_row(a.tok, b, t0 + m, c.n_max) : -1) + 1));
+  const int blocks = (most + kQ4Block - 1) / kQ4Block;
+
+  // The tokens' sums in parts: [k-step, part, lane] 16-byte words, lane (m, g) token m's
+  // channels of words 4 i + g.  The waves share the words.
+  u32x4* parts = reinterpret_cast<u32x4*>(score + 16 * stride);
+  for (int i = wave; i < KS / 2; i += SW) {
     double neg[8], pos[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) neg[j] = pos[j] = 0.0;
-    if (there)
+    if (there) {
+      const T* p = qh + (int64_t)(t0 + m) * a.q.sr + (4 * i + g) * 8;
+#pragma unroll 4
       for (int x = 0; x < a.G; ++x) {
         float f[8];
-        load8<T>(qh + x * a.q.sh + (int64_t)(t0 + m) * a.q.sr + (4 * i + g) * 8, f);
+        load8<T>(p + x * a.q.sh, f);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (!(f[j] >= 0.0f)) neg[j] += (double)f[j];
           if (f[j] > 0.0f) pos[j] += (double)f[j];
-          qsum += fabsf(f[j]);
         }
       }
+    }
+    // (float32 keeps 2^-24 of a sum, the first bf16 part 2^-8, the second 2^-16 of it)
+    float n[8], p[8];
 #pragma unroll
-    for (int p = 0; p < 3; ++p) {
-      float fn[8], fp[8];
+    for (int j = 0; j < 8; ++j) {
+      n[j] = (float)neg[j];
+      p[j] = (float)pos[j];
+    }
+    bf16x8_t np[2], pp[2];
+    split8<2>(n, np);
+    split8<2>(p, pp);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        fn[j] = (float)(__bf16)(float)neg[j];
-        fp[j] = (float)(__bf16)(float)pos[j];
-        neg[j] -= (double)fn[j];
-        pos[j] -= (double)fp[j];
-      }
-      split8<1>(fn, &q[i][p]);
-      split8<1>(fp, &q[i + KS / 2][p]);
+    for (int x = 0; x < 2; ++x) {
+      parts[(i * 2 + x) * 64 + lane] = __builtin_bit_cast(u32x4, np[x]);
+      parts[((i + KS / 2) * 2 + x) * 64 + lane] = __builtin_bit_cast(u32x4, pp[x]);
     }
   }
-  qsum += __shfl_xor(qsum, 16);
-  qsum += __shfl_xor(qsum, 32);
+  __syncthreads();
 
-  uint32_t bmax = 0;  // largest magnitude of a bound, as bf16 bits
-  for (int k0 = wave * 16; k0 < blocks; k0 += 64) {
-    const int k = std::min(k0 + m, nb - 1);
-    const u32x4* row = reinterpret_cast<const u32x4*>(bounds + (int64_t)k * 2 * D);
-    floatx4_t z = {0.f, 0.f, 0.f, 0.f};
-    u32x4 w[KS];
-#pragma unroll
-    for (int i = 0; i < KS; ++i) w[i] = row[4 * i + g];
+  // largest sum of magnitudes of this lane's scores (token m), as bits: NaN above all
+  uint32_t size = 0;
+  auto tile = [&](int k0, const u32x4* x) __attribute__((always_inline)) {
+    floatx4_t z = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
+    const u32x4 sign = {0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t lo = w[i][j] & 0x7fffu, hi = (w[i][j] >> 16) & 0x7fffu;
-        if (k0 + m < blocks) bmax = std::max(bmax, std::max(lo, hi));
-      }
-#pragma unroll
-      for (int p = 2; p >= 0; --p)
-        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w[i]), q[i][p], z,
-                                                    0, 0, 0);
+      const u32x4 q0 = parts[i * 2 * 64 + lane], q1 = parts[(i * 2 + 1) * 64 + lane];
+      const bf16x8_t v = __builtin_bit_cast(bf16x8_t, x[i]);
+      z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, q1), z, 0, 0, 0);
+      z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, q0), z, 0, 0, 0);
+      y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x[i] & ~sign),
+                                                  __builtin_bit_cast(bf16x8_t, q0 & ~sign), y, 0, 0,
+                                                  0);
     }
     *reinterpret_cast<floatx4_t*>(score + m * stride + k0 + 4 * g) = z;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (k0 + 4 * g + j < blocks) size = std::max(size, __float_as_uint(y[j]) & 0x7fffffffu);
+  };
+  for (int k0 = wave * 16; k0 < blocks; k0 += SW * 16) {
+    tile(k0, w);
+    fetch(k0 + SW * 16, w);
   }
 #pragma unroll
-  for (int x = 1; x < 64; x *= 2) bmax = std::max(bmax, (uint32_t)__shfl_xor((int)bmax, x));
-  if (lane == 0) smax[wave] = bmax;
+  for (int x = 16; x < 64; x *= 2) size = std::max(size, (uint32_t)__shfl_xor((int)size, x));
+  if (lane < 16) ssize[wave][lane] = size;
   __syncthreads();
-  bmax = std::max(std::max(smax[0], smax[1]), std::max(smax[2], smax[3]));
 
-  for (int r = wave; r < 16; r += 4) {
+  for (int r = wave; r < 16; r += SW) {
     const int t = t0 + r;
     if (t >= a.tok.T) break;
     int32_t* out = a.blocks + (s * a.tok.T + t) * a.n_sel;
@@ -520,12 +561,14 @@ __global__ __launch_bounds__(THREADS) void q4_select_kernel(Q4View c, Q4SelectAr
 #pragma unroll
         for (int i = 0; i < KPL; ++i)
           if ((best >> i & 1) && key[i] < least) least = key[i];
-#pragma unroll
-        for (int x = 1; x < 64; x *= 2) least = std::min(least, (uint32_t)__shfl_xor((int)least, x));
+        least = wave_min(least);
         // 2 eps (at least what products below the normal numbers can make); not a number or
         // infinite: every block is scored again
-        const float size = __shfl(qsum, r) * __uint_as_float(bmax << 16);
-        const float eps = fmaxf(0x1p-15f * size, 0x1p-110f);
+        uint32_t bits = 0;
+#pragma unroll
+        for (int x = 0; x < SW; ++x) bits = std::max(bits, ssize[x][r]);
+        const float size = __uint_as_float(bits);
+        const float eps = fmaxf(0x1.4p-13f * size, 0x1p-110f);
         const float mid = key_float(least), up = mid + eps, down = mid - eps;
         const bool wild = !(size < INFINITY) || !(fabsf(mid) < INFINITY);
         int sure = 0, open = 0;
@@ -622,14 +665,14 @@ hipError_t select_k(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
   const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
   const int stride = (nb + 15) / 16 * 16 + 4;
   const dim3 grid((uint32_t)((a.tok.T + 15) / 16), (uint32_t)(c.B * c.H));
-  const size_t lds = (size_t)16 * stride * 4;
+  const size_t lds = (size_t)16 * stride * 4 + 2 * D / 32 * 2 * 64 * 16;
   if (lds > 64 * 1024) {
     const hipError_t e =
         hipFuncSetAttribute(reinterpret_cast<const void*>(&q4_select_kernel<T, D, KPL>),
                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  q4_select_kernel<T, D, KPL><<<grid, THREADS, lds, st>>>(c, a, stride);
+  q4_select_kernel<T, D, KPL><<<grid, 64 * SW, lds, st>>>(c, a, stride);
   return hipGetLastError();
 }
 

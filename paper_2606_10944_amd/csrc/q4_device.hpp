@@ -57,6 +57,42 @@ __device__ __forceinline__ int q4_last_row(const Q4Tokens& tok, int b, int t, in
   return r < 0 ? -1 : (r < n_max ? r : n_max - 1);
 }
 
+// One step of a reduction over the wave's lanes: the value of another lane by data
+// parallel primitives (lanes that have no source keep `none`).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lane_move(uint32_t x, uint32_t none) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t lane_move(uint64_t x, uint64_t none) {
+  return (uint64_t)lane_move<CTRL, ROWS>((uint32_t)(x >> 32), (uint32_t)(none >> 32)) << 32 |
+         lane_move<CTRL, ROWS>((uint32_t)x, (uint32_t)none);
+}
+// op over the 64 lanes, the same in all of them; op(x, none) = x.  Rows of 16 lanes by
+// shifts, then across rows: six steps of a few cycles where a shuffle takes an LDS trip.
+template <typename K, typename F>
+__device__ __forceinline__ K wave_reduce(K x, K none, F op) {
+  x = op(x, lane_move<0x111, 0xf>(x, none));  // from 1, 2, 4, 8 lanes below
+  x = op(x, lane_move<0x112, 0xf>(x, none));
+  x = op(x, lane_move<0x114, 0xf>(x, none));
+  x = op(x, lane_move<0x118, 0xf>(x, none));
+  x = op(x, lane_move<0x142, 0xa>(x, none));  // lane 15 of a row to the next row
+  x = op(x, lane_move<0x143, 0xc>(x, none));  // lane 31 to the upper half
+  if constexpr (sizeof(K) == 8)
+    return (K)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), 63) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, 63);
+  else
+    return (K)__builtin_amdgcn_readlane((int)x, 63);
+}
+template <typename K>
+__device__ __forceinline__ K wave_min(K x) {
+  return wave_reduce<K>(x, ~(K)0, [](K a, K b) { return a < b ? a : b; });
+}
+template <typename K>
+__device__ __forceinline__ K wave_max(K x) {
+  return wave_reduce<K>(x, (K)0, [](K a, K b) { return a > b ? a : b; });
+}
+
 // Instance F<element type, head dimension> of a launch.
 #define Q4_BY_D(F, ...)                                                                      \
   return dtype == 0 ? (d == 32   ? F<float, 32>(__VA_ARGS__)                                 \
