@@ -85,7 +85,9 @@ bool plan_attention(int64_t B, int64_t H, int64_t q_heads, int64_t n_max, int64_
                                       n_sel > 0 ? n_sel * THIN_Q4_BLOCK : n_max, bf16);
   p->bytes = thin::q4_attention_bytes(B, H, tiles, p->shape.splits, d);
   p->sums = thin::q4_sums_bytes(B, H, tiles, p->shape.splits, d);
-  return tiles <= kMaxGroups;  // (B * tiles * splits is at most 2048 where splits > 1)
+  // (B * tiles * splits is at most 2048 where splits > 1; a launch's workgroups are counted
+  // in 32 bits)
+  return tiles <= kMaxGroups && B * H * tiles < ((int64_t)1 << 31);
 }
 
 }  // namespace

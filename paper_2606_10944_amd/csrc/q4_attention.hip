@@ -182,11 +182,18 @@ __global__ __launch_bounds__(64 * WV, 2) void q4_attn_kernel(Q4View c, Q4AttnArg
   const int splits = a.shape.splits;
   const int64_t slot = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   int b, h, tile, i0, i1;
-  if (LIST || splits == 1) {
+  if (splits == 1) {
+    const uint32_t piece = xcd_contiguous(), slice = piece / gridDim.x;
+    b = slice / c.H;
+    h = slice % c.H;
+    tile = piece % gridDim.x;
+    i0 = 0;
+    i1 = LIST ? a.n_sel * (kQ4Block / CH) : steps_of(c, a, b, tile_tokens(a, tile));
+  } else if (LIST) {
     b = blockIdx.y / c.H;
     h = blockIdx.y % c.H;
     tile = blockIdx.x / splits;
-    const int steps = LIST ? a.n_sel * (kQ4Block / CH) : steps_of(c, a, b, tile_tokens(a, tile));
+    const int steps = a.n_sel * (kQ4Block / CH);
     const int share = (steps + splits - 1) / splits;
     i0 = blockIdx.x % splits * share;
     i1 = i0 + share < steps ? i0 + share : steps;

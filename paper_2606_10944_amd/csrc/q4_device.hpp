@@ -57,6 +57,15 @@ __device__ __forceinline__ int q4_last_row(const Q4Tokens& tok, int b, int t, in
   return r < 0 ? -1 : (r < n_max ? r : n_max - 1);
 }
 
+// Workgroups are dealt to the eight XCDs in turn.  Which of the launch's n = gridDim.x *
+// gridDim.y pieces of work this one takes so that every XCD has a contiguous eighth of
+// them, and its L2 the rows of few slices.
+__device__ __forceinline__ uint32_t xcd_contiguous() {
+  const uint32_t l = blockIdx.y * gridDim.x + blockIdx.x, n = gridDim.x * gridDim.y;
+  const uint32_t x = l % 8;
+  return x * (n / 8) + (x < n % 8 ? x : n % 8) + l / 8;
+}
+
 // One step of a reduction over the wave's lanes: the value of another lane by data
 // parallel primitives (lanes that have no source keep `none`).
 template <int CTRL, int ROWS>

@@ -33,18 +33,10 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
 
-  // Every XCD takes a contiguous eighth of the tiles, slice by slice, so that its L2
-  // holds few slices; a slice's last tiles, which see the most rows, come first.
-  const int tiles = gridDim.x;
-  int b, h, tile;
-  {
-    const uint32_t l = blockIdx.y * gridDim.x + blockIdx.x, n = gridDim.x * gridDim.y;
-    const uint32_t x = l % 8, i = x * (n / 8) + (x < n % 8 ? x : n % 8) + l / 8;
-    const int s = i / tiles;
-    b = s / c.H;
-    h = s % c.H;
-    tile = tiles - 1 - (int)(i % tiles);
-  }
+  // slice by slice; a slice's last tiles, which see the most rows, come first
+  const uint32_t piece = xcd_contiguous();
+  const int slice = piece / gridDim.x, b = slice / c.H, h = slice % c.H;
+  const int tile = gridDim.x - 1 - (int)(piece % gridDim.x);
   const int nrows = a.tok.T * a.G;
   const int r0 = tile * (ROWS * PW);  // the workgroup's first query row
   const int cnt = a.tok.count ? std::min(a.tok.count[b], a.tok.T) : a.tok.T;

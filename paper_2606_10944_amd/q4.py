@@ -23,11 +23,15 @@ _DTYPE = {torch.float32: THIN_FP32, torch.bfloat16: THIN_BF16}
 _Strides = C.c_int64 * 3
 
 
+_get_device = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
 def _where(stream):
     """(device index, raw stream) that a call runs on."""
     if stream is None:
-        dev = torch._C._cuda_getDevice()
-        return dev, torch._C._cuda_getCurrentRawStream(dev)
+        dev = _get_device()
+        return dev, _raw_stream(dev)
     return stream.device.index, stream.cuda_stream
 
 
@@ -38,6 +42,13 @@ def _empty(shape, dtype: torch.dtype, dev: int, stream) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=dev)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _empty_like(t: torch.Tensor, dev: int, stream) -> torch.Tensor:
+    """Contiguous memory for t's shape (half the host time of _empty)."""
+    if stream is None and t.is_contiguous():
+        return torch.empty_like(t)
+    return _empty(t.shape, t.dtype, dev, stream)
 
 
 def _dtype(t: torch.Tensor, name: str) -> int:
@@ -54,17 +65,21 @@ def _on(t: torch.Tensor, dev: int, name: str) -> int:
     return t.data_ptr()
 
 
+def _strides(t: torch.Tensor, name: str):
+    """None for contiguous rows [B, heads, T, d], else their strides."""
+    if t.is_contiguous():
+        return None
+    s = t.stride()
+    if s[3] != 1:
+        raise ThinError(THIN_EINVAL, f"{name}: channels must be contiguous")
+    return _Strides(s[0], s[1], s[2])
+
+
 def _rows(t: torch.Tensor, dev: int, name: str):
     """(address, strides or None) of rows [B, heads, T, d]."""
     if t.dim() != 4:
         raise ThinError(THIN_EINVAL, f"{name} must be [B,heads,T,d]")
-    p = _on(t, dev, name)
-    if t.is_contiguous():
-        return p, None
-    s = t.stride()
-    if s[3] != 1:
-        raise ThinError(THIN_EINVAL, f"{name}: channels must be contiguous")
-    return p, _Strides(s[0], s[1], s[2])
+    return _on(t, dev, name), _strides(t, name)
 
 
 def _ints(t: Optional[torch.Tensor], shape, dev: int, name: str):
@@ -111,20 +126,23 @@ def thin_rotary(X: torch.Tensor, pos: torch.Tensor, turns: torch.Tensor, *,
     [rot/2] on the device.  inverse=True turns back (the gradient of the turn).
     out / out_Y may be X / Y themselves.  Returns out, or (out, out_Y) with Y."""
     dev, st = _where(stream)
-    if layout not in LAYOUT:
+    lay = LAYOUT.get(layout)
+    if lay is None:
         raise ThinError(THIN_EINVAL, f"unknown layout {layout!r}")
     x, xs = _rows(X, dev, "X")
-    code = _dtype(X, "X")
-    B, H, T, d = X.shape
+    shape = X.shape
+    B, H, T, d = shape
     if turns.dtype != torch.float64 or turns.dim() != 1 or not turns.is_contiguous():
         raise ThinError(THIN_EINVAL, "turns must be contiguous float64 [rot/2]")
     per_token = pos.dim() == 2
     p = _ints(pos, (B, T) if per_token else (B,), dev, "pos")
     if out is None:
-        out = _empty((B, H, T, d), X.dtype, dev, stream)
-    elif out.shape != X.shape or out.dtype != X.dtype:
-        raise ThinError(THIN_EINVAL, "out must match X")
-    o, os_ = _rows(out, dev, "out")
+        out = _empty_like(X, dev, stream)
+        o, os_ = out.data_ptr(), None
+    else:
+        if out.shape != shape or out.dtype != X.dtype:
+            raise ThinError(THIN_EINVAL, "out must match X")
+        o, os_ = _rows(out, dev, "out")
     y = ys = oy = oys = None
     Hy = 0
     if Y is not None:
@@ -135,15 +153,19 @@ def thin_rotary(X: torch.Tensor, pos: torch.Tensor, turns: torch.Tensor, *,
         if Y.dtype != X.dtype:
             raise ThinError(THIN_EDTYPE, "X and Y must share a dtype")
         if out_Y is None:
-            out_Y = _empty((B, Hy, T, d), Y.dtype, dev, stream)
-        elif out_Y.shape != Y.shape or out_Y.dtype != Y.dtype:
-            raise ThinError(THIN_EINVAL, "out_Y must match Y")
-        oy, oys = _rows(out_Y, dev, "out_Y")
+            out_Y = _empty_like(Y, dev, stream)
+            oy = out_Y.data_ptr()
+        else:
+            if out_Y.shape != Y.shape or out_Y.dtype != Y.dtype:
+                raise ThinError(THIN_EINVAL, "out_Y must match Y")
+            oy, oys = _rows(out_Y, dev, "out_Y")
     elif out_Y is not None:
         raise ThinError(THIN_EINVAL, "out_Y without Y")
-    _check(lib().thin_rotary(x, xs, H, o, os_, y, ys, Hy, oy, oys, code, B, T, d,
-                             2 * turns.shape[0], LAYOUT[layout], p, per_token,
-                             _on(turns, dev, "turns"), amp, inverse, st), "thin_rotary")
+    rc = lib().thin_rotary(x, xs, H, o, os_, y, ys, Hy, oy, oys, _dtype(X, "X"), B, T, d,
+                           2 * turns.shape[0], lay, p, per_token, _on(turns, dev, "turns"), amp,
+                           inverse, st)
+    if rc:
+        _check(rc, "thin_rotary")
     return out if Y is None else (out, out_Y)
 
 
@@ -248,7 +270,7 @@ def thin_q4_load(cache: Q4Cache, at: torch.Tensor, T: int, *,
     if K is None:
         K = _empty(shape, dtype, dev, stream)
     if V is None:
-        V = _empty(shape, K.dtype, dev, stream)
+        V = _empty_like(K, dev, stream)
     for t, name in ((K, "K"), (V, "V")):
         if t.shape != shape or not t.is_contiguous() or t.dtype != K.dtype:
             raise ThinError(THIN_EINVAL, f"{name} must be contiguous [B,H,T,d]")
@@ -324,10 +346,12 @@ def thin_q4_attention(Q: torch.Tensor, cache: Q4Cache, at: torch.Tensor, *,
         bp = _ints(blocks, (B, H, T, n_sel), dev, "blocks")
     need = _attention_bytes(B, H, Hq, cache.n_max, cache.d, T, n_sel)
     if O is None:
-        O = _empty((B, Hq, T, cache.d), Q.dtype, dev, stream)
-    elif O.shape != Q.shape or O.dtype != Q.dtype:
-        raise ThinError(THIN_EINVAL, "O must match Q")
-    o, os_ = _rows(O, dev, "O")
+        O = _empty_like(Q, dev, stream)
+        o, os_ = O.data_ptr(), None
+    else:
+        if O.shape != Q.shape or O.dtype != Q.dtype:
+            raise ThinError(THIN_EINVAL, "O must match Q")
+        o, os_ = _rows(O, dev, "O")
     ws, wp, wn = _workspace(workspace, need, dev, stream)
     _check(lib().thin_q4_attention(ref, q, qs, Hq, _dtype(Q, "Q"), T, _ints(at, (B,), dev, "at"),
                                    _ints(count, (B,), dev, "count"), bp, n_sel, o, os_, wp, wn,

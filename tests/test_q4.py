@@ -107,12 +107,12 @@ def test_select_refusals():
 def test_attention_refusals():
     L = _lib.lib()
     n = C.c_size_t(0)
-    assert L.thin_q4_attention_plan(2, 2, 6, 1000, 64, 3, 0, C.byref(n)) == 0 and n.value > 0
+    assert L.thin_q4_attention_plan(2, 2, 6, 100000, 64, 3, 0, C.byref(n)) == 0 and n.value > 0
 
     def attend(Q=FAKE, qs=None, Hq=6, dtype=1, T=3, at=FAKE, blocks=None, n_sel=0, O=FAKE, os=None,
                ws=FAKE, wsb=n.value):
-        return L.thin_q4_attention(cache(), Q, qs, Hq, dtype, T, at, None, blocks, n_sel, O, os,
-                                   ws, wsb, None)
+        return L.thin_q4_attention(cache(n_max=100000), Q, qs, Hq, dtype, T, at, None, blocks,
+                                   n_sel, O, os, ws, wsb, None)
 
     assert attend(Q=None) == attend(O=None) == attend(at=None) == attend(O=ODD) == EINVAL
     assert attend(Hq=7) == attend(Hq=0) == attend(T=0) == attend(T=(1 << 20) + 1) == EINVAL
@@ -121,7 +121,7 @@ def test_attention_refusals():
     assert attend(qs=strides(1, 192, 64)) == EINVAL and attend(dtype=2) == EDTYPE
     assert attend(ws=None) == attend(wsb=n.value - 1) == attend(ws=ODD) == EWORKSPACE
     for bad in [(0, 1, 1, 10, 64, 1, 0), (1, 1, 1, 10, 64, 0, 0), (1, 2, 3, 10, 64, 1, 0),
-                (1, 1, 1, 10, 48, 1, 0), (1, 1, 1, 10, 64, 1, -1)]:
+                (1, 1, 1, 10, 48, 1, 0), (1, 1, 1, 10, 64, 1, -1), (1, 1, 1025, 10, 64, 1, 0)]:
         assert L.thin_q4_attention_plan(*bad, C.byref(n)) == EINVAL
     assert L.thin_q4_attention_plan(1, 1, 1, 10, 64, 1, 0, None) == EINVAL
     # a call that does not share keys needs no workspace
