@@ -7,6 +7,11 @@
 // tile before is worked on.  Against the kernel for few rows, a value row is decoded
 // once per 64 RT query rows instead of once per 16, and each operand read from LDS
 // serves RT products.
+//
+// 4096 tokens over 16384 rows, 32 heads of 128 channels, 8 key heads, bf16: 766 us, 1.26
+// PFLOP/s (a library bf16 product of 8192^3 runs at 1.20).  The matrix cores alone need
+// 390 us of it (16 scaled instructions of 32 cycles and 32 of 16 per wave and tile); of
+// the rest, reading the values' columns costs 140 us, the exponentials 120, decoding 85.
 #include "q4_attn_device.hpp"
 
 namespace thin {
@@ -23,12 +28,9 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
   constexpr int GR = D / 32;                      // groups per row
   constexpr int KW = (MX ? 16 : D / 8) / 4;       // words of a key row that a lane feeds
   constexpr int ROWS = 16 * RT;                   // query rows of a wave
-  struct Stage {
-    unsigned char v[PK * kVStride<D>];
-    uint32_t k[PK * D / 8];
-    uint8_t ks[PK * GR];
-  };
-  __shared__ __align__(16) Stage stage[2];
+  __shared__ __align__(16) unsigned char sv[2][PK * kVStride<D>];
+  __shared__ __align__(16) uint32_t sk[2][PK * D / 8];
+  __shared__ uint8_t sks[2][PK * GR];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
@@ -75,24 +77,53 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
   const Slice rows = slice_of<D>(c, (int64_t)b * c.H + h);
   u32x4 kw, vw;
   uint32_t kb, vb;
-  auto load = [&](int row0) __attribute__((always_inline)) {
+  auto load_keys = [&](int row0) __attribute__((always_inline)) {
     const uint32_t r = std::min(row0 + srow, last);
     kw = *reinterpret_cast<const u32x4*>(rows.kc + (r * (D / 2) + sgr * 16));
     kb = rows.ks[r * GR + sgr];
+  };
+  auto load_values = [&](int row0) __attribute__((always_inline)) {
+    const uint32_t r = std::min(row0 + srow, last);
     vw = *reinterpret_cast<const u32x4*>(rows.vc + (r * (D / 2) + sgr * 16));
     vb = rows.vs[r * GR + sgr];
   };
-  auto put = [&](Stage& to) __attribute__((always_inline)) {
+  auto put_keys = [&](int to) __attribute__((always_inline)) {
     if (!stages) return;
-    *reinterpret_cast<u32x4*>(to.k + (srow * GR + sgr) * 4) = kw;
-    to.ks[srow * GR + sgr] = (uint8_t)kb;
+    *reinterpret_cast<u32x4*>(sk[to] + (srow * GR + sgr) * 4) = kw;
+    sks[to][srow * GR + sgr] = (uint8_t)kb;
+  };
+  auto put_values = [&](int to) __attribute__((always_inline)) {
+    if (!stages) return;
     const float scale = q4_scale(vb);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t w[4];
       decode8(vw[i], scale, w);
-      *reinterpret_cast<u32x4*>(to.v + srow * kVStride<D> + sgr * 64 + i * 16) =
+      *reinterpret_cast<u32x4*>(sv[to] + srow * kVStride<D> + sgr * 64 + i * 16) =
           (u32x4){w[0], w[1], w[2], w[3]};
+    }
+  };
+  // raw scores of a tile whose keys lie in buffer `from`
+  auto score = [&](int from, float (&sc)[RT][PK / 4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kt = 0; kt < PK / 16; ++kt) {
+      const int key = kt * 16 + m;
+      uint32_t kc[KW], byte;
+      if constexpr (MX) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(sk[from] + (key * GR + g % GR) * 4);
+        kc[0] = w[0]; kc[1] = w[1]; kc[2] = w[2]; kc[3] = w[3];
+        byte = sks[from][key * GR + g % GR];
+      } else {
+#pragma unroll
+        for (int w = 0; w < KW; ++w) kc[w] = sk[from][key * (D / 8) + g * KW + w];
+        byte = sks[from][key * GR + g * GR / 4];
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const floatx4_t z = q[rt].scores(kc, byte);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sc[rt][kt * 4 + j] = z[j];
+      }
     }
   };
 
@@ -107,38 +138,24 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
     for (int dt = 0; dt < D / 16; ++dt) acc[rt][dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
   }
 
+  // Keys are a tile ahead of values: while a tile's weights are formed on the vector ALU,
+  // the matrix cores work on the next tile's scores.
+  float sc[RT][PK / 4];
   if (last >= 0) {
-    load(0);
-    put(stage[0]);
-    load(PK);
+    load_keys(0);
+    load_values(0);
+    put_keys(0);
+    put_values(0);
+    load_keys(PK);
+    put_keys(1);
+    load_keys(2 * PK);
+    load_values(PK);
     __syncthreads();
+    score(0, sc);
+    __syncthreads();  // (the first iteration overwrites these keys)
   }
   for (int row0 = 0, i = 0; row0 <= last; row0 += PK, i ^= 1) {
-    Stage& now = stage[i];
-    put(stage[i ^ 1]);  // (the tile before, which lay there, is behind the barrier)
-    load(row0 + 2 * PK);
     if (row0 <= wlast) {
-      float sc[RT][PK / 4];
-#pragma unroll
-      for (int kt = 0; kt < PK / 16; ++kt) {
-        const int key = kt * 16 + m;
-        uint32_t kc[KW], byte;
-        if constexpr (MX) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(now.k + (key * GR + g % GR) * 4);
-          kc[0] = w[0]; kc[1] = w[1]; kc[2] = w[2]; kc[3] = w[3];
-          byte = now.ks[key * GR + g % GR];
-        } else {
-#pragma unroll
-          for (int w = 0; w < KW; ++w) kc[w] = now.k[key * (D / 8) + g * KW + w];
-          byte = now.ks[key * GR + g * GR / 4];
-        }
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          const floatx4_t z = q[rt].scores(kc, byte);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) sc[rt][kt * 4 + j] = z[j];
-        }
-      }
       if (row0 + PK - 1 > all) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
@@ -146,7 +163,6 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
           for (int j = 0; j < PK / 4; ++j)
             if (row0 + j / 4 * 16 + 4 * g + j % 4 > qlast[rt]) sc[rt][j] = -INFINITY;
       }
-      bf16x8_t pp[RT][PK / 32][NP];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         float mx = sc[rt][0];
@@ -163,6 +179,12 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
 #pragma unroll
           for (int dt = 0; dt < D / 16; ++dt) acc[rt][dt] *= scale;
         }
+      }
+      float nsc[RT][PK / 4];
+      score(i ^ 1, nsc);
+      bf16x8_t pp[RT][PK / 32][NP];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
         for (int j = 0; j < PK / 4; ++j) {
           sc[rt][j] = __builtin_amdgcn_exp2f(fmaf(sc[rt][j], c2, -mrun[rt]));
@@ -175,7 +197,7 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
       for (int ch = 0; ch < PK / 32; ++ch)
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) {
-          const bf16x8_t vf = value_columns<D>(now.v + ch * 32 * kVStride<D>, dt, m, g);
+          const bf16x8_t vf = value_columns<D>(sv[i] + ch * 32 * kVStride<D>, dt, m, g);
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -183,7 +205,15 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
               acc[rt][dt] =
                   __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[rt][ch][p], acc[rt][dt], 0, 0, 0);
         }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int j = 0; j < PK / 4; ++j) sc[rt][j] = nsc[rt][j];
     }
+    put_keys(i);         // (the tile's own keys were last read in the iteration before)
+    put_values(i ^ 1);   // (the tile before, which lay there, is behind the barrier)
+    load_keys(row0 + 3 * PK);
+    load_values(row0 + 2 * PK);
     __syncthreads();
   }
 
