@@ -77,16 +77,21 @@ __device__ __forceinline__ uint64_t lane_move(uint64_t x, uint64_t none) {
   return (uint64_t)lane_move<CTRL, ROWS>((uint32_t)(x >> 32), (uint32_t)(none >> 32)) << 32 |
          lane_move<CTRL, ROWS>((uint32_t)x, (uint32_t)none);
 }
-// op over the 64 lanes, the same in all of them; op(x, none) = x.  Rows of 16 lanes by
-// shifts, then across rows: six steps of a few cycles where a shuffle takes an LDS trip.
+// op over the lanes up to each; op(x, none) = x.  Rows of 16 lanes by shifts, then across
+// rows: six steps of a few cycles where a shuffle takes an LDS trip.
 template <typename K, typename F>
-__device__ __forceinline__ K wave_reduce(K x, K none, F op) {
+__device__ __forceinline__ K wave_scan(K x, K none, F op) {
   x = op(x, lane_move<0x111, 0xf>(x, none));  // from 1, 2, 4, 8 lanes below
   x = op(x, lane_move<0x112, 0xf>(x, none));
   x = op(x, lane_move<0x114, 0xf>(x, none));
   x = op(x, lane_move<0x118, 0xf>(x, none));
   x = op(x, lane_move<0x142, 0xa>(x, none));  // lane 15 of a row to the next row
-  x = op(x, lane_move<0x143, 0xc>(x, none));  // lane 31 to the upper half
+  return op(x, lane_move<0x143, 0xc>(x, none));  // lane 31 to the upper half
+}
+// op over all lanes, the same in each.
+template <typename K, typename F>
+__device__ __forceinline__ K wave_reduce(K x, K none, F op) {
+  x = wave_scan<K>(x, none, op);
   if constexpr (sizeof(K) == 8)
     return (K)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), 63) << 32 |
            (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, 63);
