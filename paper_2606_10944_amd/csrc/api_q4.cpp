@@ -283,7 +283,8 @@ int thin_q4_attention(const thin_q4_cache_t* cache, const void* Q, const int64_t
   a.shape = p.shape;
   if (p.bytes) {
     a.part = static_cast<float*>(workspace);
-    a.table = reinterpret_cast<int2*>(static_cast<char*>(workspace) + p.sums);
+    if (!blocks && p.shape.waves)
+      a.table = reinterpret_cast<int2*>(static_cast<char*>(workspace) + p.sums);
   }
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = observed(THIN_KERNEL_Q4_ATTENTION, -1, st, [&] {

@@ -75,10 +75,10 @@ struct Q4AttnArgs {
   const int32_t* blocks;  // null: every cached row
   int32_t n_sel;
   Q4AttnShape shape;
-  // shape.splits > 1: [slot, 16, d] sums, then [slot, 2, 16] maxima and sums; where the
-  // slots follow the sequences' lengths, the first and the number of each sequence's
-  // ([tile, B], the same for every head)
+  // shape.splits > 1: [slot, 16, d] sums, then [slot, 2, 16] maxima and sums
   float* part;
+  // where the slots follow the sequences' lengths, the first and the number of each
+  // sequence's ([tile, B], the same for every head), else null
   int2* table;
 };
 hipError_t launch_q4_attention(int dtype, int64_t d, const Q4View& c, const Q4AttnArgs& a,

@@ -418,15 +418,17 @@ __global__ __launch_bounds__(JT) void q4_join_kernel(Q4View c, Q4AttnArgs a) {
   __shared__ floatx4_t part[JT];
   const int b = blockIdx.y / c.H, h = blockIdx.y % c.H, tile = blockIdx.x;
   const int splits = a.shape.splits;
-  int nrows, n;
-  int64_t slot0;
+  int nrows;
   if (LIST) {
     const int gt = (a.G + 15) / 16;
     nrows = std::min(16, a.G - tile % gt * 16);
-    slot0 = ((int64_t)blockIdx.y * gridDim.x + tile) * splits;
-    n = splits;
   } else {
     nrows = std::min(16, a.tok.T * a.G - tile * 16);
+  }
+  // the tile's slots: `splits` of them, or those that its sequence got by its length
+  int n = splits;
+  int64_t slot0 = ((int64_t)blockIdx.y * gridDim.x + tile) * splits;
+  if (a.table) {
     const int2 mine = a.table[tile * c.B + b];
     slot0 = ((int64_t)h * gridDim.x + tile) * c.B * splits + mine.x;
     n = mine.y;

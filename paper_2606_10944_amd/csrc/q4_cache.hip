@@ -671,7 +671,7 @@ hipError_t scores_d(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
   const int64_t nb = (c.n_max + kQ4Block - 1) / kQ4Block;
   const int64_t rows = (int64_t)c.B * c.H * a.tn, per = THREADS / SLANES;
   int64_t x = (nb + per - 1) / per;
-  const int64_t most = (4096 + rows - 1) / rows;  // workgroups enough to fill the device
+  const int64_t most = (1024 + rows - 1) / rows;  // four workgroups per compute unit
   if (x > most) x = most;
   const dim3 grid((uint32_t)(x * a.tn), (uint32_t)(c.B * c.H));
   q4_scores_kernel<T, D><<<grid, THREADS, 0, st>>>(c, a);

@@ -27,16 +27,30 @@ struct Q4AttnShape {
   int32_t least;   // steps of 32 keys that a workgroup takes at least
 };
 
-// Two workgroups of four waves per compute unit (512): 8 sequences of 3000 to 65536 rows,
-// 8 key heads, d = 128, bf16: 67 us, against 85 with 256, 68 with 768, 84 with 1024 (the
-// last of them run alone).  Up to 2048 keys one workgroup of eight waves takes them all:
-// no second launch to join sums.  Long caches of more slices are shared out in two, so
-// that one long sequence among short ones is not left to one workgroup per head.
+// Few query rows per slice.  Two workgroups of four waves per compute unit (512): 8
+// sequences of 3000 to 65536 rows, 8 key heads, d = 128, bf16: 67 us, against 85 with 256,
+// 68 with 768, 84 with 1024 (the last of them run alone).  Up to 2048 keys one workgroup
+// of eight waves takes them all: no second launch to join sums.  Long caches of more
+// slices are shared out in two, so that one long sequence among short ones is not left
+// to one workgroup per head.
+//
+// Many query rows.  The kernel that shares decoded rows takes 1.3 us per 64 keys where a
+// compute unit has one workgroup, so it pays where there is one for each (16 sequences x 8
+// heads x 1024 rows, 256 query rows a head, 256 workgroups: 32 us against 42; 128 query
+// rows, 128 workgroups: 29 against 25), or where keys are shared out: 8 key heads x 16384
+// rows, 192 query rows a head, 96 tiles of 16: 38 against 41 us; 64 query rows: 28 against
+// 24; 32 slices x 4096 rows, 96 query rows, 192 tiles: 27 against 41.
 inline Q4AttnShape q4_attention_shape(int64_t B, int64_t H, int64_t G, int64_t T, bool list,
                                       int64_t keys, bool bf16) {
-  const int64_t per = q4_prompt_rows(bf16), prompt = B * H * ((T * G + per - 1) / per);
-  if (!list && prompt >= 256) return {0, 1, 1};
   const int64_t groups = B * H * q4_row_tiles(G, T, list);
+  if (!list && T * G >= 64) {
+    const int64_t per = q4_prompt_rows(bf16), wide = B * H * ((T * G + per - 1) / per);
+    if (keys <= 2048 ? wide >= 256 : groups >= 128) {
+      if (keys <= 2048 || wide >= 512) return {0, 1, 1};
+      const int64_t splits = 512 / wide, most = keys / 512;
+      return {0, (int32_t)(splits < most ? splits : most), 1};
+    }
+  }
   if (keys <= 2048 || groups > 1024 || B > kQ4SharedEntries) return {groups > 511 ? 4 : 8, 1, 1};
   const int64_t steps = (keys + kQ4Step - 1) / kQ4Step;
   int64_t splits = 512 / groups;

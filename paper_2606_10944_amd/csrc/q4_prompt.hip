@@ -35,10 +35,12 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
 
-  // slice by slice; a slice's last tiles, which see the most rows, come first
+  // slice by slice; a slice's last tiles, which see the most rows, come first; the
+  // workgroups that share a tile's keys side by side
   const uint32_t piece = xcd_contiguous();
   const int slice = piece / gridDim.x, b = slice / c.H, h = slice % c.H;
-  const int tile = gridDim.x - 1 - (int)(piece % gridDim.x);
+  const int splits = a.shape.splits, split = piece % splits;
+  const int tile = (int)(gridDim.x / splits) - 1 - (int)(piece % gridDim.x / splits);
   const int nrows = a.tok.T * a.G;
   const int r0 = tile * (ROWS * PW);  // the workgroup's first query row
   const int cnt = a.tok.count ? std::min(a.tok.count[b], a.tok.T) : a.tok.T;
@@ -70,6 +72,10 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
 #pragma unroll
   for (int x = 1; x < 16; x *= 2) all = std::min(all, __shfl_xor(all, x));
   all = __builtin_amdgcn_readfirstlane(all);
+
+  // this workgroup's share of the rows: k0 .. k1 - 1, whole tiles of them
+  const int share = (last / PK + splits) / splits * PK;
+  const int k0 = split * share, k1 = std::min(last + 1, k0 + share);
 
   // this thread's word of a tile: row and group
   const int srow = threadIdx.x / GR, sgr = threadIdx.x % GR;
@@ -141,20 +147,20 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
   // Keys are a tile ahead of values: while a tile's weights are formed on the vector ALU,
   // the matrix cores work on the next tile's scores.
   float sc[RT][PK / 4];
-  if (last >= 0) {
-    load_keys(0);
-    load_values(0);
+  if (k0 < k1) {
+    load_keys(k0);
+    load_values(k0);
     put_keys(0);
     put_values(0);
-    load_keys(PK);
+    load_keys(k0 + PK);
     put_keys(1);
-    load_keys(2 * PK);
-    load_values(PK);
+    load_keys(k0 + 2 * PK);
+    load_values(k0 + PK);
     __syncthreads();
     score(0, sc);
     __syncthreads();  // (the first iteration overwrites these keys)
   }
-  for (int row0 = 0, i = 0; row0 <= last; row0 += PK, i ^= 1) {
+  for (int row0 = k0, i = 0; row0 < k1; row0 += PK, i ^= 1) {
     if (row0 <= wlast) {
       if (row0 + PK - 1 > all) {
 #pragma unroll
@@ -222,9 +228,23 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
     float l = lrun[rt];
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     const int r = w0 + rt * 16 + m;
     if (r >= nrows) continue;
+    if (splits > 1) {  // sums, maximum and sum of weights of the row, for the join
+      const int tiles = (nrows + 15) / 16;
+      const int64_t slots = (int64_t)gridDim.y * tiles * splits;
+      const int64_t slot = ((int64_t)slice * tiles + r / 16) * splits + split;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt)
+        *reinterpret_cast<floatx4_t*>(a.part + (slot * 16 + m) * D + dt * 16 + 4 * g) = acc[rt][dt];
+      float* ml = a.part + slots * 16 * D + slot * 32;
+      if (g == 0) {
+        ml[m] = mrun[rt];
+        ml[16 + m] = l;
+      }
+      continue;
+    }
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     T* p = static_cast<T*>(const_cast<void*>(a.o.p)) + b * a.o.sb +
            ((int64_t)h * a.G + r % a.G) * a.o.sh + r / a.G * a.o.sr + 4 * g;
 #pragma unroll
@@ -244,7 +264,7 @@ hipError_t prompt_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
   constexpr int RT = Elem<T>::bytes == 2 ? 2 : 1;
   static_assert(16 * RT * PW == q4_prompt_rows(Elem<T>::bytes == 2), "rows of a workgroup");
   const int64_t tiles = ((int64_t)a.tok.T * a.G + 16 * RT * PW - 1) / (16 * RT * PW);
-  const dim3 grid((uint32_t)tiles, (uint32_t)(c.B * c.H));
+  const dim3 grid((uint32_t)(tiles * a.shape.splits), (uint32_t)(c.B * c.H));
   q4_prompt_kernel<T, D, RT><<<grid, 64 * PW, 0, st>>>(c, a);
   return hipGetLastError();
 }

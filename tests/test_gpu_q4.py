@@ -422,14 +422,17 @@ def check_dense(c, q, at, count, got, dtype):
             assert ok.all(), (b, h, (~ok).nonzero()[:3].tolist())
 
 
-# Enough query rows for the kernel that shares decoded rows: 256 workgroups of 128 (64
-# float32) rows, the last one of a slice partly filled.
+# Enough query rows for the kernel that shares decoded rows, the last workgroup of a slice
+# partly filled; the last three with workgroups that share a tile's keys, too.
 PROMPT = [
     (128, 4, 16, 4, 130, 700, [0, 300, 570, 650], None),
     (64, 8, 8, 1, 513, 600, [0, 5, 87, -20, 60, 300, 1, 80], [513, 500, 0, 400, 1, 300, 129, 64]),
     (32, 16, 16, 16, 9, 300, list(range(0, 288, 18)), None),
     (128, 2, 50, 3, 171, 171, [0, 0], [171, 100]),
     (64, 43, 2, 7, 55, 200, [3 * b for b in range(43)], None),
+    (128, 1, 8, 4, 67, 5000, [4900], None),
+    (64, 4, 4, 2, 70, 3000, [2930, 0, -30, 1500], [70, 70, 60, 0]),
+    (32, 2, 3, 9, 60, 9000, [8940, 1000], None),
 ]
 
 
