@@ -15,7 +15,10 @@ constexpr int64_t kMaxTokens = thin::kQ4MaxTokens;
 // workgroups of a grid row: the runtime takes fewer than 2^32 threads
 constexpr int64_t kMaxGroups = ((int64_t)1 << 24) - 1;
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+bool aligned16(const void* p) { return aligned(p, 16); }
+// device int32 arguments: the first required, the second nullable
+bool valid_ints(const int32_t* p, const int32_t* q) { return p && aligned(p, 4) && aligned(q, 4); }
 
 bool supported_d(int64_t d) { return d == 32 || d == 64 || d == 128; }
 
@@ -106,7 +109,9 @@ int thin_rotary(const void* X, const int64_t* x_strides, int64_t x_heads, void* 
     return THIN_EINVAL;
   if (rot < 16 || rot > d || rot % 16 != 0) return THIN_EINVAL;
   if (layout != THIN_ROTARY_HALF && layout != THIN_ROTARY_INTERLEAVED) return THIN_EINVAL;
-  if (x_heads < 1 || x_heads > kMaxSlices || !pos || !turns || !isfinite(amp)) return THIN_EINVAL;
+  if (x_heads < 1 || x_heads > kMaxSlices || !valid_ints(pos, nullptr) ||
+      !turns || !aligned(turns, 8) || !isfinite(amp))
+    return THIN_EINVAL;
   if (Y ? (y_heads < 1 || y_heads > kMaxSlices) : (y_heads != 0 || Y_out)) return THIN_EINVAL;
   thin::RotaryArgs a{};
   int rc = rows_view(X, x_strides, B, x_heads, T, d, dtype, false, &a.x);
@@ -163,7 +168,7 @@ int thin_q4_store(const thin_q4_cache_t* cache, const void* K, const int64_t* k_
   int rc = cache_view(cache, &c);
   if (rc) return rc;
   if (!known_dtype(dtype)) return THIN_EDTYPE;
-  if (T < 1 || T > kMaxTokens || !at) return THIN_EINVAL;
+  if (T < 1 || T > kMaxTokens || !valid_ints(at, count)) return THIN_EINVAL;
   thin::RowsView k, v;
   rc = rows_view(K, k_strides, c.B, c.H, T, cache->d, dtype, false, &k);
   if (!rc) rc = rows_view(V, v_strides, c.B, c.H, T, cache->d, dtype, false, &v);
@@ -181,7 +186,8 @@ int thin_q4_load(const thin_q4_cache_t* cache, int64_t T, const int32_t* at, voi
   const int rc = cache_view(cache, &c);
   if (rc) return rc;
   if (!known_dtype(dtype)) return THIN_EDTYPE;
-  if (T < 1 || T > THIN_Q4_MAX_ROWS || !at || !K || !V || !aligned16(K) || !aligned16(V))
+  if (T < 1 || T > THIN_Q4_MAX_ROWS || !valid_ints(at, nullptr) || !K || !V || !aligned16(K) ||
+      !aligned16(V))
     return THIN_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = observed(THIN_KERNEL_Q4_LOAD, -1, st, [&] {
@@ -208,7 +214,8 @@ int thin_q4_select(const thin_q4_cache_t* cache, const void* Q, const int64_t* q
   if (rc) return rc;
   if (!known_dtype(dtype)) return THIN_EDTYPE;
   size_t need = 0;
-  if (thin_q4_select_plan(c.B, c.H, c.n_max, T, &need) != THIN_OK || !at || !blocks)
+  if (thin_q4_select_plan(c.B, c.H, c.n_max, T, &need) != THIN_OK ||
+      !valid_ints(at, count) || !valid_ints(blocks, nullptr))
     return THIN_EINVAL;
   if (!group_of(q_heads, c.H)) return THIN_EINVAL;
   if (n_sel < 1 || n_sel > 32768 || n_sinks < 0 || n_window < 1 || n_sinks > n_sel ||
@@ -267,7 +274,7 @@ int thin_q4_attention(const thin_q4_cache_t* cache, const void* Q, const int64_t
   if (rc) return rc;
   if (!known_dtype(dtype)) return THIN_EDTYPE;
   AttnPlan p;
-  if (!at || (blocks != nullptr) != (n_sel > 0) ||
+  if (!valid_ints(at, count) || !aligned(blocks, 4) || (blocks != nullptr) != (n_sel > 0) ||
       !plan_attention(c.B, c.H, q_heads, c.n_max, cache->d, T, n_sel, dtype == THIN_BF16, &p))
     return THIN_EINVAL;
   thin::Q4AttnArgs a{};

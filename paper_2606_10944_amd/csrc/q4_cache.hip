@@ -62,7 +62,7 @@ __global__ __launch_bounds__(THREADS) void q4_store_kernel(Q4View c, RowsView k,
   // the new rows that are rows of the cache
   const int64_t lo = at < 0 ? 0 : at, hi = at + cnt < c.n_max ? at + cnt : c.n_max;
   const int64_t r0 = (lo / kQ4Block + blockIdx.x) * kQ4Block;
-  if (r0 >= hi) return;
+  if (lo >= hi || r0 >= hi) return;  // (no new row, here or at all)
   const int l = threadIdx.x % LR, rp = threadIdx.x / LR;
   float mn[8], mx[8];
 #pragma unroll

@@ -21,7 +21,8 @@ namespace {
 constexpr int PW = 4;    // waves
 constexpr int PK = 64;   // cached rows per tile
 
-template <typename T, int D, int RT>
+// SPLIT: workgroups share a tile's keys and leave sums for the join.
+template <typename T, int D, int RT, bool SPLIT>
 __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnArgs a) {
   constexpr bool MX = Elem<T>::bytes == 2;
   constexpr int NP = MX ? 1 : 3;                  // bf16 parts of the weights
@@ -39,7 +40,7 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
   // workgroups that share a tile's keys side by side
   const uint32_t piece = xcd_contiguous();
   const int slice = piece / gridDim.x, b = slice / c.H, h = slice % c.H;
-  const int splits = a.shape.splits, split = piece % splits;
+  const int splits = SPLIT ? a.shape.splits : 1, split = SPLIT ? piece % splits : 0;
   const int tile = (int)(gridDim.x / splits) - 1 - (int)(piece % gridDim.x / splits);
   const int nrows = a.tok.T * a.G;
   const int r0 = tile * (ROWS * PW);  // the workgroup's first query row
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
 
   // this workgroup's share of the rows: k0 .. k1 - 1, whole tiles of them
   const int share = (last / PK + splits) / splits * PK;
-  const int k0 = split * share, k1 = std::min(last + 1, k0 + share);
+  const int k0 = split * share, k1 = SPLIT ? std::min(last + 1, k0 + share) : last + 1;
 
   // this thread's word of a tile: row and group
   const int srow = threadIdx.x / GR, sgr = threadIdx.x % GR;
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
     l += __shfl_xor(l, 32);
     const int r = w0 + rt * 16 + m;
     if (r >= nrows) continue;
-    if (splits > 1) {  // sums, maximum and sum of weights of the row, for the join
+    if (SPLIT) {  // sums, maximum and sum of weights of the row, for the join
       const int tiles = (nrows + 15) / 16;
       const int64_t slots = (int64_t)gridDim.y * tiles * splits;
       const int64_t slot = ((int64_t)slice * tiles + r / 16) * splits + split;
@@ -265,7 +266,10 @@ hipError_t prompt_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
   static_assert(16 * RT * PW == q4_prompt_rows(Elem<T>::bytes == 2), "rows of a workgroup");
   const int64_t tiles = ((int64_t)a.tok.T * a.G + 16 * RT * PW - 1) / (16 * RT * PW);
   const dim3 grid((uint32_t)(tiles * a.shape.splits), (uint32_t)(c.B * c.H));
-  q4_prompt_kernel<T, D, RT><<<grid, 64 * PW, 0, st>>>(c, a);
+  if (a.shape.splits > 1)
+    q4_prompt_kernel<T, D, RT, true><<<grid, 64 * PW, 0, st>>>(c, a);
+  else
+    q4_prompt_kernel<T, D, RT, false><<<grid, 64 * PW, 0, st>>>(c, a);
   return hipGetLastError();
 }
 

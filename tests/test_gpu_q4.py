@@ -136,7 +136,8 @@ def fresh(B, H, n_max, d, fill=0x55):
 @pytest.mark.parametrize("B,H,n_max,T,at,count", [
     (1, 1, 1, 1, [0], None), (2, 3, 200, 1, [63, 64], None), (3, 2, 130, 70, [0, 1, 60], None),
     (3, 1, 200, 65, [100, 0, 135], [65, 0, 30]), (2, 2, 100, 64, [-10, 80], None),
-    (2, 1, 64, 3, [64, 70], None), (2, 1, 300, 129, [127, 1], [129, 200])])
+    (2, 1, 64, 3, [64, 70], None), (2, 1, 300, 129, [127, 1], [129, 200]),
+    (3, 2, 100, 2, [70, 105, 98], [0, 2, -3])])
 def test_store(dtype, d, B, H, n_max, T, at, count):
     g = gen(4)
     k = randn(g, B, H, T, d, dtype=dtype) * torch.exp2(
@@ -207,6 +208,20 @@ def test_load(d):
             want[0, :, 3:] = all_[0, :, :27]
             want[1, :, :20] = all_[1, :, 70:]
             assert torch.equal(got.cpu().double(), want)
+
+
+def test_calls_without_new_rows_leave_the_bounds():
+    """No token (count 0), or tokens behind the cache: nothing changes, though rows of the
+    position's block stand before it."""
+    g = gen(23)
+    c = fresh(3, 1, 100, 64)
+    x = randn(g, 3, 1, 100, 64).to(DEV)
+    thin_q4_store(x, x, c, i32([0, 0, 0]))
+    before = [t.clone() for t in (c.k_codes, c.k_scales, c.v_codes, c.v_scales, c.bounds)]
+    thin_q4_store(x[:, :, :4] * 9, x[:, :, :4], c, i32([70, 101, 2000000000]),
+                  count=i32([0, 4, 4]))
+    for t, was in zip((c.k_codes, c.k_scales, c.v_codes, c.v_scales, c.bounds), before):
+        assert torch.equal(t, was)
 
 
 def test_rewound_rows_leave_the_bounds():
@@ -358,13 +373,15 @@ def test_select_in_pieces():
 # ---------------------------------------------------------------------------
 # Attention
 # ---------------------------------------------------------------------------
-# Scores: products of float32 sums; the matrix instructions add a row's d products
-# in float32 (2^-24 of the sum of magnitudes for each of at most d additions, far
-# fewer in sequence: 16 for d = 128 with the parts of float32 queries), the scale
-# and the exponential another few 2^-24 of the score: at most 2^-19 S, S = the
-# largest sum |q_c k_c| / sqrt d.  A weight's relative error is that, twice (its own
-# and the maximum's), and the sums of weights and of products 2^-20.  A weight rounds
-# by half a step of bf16 for bf16 queries, the output by half a step of its type.
+# float32 queries: the matrix instructions add a row's d products in float32 (2^-24 of the
+# sum of magnitudes for each of at most d additions, far fewer in sequence: 16 for d = 128
+# with the parts of the queries), the scale and the exponential another few 2^-24 of the
+# score: at most 2^-19 S, S = the largest sum |q_c k_c| / sqrt d.  A weight's relative error
+# is that, twice (its own and the maximum's), and the sums of weights and of products
+# 2^-20; the output rounds by half a step.  All of it is taken twice.  bf16 queries: a
+# weight rounds by half a step of bf16 as well; the second half-step that the factor of two
+# leaves covers what the scaled instruction cuts (1e-6 S for normal values, 6e-5 S seen at
+# most: below 2^-8 up to S = 32).
 def attention_bound(want, A, S, dtype):
     rel = 2 * 2.0 ** -19 * S + 2.0 ** -20 + (half_step("bf16") if dtype == "bf16" else 0.0)
     return rel * A * 2 + half_step(dtype) * want.abs() + 1e-30
@@ -608,6 +625,11 @@ def test_steps_together(n_sel):
         lens = [a + x for a, x in zip(lens, cnt)]
 
 
+def same_contents(a, b):
+    return all(torch.equal(getattr(a, name), getattr(b, name))
+               for name in ("k_codes", "k_scales", "v_codes", "v_scales", "bounds"))
+
+
 def test_replayed_step_follows_its_positions():
     """A captured step on another stream, replayed with new rows and positions."""
     g = gen(16)
@@ -633,8 +655,85 @@ def test_replayed_step_follows_its_positions():
         want = caches[1].step(q, k, v, at.clone(), turns=t, n_sel=6)
         torch.cuda.synchronize()
         assert torch.equal(o, want)
-        for name in ("k_codes", "k_scales", "v_codes", "v_scales", "bounds"):
-            assert torch.equal(getattr(caches[0], name), getattr(caches[1], name))
+        assert same_contents(*caches)
+
+
+@pytest.mark.parametrize("T,n_max,d,n_sel", [(33, 60000, 32, 5), (70, 5000, 128, 0)])
+def test_replayed_prompt_follows_its_positions(T, n_max, d, n_sel):
+    """A captured chunk (choice with over 64 KiB of LDS; shared tiles and their join),
+    replayed with new rows, positions and counts, eager work between."""
+    g = gen(24)
+    B, H, G = 2, 32 if n_sel else 2, 2
+    caches = [filled(gen(25), B, H, n_max, d, [n_max, n_max]) for _ in range(2)]
+    q, k, v = (torch.zeros(B, n, T, d, dtype=torch.bfloat16, device=DEV) for n in (H * G, H, H))
+    at, count = i32([n_max - T, 100]), i32([T, T])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for c in caches:
+            c.step(q, k, v, at, count=count, n_sel=n_sel)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o = caches[0].step(q, k, v, at, count=count, n_sel=n_sel)
+    for i in range(4):
+        for x in (q, k, v):
+            x.copy_(randn(g, *x.shape, dtype="bf16"))
+        at.copy_(i32([n_max - T - 7 * i, 100 + 900 * i]))
+        count.copy_(i32([T - i, T if i % 2 else 1]))
+        graph.replay()
+        want = caches[1].step(q, k, v, at.clone(), count=count.clone(), n_sel=n_sel)
+        torch.cuda.synchronize()
+        assert torch.equal(o, want)
+        assert same_contents(*caches)
+
+
+def test_binding_refuses_what_does_not_fit():
+    from paper_2606_10944_amd._lib import THIN_EDTYPE, THIN_EINVAL, THIN_EWORKSPACE, ThinError
+    g = gen(26)
+    c = filled(g, 2, 2, 5000, 64, [5000, 5000])
+    q = randn(g, 2, 4, 1, 64, dtype="bf16").to(DEV)
+    at = i32([10, 20])
+    turns = thin_rotary_turns(64)[0].to(DEV)
+    kv = randn(g, 2, 2, 1, 64).to(DEV)
+    wide = torch.zeros(2, 4, 1, 128, dtype=torch.bfloat16, device=DEV)
+
+    def refused(status, f, *a, **kw):
+        with pytest.raises(ThinError) as e:
+            f(*a, **kw)
+        assert e.value.status == status
+
+    for bad in (q.cpu(), q[:1], q[..., :32], q[:, :3], q[0], wide[..., ::2]):
+        refused(THIN_EINVAL, thin_q4_attention, bad, c, at)
+        refused(THIN_EINVAL, thin_q4_select, bad, c, at, 4)
+    refused(THIN_EINVAL, thin_q4_attention, wide[..., 4:68], c, at)  # not 16-byte aligned
+    refused(THIN_EDTYPE, thin_q4_attention, q.half(), c, at)
+    for bad in (at.long(), at[:1], at.cpu(), torch.stack((at, at), 1)[:, 0]):
+        refused(THIN_EINVAL, thin_q4_attention, q, c, bad)
+        refused(THIN_EINVAL, thin_q4_attention, q, c, at, count=bad)
+        refused(THIN_EINVAL, thin_q4_store, kv, kv, c, bad)
+        refused(THIN_EINVAL, thin_rotary, q, bad, turns)
+    refused(THIN_EINVAL, thin_q4_attention, q, c, at, O=q.float())
+    refused(THIN_EINVAL, thin_q4_attention, q, c, at, O=torch.zeros_like(q[:1]).expand(2, 4, 1, 64))
+    refused(THIN_EINVAL, thin_q4_attention, q, c, at, blocks=i32([[1]]))
+    refused(THIN_EINVAL, thin_q4_attention, q, c, at,
+            blocks=torch.zeros(2, 2, 1, 4, dtype=torch.int64, device=DEV))
+    refused(THIN_EWORKSPACE, thin_q4_attention, q, c, at,
+            workspace=torch.zeros(256, dtype=torch.uint8, device=DEV))
+    refused(THIN_EINVAL, thin_q4_select, q, c, at, 4, n_sinks=3)
+    refused(THIN_EINVAL, thin_q4_select, q, c, at, 0)
+    refused(THIN_EINVAL, thin_q4_store, kv[:, :1], kv, c, at)
+    refused(THIN_EDTYPE, thin_q4_store, kv, kv.bfloat16(), c, at)
+    refused(THIN_EINVAL, thin_q4_load, c, at, 0)
+    refused(THIN_EINVAL, thin_q4_load, c, at, 3, K=kv)
+    for bad in (turns.float(), turns.cpu(), turns[:12], turns[::2]):
+        refused(THIN_EINVAL, thin_rotary, q, at, bad)
+    refused(THIN_EINVAL, thin_rotary, q, at, turns, layout="other")
+    refused(THIN_EINVAL, thin_rotary, q, at, turns, Y=kv[:1].bfloat16())
+    refused(THIN_EDTYPE, thin_rotary, q, at, turns, Y=kv)
+    refused(THIN_EINVAL, thin_rotary, q, at, turns, out_Y=q)
+    # the current device has not stopped working
+    check_attention(c, q.cpu(), [10, 20], None, None, thin_q4_attention(q, c, at), "bf16")
 
 
 def test_calls_on_a_stream_of_their_own():
