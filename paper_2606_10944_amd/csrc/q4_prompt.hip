@@ -135,19 +135,24 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
   };
 
   const float c2 = (float)(kQ4Log2e / sqrt((double)D));
-  float mrun[RT], lrun[RT];
+  float mrun[RT];
   floatx4_t acc[RT][D / 16];
+  // sums of weights: one more row of values, all ones (32 vector additions less per tile)
+  floatx4_t lrun[RT];
+  bf16x8_t ones;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) ones[j] = (__bf16)1.0f;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     mrun[rt] = kLowest;
-    lrun[rt] = 0.0f;
+    lrun[rt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) acc[rt][dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
   }
 
   // Keys are a tile ahead of values: while a tile's weights are formed on the vector ALU,
   // the matrix cores work on the next tile's scores.
-  float sc[RT][PK / 4];
+  float sc[2][RT][PK / 4];
   if (k0 < k1) {
     load_keys(k0);
     load_values(k0);
@@ -158,23 +163,25 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
     load_keys(k0 + 2 * PK);
     load_values(k0 + PK);
     __syncthreads();
-    score(0, sc);
-    __syncthreads();  // (the first iteration overwrites these keys)
+    score(0, sc[0]);
+    __syncthreads();  // (the first tile overwrites these keys)
   }
-  for (int row0 = k0, i = 0; row0 < k1; row0 += PK, i ^= 1) {
+  // One tile, its scores in s, the next one's to ns; i: its buffers.
+  auto tile_step = [&](int row0, int i, float (&s)[RT][PK / 4],
+                       float (&ns)[RT][PK / 4]) __attribute__((always_inline)) {
     if (row0 <= wlast) {
       if (row0 + PK - 1 > all) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
           for (int j = 0; j < PK / 4; ++j)
-            if (row0 + j / 4 * 16 + 4 * g + j % 4 > qlast[rt]) sc[rt][j] = -INFINITY;
+            if (row0 + j / 4 * 16 + 4 * g + j % 4 > qlast[rt]) s[rt][j] = -INFINITY;
       }
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        float mx = sc[rt][0];
+        float mx = s[rt][0];
 #pragma unroll
-        for (int j = 1; j < PK / 4; ++j) mx = fmaxf(mx, sc[rt][j]);
+        for (int j = 1; j < PK / 4; ++j) mx = fmaxf(mx, s[rt][j]);
         mx *= c2;
         if (__any(mx > mrun[rt] + kSlack)) {
           mx = fmaxf(mx, __shfl_xor(mx, 16));
@@ -187,21 +194,23 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
           for (int dt = 0; dt < D / 16; ++dt) acc[rt][dt] *= scale;
         }
       }
-      float nsc[RT][PK / 4];
-      score(i ^ 1, nsc);
+      score(i ^ 1, ns);
       bf16x8_t pp[RT][PK / 32][NP];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
 #pragma unroll
-        for (int j = 0; j < PK / 4; ++j) {
-          sc[rt][j] = __builtin_amdgcn_exp2f(fmaf(sc[rt][j], c2, -mrun[rt]));
-          lrun[rt] += sc[rt][j];
-        }
+        for (int j = 0; j < PK / 4; ++j)
+          s[rt][j] = __builtin_amdgcn_exp2f(fmaf(s[rt][j], c2, -mrun[rt]));
 #pragma unroll
-        for (int ch = 0; ch < PK / 32; ++ch) split8<NP>(sc[rt] + ch * 8, pp[rt][ch]);
+        for (int ch = 0; ch < PK / 32; ++ch) split8<NP>(s[rt] + ch * 8, pp[rt][ch]);
       }
 #pragma unroll
-      for (int ch = 0; ch < PK / 32; ++ch)
+      for (int ch = 0; ch < PK / 32; ++ch) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int p = NP - 1; p >= 0; --p)
+            lrun[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pp[rt][ch][p], lrun[rt], 0, 0, 0);
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) {
           const bf16x8_t vf = value_columns<D>(sv[i] + ch * 32 * kVStride<D>, dt, m, g);
@@ -212,23 +221,23 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
               acc[rt][dt] =
                   __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[rt][ch][p], acc[rt][dt], 0, 0, 0);
         }
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int j = 0; j < PK / 4; ++j) sc[rt][j] = nsc[rt][j];
+      }
     }
-    put_keys(i);         // (the tile's own keys were last read in the iteration before)
+    put_keys(i);         // (the tile's own keys were last read in the tile before)
     put_values(i ^ 1);   // (the tile before, which lay there, is behind the barrier)
     load_keys(row0 + 3 * PK);
     load_values(row0 + 2 * PK);
     __syncthreads();
+  };
+  for (int row0 = k0; row0 < k1; row0 += 2 * PK) {
+    tile_step(row0, 0, sc[0], sc[1]);
+    if (row0 + PK >= k1) break;
+    tile_step(row0 + PK, 1, sc[1], sc[0]);
   }
 
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    float l = lrun[rt];
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    const float l = lrun[rt][0];
     const int r = w0 + rt * 16 + m;
     if (r >= nrows) continue;
     if (SPLIT) {  // sums, maximum and sum of weights of the row, for the join
