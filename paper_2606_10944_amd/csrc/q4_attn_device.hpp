@@ -85,7 +85,7 @@ __device__ __forceinline__ Slice slice_of(const Q4View& c, int64_t s) {
 // float32: three bf16 parts (24 bits), the keys decoded to bf16.
 template <typename T, int D>
 struct Queries {
-  static constexpr int KS = D / 32;
+  static constexpr int KS = D / 32, N = 3 * KS;  // N: matrix instructions for 16 keys
   bf16x8_t q[3][KS];
   // row: this lane's query row (null: zeros); g: lane / 16
   __device__ __forceinline__ void load(const T* row, int g) {
@@ -130,17 +130,17 @@ struct Queries {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 template <int D>
 struct Queries<bf16_t, D> {
-  static constexpr int NI = D == 128 ? 2 : 1;  // instructions
-  i32x8 q[NI];
+  static constexpr int N = D == 128 ? 2 : 1;  // matrix instructions for 16 keys
+  i32x8 q[N];
   int scale;
   __device__ __forceinline__ void load(const bf16_t* row, int g) {
     // this lane's 16 channels (d = 128: 32) and the part that it holds
-    constexpr int N = D == 128 ? 32 : 16;
-    float f[N];
+    constexpr int C = D == 128 ? 32 : 16;
+    float f[C];
     const int c0 = D == 32 ? g % 2 * 16 : g * 16;
     float amax = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; i += 8) {
+    for (int i = 0; i < C; i += 8) {
       if (row)
         load8<bf16_t>(row + c0 + i / 16 * 64 + i % 16, f + i);
       else
@@ -148,7 +148,7 @@ struct Queries<bf16_t, D> {
         for (int j = 0; j < 8; ++j) f[i + j] = 0.0f;
     }
 #pragma unroll
-    for (int i = 0; i < N; ++i) amax = fmaxf(amax, fabsf(f[i]));
+    for (int i = 0; i < C; ++i) amax = fmaxf(amax, fabsf(f[i]));
     amax = fmaxf(amax, __shfl_xor(amax, 16));
     amax = fmaxf(amax, __shfl_xor(amax, 32));
     // the largest value lands in [2^7, 2^8)
@@ -156,11 +156,11 @@ struct Queries<bf16_t, D> {
     byte = byte < 1 ? 1 : byte;
     scale = byte;
     const float up = __uint_as_float((uint32_t)(254 - byte) << 23);
-    int part[2][N / 4];
+    int part[2][C / 4];
 #pragma unroll
     for (int p = 0; p < 2; ++p)
 #pragma unroll
-      for (int i = 0; i < N / 4; ++i) {
+      for (int i = 0; i < C / 4; ++i) {
         float* x = f + 4 * i;
         if (p == 0)
 #pragma unroll
@@ -177,7 +177,7 @@ struct Queries<bf16_t, D> {
     for (int i = 0; i < 8; ++i) {
       if (D == 128) {
         q[0][i] = part[0][i];
-        q[NI - 1][i] = part[1][i];
+        q[N - 1][i] = part[1][i];
       } else if (D == 64) {
         q[0][i] = part[i / 4][i % 4];
       } else {
@@ -189,7 +189,7 @@ struct Queries<bf16_t, D> {
     floatx4_t z = {0.f, 0.f, 0.f, 0.f};
     const i32x8 k = {(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3], 0, 0, 0, 0};
 #pragma unroll
-    for (int i = NI - 1; i >= 0; --i)
+    for (int i = N - 1; i >= 0; --i)
       z = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q[i], z, 4, 0, 0, (int)byte, 0, scale);
     return z;
   }

@@ -8,10 +8,11 @@
 // once per 64 RT query rows instead of once per 16, and each operand read from LDS
 // serves RT products.
 //
-// 4096 tokens over 16384 rows, 32 heads of 128 channels, 8 key heads, bf16: 766 us, 1.26
+// 4096 tokens over 16384 rows, 32 heads of 128 channels, 8 key heads, bf16: 685 us, 1.40
 // PFLOP/s (a library bf16 product of 8192^3 runs at 1.20).  The matrix cores alone need
-// 390 us of it (16 scaled instructions of 32 cycles and 32 of 16 per wave and tile); of
-// the rest, reading the values' columns costs 140 us, the exponentials 120, decoding 85.
+// 410 us of it (16 scaled instructions of 32 cycles and 36 of 16 per wave and tile), the
+// vector ALU 360; without the reads of the values' columns it takes 140 us less, without
+// the exponentials 120, without decoding 85.
 #include "q4_attn_device.hpp"
 
 namespace thin {
@@ -20,6 +21,16 @@ namespace {
 
 constexpr int PW = 4;    // waves
 constexpr int PK = 64;   // cached rows per tile
+
+// The schedule of a region: N times a matrix instruction, then V vector ones.
+template <int N, int V>
+__device__ __forceinline__ void interleave() {
+  if constexpr (N > 0) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
+    interleave<N - 1, V>();
+  }
+}
 
 // SPLIT: workgroups share a tile's keys and leave sums for the join.
 template <typename T, int D, int RT, bool SPLIT>
@@ -194,6 +205,11 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
           for (int dt = 0; dt < D / 16; ++dt) acc[rt][dt] *= scale;
         }
       }
+      // The next tile's scores among this one's exponentials, a matrix instruction to every
+      // few of them; and whichever wave of a SIMD has products to issue goes first (754 ->
+      // 732 us by the order alone, 710 by the priority alone, 685 by both).
+      __builtin_amdgcn_s_setprio(1);
+      __builtin_amdgcn_sched_barrier(0);
       score(i ^ 1, ns);
       bf16x8_t pp[RT][PK / 32][NP];
 #pragma unroll
@@ -204,6 +220,9 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
 #pragma unroll
         for (int ch = 0; ch < PK / 32; ++ch) split8<NP>(s[rt] + ch * 8, pp[rt][ch]);
       }
+      constexpr int NS = PK / 16 * RT * Queries<T, D>::N;  // matrix instructions of the scores
+      interleave<NS, std::max(1, RT * (PK / 4) * 7 / 2 / NS)>();
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int ch = 0; ch < PK / 32; ++ch) {
 #pragma unroll
@@ -222,6 +241,7 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
                   __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pp[rt][ch][p], acc[rt][dt], 0, 0, 0);
         }
       }
+      __builtin_amdgcn_s_setprio(0);
     }
     put_keys(i);         // (the tile's own keys were last read in the tile before)
     put_values(i ^ 1);   // (the tile before, which lay there, is behind the barrier)
