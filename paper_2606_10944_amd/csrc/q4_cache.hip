@@ -408,6 +408,25 @@ __device__ __forceinline__ float key_float(uint32_t k) {
   return __uint_as_float((k >> 31) ? k & 0x7fffffffu : ~k);
 }
 
+// N elements from an aligned place, N * sizeof(T) a power of two up to 16.
+template <typename T, int N>
+__device__ __forceinline__ void load_few(const T* p, float* f) {
+  constexpr int BYTES = N * Elem<T>::bytes;
+  typedef uint32_t words __attribute__((ext_vector_type(BYTES >= 4 ? BYTES / 4 : 1)));
+  if constexpr (BYTES < 4) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = elem<T>(p, j);
+  } else {
+    words w = *reinterpret_cast<const words*>(p);
+    uint32_t u[BYTES / 4];
+    __builtin_memcpy(u, &w, BYTES);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      f[j] = Elem<T>::bytes == 4 ? __uint_as_float(u[j])
+                                 : __uint_as_float(j % 2 ? u[j / 2] & 0xffff0000u : u[j / 2] << 16);
+  }
+}
+
 // Of the keys of a wave (key i of lane l stands at place 64 i + l) the largest `want`,
 // ties to the lowest places: bit i of the result says whether this lane's key i is one.
 // Keys of 0 are none; there are at least `want` others.
@@ -608,16 +627,20 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
         }
         // (all scores 0: the lowest blocks are chosen already)
         if (open > free - sure && !(size == 0.0f)) {
-          constexpr int N = 2 * D / 64;  // products per lane
+          // products of 2 D / 64 neighbouring channels per lane, q- beside lo, q+ beside hi
+          constexpr int N = 2 * D / 64;
+          const bool low = lane < 32;
           double qd[N];
 #pragma unroll
-          for (int j = 0; j < N; ++j) {
-            const int e = lane * N + j;
-            qd[j] = 0.0;
-            for (int x = 0; x < a.G; ++x) {
-              const float f = elem<T>(qh + x * a.q.sh + (int64_t)t * a.q.sr, e % D);
-              if (e < D ? !(f >= 0.0f) : f > 0.0f) qd[j] += (double)f;
-            }
+          for (int j = 0; j < N; ++j) qd[j] = 0.0;
+          const T* row = qh + (int64_t)t * a.q.sr + lane % 32 * N;
+#pragma unroll 4
+          for (int x = 0; x < a.G; ++x) {
+            float f[N];
+            load_few<T, N>(row + x * a.q.sh, f);
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+              if (low ? !(f[j] >= 0.0f) : f[j] > 0.0f) qd[j] += (double)f[j];
           }
           uint64_t wide[KPL];
 #pragma unroll
@@ -625,12 +648,13 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
             wide[i] = 0;
             for (uint64_t todo = __ballot(maybe >> i & 1); todo; todo &= todo - 1) {
               const int l = __ffsll((unsigned long long)todo) - 1;
-              const uint16_t* p = bounds + (int64_t)(i * 64 + l) * 2 * D + lane * N;
+              float f[N];
+              load_few<bf16_t, N>(reinterpret_cast<const bf16_t*>(bounds) +
+                                      (int64_t)(i * 64 + l) * 2 * D + lane * N, f);
               double sum = 0.0;
 #pragma unroll
-              for (int j = 0; j < N; ++j) sum += qd[j] * (double)bf16_to_float(p[j]);
-#pragma unroll
-              for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+              for (int j = 0; j < N; ++j) sum += qd[j] * (double)f[j];
+              sum = wave_sum(sum);
               if (lane == l) wide[i] = score_key(sum);
             }
           }

@@ -107,6 +107,15 @@ __device__ __forceinline__ K wave_max(K x) {
   return wave_reduce<K>(x, (K)0, [](K a, K b) { return a > b ? a : b; });
 }
 
+__device__ __forceinline__ double wave_sum(double x) {
+  const uint64_t r = wave_reduce<uint64_t>(
+      (uint64_t)__double_as_longlong(x), 0ull, [](uint64_t a, uint64_t b) {
+        return (uint64_t)__double_as_longlong(__longlong_as_double((long long)a) +
+                                              __longlong_as_double((long long)b));
+      });
+  return __longlong_as_double((long long)r);
+}
+
 // Instance F<element type, head dimension> of a launch.
 #define Q4_BY_D(F, ...)                                                                      \
   return dtype == 0 ? (d == 32   ? F<float, 32>(__VA_ARGS__)                                 \
