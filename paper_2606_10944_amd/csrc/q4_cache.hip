@@ -387,14 +387,17 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
 // Selection for several tokens of a slice in one launch.  A workgroup takes 16 tokens:
 // their scores of every block come from the bf16 matrix instructions, the queries'
 // float64 sums split into two bf16 parts (bounds are bf16), and stay in LDS.  Such a
-// score is off by less than eps = 1.25 * 2^-14 size, size = the token's largest sum of
-// the products' magnitudes: 4 d additions that lose at most 2^-23 of it each make 2^-14
-// for d = 128, the split leaves 2^-17 of each query sum.  So a block more than 2 eps
+// score is off by less than eps = 1.25 * 2^-16 size, size = the token's largest sum of
+// the products' magnitudes: the split leaves at most 2^-16 of each query sum (two
+// roundings by half a step, 2^-8), and a chain of 16 instructions was never seen more
+// than 2^-20.5 of the sum of magnitudes off (16 roundings of 2^-24 make 2^-20), against
+// the 2^-18 that is left for it.  So a block more than 2 eps
 // above the last one that fits is in, one more than 2 eps below it is out, whatever the
 // rounding; the others between (mostly that one alone) are scored again in float64.
 //
-// 2047 tokens x 8 key heads over up to 512 blocks, d = 128: 8e6 scores of 256 products,
-// 62 us in float64 at the rate of a large float64 matrix product.
+// 2047 tokens x 8 key heads over up to 512 blocks, d = 128 (8e6 scores of 256 products:
+// 62 us in float64 at the rate of a large float64 matrix product): 69 us, of which the
+// scores take 37, second scores 12, and the choice the rest.  In float64 throughout: 343.
 constexpr int SW = 8;  // waves
 
 // A float's key: integers of the same order, NaN below everything, 0 left free.
@@ -612,7 +615,7 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
 #pragma unroll
         for (int x = 0; x < SW; ++x) bits = std::max(bits, ssize[x][r]);
         const float size = __uint_as_float(bits);
-        const float eps = fmaxf(0x1.4p-13f * size, 0x1p-110f);
+        const float eps = fmaxf(0x1.4p-15f * size, 0x1p-110f);
         const float mid = key_float(least), up = mid + eps, down = mid - eps;
         const bool wild = !(size < INFINITY) || !(fabsf(mid) < INFINITY);
         int sure = 0, open = 0;
