@@ -2,7 +2,15 @@
 // row, or over the rows of the blocks listed for a token and key head.
 //
 // The kernel for few query rows: a wave takes 32 keys at a time on its own, its
-// decoded value rows in LDS.
+// decoded value rows in LDS, the next step's codes on their way meanwhile.
+//
+// d = 128, bf16, 8 key heads.  8 sequences of 3000 to 65536 rows, one token: 52 us for 298
+// MB, 5.7 TB/s (a stream of reads reaches 6.5), then 5 us for the join of the shared
+// tiles.  64 of 2048 blocks for 8 sequences: 11.5 + 4 us for 36 MB, latencies (a launch,
+// positions, lists, codes, four steps per wave, the join's three loads in turn).  32
+// blocks for each of 509 tokens: 110 us, LDS: writing 32 decoded value rows costs a
+// compute unit 128 cycles (64 bytes each) and reading them transposed 53, of the 260 that
+// a step takes.
 #include "q4_attn_device.hpp"
 
 namespace thin {
