@@ -12,8 +12,11 @@ namespace {
 
 constexpr int64_t kMaxSlices = 65535;  // grid y
 constexpr int64_t kMaxTokens = thin::kQ4MaxTokens;
-// workgroups of a grid row: the runtime takes fewer than 2^32 threads
-constexpr int64_t kMaxGroups = ((int64_t)1 << 24) - 1;
+// Query rows of an attention call, of a key head and in all: tiles of 16 of them (at least
+// one per token) stay below 2^24 a grid row, whose threads the runtime counts in 32 bits,
+// and below 2^31 in all.
+constexpr int64_t kMaxGroupRows = (int64_t)1 << 27;
+constexpr int64_t kMaxRows = (int64_t)1 << 30;
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 bool aligned16(const void* p) { return aligned(p, 16); }
@@ -83,14 +86,13 @@ bool plan_attention(int64_t B, int64_t H, int64_t q_heads, int64_t n_max, int64_
   if (!valid_sizes(B, H, n_max, T) || !supported_d(d) || !group_of(q_heads, H) || n_sel < 0 ||
       n_sel > 32768)
     return false;
+  if (T * (q_heads / H) > kMaxGroupRows || B * q_heads * T > kMaxRows) return false;
   const int64_t tiles = thin::q4_row_tiles(q_heads / H, T, n_sel > 0);
   p->shape = thin::q4_attention_shape(B, H, q_heads / H, T, n_sel > 0,
                                       n_sel > 0 ? n_sel * THIN_Q4_BLOCK : n_max, bf16);
   p->bytes = thin::q4_attention_bytes(B, H, tiles, p->shape.splits, d);
   p->sums = thin::q4_sums_bytes(B, H, tiles, p->shape.splits, d);
-  // (B * tiles * splits is at most 2048 where splits > 1; a launch's workgroups are counted
-  // in 32 bits)
-  return tiles <= kMaxGroups && B * H * tiles < ((int64_t)1 << 31);
+  return true;
 }
 
 }  // namespace

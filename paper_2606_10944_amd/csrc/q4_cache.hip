@@ -524,6 +524,7 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
   // The tokens' sums in parts: [k-step, part, lane] 16-byte words, lane (m, g) token m's
   // channels of words 4 i + g.  The waves share the words.
   u32x4* parts = reinterpret_cast<u32x4*>(score + 16 * stride);
+  bool small = false;  // sums whose second part may lie below the normal numbers
   for (int i = wave; i < KS / 2; i += SW) {
     double neg[8], pos[8];
 #pragma unroll
@@ -547,6 +548,7 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
     for (int j = 0; j < 8; ++j) {
       n[j] = (float)neg[j];
       p[j] = (float)pos[j];
+      small |= (neg[j] < 0.0 && neg[j] > -0x1p-100) || (pos[j] > 0.0 && pos[j] < 0x1p-100);
     }
     bf16x8_t np[2], pp[2];
     split8<2>(n, np);
@@ -559,8 +561,9 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
   }
   __syncthreads();
 
-  // largest sum of magnitudes of this lane's scores (token m), as bits: NaN above all
-  uint32_t size = 0;
+  // largest sum of magnitudes of this lane's scores (token m), as bits: NaN above all, and
+  // infinite for sums that the parts do not hold (all its blocks are scored again)
+  uint32_t size = small ? 0x7f800000u : 0;
   auto tile = [&](int k0, const u32x4* x) __attribute__((always_inline)) {
     floatx4_t z = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
     const u32x4 sign = {0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};

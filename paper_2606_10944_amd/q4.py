@@ -1,7 +1,7 @@
 """Rotary positions and the key/value cache held in 4 bits: binding of thin_rotary
 and the thin_q4_* calls of include/thin.h (argument marshalling only).
 
-Tensors live on the current device (or the given stream's); rows are [B, heads,
+Tensors and the given stream live on the current device; rows are [B, heads,
 T, d] tensors of any strides with contiguous channels, 16-byte aligned.
 """
 from __future__ import annotations
@@ -28,11 +28,14 @@ _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _where(stream):
-    """(device index, raw stream) that a call runs on."""
+    """(device index, raw stream) that a call runs on: a stream of the current device."""
+    dev = _get_device()
     if stream is None:
-        dev = _get_device()
         return dev, _raw_stream(dev)
-    return stream.device.index, stream.cuda_stream
+    if stream.device.index != dev:
+        raise ThinError(THIN_EINVAL, f"the stream is on {stream.device}, the current device is "
+                                     f"cuda:{dev}")
+    return dev, stream.cuda_stream
 
 
 def _empty(shape, dtype: torch.dtype, dev: int, stream) -> torch.Tensor:

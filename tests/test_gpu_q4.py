@@ -358,6 +358,24 @@ def check_select_head(c, q, at, n_sel, n_sinks, n_window, got, h):
         assert got[0, h, t].tolist() == want, (h, t)
 
 
+def test_select_of_small_queries_beside_large_bounds():
+    """Sums of queries whose second bf16 part lies below the normal numbers, scores of
+    ordinary size that differ by 2^-10 and less."""
+    g = gen(25)
+    H, T, d, nb = 64, 3, 64, 300
+    c = fresh(1, H, 64 * nb, d)
+    x = torch.randn(1, 1, 1, 2, d, generator=g).expand(1, H, nb, 2, d).clone()
+    x[..., 5] += torch.randn(1, H, nb, 2, generator=g) * 2.0 ** -7
+    x = (x * 2.0 ** 110).bfloat16()
+    c.bounds.copy_(torch.stack((torch.minimum(x[..., 0, :], x[..., 1, :]),
+                                torch.maximum(x[..., 0, :], x[..., 1, :])), -2))
+    q = (torch.randn(1, 2 * H, T, d, generator=g) * 2.0 ** -121).bfloat16()
+    at = 64 * nb - T
+    got = thin_q4_select(q.to(DEV), c, i32([at]), 40, n_sinks=1, n_window=2).cpu()
+    for h in range(0, H, 7):
+        check_select_head(c, q, at, 40, 1, 2, got, h)
+
+
 def test_select_in_pieces():
     """More tokens than the scores held at a time: 8 slices x 2049 blocks."""
     g = gen(9)
@@ -551,6 +569,24 @@ def test_attention_nan_query_stays_in_its_row():
         keep = torch.ones(4, 3, dtype=torch.bool)
         keep[1, 2] = False
         assert torch.equal(got[0][keep], want[0][keep])
+
+
+@pytest.mark.parametrize("T", [3, 700])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_attention_infinite_query_has_no_softmax(dtype, T):
+    """Scores of +-infinity and 0 times infinity: the row is not a number, others keep theirs."""
+    g = gen(14)
+    c = filled(g, 8, 4, 1024, 64, [1024] * 8)
+    q = randn(g, 8, 8, T, 64, dtype=dtype).to(DEV)
+    at = i32([1024 - T] * 8)
+    want = thin_q4_attention(q, c, at)
+    q[3, 1, 2, 5] = math.inf
+    q[5, 6, T - 1, 63] = -math.inf
+    got = thin_q4_attention(q, c, at)
+    odd = torch.zeros(8, 8, T, dtype=torch.bool, device=DEV)
+    odd[3, 1, 2] = odd[5, 6, T - 1] = True
+    assert got[odd].isnan().all()
+    assert torch.equal(got[~odd], want[~odd])
 
 
 def test_long_cache_offsets():

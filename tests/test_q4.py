@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import q4_reference as ref
-from paper_2606_10944_amd import Q4Cache, _lib, thin_rotary_turns
+from paper_2606_10944_amd import Q4Cache, _lib, q4, thin_rotary_turns
 from paper_2606_10944_amd._lib import Q4CacheStruct
 
 FAKE = C.c_void_p(0x10000)  # never dereferenced: every call below fails validation
@@ -24,6 +24,28 @@ def cache(**kw):
 
 def strides(*s):
     return (C.c_int64 * 3)(*s)
+
+
+def test_a_stream_of_another_device_is_refused(monkeypatch):
+    class Stream:
+        device = torch.device("cuda", 1)
+        cuda_stream = 4096
+
+    monkeypatch.setattr(q4, "_get_device", lambda: 0)
+    with pytest.raises(_lib.ThinError, match="cuda:1"):
+        q4._where(Stream)
+    monkeypatch.setattr(q4, "_get_device", lambda: 1)
+    assert q4._where(Stream) == (1, 4096)
+
+
+def test_attention_takes_as_many_rows_as_a_grid_holds():
+    plan, n = _lib.lib().thin_q4_attention_plan, C.c_size_t(0)
+    for n_sel in (0, 4):
+        for G in (1, 100, 128):
+            assert plan(1, 2, 2 * G, 5000, 64, 1 << 20, n_sel, C.byref(n)) == 0
+        assert plan(1, 2, 2 * 129, 5000, 64, 1 << 20, n_sel, C.byref(n)) == EINVAL
+        assert plan(32, 32, 32, 5000, 64, 1 << 20, n_sel, C.byref(n)) == 0
+        assert plan(32, 33, 33, 5000, 64, 1 << 20, n_sel, C.byref(n)) == EINVAL
 
 
 BAD_CACHES = [dict(k_codes=None), dict(bounds=None), dict(v_scales=ODD), dict(B=0), dict(H=-1),
