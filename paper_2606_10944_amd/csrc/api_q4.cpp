@@ -89,7 +89,7 @@ bool plan_attention(int64_t B, int64_t H, int64_t q_heads, int64_t n_max, int64_
   if (T * (q_heads / H) > kMaxGroupRows || B * q_heads * T > kMaxRows) return false;
   const int64_t tiles = thin::q4_row_tiles(q_heads / H, T, n_sel > 0);
   p->shape = thin::q4_attention_shape(B, H, q_heads / H, T, n_sel > 0,
-                                      n_sel > 0 ? n_sel * THIN_Q4_BLOCK : n_max, bf16);
+                                      n_sel > 0 ? n_sel * THIN_Q4_BLOCK : n_max, d, bf16);
   p->bytes = thin::q4_attention_bytes(B, H, tiles, p->shape.splits, d);
   p->sums = thin::q4_sums_bytes(B, H, tiles, p->shape.splits, d);
   return true;

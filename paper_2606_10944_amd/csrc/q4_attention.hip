@@ -8,7 +8,7 @@
 // MB, 5.7 TB/s (a stream of reads reaches 6.5), then 5 us for the join of the shared
 // tiles.  64 of 2048 blocks for 8 sequences: 11.5 + 4 us for 36 MB, latencies (a launch,
 // positions, lists, codes, four steps per wave, the join's three loads in turn).  32
-// blocks for each of 509 tokens: 110 us, LDS: writing 32 decoded value rows costs a
+// blocks for each of 509 tokens: 103 us, LDS: writing 32 decoded value rows costs a
 // compute unit 128 cycles (64 bytes each) and reading them transposed 53, of the 260 that
 // a step takes.
 #include "q4_attn_device.hpp"
@@ -175,10 +175,10 @@ struct Shares {
   }
 };
 
-// WV waves.  Without splits a workgroup takes a tile's whole keys; with them
+// WV waves, OCC of them on a SIMD at least.  Without splits a workgroup takes a tile's whole keys; with them
 // workgroups share the keys and leave sums in a.part, one slot of existing rows each.
-template <typename T, int D, bool LIST, int WV>
-__global__ __launch_bounds__(64 * WV, 2) void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
+template <typename T, int D, bool LIST, int WV, int OCC>
+__global__ __launch_bounds__(64 * WV, OCC) void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
   constexpr int NP = Elem<T>::bytes == 2 ? 1 : 3;  // bf16 parts of the weights
   using C = Codes<T, D>;
   __shared__ __align__(16) unsigned char lds[WV * CH * kVStride<D>];
@@ -504,19 +504,28 @@ __global__ __launch_bounds__(JT) void q4_join_kernel(Q4View c, Q4AttnArgs a) {
   }
 }
 
-template <typename T, int D, bool LIST, int WV>
+template <typename T, int D, bool LIST, int WV, int OCC = 2>
 hipError_t attn(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
   const int64_t tiles = q4_row_tiles(a.G, a.tok.T, LIST);
   const int64_t splits = a.shape.splits;
   const dim3 grid = LIST || splits == 1
                         ? dim3((uint32_t)(tiles * splits), (uint32_t)(c.B * c.H))
                         : dim3((uint32_t)(tiles * splits * c.B), (uint32_t)c.H);
-  q4_attn_kernel<T, D, LIST, WV><<<grid, 64 * WV, 0, st>>>(c, a);
+  q4_attn_kernel<T, D, LIST, WV, OCC><<<grid, 64 * WV, 0, st>>>(c, a);
   return hipGetLastError();
 }
 
+// d = 128, bf16: 144 registers leave a compute unit three workgroups of four waves; within
+// 128 it holds four, which pays once there are as many (32 blocks for each token, 8 key
+// heads: 1024 workgroups 35.0 -> 33.0 us, 4096 109 -> 102.6; 768 26.9 -> 27.3, 512 21.7 ->
+// 22.5).  float32 rows of 128 need 185.
 template <typename T, int D>
 hipError_t attn_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
+  if constexpr (D == 128 && Elem<T>::bytes == 2) {
+    const int64_t tiles = q4_row_tiles(a.G, a.tok.T, a.blocks != nullptr);
+    if (a.shape.splits == 1 && (int64_t)c.B * c.H * tiles >= 1024)
+      return a.blocks ? attn<T, D, true, 4, 4>(c, a, st) : attn<T, D, false, 4, 4>(c, a, st);
+  }
   if (a.shape.waves == 8)
     return a.blocks ? attn<T, D, true, 8>(c, a, st) : attn<T, D, false, 8>(c, a, st);
   return a.blocks ? attn<T, D, true, 4>(c, a, st) : attn<T, D, false, 4>(c, a, st);

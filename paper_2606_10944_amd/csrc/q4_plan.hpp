@@ -30,7 +30,10 @@ struct Q4AttnShape {
 // Few query rows per slice.  Two workgroups of four waves per compute unit (512): 8
 // sequences of 3000 to 65536 rows, 8 key heads, d = 128, bf16: 67 us, against 85 with 256,
 // 68 with 768, 84 with 1024 (the last of them run alone).  Up to 2048 keys one workgroup
-// of eight waves takes them all: no second launch to join sums.  Long caches of more
+// of eight waves takes them all: no second launch to join sums.  A compute unit holds one
+// such of d = 128 (its registers), two of less: four waves where there are more (d = 128,
+// 384 workgroups over 1024 rows: 18.3 us with eight, 14.0 with four; 264 over 2000: 25.9,
+// 20.3; d = 64, 320 over lists of 32 blocks: 13.6, 14.9).  Long caches of more
 // slices are shared out in two, so that one long sequence among short ones is not left
 // to one workgroup per head.
 //
@@ -41,7 +44,7 @@ struct Q4AttnShape {
 // rows, 192 query rows a head, 96 tiles of 16: 38 against 41 us; 64 query rows: 28 against
 // 24; 32 slices x 4096 rows, 96 query rows, 192 tiles: 27 against 41.
 inline Q4AttnShape q4_attention_shape(int64_t B, int64_t H, int64_t G, int64_t T, bool list,
-                                      int64_t keys, bool bf16) {
+                                      int64_t keys, int64_t d, bool bf16) {
   const int64_t groups = B * H * q4_row_tiles(G, T, list);
   if (!list && T * G >= 64) {
     const int64_t per = q4_prompt_rows(bf16), wide = B * H * ((T * G + per - 1) / per);
@@ -51,7 +54,7 @@ inline Q4AttnShape q4_attention_shape(int64_t B, int64_t H, int64_t G, int64_t T
       return {0, (int32_t)(splits < most ? splits : most), 1};
     }
   }
-  if (keys <= 2048 || groups > 1024 || B > kQ4SharedEntries) return {groups > 511 ? 4 : 8, 1, 1};
+  if (keys <= 2048 || groups > 1024 || B > kQ4SharedEntries) return {groups > (d == 128 ? 256 : 511) ? 4 : 8, 1, 1};
   const int64_t steps = (keys + kQ4Step - 1) / kQ4Step;
   int64_t splits = 512 / groups;
   if (splits < 2) splits = 2;

@@ -15,8 +15,8 @@ SHIM = r"""
 #include "q4_plan.hpp"
 extern "C" {
 void shape(int64_t B, int64_t H, int64_t G, int64_t T, int list, int64_t keys, int bf16,
-           int64_t* out) {
-  const thin::Q4AttnShape s = thin::q4_attention_shape(B, H, G, T, list != 0, keys, bf16 != 0);
+           int64_t d, int64_t* out) {
+  const thin::Q4AttnShape s = thin::q4_attention_shape(B, H, G, T, list != 0, keys, d, bf16 != 0);
   out[0] = s.waves;
   out[1] = s.splits;
   out[2] = s.least;
@@ -45,11 +45,11 @@ def plan(tmp_path_factory):
     return lib
 
 
-def shape(plan, *a):
+def shape(plan, *a, d=128):
     out = (C.c_int64 * 5)()
     B, H, G, T, lst, keys, bf16 = a
     plan.shape(*[C.c_int64(x) for x in (B, H, G, T)], C.c_int(lst), C.c_int64(keys), C.c_int(bf16),
-               out)
+               C.c_int64(d), out)
     return list(out)
 
 
@@ -63,7 +63,8 @@ def test_attention_shapes_hold_what_the_kernels_assume(plan):
         T = 1 if rng.random() < 0.4 else int(2 ** rng.uniform(0, 20))
         lst, bf16 = rng.random() < 0.4, rng.random() < 0.5
         keys = 64 * rng.randint(1, 32768) if lst else int(2 ** rng.uniform(0, 21))
-        waves, splits, least, tiles, ws = shape(plan, B, H, G, T, lst, keys, bf16)
+        waves, splits, least, tiles, ws = shape(plan, B, H, G, T, lst, keys, bf16,
+                                                  d=rng.choice((32, 64, 128)))
         kinds.add((waves, splits > 1, lst))
         assert waves in (0, 4, 8) and 1 <= splits <= 512 and least >= 1
         assert waves or not lst  # lists have no kernel for many rows
@@ -91,6 +92,12 @@ def test_attention_shapes_hold_what_the_kernels_assume(plan):
 ])
 def test_attention_shapes_of_ordinary_calls(plan, a, want):
     assert tuple(shape(plan, *a)[:2]) == want
+
+
+def test_waves_follow_the_workgroups_a_compute_unit_holds(plan):
+    for lst in (0, 1):
+        for n, d, waves in ((256, 128, 8), (257, 128, 4), (257, 64, 8), (511, 32, 8), (512, 64, 4)):
+            assert shape(plan, n, 1, 4, 1, lst, 1024, 1, d=d)[0] == waves
 
 
 def test_selection_holds_bounded_scores(plan):
