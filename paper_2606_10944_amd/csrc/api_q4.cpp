@@ -237,12 +237,15 @@ int thin_q4_select(const thin_q4_cache_t* cache, const void* Q, const int64_t* q
   a.scores = static_cast<uint64_t*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
-  if (thin::q4_select_fused((int64_t)c.B * c.H, blocks_of(c.n_max), T)) {
+  const int64_t slices = (int64_t)c.B * c.H, nb = blocks_of(c.n_max);
+  a.grouped = thin::q4_select_grouped(slices, T);
+  if (a.grouped) {
     e = observed(THIN_KERNEL_Q4_SELECT, -1, st,
                  [&] { return thin::launch_q4_select(dtype, cache->d, c, a, st); });
-    return e == hipSuccess ? THIN_OK : THIN_EHIP;
+    if (e != hipSuccess || thin::q4_select_fused(slices, nb, T))
+      return e == hipSuccess ? THIN_OK : THIN_EHIP;
   }
-  const int64_t step = thin::q4_select_tokens((int64_t)c.B * c.H, blocks_of(c.n_max), T);
+  const int64_t step = thin::q4_select_tokens(slices, nb, T);
   for (int64_t t0 = 0; t0 < T && e == hipSuccess; t0 += step) {
     a.t0 = (int32_t)t0;
     a.tn = (int32_t)(T - t0 < step ? T - t0 : step);

@@ -59,9 +59,10 @@ struct Q4SelectArgs {
   int32_t* blocks;   // [B, H, T, n_sel]
   int32_t t0, tn;    // the launch's tokens: t0 .. t0 + tn - 1
   uint64_t* scores;  // [B, H, tn, ceil(n_max / 64)]
+  bool grouped;      // launch_q4_select has run: the others take what it left
 };
-// Scores and choice of all tokens in one launch (at most kQ4SelectBlocks blocks), without
-// a workspace; else scores, then the choice by them.
+// Scores and choice in one launch, without a workspace, of the tokens whose 16 see at most
+// kQ4SelectBlocks blocks; scores, then the choice by them, of tokens t0 .. t0 + tn - 1.
 hipError_t launch_q4_select(int dtype, int64_t d, const Q4View& c, const Q4SelectArgs& a,
                             hipStream_t st);
 hipError_t launch_q4_scores(int dtype, int64_t d, const Q4View& c, const Q4SelectArgs& a,

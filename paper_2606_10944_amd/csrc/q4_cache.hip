@@ -189,6 +189,14 @@ __device__ __forceinline__ uint64_t score_key(double s) {
   return k < 2 ? 2 : k;
 }
 
+// Whether launch_q4_select takes token t: none of its 16 sees more blocks than LDS holds.
+__device__ __forceinline__ bool q4_grouped(const Q4View& c, const Q4SelectArgs& a, int b, int t) {
+  int end = std::min(t / 16 * 16 + 16, a.tok.T);
+  if (a.tok.count) end = std::min(end, a.tok.count[b]);
+  return end <= t / 16 * 16 ||
+         q4_last_row(a.tok, b, end - 1, c.n_max) < kQ4SelectBlocks * kQ4Block;
+}
+
 constexpr int SLANES = 8;  // lanes per block's bounds
 
 template <typename T, int D>
@@ -210,7 +218,7 @@ __global__ __launch_bounds__(THREADS) void q4_scores_kernel(Q4View c, Q4SelectAr
   };
   fetch(k);  // (on its way while the queries are summed)
   const int last_row = q4_last_row(a.tok, b, t, c.n_max);
-  if (last_row < 0) return;
+  if (last_row < 0 || (a.grouped && q4_grouped(c, a, b, t))) return;
   const int last = last_row / kQ4Block;
   __shared__ double sq[2 * D];  // q- beside lo, then q+ beside hi
   if (threadIdx.x < D) {
@@ -256,6 +264,7 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
   const int64_t s = blockIdx.y;
   const int b = blockIdx.y / c.H, t = a.t0 + blockIdx.x;
   const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  if (a.grouped && q4_grouped(c, a, b, t)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
   int32_t* out = a.blocks + (s * a.tok.T + t) * a.n_sel;
   const uint64_t* keys = a.scores + (s * a.tn + blockIdx.x) * nb;
@@ -520,6 +529,7 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
   const int most = (int)wave_max((uint32_t)(
       (there ? q4_last_row(a.tok, b, t0 + m, c.n_max) : -1) + 1));
   const int blocks = (most + kQ4Block - 1) / kQ4Block;
+  if (blocks > kQ4SelectBlocks) return;  // (left to the other launches)
 
   // The tokens' sums in parts: [k-step, part, lane] 16-byte words, lane (m, g) token m's
   // channels of words 4 i + g.  The waves share the words.
@@ -727,7 +737,7 @@ hipError_t pick(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
 
 template <typename T, int D, int KPL>
 hipError_t select_k(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
-  const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  const int nb = std::min<int>((c.n_max + kQ4Block - 1) / kQ4Block, kQ4SelectBlocks);
   const int stride = (nb + 15) / 16 * 16 + 4;
   const dim3 grid((uint32_t)((a.tok.T + 15) / 16), (uint32_t)(c.B * c.H));
   const size_t lds = (size_t)16 * stride * 4 + 2 * D / 32 * 2 * 64 * 16;

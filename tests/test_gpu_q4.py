@@ -376,6 +376,28 @@ def test_select_of_small_queries_beside_large_bounds():
         check_select_head(c, q, at, 40, 1, 2, got, h)
 
 
+@pytest.mark.parametrize("count", [None, [40, 17, 0]])
+def test_select_of_prompts_in_large_caches(count):
+    """Tokens that see more blocks than the launch of 16 tokens holds beside others."""
+    g = gen(26)
+    B, H, T, d, n = 3, 12, 40, 32, 140000
+    at = [131072 - 20, 139950, 700]
+    c = fresh(B, H, n, d)
+    x = torch.randn(B, H, (n + 63) // 64, 2, d, generator=g)
+    c.bounds.copy_(x.sort(-2)[0].bfloat16())
+    q = randn(g, B, 2 * H, T, d, dtype="bf16")
+    got = thin_q4_select(q.to(DEV), c, i32(at), 9,
+                         count=None if count is None else i32(count)).cpu()
+    bnd = c.bounds.cpu()
+    for b in range(B):
+        for h in (0, 7, 11):
+            for t in range(T):
+                last = at[b] + t if count is None or t < count[b] else -1
+                sc = ref.block_scores(q[b, 2 * h:2 * h + 2, t], bnd[b, h]).tolist()
+                want = ref.select(sc, min(last, n - 1), 9, 1, 2)
+                assert got[b, h, t].tolist() == want + [-1] * (9 - len(want)), (b, h, t)
+
+
 def test_select_in_pieces():
     """More tokens than the scores held at a time: 8 slices x 2049 blocks."""
     g = gen(9)
