@@ -119,6 +119,7 @@ struct Shares {
 
   __device__ __forceinline__ Shares(const Q4View& c, const Q4AttnArgs& a, int tile, int lane) {
     const TileTokens tt = tile_tokens(a, tile);
+    auto add = [](uint32_t x, uint32_t y) { return x + y; };
     int sum = 0;  // (at most 2^24: 256 sequences, 2^16 steps each)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -126,8 +127,7 @@ struct Shares {
       if (i * 64 < c.B && i * 64 + lane < c.B) steps[i] = steps_of(c, a, i * 64 + lane, tt);
       sum += steps[i];
     }
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
+    sum = (int)wave_reduce<uint32_t>((uint32_t)sum, 0u, add);
     // rounded up per sequence, the shares are at most B more than the sum's
     const int groups = c.B * a.shape.splits, spare = groups - c.B;
     const int least = (int)((uint32_t)(sum + spare - 1) / (uint32_t)spare);
@@ -137,14 +137,8 @@ struct Shares {
     for (int i = 0; i < N; ++i) {
       upto[i] = before;
       if (i * 64 >= c.B) continue;
-      int x = (int)count(i);
-#pragma unroll
-      for (int m = 1; m < 64; m *= 2) {
-        const int y = __shfl_up(x, m);
-        if (lane >= m) x += y;
-      }
-      upto[i] += x;
-      before = __shfl(upto[i], 63);
+      upto[i] += (int)wave_scan<uint32_t>(count(i), 0u, add);
+      before = __builtin_amdgcn_readlane(upto[i], 63);
     }
   }
 
@@ -157,9 +151,9 @@ struct Shares {
       const uint64_t past = __ballot(upto[i] > j);
       if (!past) continue;
       const int l = __ffsll((unsigned long long)past) - 1;
-      const int first = __shfl(upto[i] - (int)count(i), l);
+      const int first = __builtin_amdgcn_readlane(upto[i] - (int)count(i), l);
       *i0 = __builtin_amdgcn_readfirstlane((j - first) * (int)share);
-      const int end = __builtin_amdgcn_readfirstlane(__shfl(steps[i], l));
+      const int end = __builtin_amdgcn_readlane(steps[i], l);
       *i1 = *i0 + (int)share < end ? *i0 + (int)share : end;
       b = i * 64 + l;
     }
@@ -175,10 +169,10 @@ struct Shares {
   }
 };
 
-// WV waves, OCC of them on a SIMD at least.  Without splits a workgroup takes a tile's whole keys; with them
+// WV waves.  Without splits a workgroup takes a tile's whole keys; with them
 // workgroups share the keys and leave sums in a.part, one slot of existing rows each.
-template <typename T, int D, bool LIST, int WV, int OCC>
-__global__ __launch_bounds__(64 * WV, OCC) void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
+template <typename T, int D, bool LIST, int WV>
+__global__ __launch_bounds__(64 * WV, 2) void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
   constexpr int NP = Elem<T>::bytes == 2 ? 1 : 3;  // bf16 parts of the weights
   using C = Codes<T, D>;
   __shared__ __align__(16) unsigned char lds[WV * CH * kVStride<D>];
@@ -294,9 +288,8 @@ __global__ __launch_bounds__(64 * WV, OCC) void q4_attn_kernel(Q4View c, Q4AttnA
   unsigned char* sv = lds + wave * CH * kVStride<D>;
   // rows that every query of the tile sees need no mask
   int all = there ? qlast : 0x7fffffff;
-#pragma unroll
-  for (int x = 1; x < 16; x *= 2) all = std::min(all, __shfl_xor(all, x));
-  all = __builtin_amdgcn_readfirstlane(all);
+  all = __builtin_amdgcn_readfirstlane(
+      row_reduce(all, [](int x, int y) { return std::min(x, y); }));
 
   auto step = [&](const C& x, int row0) __attribute__((always_inline)) {
     float sc[8];
@@ -329,8 +322,7 @@ __global__ __launch_bounds__(64 * WV, OCC) void q4_attn_kernel(Q4View c, Q4AttnA
     for (int j = 1; j < 8; ++j) mx = fmaxf(mx, sc[j]);
     mx *= c2;
     if (__any(mx > mrun + kSlack)) {
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      mx = across_rows(mx, true, [](float x, float y) { return fmaxf(x, y); });
       const float mnew = fmaxf(mrun, mx);
       const float scale = __builtin_amdgcn_exp2f(mrun - mnew);
       mrun = mnew;
@@ -364,8 +356,7 @@ __global__ __launch_bounds__(64 * WV, OCC) void q4_attn_kernel(Q4View c, Q4AttnA
       step(buf[k], row0[k]);
     }
   }
-  lrun += __shfl_xor(lrun, 16);
-  lrun += __shfl_xor(lrun, 32);
+  lrun = across_rows(lrun, true, [](float x, float y) { return x + y; });
 
   // the waves' sums under one maximum
   if (g == 0) {
@@ -462,19 +453,20 @@ __global__ __launch_bounds__(JT) void q4_join_kernel(Q4View c, Q4AttnArgs a) {
   {
     // JT / 16 threads per row
     constexpr int RT = JT / 16;
+    static_assert(RT == 32, "lanes of two rows of 16");
     const int r = threadIdx.x / RT, k = threadIdx.x % RT;
     float mall = kLowest, l = 0.0f;
     if (r < nrows) {
       for (int p = k; p < n; p += RT) mall = fmaxf(mall, ml[p * 32 + r]);
-#pragma unroll
-      for (int x = 1; x < RT; x *= 2) mall = fmaxf(mall, __shfl_xor(mall, x));
+      auto larger = [](float x, float y) { return fmaxf(x, y); };
+      mall = across_rows(row_reduce(mall, larger), false, larger);
       for (int p = k; p < n; p += RT) {
         const float f = __builtin_amdgcn_exp2f(ml[p * 32 + r] - mall);
         w[p][r] = f;
         l += ml[p * 32 + 16 + r] * f;
       }
-#pragma unroll
-      for (int x = 1; x < RT; x *= 2) l += __shfl_xor(l, x);
+      auto add = [](float x, float y) { return x + y; };
+      l = across_rows(row_reduce(l, add), false, add);
       if (k == 0) inv[r] = l > 0.0f ? 1.0f / l : 0.0f;
     }
   }
@@ -504,28 +496,19 @@ __global__ __launch_bounds__(JT) void q4_join_kernel(Q4View c, Q4AttnArgs a) {
   }
 }
 
-template <typename T, int D, bool LIST, int WV, int OCC = 2>
+template <typename T, int D, bool LIST, int WV>
 hipError_t attn(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
   const int64_t tiles = q4_row_tiles(a.G, a.tok.T, LIST);
   const int64_t splits = a.shape.splits;
   const dim3 grid = LIST || splits == 1
                         ? dim3((uint32_t)(tiles * splits), (uint32_t)(c.B * c.H))
                         : dim3((uint32_t)(tiles * splits * c.B), (uint32_t)c.H);
-  q4_attn_kernel<T, D, LIST, WV, OCC><<<grid, 64 * WV, 0, st>>>(c, a);
+  q4_attn_kernel<T, D, LIST, WV><<<grid, 64 * WV, 0, st>>>(c, a);
   return hipGetLastError();
 }
 
-// d = 128, bf16: 144 registers leave a compute unit three workgroups of four waves; within
-// 128 it holds four, which pays once there are as many (32 blocks for each token, 8 key
-// heads: 1024 workgroups 35.0 -> 33.0 us, 4096 109 -> 102.6; 768 26.9 -> 27.3, 512 21.7 ->
-// 22.5).  float32 rows of 128 need 185.
 template <typename T, int D>
 hipError_t attn_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
-  if constexpr (D == 128 && Elem<T>::bytes == 2) {
-    const int64_t tiles = q4_row_tiles(a.G, a.tok.T, a.blocks != nullptr);
-    if (a.shape.splits == 1 && (int64_t)c.B * c.H * tiles >= 1024)
-      return a.blocks ? attn<T, D, true, 4, 4>(c, a, st) : attn<T, D, false, 4, 4>(c, a, st);
-  }
   if (a.shape.waves == 8)
     return a.blocks ? attn<T, D, true, 8>(c, a, st) : attn<T, D, false, 8>(c, a, st);
   return a.blocks ? attn<T, D, true, 4>(c, a, st) : attn<T, D, false, 4>(c, a, st);

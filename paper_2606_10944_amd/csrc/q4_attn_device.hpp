@@ -149,8 +149,7 @@ struct Queries<bf16_t, D> {
     }
 #pragma unroll
     for (int i = 0; i < C; ++i) amax = fmaxf(amax, fabsf(f[i]));
-    amax = fmaxf(amax, __shfl_xor(amax, 16));
-    amax = fmaxf(amax, __shfl_xor(amax, 32));
+    amax = across_rows(amax, true, [](float a, float b) { return fmaxf(a, b); });
     // the largest value lands in [2^7, 2^8)
     int byte = (int)(__float_as_uint(amax) >> 23) - 7;
     byte = byte < 1 ? 1 : byte;

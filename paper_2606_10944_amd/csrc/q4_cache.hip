@@ -25,8 +25,9 @@ constexpr int THREADS = 256;
 // channels each.
 //
 // Bound by HBM: 2 x 8 x 16384 rows of keys and values, d = 128, bf16, 40 us for 134 MB
-// read and 36 written, 4.2 TB/s; one row for 64 x 8 slices, 5.4 us, of which the reading
-// back of the block's older rows (up to 4 KB a slice) is 2.
+// read and 36 written, 4.2 TB/s; one row for 64 x 8 slices, 4.9 us, of which the reading
+// back of the block's older rows (up to 4 KB a slice) is 2.  20240 slices of 8 tokens, d =
+// 32: 66 us, vector ALU (126 with the rows' values passed on by LDS shuffles).
 // ---------------------------------------------------------------------------
 // Codes of eight channels of a group that four neighbouring lanes hold; *byte
 // gets the group's scale byte.
@@ -37,8 +38,8 @@ __device__ __forceinline__ uint32_t encode8(float* f, uint32_t* byte) {
     f[i] = f[i] != f[i] ? 0.0f : f[i];
     amax = fmaxf(amax, fabsf(f[i]));
   }
-  amax = fmaxf(amax, __shfl_xor(amax, 1));
-  amax = fmaxf(amax, __shfl_xor(amax, 2));
+  amax = fmaxf(amax, lane_move<kSwapOnes>(amax));
+  amax = fmaxf(amax, lane_move<kSwapTwos>(amax));
   // amax = 1.m * 2^(E - 127): e = E - 129 if 1.m <= 1.75, else E - 128
   const uint32_t bits = __float_as_uint(amax);
   int s = (int)(bits >> 23) - ((bits & 0x7fffffu) <= 0x600000u ? 2 : 1);
@@ -106,21 +107,38 @@ __global__ __launch_bounds__(THREADS) void q4_store_kernel(Q4View c, RowsView k,
       mx[2 * i + 1] = fmaxf(mx[2 * i + 1], d);
     }
   }
-  // over the wave's rows, then the four waves
+  // over the wave's rows, then the four waves.  Halves of the wave, then its quarters,
+  // trade values so that each keeps half of them: quarter g is left with channels 2 g and
+  // 2 g + 1 of the eight.
 #pragma unroll
-  for (int m = LR; m < 64; m *= 2)
+  for (int n = 4; n > 1; n /= 2)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      mn[i] = fminf(mn[i], __shfl_xor(mn[i], m));
-      mx[i] = fmaxf(mx[i], __shfl_xor(mx[i], m));
+    for (int i = 0; i < n; ++i) {
+      trade(n == 4, mn[i], mn[i + n]);
+      trade(n == 4, mx[i], mx[i + n]);
+      mn[i] = fminf(mn[i], mn[i + n]);
+      mx[i] = fmaxf(mx[i], mx[i + n]);
     }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (LR <= 8) {
+      mn[i] = fminf(mn[i], lane_move<kTurn8>(mn[i]));
+      mx[i] = fmaxf(mx[i], lane_move<kTurn8>(mx[i]));
+    }
+    if (LR <= 4) {
+      mn[i] = fminf(mn[i], lane_move<kTurn4>(mn[i]));
+      mx[i] = fmaxf(mx[i], lane_move<kTurn4>(mx[i]));
+    }
+  }
   __shared__ float sm[4][2][D];
-  if ((threadIdx.x & 63) < LR)
+  if ((threadIdx.x & 15) < LR) {
+    const int ch = l * 8 + (threadIdx.x & 63) / 16 * 2;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      sm[threadIdx.x / 64][0][l * 8 + i] = mn[i];
-      sm[threadIdx.x / 64][1][l * 8 + i] = mx[i];
+    for (int i = 0; i < 2; ++i) {
+      sm[threadIdx.x / 64][0][ch + i] = mn[i];
+      sm[threadIdx.x / 64][1][ch + i] = mx[i];
     }
+  }
   __syncthreads();
   if (threadIdx.x < 2 * D) {
     const int which = threadIdx.x / D, ch = threadIdx.x % D;
@@ -197,7 +215,7 @@ __device__ __forceinline__ bool q4_grouped(const Q4View& c, const Q4SelectArgs& 
          q4_last_row(a.tok, b, end - 1, c.n_max) < kQ4SelectBlocks * kQ4Block;
 }
 
-constexpr int SLANES = 8;  // lanes per block's bounds
+constexpr int SLANES = 8;  // lanes per block's bounds, whose sums meet by moves within eight
 
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS) void q4_scores_kernel(Q4View c, Q4SelectArgs a) {
@@ -247,8 +265,9 @@ __global__ __launch_bounds__(THREADS) void q4_scores_kernel(Q4View c, Q4SelectAr
         sum += q[w][2 * i] * (double)__uint_as_float(x[w][i] << 16);
         sum += q[w][2 * i + 1] * (double)__uint_as_float(x[w][i] & 0xffff0000u);
       }
-#pragma unroll
-    for (int m = 1; m < SLANES; m *= 2) sum += __shfl_xor(sum, m);
+    sum += lane_move<kSwapOnes>(sum);
+    sum += lane_move<kSwapTwos>(sum);
+    sum += lane_move<kMirror8>(sum);
     if (j == 0) a.scores[(s * a.tn + t - a.t0) * nb + k] = score_key(sum);
     fetch(k + step);
   }
@@ -596,8 +615,9 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
     tile(k0, w);
     fetch(k0 + SW * 16, w);
   }
-#pragma unroll
-  for (int x = 16; x < 64; x *= 2) size = std::max(size, (uint32_t)__shfl_xor((int)size, x));
+  size = __float_as_uint(across_rows(__uint_as_float(size), true, [](float x, float y) {
+    return __uint_as_float(std::max(__float_as_uint(x), __float_as_uint(y)));
+  }));
   if (lane < 16) ssize[wave][lane] = size;
   __syncthreads();
 

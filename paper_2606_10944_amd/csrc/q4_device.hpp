@@ -77,6 +77,56 @@ __device__ __forceinline__ uint64_t lane_move(uint64_t x, uint64_t none) {
   return (uint64_t)lane_move<CTRL, ROWS>((uint32_t)(x >> 32), (uint32_t)(none >> 32)) << 32 |
          lane_move<CTRL, ROWS>((uint32_t)x, (uint32_t)none);
 }
+// Lanes of four, of eight and of a row of 16.
+constexpr int kSwapOnes = 0xb1, kSwapTwos = 0x4e;  // lane ^ 1, lane ^ 2
+constexpr int kMirror8 = 0x141, kMirror16 = 0x140;  // lane i of eight: 7 - i; of 16: 15 - i
+constexpr int kTurn4 = 0x124, kTurn8 = 0x128;      // four, eight lanes round
+template <int CTRL>
+__device__ __forceinline__ int lane_move(int x) {
+  return (int)lane_move<CTRL, 0xf>((uint32_t)x, 0u);
+}
+template <int CTRL>
+__device__ __forceinline__ float lane_move(float x) {
+  return __uint_as_float(lane_move<CTRL, 0xf>(__float_as_uint(x), 0u));
+}
+template <int CTRL>
+__device__ __forceinline__ double lane_move(double x) {
+  return __longlong_as_double(
+      (long long)lane_move<CTRL, 0xf>((uint64_t)__double_as_longlong(x), (uint64_t)0));
+}
+
+// op over a row of 16 lanes, the same in each of them.
+template <typename K, typename F>
+__device__ __forceinline__ K row_reduce(K x, F op) {
+  x = op(x, lane_move<kSwapOnes>(x));
+  x = op(x, lane_move<kSwapTwos>(x));
+  x = op(x, lane_move<kMirror8>(x));
+  return op(x, lane_move<kMirror16>(x));
+}
+
+// The upper half of a for the lower half of b (halves), or the odd rows of 16 lanes of a for
+// the even ones of b: a then holds the lower (even) lanes' a and b, b the others'.
+__device__ __forceinline__ void trade(bool halves, float& a, float& b) {
+  const auto r = halves ? __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b),
+                                                           false, false)
+                        : __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b),
+                                                           false, false);
+  a = __uint_as_float(r[0]);
+  b = __uint_as_float(r[1]);
+}
+
+// op over lanes 16 (and, with all, 32) apart, the same in each of them.
+template <typename F>
+__device__ __forceinline__ float across_rows(float x, bool all, F op) {
+  float y = x;
+  trade(false, x, y);
+  x = op(x, y);
+  if (!all) return x;
+  y = x;
+  trade(true, x, y);
+  return op(x, y);
+}
+
 // op over the lanes up to each; op(x, none) = x.  Rows of 16 lanes by shifts, then across
 // rows: six steps of a few cycles where a shuffle takes an LDS trip.
 template <typename K, typename F>

@@ -31,9 +31,10 @@ struct Q4AttnShape {
 // sequences of 3000 to 65536 rows, 8 key heads, d = 128, bf16: 67 us, against 85 with 256,
 // 68 with 768, 84 with 1024 (the last of them run alone).  Up to 2048 keys one workgroup
 // of eight waves takes them all: no second launch to join sums.  A compute unit holds one
-// such of d = 128 (its registers), two of less: four waves where there are more (d = 128,
-// 384 workgroups over 1024 rows: 18.3 us with eight, 14.0 with four; 264 over 2000: 25.9,
-// 20.3; d = 64, 320 over lists of 32 blocks: 13.6, 14.9).  Long caches of more
+// such of float32 rows of 128 (their registers), two of others: four waves where there are
+// more (d = 128, 384 workgroups over 1024 rows: float32 25.0 us with eight, 19.8 with four,
+// bf16 15.0, 14.5; over 2000 rows 35.2, 29.3 and 23.1, 21.6; d = 64, 320 over lists of 32
+// blocks: 13.6, 14.9).  Long caches of more
 // slices are shared out in two, so that one long sequence among short ones is not left
 // to one workgroup per head.
 //

@@ -81,9 +81,8 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
                      : nullptr,
                g);
   }
-#pragma unroll
-  for (int x = 1; x < 16; x *= 2) all = std::min(all, __shfl_xor(all, x));
-  all = __builtin_amdgcn_readfirstlane(all);
+  all = __builtin_amdgcn_readfirstlane(
+      row_reduce(all, [](int x, int y) { return std::min(x, y); }));
 
   // this workgroup's share of the rows: k0 .. k1 - 1, whole tiles of them
   const int share = (last / PK + splits) / splits * PK;
@@ -195,8 +194,7 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
         for (int j = 1; j < PK / 4; ++j) mx = fmaxf(mx, s[rt][j]);
         mx *= c2;
         if (__any(mx > mrun[rt] + kSlack)) {
-          mx = fmaxf(mx, __shfl_xor(mx, 16));
-          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          mx = across_rows(mx, true, [](float x, float y) { return fmaxf(x, y); });
           const float mnew = fmaxf(mrun[rt], mx);
           const float scale = __builtin_amdgcn_exp2f(mrun[rt] - mnew);
           mrun[rt] = mnew;

@@ -68,21 +68,17 @@ def _on(t: torch.Tensor, dev: int, name: str) -> int:
     return t.data_ptr()
 
 
-def _strides(t: torch.Tensor, name: str):
-    """None for contiguous rows [B, heads, T, d], else their strides."""
+def _rows(t: torch.Tensor, dev: int, name: str):
+    """(address, strides or None if contiguous) of rows [B, heads, T, d]."""
+    if t.dim() != 4:
+        raise ThinError(THIN_EINVAL, f"{name} must be [B,heads,T,d]")
+    p = _on(t, dev, name)
     if t.is_contiguous():
-        return None
+        return p, None
     s = t.stride()
     if s[3] != 1:
         raise ThinError(THIN_EINVAL, f"{name}: channels must be contiguous")
-    return _Strides(s[0], s[1], s[2])
-
-
-def _rows(t: torch.Tensor, dev: int, name: str):
-    """(address, strides or None) of rows [B, heads, T, d]."""
-    if t.dim() != 4:
-        raise ThinError(THIN_EINVAL, f"{name} must be [B,heads,T,d]")
-    return _on(t, dev, name), _strides(t, name)
+    return p, _Strides(s[0], s[1], s[2])
 
 
 def _ints(t: Optional[torch.Tensor], shape, dev: int, name: str):
