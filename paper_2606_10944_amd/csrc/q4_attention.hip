@@ -128,10 +128,21 @@ struct Shares {
       sum += steps[i];
     }
     sum = (int)wave_reduce<uint32_t>((uint32_t)sum, 0u, add);
-    // rounded up per sequence, the shares are at most B more than the sum's
-    const int groups = c.B * a.shape.splits, spare = groups - c.B;
-    const int least = (int)((uint32_t)(sum + spare - 1) / (uint32_t)spare);
-    share = (uint32_t)__builtin_amdgcn_readfirstlane(least < a.shape.least ? a.shape.least : least);
+    // Rounded up per sequence, the shares are up to B more than the sum's: none of that is
+    // set aside at first, then quarters of B, until the workgroups are enough.  (Setting B
+    // aside at once left 32 sequences of one length half of theirs.)
+    const int groups = c.B * a.shape.splits;
+    for (int q = 0; q <= 4; ++q) {
+      const uint32_t spare = (uint32_t)(groups - c.B * q / 4);
+      const uint32_t even = ((uint32_t)sum + spare - 1) / spare;
+      share = (uint32_t)__builtin_amdgcn_readfirstlane(
+          (int)std::max(even, (uint32_t)a.shape.least));
+      uint32_t taken = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (i * 64 < c.B) taken += count(i);
+      if (wave_reduce<uint32_t>(taken, 0u, add) <= (uint32_t)groups) break;
+    }
     int before = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {

@@ -27,35 +27,40 @@ struct Q4AttnShape {
   int32_t least;   // steps of 32 keys that a workgroup takes at least
 };
 
-// Few query rows per slice.  Two workgroups of four waves per compute unit (512): 8
+// Few query rows per slice.  A tile's keys go to one workgroup, without a second launch to
+// join sums, up to 2048 keys, and up to 4096 where there are workgroups for most compute
+// units (d = 128, 4000 rows, one token: 256 workgroups, bf16 25.4 us against 29.5 shared
+// out, 21.6 against 23.6 with lengths of 10 to 4000; 160: 20.9, 22.7 and 20.6, 20.2; 128:
+// 20.5, 20.3 and 20.3, 17.2).  A compute unit holds one workgroup of eight waves of float32
+// rows of 128 (their registers), two of others: four waves where there are more (d = 128,
+// 384 workgroups over 1024 rows: float32 25.0 us with eight, 19.8 with four, bf16 15.0,
+// 14.5; over 2000 rows 35.2, 29.3 and 23.1, 21.6; d = 64, 320 over lists of 32 blocks: 13.6,
+// 14.9).
+// Longer keys are shared out to two workgroups of four waves per compute unit (512; 8
 // sequences of 3000 to 65536 rows, 8 key heads, d = 128, bf16: 67 us, against 85 with 256,
-// 68 with 768, 84 with 1024 (the last of them run alone).  Up to 2048 keys one workgroup
-// of eight waves takes them all: no second launch to join sums.  A compute unit holds one
-// such of float32 rows of 128 (their registers), two of others: four waves where there are
-// more (d = 128, 384 workgroups over 1024 rows: float32 25.0 us with eight, 19.8 with four,
-// bf16 15.0, 14.5; over 2000 rows 35.2, 29.3 and 23.1, 21.6; d = 64, 320 over lists of 32
-// blocks: 13.6, 14.9).  Long caches of more
-// slices are shared out in two, so that one long sequence among short ones is not left
-// to one workgroup per head.
+// 68 with 768, 84 with 1024, the last of them run alone), those of more slices in two, so
+// that one long sequence among short ones is not left to one workgroup per head.
 //
-// Many query rows.  The kernel that shares decoded rows takes 1.3 us per 64 keys where a
-// compute unit has one workgroup, so it pays where there is one for each (16 sequences x 8
-// heads x 1024 rows, 256 query rows a head, 256 workgroups: 32 us against 42; 128 query
-// rows, 128 workgroups: 29 against 25), or where keys are shared out: 8 key heads x 16384
-// rows, 192 query rows a head, 96 tiles of 16: 38 against 41 us; 64 query rows: 28 against
-// 24; 32 slices x 4096 rows, 96 query rows, 192 tiles: 27 against 41.
+// Many query rows.  The kernel that shares decoded rows pays where each compute unit has a
+// workgroup of it (16 sequences x 8 heads x 1024 rows, 256 query rows a head, 256
+// workgroups: 32 us against 42; 128 query rows, 128 workgroups: 29 against 25), or where its
+// keys are shared out.  Tiles of 16 of 8 key heads, bf16: 192 over 40000 rows 68 us against
+// 141, over 16000 42 and 64, over 4500 29 and 28; 128 over 16000 36 and 39, over 4500 27 and
+// 22, 64 over 16384 28 and 24.  Up to 4096 rows one workgroup per tile is quicker for longer:
+// 512 tiles over 4000 rows 35 against 39, 1024 57 against 51.
 inline Q4AttnShape q4_attention_shape(int64_t B, int64_t H, int64_t G, int64_t T, bool list,
                                       int64_t keys, int64_t d, bool bf16) {
   const int64_t groups = B * H * q4_row_tiles(G, T, list);
   if (!list && T * G >= 64) {
     const int64_t per = q4_prompt_rows(bf16), wide = B * H * ((T * G + per - 1) / per);
-    if (keys <= 2048 ? wide >= 256 : groups >= 128) {
+    if (keys <= 2048 ? wide >= 256 : groups > (keys <= 4096 ? 512 : 127)) {
       if (keys <= 2048 || wide >= 512) return {0, 1, 1};
       const int64_t splits = 512 / wide, most = keys / 512;
       return {0, (int32_t)(splits < most ? splits : most), 1};
     }
   }
-  if (keys <= 2048 || groups > 1024 || B > kQ4SharedEntries) return {groups > (d == 128 ? 256 : 511) ? 4 : 8, 1, 1};
+  if (keys <= (groups < 192 ? 2048 : 4096) || groups > 1024 || B > kQ4SharedEntries)
+    return {groups > (d == 128 ? 256 : 511) ? 4 : 8, 1, 1};
   const int64_t steps = (keys + kQ4Step - 1) / kQ4Step;
   int64_t splits = 512 / groups;
   if (splits < 2) splits = 2;

@@ -568,6 +568,18 @@ def test_attention_over_blocks(dtype, d, B, H, G, T, n_max, at, count, n_sel):
     check_attention(c, q, at, count, chosen.cpu(), got, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lengths", [[4200] * 20, [4200, 1, 0, 4199, 77] * 5, [0] * 19 + [4200]])
+def test_attention_shares_of_many_sequences(dtype, lengths):
+    """Sequences of one length, of many and almost none: every one's keys are shared out."""
+    g = gen(15)
+    B = len(lengths)
+    c = filled(g, B, 2, 4200, 32, lengths)
+    q = randn(g, B, 6, 1, 32, dtype=dtype)
+    at = [n - 1 for n in lengths]
+    check_attention(c, q, at, None, None, thin_q4_attention(q.to(DEV), c, i32(at)), dtype)
+
+
 def test_attention_large_scores():
     """Scores in the thousands: the running maximum moves, weights underflow."""
     g = gen(12)

@@ -86,6 +86,8 @@ def test_attention_shapes_hold_what_the_kernels_assume(plan):
     ((8, 8, 4, 1, 0, 65536, 1), (4, 8)),       # a step over long caches: 512 workgroups
     ((2, 4, 4, 1, 0, 1000, 0), (8, 1)),        # short caches: one launch
     ((256, 4, 4, 1, 0, 65536, 1), (4, 2)),     # many slices: in two, for unequal lengths
+    ((32, 8, 4, 1, 0, 4096, 1), (8, 1)),       # a workgroup for every compute unit
+    ((16, 8, 4, 1, 0, 4096, 1), (4, 4)),       # for half of them
     ((1, 8, 4, 4096, 0, 16384, 1), (0, 1)),    # a prompt
     ((1, 8, 4, 256, 0, 16384, 1), (0, 8)),     # a chunk: 64 workgroups share out 16384 rows
     ((1, 8, 4, 4096, 1, 2048, 1), (4, 1)),     # lists for every token of a prompt
