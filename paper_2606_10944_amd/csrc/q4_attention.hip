@@ -4,12 +4,12 @@
 // The kernel for few query rows: a wave takes 32 keys at a time on its own, its
 // decoded value rows in LDS, the next step's codes on their way meanwhile.
 //
-// d = 128, bf16, 8 key heads.  8 sequences of 3000 to 65536 rows, one token: 52 us for 298
-// MB, 5.7 TB/s (a stream of reads reaches 6.5), then 5 us for the join of the shared
+// d = 128, bf16, 8 key heads.  8 sequences of 3000 to 65536 rows, one token: 50 us for 298
+// MB, 6.0 TB/s (a stream of reads reaches 6.5), then 5 us for the join of the shared
 // tiles.  64 of 2048 blocks for 8 sequences: 11.5 + 4 us for 36 MB, latencies (a launch,
 // positions, lists, codes, four steps per wave, the join's three loads in turn).  32
 // blocks for each of 509 tokens: 103 us, LDS: writing 32 decoded value rows costs a
-// compute unit 128 cycles (64 bytes each) and reading them transposed 53, of the 260 that
+// compute unit 128 cycles (64 bytes each) and reading them transposed 53, of the 240 that
 // a step takes.
 #include "q4_attn_device.hpp"
 
@@ -417,12 +417,14 @@ __global__ __launch_bounds__(64 * WV, 2) void q4_attn_kernel(Q4View c, Q4AttnArg
   }
 }
 
-// The splits' sums of a tile of rows under one maximum.  A workgroup per tile: its
-// threads take rows x four channels, and share the splits where that leaves threads.
+// The splits' sums of a tile of rows under one maximum.  A workgroup takes a tile, or the
+// z-th part of its channels: its threads take rows x four channels, and share the splits
+// where that leaves threads.  (One row of 128 channels in 512 splits, a workgroup: 22 us, by
+// one compute unit's loads; in eight parts 9.6.)
 constexpr int JT = 512;  // threads
 template <typename T, int D, bool LIST>
 __global__ __launch_bounds__(JT) void q4_join_kernel(Q4View c, Q4AttnArgs a) {
-  constexpr int V = D / 4;
+  const int V = D / 4 / gridDim.z, c0 = (int)blockIdx.z * V;
   __shared__ float w[kQ4MaxSplits][16];  // the splits' factors
   __shared__ float inv[16];
   __shared__ floatx4_t part[JT];
@@ -459,7 +461,7 @@ __global__ __launch_bounds__(JT) void q4_join_kernel(Q4View c, Q4AttnArgs a) {
     early[e] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
     if (k < items && way < ways && p < n)
       early[e] = *reinterpret_cast<const floatx4_t*>(a.part + ((slot0 + p) * 16 + k / V) * D +
-                                                     k % V * 4);
+                                                     (c0 + k % V) * 4);
   }
   {
     // JT / 16 threads per row
@@ -468,13 +470,27 @@ __global__ __launch_bounds__(JT) void q4_join_kernel(Q4View c, Q4AttnArgs a) {
     const int r = threadIdx.x / RT, k = threadIdx.x % RT;
     float mall = kLowest, l = 0.0f;
     if (r < nrows) {
-      for (int p = k; p < n; p += RT) mall = fmaxf(mall, ml[p * 32 + r]);
+      constexpr int MOST = kQ4MaxSplits / RT;  // (n is at most that: all loads at once)
+      float mx[MOST], sums[MOST];
+#pragma unroll
+      for (int i = 0; i < MOST; ++i) {
+        mx[i] = kLowest;
+        sums[i] = 0.0f;
+        if (i * RT < n && i * RT + k < n) {
+          mx[i] = ml[(i * RT + k) * 32 + r];
+          sums[i] = ml[(i * RT + k) * 32 + 16 + r];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < MOST; ++i) mall = fmaxf(mall, mx[i]);
       auto larger = [](float x, float y) { return fmaxf(x, y); };
       mall = across_rows(row_reduce(mall, larger), false, larger);
-      for (int p = k; p < n; p += RT) {
-        const float f = __builtin_amdgcn_exp2f(ml[p * 32 + r] - mall);
-        w[p][r] = f;
-        l += ml[p * 32 + 16 + r] * f;
+#pragma unroll
+      for (int i = 0; i < MOST; ++i) {
+        if (i * RT >= n) break;
+        const float f = __builtin_amdgcn_exp2f(mx[i] - mall);
+        if (i * RT + k < n) w[i * RT + k][r] = f;
+        l += sums[i] * f;
       }
       auto add = [](float x, float y) { return x + y; };
       l = across_rows(row_reduce(l, add), false, add);
@@ -484,7 +500,7 @@ __global__ __launch_bounds__(JT) void q4_join_kernel(Q4View c, Q4AttnArgs a) {
   __syncthreads();
   for (int k0 = 0; k0 < items; k0 += span) {
     const int k = k0 + (int)threadIdx.x % span;
-    const int r = k / V, ch = k % V * 4;
+    const int r = k / V, ch = (c0 + k % V) * 4;
     floatx4_t o = {0.f, 0.f, 0.f, 0.f};
     if (k < items && way < ways) {
       int p = way;
@@ -527,8 +543,11 @@ hipError_t attn_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
 
 template <typename T, int D>
 hipError_t join_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
-  const dim3 grid((uint32_t)q4_row_tiles(a.G, a.tok.T, a.blocks != nullptr),
-                  (uint32_t)(c.B * c.H));
+  const int64_t tiles = q4_row_tiles(a.G, a.tok.T, a.blocks != nullptr);
+  // parts of at least 16 channels, while compute units are left for them
+  int parts = 1;
+  while (parts * 2 <= D / 16 && tiles * c.B * c.H * parts * 2 <= 256) parts *= 2;
+  const dim3 grid((uint32_t)tiles, (uint32_t)(c.B * c.H), (uint32_t)parts);
   if (a.blocks)
     q4_join_kernel<T, D, true><<<grid, JT, 0, st>>>(c, a);
   else
