@@ -553,7 +553,11 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
   // The tokens' sums in parts: [k-step, part, lane] 16-byte words, lane (m, g) token m's
   // channels of words 4 i + g.  The waves share the words.
   u32x4* parts = reinterpret_cast<u32x4*>(score + 16 * stride);
-  bool small = false;  // sums whose second part may lie below the normal numbers
+  // sums whose second part may lie below the normal numbers: not 0, less than 2^-100
+  bool small = false;
+  auto below = [](float x) {
+    return (__float_as_uint(x) << 1) - 1 < (__float_as_uint(0x1p-100f) << 1) - 1;
+  };
   for (int i = wave; i < KS / 2; i += SW) {
     double neg[8], pos[8];
 #pragma unroll
@@ -577,7 +581,7 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
     for (int j = 0; j < 8; ++j) {
       n[j] = (float)neg[j];
       p[j] = (float)pos[j];
-      small |= (neg[j] < 0.0 && neg[j] > -0x1p-100) || (pos[j] > 0.0 && pos[j] < 0x1p-100);
+      small |= below(n[j]) || below(p[j]);
     }
     bf16x8_t np[2], pp[2];
     split8<2>(n, np);
