@@ -24,8 +24,8 @@ constexpr int THREADS = 256;
 // rows that a rewound sequence no longer holds.  Four lanes hold a group, eight
 // channels each.
 //
-// Bound by HBM: 2 x 8 x 16384 rows of keys and values, d = 128, bf16, 40 us for 134 MB
-// read and 36 written, 4.2 TB/s; one row for 64 x 8 slices, 4.9 us, of which the reading
+// Bound by HBM: 2 x 8 x 16384 rows of keys and values, d = 128, bf16, 37 us for 134 MB
+// read and 36 written, 4.6 TB/s; one row for 64 x 8 slices, 4.9 us, of which the reading
 // back of the block's older rows (up to 4 KB a slice) is 2.  20240 slices of 8 tokens, d =
 // 32: 66 us, vector ALU (126 with the rows' values passed on by LDS shuffles).
 // ---------------------------------------------------------------------------
