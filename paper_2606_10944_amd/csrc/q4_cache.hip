@@ -434,9 +434,9 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
 // rounding; the others between (mostly that one alone) are scored again in float64.
 //
 // 2047 tokens x 8 key heads over up to 512 blocks, d = 128 (8e6 scores of 256 products:
-// 62 us in float64 at the rate of a large float64 matrix product): 69 us, of which the
-// scores take 37, second scores 12, and the choice the rest.  In float64 throughout: 343.
-constexpr int SW = 8;  // waves
+// 62 us in float64 at the rate of a large float64 matrix product): 63 us, of which the
+// scores take about half, second scores a fifth, and the choice the rest.  In float64
+// throughout: 343.
 
 // A float's key: integers of the same order, NaN below everything, 0 left free.
 __device__ __forceinline__ uint32_t float_key(float f) {
@@ -520,8 +520,10 @@ __device__ __forceinline__ uint32_t largest(const K* key, int want, int lane) {
   return in;
 }
 
-template <typename T, int D, int KPL>
-__global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectArgs a, int stride) {
+// SW waves.
+template <typename T, int D, int KPL, int SW>
+__global__ __launch_bounds__(64 * SW, SW == 8 ? 6 : KPL > 8 ? 4 : 8) void q4_select_kernel(
+    Q4View c, Q4SelectArgs a, int stride) {
   constexpr int KS = 2 * D / 32;  // k-steps: q- beside lo, then q+ beside hi
   extern __shared__ __align__(16) float score[];  // [16, stride], then the queries' parts
   __shared__ uint32_t ssize[SW][16];
@@ -541,7 +543,6 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
 #pragma unroll
     for (int i = 0; i < KS; ++i) to[i] = row[4 * i + g];
   };
-  fetch(wave * 16, w);
 
   // the last block that any of the tokens sees
   const bool there = t0 + m < a.tok.T;
@@ -564,7 +565,7 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
     for (int j = 0; j < 8; ++j) neg[j] = pos[j] = 0.0;
     if (there) {
       const T* p = qh + (int64_t)(t0 + m) * a.q.sr + (4 * i + g) * 8;
-#pragma unroll 4
+#pragma unroll 2
       for (int x = 0; x < a.G; ++x) {
         float f[8];
         load8<T>(p + x * a.q.sh, f);
@@ -592,6 +593,7 @@ __global__ __launch_bounds__(64 * SW) void q4_select_kernel(Q4View c, Q4SelectAr
       parts[((i + KS / 2) * 2 + x) * 64 + lane] = __builtin_bit_cast(u32x4, pp[x]);
     }
   }
+  fetch(wave * 16, w);
   __syncthreads();
 
   // largest sum of magnitudes of this lane's scores (token m), as bits: NaN above all, and
@@ -759,7 +761,7 @@ hipError_t pick(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <typename T, int D, int KPL>
+template <typename T, int D, int KPL, int SW>
 hipError_t select_k(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
   const int nb = std::min<int>((c.n_max + kQ4Block - 1) / kQ4Block, kQ4SelectBlocks);
   const int stride = (nb + 15) / 16 * 16 + 4;
@@ -767,21 +769,27 @@ hipError_t select_k(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
   const size_t lds = (size_t)16 * stride * 4 + 2 * D / 32 * 2 * 64 * 16;
   if (lds > 64 * 1024) {
     const hipError_t e =
-        hipFuncSetAttribute(reinterpret_cast<const void*>(&q4_select_kernel<T, D, KPL>),
+        hipFuncSetAttribute(reinterpret_cast<const void*>(&q4_select_kernel<T, D, KPL, SW>),
                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
   }
-  q4_select_kernel<T, D, KPL><<<grid, 64 * SW, lds, st>>>(c, a, stride);
+  q4_select_kernel<T, D, KPL, SW><<<grid, 64 * SW, lds, st>>>(c, a, stride);
   return hipGetLastError();
 }
 
+// Up to 1024 workgroups (two per compute unit at a time) 16 waves share a workgroup's blocks
+// and tokens, beyond that eight, three workgroups to a compute unit (8 key heads over up to
+// 512 blocks: 1024 workgroups 62.6 us against 71.1, 256 11.0 and 13.9; all 16384 tokens of
+// a cache, 8192 workgroups 291 and 252).  Scores of more blocks leave one workgroup to a
+// compute unit: 16 waves (1024 tokens over 1024 blocks: 72.5 against 88.7 with eight).
 template <typename T, int D>
 hipError_t select_d(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
   const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
-  if (nb <= 128) return select_k<T, D, 2>(c, a, st);
-  if (nb <= 512) return select_k<T, D, 8>(c, a, st);
-  if (nb <= 1024) return select_k<T, D, 16>(c, a, st);
-  return select_k<T, D, 32>(c, a, st);
+  if (nb > 1024) return select_k<T, D, 32, 16>(c, a, st);
+  if (nb > 512) return select_k<T, D, 16, 16>(c, a, st);
+  if ((int64_t)c.B * c.H * ((a.tok.T + 15) / 16) > 1024)
+    return nb <= 128 ? select_k<T, D, 2, 8>(c, a, st) : select_k<T, D, 8, 8>(c, a, st);
+  return nb <= 128 ? select_k<T, D, 2, 16>(c, a, st) : select_k<T, D, 8, 16>(c, a, st);
 }
 
 }  // namespace

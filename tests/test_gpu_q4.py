@@ -376,6 +376,19 @@ def test_select_of_small_queries_beside_large_bounds():
         check_select_head(c, q, at, 40, 1, 2, got, h)
 
 
+@pytest.mark.parametrize("d,n_max", [(32, 2000), (128, 2000), (64, 12000)])
+def test_select_of_long_prompts(d, n_max):
+    """More than 1024 times 16 tokens."""
+    g = gen(27)
+    H, T = 64, 290
+    c = filled(g, 1, H, n_max, d, [n_max])
+    q = randn(g, 1, 2 * H, T, d, dtype="bf16")
+    at = n_max - T
+    got = thin_q4_select(q.to(DEV), c, i32([at]), 9, n_sinks=1, n_window=2).cpu()
+    for h in (0, 31, 63):
+        check_select_head(c, q, at, 9, 1, 2, got, h)
+
+
 @pytest.mark.parametrize("count", [None, [40, 17, 0]])
 def test_select_of_prompts_in_large_caches(count):
     """Tokens that see more blocks than the launch of 16 tokens holds beside others."""
