@@ -24,12 +24,9 @@ constexpr int CH = kQ4Step;
 constexpr int PF = 2;
 
 // One wave's step: the codes of 32 keys and values.
-template <typename T, int D>
+template <int D>
 struct Codes {
-  // bytes of a key row that a lane holds: a group of 32 channels (bf16 queries, see
-  // Queries), else a quarter of the row
-  static constexpr bool MX = Elem<T>::bytes == 2;
-  static constexpr int KB = MX ? 16 : D / 8;
+  static constexpr int KB = D / 8;  // bytes of a lane's quarter of a key row
   static constexpr int KW = KB / 4;
   uint32_t k[2][KW];
   uint32_t ks[2];
@@ -42,11 +39,11 @@ struct Codes {
 };
 
 // Rows row0 .. row0 + 31; rows past `last` stand for `last`.
-template <typename T, int D>
+template <int D>
 __device__ __forceinline__ void load_codes(const Slice& c, int row0, int last, int lane,
-                                           Codes<T, D>& x) {
-  using C = Codes<T, D>;
-  const int m = lane & 15, g = (lane >> 4) % (D / 2 / C::KB);
+                                           Codes<D>& x) {
+  using C = Codes<D>;
+  const int m = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const uint32_t r = std::min(row0 + t * 16 + m, last);
@@ -185,7 +182,7 @@ struct Shares {
 template <typename T, int D, bool LIST, int WV>
 __global__ __launch_bounds__(64 * WV, 2) void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
   constexpr int NP = Elem<T>::bytes == 2 ? 1 : 3;  // bf16 parts of the weights
-  using C = Codes<T, D>;
+  using C = Codes<D>;
   __shared__ __align__(16) unsigned char lds[WV * CH * kVStride<D>];
   __shared__ float sm[WV][16], sl[WV][16];
   const int lane = threadIdx.x & 63;
@@ -280,7 +277,7 @@ __global__ __launch_bounds__(64 * WV, 2) void q4_attn_kernel(Q4View c, Q4AttnArg
     row0[k] = c.n_max;
     n = next(n + 1, &row0[k]);
     go[k] = more(n);
-    load_codes<T, D>(rows, row0[k], std::max(last, 0), lane, buf[k]);
+    load_codes<D>(rows, row0[k], std::max(last, 0), lane, buf[k]);
   };
 #pragma unroll
   for (int k = 0; k + 1 < PF; ++k) fetch(k);

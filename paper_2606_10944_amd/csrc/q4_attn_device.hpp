@@ -2,10 +2,15 @@
 //
 // o = sum_j p_j v_j / sum_j p_j,  p_j = exp(<q, k_j> / sqrt(d) - max).
 //
-// A code times its power of two is exactly a bf16, so values (and, for float32
-// queries, keys) enter the bf16 matrix instructions without loss.  float32 weights p
-// split into three bf16 parts; bf16 queries use one bf16 weight: its rounding (2^-8 of
-// a term at most) is that of the output.
+// A code times its power of two is exactly a bf16, so keys and values enter the bf16
+// matrix instructions without loss.  float32 queries and weights p split into three bf16
+// parts; bf16 queries are exact and use one bf16 weight: its rounding (2^-8 of a term at
+// most) is that of the output.
+//
+// (The scaled instruction would take keys' codes as they are stored, beside bf16 queries in
+// two e4m3 parts: 687 us instead of 800 for 4096 tokens over 16384 rows.  But it cuts
+// products below about 2^-15 of the largest under its scale, and the parts lose bits of
+// channels 2^-9 below the row's largest: one outlier channel then hides the others.)
 //
 // Lanes are l = 16 g + m.  Scores S^T = K Q^T (keys x query rows): lane (m, g) feeds
 // key row m's share of the channels, and query row m's.  It then holds the scores of
@@ -81,22 +86,23 @@ __device__ __forceinline__ Slice slice_of(const Q4View& c, int64_t s) {
 }
 
 // A tile's 16 query rows as the second operand of the scores, and the scores of 16 keys.
-//
-// float32: three bf16 parts (24 bits), the keys decoded to bf16.
+// Queries are bf16 as they are, or three bf16 parts of float32 (24 bits); keys are decoded
+// to bf16.  Both are exact, and products are summed in float32.
 template <typename T, int D>
 struct Queries {
-  static constexpr int KS = D / 32, N = 3 * KS;  // N: matrix instructions for 16 keys
-  bf16x8_t q[3][KS];
+  static constexpr int KS = D / 32, QP = Elem<T>::bytes == 2 ? 1 : 3;
+  static constexpr int N = QP * KS;  // matrix instructions for 16 keys
+  bf16x8_t q[QP][KS];
   // row: this lane's query row (null: zeros); g: lane / 16
   __device__ __forceinline__ void load(const T* row, int g) {
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
       float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (row) load8<T>(row + g * (D / 4) + k * 8, f);
-      bf16x8_t part[3];
-      split8<3>(f, part);
+      bf16x8_t part[QP];
+      split8<QP>(f, part);
 #pragma unroll
-      for (int p = 0; p < 3; ++p) q[p][k] = part[p];
+      for (int p = 0; p < QP; ++p) q[p][k] = part[p];
     }
   }
   __device__ __forceinline__ floatx4_t scores(const uint32_t* codes, uint32_t byte) const {
@@ -108,88 +114,9 @@ struct Queries {
       decode8(codes[k], ks, w);
       const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, (u32x4){w[0], w[1], w[2], w[3]});
 #pragma unroll
-      for (int p = 2; p >= 0; --p)
+      for (int p = QP - 1; p >= 0; --p)
         z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[p][k], z, 0, 0, 0);
     }
-    return z;
-  }
-};
-
-// bf16: the scaled 16x16x128 instruction takes the codes and their scales as they are
-// stored, 128 channels at a time, beside fp8 queries.  A bf16 is the sum of two e4m3
-// numbers (four significant bits each) under one power of two per row, exactly for
-// values down to 2^-9 of the row's largest, within 2^-18 of that below.  (The
-// instruction cuts products below about 2^-15 of its largest one: 1e-6 of the sum of
-// magnitudes for normal values.)  Against decoding the keys to bf16 it saves 32 of 64
-// conversions per step of 32 keys and takes two thirds of the matrix cores' time.
-//
-// Channels of k-slot 16 g + i and 64 + 16 g + i in lane (m, g) of the fp8 operand; the
-// fp4 operand's lane (m, g) holds k-slots 32 g .. 32 g + 31, all under its own scale.
-// d = 128: an instruction for each part; d = 64: k-slots 0 .. 63 take the first part,
-// the others the second, beside the same keys; d = 32: 0 .. 31 and 32 .. 63.
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-template <int D>
-struct Queries<bf16_t, D> {
-  static constexpr int N = D == 128 ? 2 : 1;  // matrix instructions for 16 keys
-  i32x8 q[N];
-  int scale;
-  __device__ __forceinline__ void load(const bf16_t* row, int g) {
-    // this lane's 16 channels (d = 128: 32) and the part that it holds
-    constexpr int C = D == 128 ? 32 : 16;
-    float f[C];
-    const int c0 = D == 32 ? g % 2 * 16 : g * 16;
-    float amax = 0.0f;
-#pragma unroll
-    for (int i = 0; i < C; i += 8) {
-      if (row)
-        load8<bf16_t>(row + c0 + i / 16 * 64 + i % 16, f + i);
-      else
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[i + j] = 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < C; ++i) amax = fmaxf(amax, fabsf(f[i]));
-    amax = across_rows(amax, true, [](float a, float b) { return fmaxf(a, b); });
-    // the largest value lands in [2^7, 2^8)
-    int byte = (int)(__float_as_uint(amax) >> 23) - 7;
-    byte = byte < 1 ? 1 : byte;
-    scale = byte;
-    const float up = __uint_as_float((uint32_t)(254 - byte) << 23);
-    int part[2][C / 4];
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-      for (int i = 0; i < C / 4; ++i) {
-        float* x = f + 4 * i;
-        if (p == 0)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] *= up;
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], 0, false);
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], w, true);
-        part[p][i] = w;
-        x[0] -= __builtin_amdgcn_cvt_f32_fp8(w, 0);
-        x[1] -= __builtin_amdgcn_cvt_f32_fp8(w, 1);
-        x[2] -= __builtin_amdgcn_cvt_f32_fp8(w, 2);
-        x[3] -= __builtin_amdgcn_cvt_f32_fp8(w, 3);
-      }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (D == 128) {
-        q[0][i] = part[0][i];
-        q[N - 1][i] = part[1][i];
-      } else if (D == 64) {
-        q[0][i] = part[i / 4][i % 4];
-      } else {
-        q[0][i] = i < 4 ? part[g / 2][i % 4] : 0;
-      }
-    }
-  }
-  __device__ __forceinline__ floatx4_t scores(const uint32_t* codes, uint32_t byte) const {
-    floatx4_t z = {0.f, 0.f, 0.f, 0.f};
-    const i32x8 k = {(int)codes[0], (int)codes[1], (int)codes[2], (int)codes[3], 0, 0, 0, 0};
-#pragma unroll
-    for (int i = N - 1; i >= 0; --i)
-      z = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q[i], z, 4, 0, 0, (int)byte, 0, scale);
     return z;
   }
 };

@@ -38,7 +38,7 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
   constexpr bool MX = Elem<T>::bytes == 2;
   constexpr int NP = MX ? 1 : 3;                  // bf16 parts of the weights
   constexpr int GR = D / 32;                      // groups per row
-  constexpr int KW = (MX ? 16 : D / 8) / 4;       // words of a key row that a lane feeds
+  constexpr int KW = D / 32;                      // words of a key row that a lane feeds
   constexpr int ROWS = 16 * RT;                   // query rows of a wave
   __shared__ __align__(16) unsigned char sv[2][PK * kVStride<D>];
   __shared__ __align__(16) uint32_t sk[2][PK * D / 8];
@@ -125,16 +125,9 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
 #pragma unroll
     for (int kt = 0; kt < PK / 16; ++kt) {
       const int key = kt * 16 + m;
-      uint32_t kc[KW], byte;
-      if constexpr (MX) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(sk[from] + (key * GR + g % GR) * 4);
-        kc[0] = w[0]; kc[1] = w[1]; kc[2] = w[2]; kc[3] = w[3];
-        byte = sks[from][key * GR + g % GR];
-      } else {
-#pragma unroll
-        for (int w = 0; w < KW; ++w) kc[w] = sk[from][key * (D / 8) + g * KW + w];
-        byte = sks[from][key * GR + g * GR / 4];
-      }
+      uint32_t kc[KW];
+      load_words<KW>(reinterpret_cast<const uint8_t*>(sk[from] + key * (D / 8) + g * KW), kc);
+      const uint32_t byte = sks[from][key * GR + g * GR / 4];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         const floatx4_t z = q[rt].scores(kc, byte);
@@ -218,8 +211,9 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
 #pragma unroll
         for (int ch = 0; ch < PK / 32; ++ch) split8<NP>(s[rt] + ch * 8, pp[rt][ch]);
       }
-      constexpr int NS = PK / 16 * RT * Queries<T, D>::N;  // matrix instructions of the scores
-      interleave<NS, std::max(1, RT * (PK / 4) * 7 / 2 / NS)>();
+      // matrix instructions of the scores, and vector ones for each: weights, keys decoded
+      constexpr int NS = PK / 16 * RT * Queries<T, D>::N;
+      interleave<NS, std::max(1, (RT * (PK / 4) * 7 / 2 + PK / 16 * KW * 4) / NS)>();
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int ch = 0; ch < PK / 32; ++ch) {

@@ -1,0 +1,82 @@
+"""The 4-bit cache's operators where rounding and ends of ranges show: outlier
+channels, weights that sum to one, borders of a selection, many sequences."""
+import math
+
+import pytest
+import torch
+
+import q4_reference as ref
+from paper_2606_10944_amd import Q4Cache, thin_q4_attention, thin_q4_load, thin_q4_select, thin_q4_store
+from test_gpu_q4 import (DEV, attention_bound, check_attention, check_select_head, filled, fresh,
+                         gen, i32, randn)
+
+pytestmark = pytest.mark.gpu
+
+
+# Calls (B, H, G, T, blocks listed) of the kernel for few query rows, over every row and
+# over lists, and of the kernel for many.
+KERNELS = {"few": (1, 1, 4, 1, False), "listed": (1, 2, 4, 2, True),
+           "many": (16, 16, 4, 32, False)}
+
+
+def two_kinds(kind, k, q, n_max=300):
+    """Attention over rows that hold k[0] and k[1] in turn, whose values are 1 and -1: a
+    cache, queries of the rows q, and the call's arguments."""
+    B, H, G, T, listed = KERNELS[kind]
+    d = q.numel()
+    c = fresh(B, H, n_max, d)
+    rows = torch.stack((k[0], k[1])).repeat(n_max // 2, 1).expand(B, H, n_max, d)
+    vals = torch.tensor([1.0, -1.0]).repeat(n_max // 2).view(1, 1, n_max, 1).expand(B, H, n_max, d)
+    thin_q4_store(rows.contiguous().to(DEV), vals.contiguous().to(DEV), c, i32([0] * B))
+    assert torch.equal(ref.cached(c.k_codes[0, 0, :2], c.k_scales[0, 0, :2]),
+                       torch.stack(k).double())  # the cache holds them exactly
+    queries = q.view(1, 1, 1, d).expand(B, H * G, T, d).contiguous()
+    blocks = None
+    if listed:
+        blocks = torch.arange((n_max + 63) // 64, dtype=torch.int32).expand(B, H, T, -1).contiguous()
+    return c, queries, [n_max - T] * B, blocks
+
+
+def check_two_kinds(kind, k, q):
+    for dtype in (torch.bfloat16, torch.float32):
+        c, queries, at, blocks = two_kinds(kind, k, q.to(dtype))
+        got = thin_q4_attention(queries.to(DEV), c, i32(at),
+                                blocks=None if blocks is None else blocks.to(DEV))
+        one = Q4Cache.over(*[x[:1, :1].contiguous() for x in (c.k_codes, c.k_scales, c.v_codes,
+                                                               c.v_scales, c.bounds)])
+        G = KERNELS[kind][2]
+        name = "bf16" if dtype == torch.bfloat16 else "fp32"
+        check_attention(one, queries[:1, :G], at[:1], None,
+                        None if blocks is None else blocks[:1, :1], got[:1, :G], name)
+        B, H = c.B, c.H  # (the slices are alike)
+        assert torch.equal(got.view(B, H, G, *got.shape[2:]),
+                           got[:1, :G].view(1, 1, G, *got.shape[2:]).expand(B, H, -1, -1, -1))
+
+
+@pytest.mark.parametrize("kind", list(KERNELS))
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_attention_keeps_small_products_beside_a_large_one(d, kind):
+    """One channel of every key and query makes a product of 6144, the same for all keys;
+    products of 1/8 of the others order them (2^-15.6 of it: below half a step of a sum in
+    16 bits, 2^8 steps of one in float32)."""
+    k = torch.zeros(2, d)
+    q = torch.zeros(d)
+    # beside it, under its scale, and under scales of their own
+    k[0, 1:32], k[1, 1:32], q[1:32] = 8.0, -8.0, 2.0 ** -6
+    k[0, 32:], k[1, 32:], q[32:] = 0.5, -0.5, 0.25
+    k[:, 0] = 96.0
+    q[0] = 64.0
+    check_two_kinds(kind, list(k), q)
+
+
+@pytest.mark.parametrize("kind", list(KERNELS))
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_attention_keeps_all_bits_of_small_query_channels(d, kind):
+    """Channels 2^-12 of the row's largest that differ in their last bf16 bit alone, which
+    decides between two kinds of keys; the largest meets zeros."""
+    k = torch.zeros(2, d)
+    k[0, 1::2], k[0, 2::2] = 0.5, -0.5
+    q = torch.full((d,), 64.0)
+    q[1::2] = 64.5
+    q[0] = 2.0 ** 18
+    check_two_kinds(kind, list(k), q)
