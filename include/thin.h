@@ -530,8 +530,9 @@ int thin_q4_select(const thin_q4_cache_t* cache, const void* Q, const int64_t* q
  *           are no block of the cache, or lie behind the token, count for nothing,
  *           a block listed twice counts twice.  NULL with n_sel = 0: every row.
  * T * q_heads / H <= 2^27, B * q_heads * T <= 2^30.  A row that sees nothing is
- * zeros.  float32 queries: products and weights to float32 accuracy.  bf16: exact
- * products, weights rounded to bf16, sums in float32.
+ * zeros.  Sums in float32.  float32 queries: products and weights to float32
+ * accuracy.  bf16: exact products; weights to 17 bits, or, where a call has many query
+ * rows, rounded to bf16 with the sum of the rounded ones below.
  *   workspace as for thin_q4_select (may be NULL where the plan asks for 0 bytes).
  * Errors: THIN_EINVAL, THIN_EDTYPE, THIN_EWORKSPACE, THIN_EHIP.
  */

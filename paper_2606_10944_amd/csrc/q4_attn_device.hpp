@@ -3,9 +3,11 @@
 // o = sum_j p_j v_j / sum_j p_j,  p_j = exp(<q, k_j> / sqrt(d) - max).
 //
 // A code times its power of two is exactly a bf16, so keys and values enter the bf16
-// matrix instructions without loss.  float32 queries and weights p split into three bf16
-// parts; bf16 queries are exact and use one bf16 weight: its rounding (2^-8 of a term at
-// most) is that of the output.
+// matrix instructions without loss, and so do bf16 queries; float32 queries and their
+// weights p split into three bf16 parts.  Weights of bf16 queries are two parts (off by
+// 2^-17) where few rows read a cache, and one (2^-8 at most, as the output's rounding)
+// where the matrix instructions of many rows bound the call; there the sum of the weights
+// is that of the rounded ones, so that they make one in all.
 //
 // (The scaled instruction would take keys' codes as they are stored, beside bf16 queries in
 // two e4m3 parts: 687 us instead of 800 for 4096 tokens over 16384 rows.  But it cuts

@@ -80,3 +80,43 @@ def test_attention_keeps_all_bits_of_small_query_channels(d, kind):
     q[1::2] = 64.5
     q[0] = 2.0 ** 18
     check_two_kinds(kind, list(k), q)
+
+
+# Weights are rounded, but their sum is that of the rounded ones: values that are all one
+# number come back as it, whatever the weights (sums and quotient are off by 2^-18 at most,
+# and the output's nearest bf16 is the number itself).
+def ones_cache(k):
+    B, H, n, d = k.shape
+    c = fresh(B, H, n, d)
+    thin_q4_store(k.to(DEV), torch.ones(B, H, n, d).to(DEV), c, i32([0] * B))
+    return c
+
+
+def test_constant_values_come_back_under_a_dominating_key():
+    """One key with nearly all of the weight, found when the maximum stands 2^7 and more
+    below it: its weight is no power of two."""
+    for d in (32, 64, 128):
+        n = 300
+        k = torch.zeros(1, 1, n, d)
+        k[..., 0] = -4.0
+        k[0, 0, 0, 0] = 0.0
+        k[0, 0, 256, 0] = 1.0
+        c = ones_cache(k)
+        bits = torch.linspace(7.02, 7.9, 60).view(1, 15, 4, 1)  # of the weight, to base 2
+        q = torch.zeros(1, 15, 4, d)
+        q[..., :1] = bits * math.sqrt(d) * math.log(2.0)
+        got = thin_q4_attention(q.bfloat16().to(DEV), c, i32([n - 4]))
+        assert (got == 1.0).all(), (d, got.unique())
+
+
+@pytest.mark.parametrize("d,B,H,G,T,n,n_sel", [
+    (128, 2, 3, 4, 1, 700, 0), (64, 1, 2, 5, 3, 9000, 0), (32, 2, 2, 2, 9, 900, 6),
+    (128, 1, 1, 4, 1, 20000, 200), (64, 16, 16, 4, 33, 300, 0), (128, 1, 8, 4, 67, 5000, 0)])
+def test_constant_values_come_back(d, B, H, G, T, n, n_sel):
+    g = gen(30)
+    c = ones_cache(randn(g, B, H, n, d) * 2)
+    q = randn(g, B, H * G, T, d, dtype="bf16").to(DEV)
+    at = i32([n - T] * B)
+    blocks = thin_q4_select(q, c, at, n_sel) if n_sel else None
+    got = thin_q4_attention(q, c, at, blocks=blocks)
+    assert (got == 1.0).all(), got.unique()
