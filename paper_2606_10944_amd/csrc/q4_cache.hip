@@ -425,16 +425,16 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
 // Selection for several tokens of a slice in one launch.  A workgroup takes 16 tokens:
 // their scores of every block come from the bf16 matrix instructions, the queries'
 // float64 sums split into two bf16 parts (bounds are bf16), and stay in LDS.  Such a
-// score is off by less than eps = 1.25 * 2^-16 size, size = the token's largest sum of
-// the products' magnitudes: the split leaves at most 2^-16 of each query sum (two
-// roundings by half a step, 2^-8), and a chain of 16 instructions was never seen more
-// than 2^-20.5 of the sum of magnitudes off (16 roundings of 2^-24 make 2^-20), against
-// the 2^-18 that is left for it.  So a block more than 2 eps
+// score is off by less than eps = (4 d 2^-23 + 2^-16) (1 + 2^-6) size, size = the token's
+// largest sum of the products' magnitudes as the instructions add it up: 4 d additions,
+// rounded or cut to float32, lose at most 2^-23 of it each, the split 2^-16 of each query
+// sum (two roundings by half a step, 2^-8), and size itself may be short by 2^-7 (first
+// parts only, and its additions).  So a block more than 2 eps
 // above the last one that fits is in, one more than 2 eps below it is out, whatever the
 // rounding; the others between (mostly that one alone) are scored again in float64.
 //
 // 2047 tokens x 8 key heads over up to 512 blocks, d = 128 (8e6 scores of 256 products:
-// 62 us in float64 at the rate of a large float64 matrix product): 63 us, of which the
+// 62 us in float64 at the rate of a large float64 matrix product): 64 us, of which the
 // scores take about half, second scores a fifth, and the choice the rest.  In float64
 // throughout: 343.
 
@@ -664,8 +664,9 @@ __global__ __launch_bounds__(64 * SW, SW == 8 ? 6 : KPL > 8 ? 4 : 8) void q4_sel
 #pragma unroll
         for (int x = 0; x < SW; ++x) bits = std::max(bits, ssize[x][r]);
         const float size = __uint_as_float(bits);
-        const float eps = fmaxf(0x1.4p-15f * size, 0x1p-110f);
-        const float mid = key_float(least), up = mid + eps, down = mid - eps;
+        constexpr float kEps2 = 2.0f * (4.0f * D * 0x1p-23f + 0x1p-16f) * (1.0f + 0x1p-6f);
+        const float eps2 = fmaxf(kEps2 * size, 0x1p-110f);
+        const float mid = key_float(least), up = mid + eps2, down = mid - eps2;
         const bool wild = !(size < INFINITY) || !(fabsf(mid) < INFINITY);
         int sure = 0, open = 0;
         uint32_t maybe = 0;

@@ -120,3 +120,26 @@ def test_constant_values_come_back(d, B, H, G, T, n, n_sel):
     blocks = thin_q4_select(q, c, at, n_sel) if n_sel else None
     got = thin_q4_attention(q, c, at, blocks=blocks)
     assert (got == 1.0).all(), got.unique()
+
+
+def test_select_of_prompts_with_small_products_beside_a_large_one():
+    """Blocks whose score is one large product and 126 products just under a float32 unit
+    of it, all of one sign: a sum that cuts each of them is off by 2^-16, which is half of
+    what two kinds of blocks differ by, and turns their order round."""
+    H, T, d, nb = 64, 2, 128, 100
+    c = fresh(1, H, 64 * nb, d)
+    up = torch.arange(nb) % 2 == 1
+    x = torch.zeros(nb, 2, d)
+    x[:, 1] = torch.where(up, 123 / 128, -123 / 128).view(nb, 1)
+    x[:, 1, 0] = 1.0
+    x[:, 1, 1] = torch.where(up, 0.0, 0.875)  # less than the others make: `up` scores higher
+    x[:, 0] = x[:, 1] - 1.0
+    c.bounds.copy_(x.expand(1, H, nb, 2, d))
+    q = torch.full((1, H, T, d), 2.0 ** -23)
+    q[..., 0], q[..., 1] = 1.0, 2.0 ** -15
+    q = q.bfloat16()
+    at = 64 * nb - T
+    for n_sel in (7, 40, 60):
+        got = thin_q4_select(q.to(DEV), c, i32([at]), n_sel, n_sinks=0, n_window=1).cpu()
+        for h in (0, H - 1):
+            check_select_head(c, q, at, n_sel, 0, 1, got, h)
