@@ -555,7 +555,7 @@ __global__ __launch_bounds__(64 * SW, SW == 8 ? 6 : KPL > 8 ? 4 : 8) void q4_sel
   // channels of words 4 i + g.  The waves share the words.
   u32x4* parts = reinterpret_cast<u32x4*>(score + 16 * stride);
   // sums whose second part may lie below the normal numbers: not 0, less than 2^-100
-  bool small = false;
+  bool small = false, some = false;  // some: a sum that is not 0
   auto below = [](float x) {
     return (__float_as_uint(x) << 1) - 1 < (__float_as_uint(0x1p-100f) << 1) - 1;
   };
@@ -583,6 +583,7 @@ __global__ __launch_bounds__(64 * SW, SW == 8 ? 6 : KPL > 8 ? 4 : 8) void q4_sel
       n[j] = (float)neg[j];
       p[j] = (float)pos[j];
       small |= below(n[j]) || below(p[j]);
+      some |= n[j] != 0.0f || p[j] != 0.0f;
     }
     bf16x8_t np[2], pp[2];
     split8<2>(n, np);
@@ -597,8 +598,9 @@ __global__ __launch_bounds__(64 * SW, SW == 8 ? 6 : KPL > 8 ? 4 : 8) void q4_sel
   __syncthreads();
 
   // largest sum of magnitudes of this lane's scores (token m), as bits: NaN above all, and
-  // infinite for sums that the parts do not hold (all its blocks are scored again)
-  uint32_t size = small ? 0x7f800000u : 0;
+  // infinite for sums that the parts do not hold (all its blocks are scored again).  0 only
+  // where every query is: products of others may lie below the normal numbers.
+  uint32_t size = small ? 0x7f800000u : some ? 0x00800000u : 0;
   auto tile = [&](int k0, const u32x4* x) __attribute__((always_inline)) {
     floatx4_t z = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
     const u32x4 sign = {0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
@@ -678,7 +680,7 @@ __global__ __launch_bounds__(64 * SW, SW == 8 ? 6 : KPL > 8 ? 4 : 8) void q4_sel
           open += __popcll(__ballot(x));
           sure += __popcll(__ballot((best >> i & 1) && !x));
         }
-        // (all scores 0: the lowest blocks are chosen already)
+        // (all queries 0: the lowest blocks are chosen already)
         if (open > free - sure && !(size == 0.0f)) {
           // products of 2 D / 64 neighbouring channels per lane, q- beside lo, q+ beside hi
           constexpr int N = 2 * D / 64;

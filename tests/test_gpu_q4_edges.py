@@ -143,3 +143,18 @@ def test_select_of_prompts_with_small_products_beside_a_large_one():
         got = thin_q4_select(q.to(DEV), c, i32([at]), n_sel, n_sinks=0, n_window=1).cpu()
         for h in (0, H - 1):
             check_select_head(c, q, at, n_sel, 0, 1, got, h)
+
+
+def test_select_of_prompts_whose_products_underflow():
+    """Scores of 2^-160 that are no float32 numbers, but differ."""
+    g = gen(31)
+    H, T, d, nb = 64, 3, 64, 200
+    c = fresh(1, H, 64 * nb, d)
+    x = torch.randn(1, H, nb, 2, d, generator=g) * 2.0 ** -100
+    c.bounds.copy_(x.sort(-2)[0].bfloat16())
+    q = (torch.randn(1, 2 * H, T, d, generator=g) * 2.0 ** -60).bfloat16()
+    q[:, :, 1] = 0.0  # (a token whose scores are all 0)
+    at = 64 * nb - T
+    got = thin_q4_select(q.to(DEV), c, i32([at]), 20, n_sinks=1, n_window=2).cpu()
+    for h in range(0, H, 9):
+        check_select_head(c, q, at, 20, 1, 2, got, h)
