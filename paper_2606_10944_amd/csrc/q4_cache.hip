@@ -275,8 +275,8 @@ __global__ __launch_bounds__(THREADS) void q4_scores_kernel(Q4View c, Q4SelectAr
 
 // The n_sel best of a row's blocks, in order.  A workgroup of W waves holds the
 // row's keys, KPL per lane.  The border is found by counting keys in equal parts of
-// the interval that it lies in, 512 W at a time (a step or two for scores that differ;
-// six at most, for the key's 64 bits).  Equal keys at the border: the lowest blocks.
+// the interval that it lies in, 512 W at a time (a step or two for scores that differ; for
+// the key's 64 bits 8 at most with one wave, 6 with four, 5 with 16).  Equal keys at the border: the lowest blocks.
 // (Halving the interval instead took 6 of 9.5 us for 32 rows of 2048 blocks.)
 template <int W, int KPL>
 __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs a) {

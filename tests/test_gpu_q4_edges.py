@@ -158,3 +158,23 @@ def test_select_of_prompts_whose_products_underflow():
     got = thin_q4_select(q.to(DEV), c, i32([at]), 20, n_sinks=1, n_window=2).cpu()
     for h in range(0, H, 9):
         check_select_head(c, q, at, 20, 1, 2, got, h)
+
+
+@pytest.mark.parametrize("d", [32, 128])
+@pytest.mark.parametrize("nb", [100, 500, 1500, 5000, 9000, 20000])
+def test_select_border_in_the_last_bit(nb, d):
+    """One token; scores of both signs, those around the border 1 and a few units of the
+    last bit of a float64 more, some of them equal."""
+    g = gen(32)
+    c = Q4Cache(1, 1, 64 * nb, d, device=DEV)
+    x = torch.zeros(1, 1, nb, 2, d)
+    x[..., 1, 0] = torch.where(torch.rand(nb, generator=g) < 0.3, -1.0, 1.0)
+    x[..., 1, 1] = torch.randint(0, 40, (nb,), generator=g) / 128.0
+    x[..., 0, :] = x[..., 1, :] - 1.0
+    c.bounds.copy_(x)
+    q = torch.zeros(1, 1, 1, d)
+    q[..., 0], q[..., 1] = 1.0, 2.0 ** -45
+    at = 64 * nb - 1
+    for n_sel in (20, nb // 3, nb // 2):
+        got = thin_q4_select(q.to(DEV), c, i32([at]), n_sel, n_sinks=1, n_window=2).cpu()
+        check_select_head(c, q, at, n_sel, 1, 2, got, 0)
