@@ -769,11 +769,15 @@ hipError_t select_k(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
   const int nb = std::min<int>((c.n_max + kQ4Block - 1) / kQ4Block, kQ4SelectBlocks);
   const int stride = (nb + 15) / 16 * 16 + 4;
   const dim3 grid((uint32_t)((a.tok.T + 15) / 16), (uint32_t)(c.B * c.H));
-  const size_t lds = (size_t)16 * stride * 4 + 2 * D / 32 * 2 * 64 * 16;
-  if (lds > 64 * 1024) {
+  constexpr size_t kParts = 2 * D / 32 * 2 * 64 * 16;
+  const size_t lds = (size_t)16 * stride * 4 + kParts;
+  // Dynamic LDS past 64 KiB is allowed by an attribute of the kernel, which all host threads
+  // share: every call sets it to the most that this instance takes, never to its own need.
+  constexpr size_t most = (size_t)16 * (64 * KPL + 4) * 4 + kParts;
+  if constexpr (most > 64 * 1024) {
     const hipError_t e =
         hipFuncSetAttribute(reinterpret_cast<const void*>(&q4_select_kernel<T, D, KPL, SW>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)most);
     if (e != hipSuccess) return e;
   }
   q4_select_kernel<T, D, KPL, SW><<<grid, 64 * SW, lds, st>>>(c, a, stride);

@@ -178,3 +178,37 @@ def test_select_border_in_the_last_bit(nb, d):
     for n_sel in (20, nb // 3, nb // 2):
         got = thin_q4_select(q.to(DEV), c, i32([at]), n_sel, n_sinks=1, n_window=2).cpu()
         check_select_head(c, q, at, n_sel, 1, 2, got, 0)
+
+
+def test_selections_of_two_threads():
+    """Prompts over a large and a small cache from two host threads: each has the LDS that
+    its own scores need."""
+    import threading
+    g = gen(34)
+    H, T, d = 64, 3, 32
+    calls = []
+    for nb in (2000, 1100):
+        c = Q4Cache(1, H, 64 * nb, d, device=DEV)
+        c.bounds.copy_(torch.randn(1, H, nb, 2, d, generator=g).sort(-2)[0])
+        q = randn(g, 1, H, T, d, dtype="bf16").to(DEV)
+        at = i32([64 * nb - T])
+        calls.append((c, q, at, thin_q4_select(q, c, at, 9)))
+    failed = []
+
+    def work(c, q, at, want):
+        try:
+            st = torch.cuda.Stream()
+            with torch.cuda.stream(st):
+                for _ in range(200):
+                    if not torch.equal(thin_q4_select(q, c, at, 9), want):
+                        failed.append("differs")
+        except Exception as e:  # noqa: BLE001
+            failed.append(repr(e))
+
+    torch.cuda.synchronize()
+    threads = [threading.Thread(target=work, args=a) for a in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
