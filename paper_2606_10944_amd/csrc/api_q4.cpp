@@ -201,9 +201,12 @@ int thin_q4_load(const thin_q4_cache_t* cache, int64_t T, const int32_t* at, voi
 int thin_q4_select_plan(int64_t B, int64_t H, int64_t n_max, int64_t T, size_t* workspace_bytes) {
   if (!workspace_bytes || !valid_sizes(B, H, n_max, T)) return THIN_EINVAL;
   const int64_t nb = blocks_of(n_max);
-  *workspace_bytes = thin::q4_select_fused(B * H, nb, T)
-                         ? 0
-                         : (size_t)(B * H * nb * thin::q4_select_tokens(B * H, nb, T)) * 8;
+  int64_t rows = 0;  // of scores
+  if (!thin::q4_select_grouped(B * H, T))
+    rows = B * H * thin::q4_select_tokens(B * H, nb, T);
+  else if (!thin::q4_select_fused(B * H, nb, T))
+    rows = thin::q4_select_slots(B * H, nb, T);
+  *workspace_bytes = (size_t)(rows * nb) * 8;
   return THIN_OK;
 }
 
@@ -238,12 +241,13 @@ int thin_q4_select(const thin_q4_cache_t* cache, const void* Q, const int64_t* q
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
   const int64_t slices = (int64_t)c.B * c.H, nb = blocks_of(c.n_max);
-  a.grouped = thin::q4_select_grouped(slices, T);
-  if (a.grouped) {
+  if (thin::q4_select_grouped(slices, T)) {
     e = observed(THIN_KERNEL_Q4_SELECT, -1, st,
                  [&] { return thin::launch_q4_select(dtype, cache->d, c, a, st); });
-    if (e != hipSuccess || thin::q4_select_fused(slices, nb, T))
-      return e == hipSuccess ? THIN_OK : THIN_EHIP;
+    if (e == hipSuccess && !thin::q4_select_fused(slices, nb, T))
+      e = observed(THIN_KERNEL_Q4_SELECT, -1, st,
+                   [&] { return thin::launch_q4_select_rest(dtype, cache->d, c, a, st); });
+    return e == hipSuccess ? THIN_OK : THIN_EHIP;
   }
   const int64_t step = thin::q4_select_tokens(slices, nb, T);
   for (int64_t t0 = 0; t0 < T && e == hipSuccess; t0 += step) {

@@ -58,13 +58,15 @@ struct Q4SelectArgs {
   int32_t n_sel, n_sinks, n_window;
   int32_t* blocks;   // [B, H, T, n_sel]
   int32_t t0, tn;    // the launch's tokens: t0 .. t0 + tn - 1
-  uint64_t* scores;  // [B, H, tn, ceil(n_max / 64)]
-  bool grouped;      // launch_q4_select has run: the others take what it left
+  uint64_t* scores;  // [B, H, tn, ceil(n_max / 64)], or a slot per workgroup (the rest)
 };
-// Scores and choice in one launch, without a workspace, of the tokens whose 16 see at most
-// kQ4SelectBlocks blocks; scores, then the choice by them, of tokens t0 .. t0 + tn - 1.
+// Many tokens: scores and choice in one launch, without a workspace, of the tokens whose 16
+// see at most kQ4SelectBlocks blocks, then of the others.  Few: scores, then the choice by
+// them, of tokens t0 .. t0 + tn - 1.
 hipError_t launch_q4_select(int dtype, int64_t d, const Q4View& c, const Q4SelectArgs& a,
                             hipStream_t st);
+hipError_t launch_q4_select_rest(int dtype, int64_t d, const Q4View& c, const Q4SelectArgs& a,
+                                 hipStream_t st);
 hipError_t launch_q4_scores(int dtype, int64_t d, const Q4View& c, const Q4SelectArgs& a,
                             hipStream_t st);
 hipError_t launch_q4_pick(const Q4View& c, const Q4SelectArgs& a, hipStream_t st);

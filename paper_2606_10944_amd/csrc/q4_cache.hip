@@ -207,70 +207,85 @@ __device__ __forceinline__ uint64_t score_key(double s) {
   return k < 2 ? 2 : k;
 }
 
-// Whether launch_q4_select takes token t: none of its 16 sees more blocks than LDS holds.
-__device__ __forceinline__ bool q4_grouped(const Q4View& c, const Q4SelectArgs& a, int b, int t) {
-  int end = std::min(t / 16 * 16 + 16, a.tok.T);
-  if (a.tok.count) end = std::min(end, a.tok.count[b]);
-  return end <= t / 16 * 16 ||
-         q4_last_row(a.tok, b, end - 1, c.n_max) < kQ4SelectBlocks * kQ4Block;
+constexpr int SLANES = 8;  // lanes per block's bounds, whose sums meet by moves within eight
+
+// The sums of a token's queries over its group, q- beside lo, then q+ beside hi, by the
+// first D threads.
+template <typename T, int D>
+__device__ __forceinline__ void sum_queries(const Q4SelectArgs& a, int b, int h, int t, double* sq) {
+  if (threadIdx.x >= D) return;
+  const T* q = static_cast<const T*>(a.q.p) + b * a.q.sb + (int64_t)h * a.G * a.q.sh + t * a.q.sr;
+  double neg = 0.0, pos = 0.0;
+  for (int g = 0; g < a.G; ++g) {
+    const double v = (double)elem<T>(q + g * a.q.sh, threadIdx.x);
+    if (!(v >= 0.0)) neg += v;  // (NaN here, and so in the score)
+    if (v > 0.0) pos += v;
+  }
+  sq[threadIdx.x] = neg;
+  sq[D + threadIdx.x] = pos;
 }
 
-constexpr int SLANES = 8;  // lanes per block's bounds, whose sums meet by moves within eight
+// A lane's share of blocks' scores: SLANES lanes to a block.
+template <int D>
+struct BlockScores {
+  static constexpr int W = 2 * D / 8 / SLANES;  // 16-byte words of bounds per lane
+  u32x4 x[W];
+  double q[W][8];
+  const uint16_t* bounds;  // the slice's
+  int nb, j;
+
+  __device__ __forceinline__ BlockScores(const Q4View& c, int64_t s)
+      : nb((c.n_max + kQ4Block - 1) / kQ4Block), j(threadIdx.x % SLANES) {
+    bounds = c.bounds + s * nb * 2 * D;
+  }
+  __device__ __forceinline__ void fetch(int block) {
+    const u32x4* p =
+        reinterpret_cast<const u32x4*>(bounds + (int64_t)(block < nb ? block : nb - 1) * 2 * D);
+#pragma unroll
+    for (int w = 0; w < W; ++w) x[w] = p[w * SLANES + j];
+  }
+  __device__ __forceinline__ void queries(const double* sq) {
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[w][i] = sq[(w * SLANES + j) * 8 + i];
+  }
+  // Scores of blocks k, k + step, .. up to `last` to `out`; block k's bounds are fetched.
+  __device__ __forceinline__ void run(int k, int step, int last, uint64_t* out) {
+    for (; k <= last; k += step) {
+      double sum = 0.0;
+#pragma unroll
+      for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sum += q[w][2 * i] * (double)__uint_as_float(x[w][i] << 16);
+          sum += q[w][2 * i + 1] * (double)__uint_as_float(x[w][i] & 0xffff0000u);
+        }
+      sum += lane_move<kSwapOnes>(sum);
+      sum += lane_move<kSwapTwos>(sum);
+      sum += lane_move<kMirror8>(sum);
+      if (j == 0) out[k] = score_key(sum);
+      fetch(k + step);
+    }
+  }
+};
 
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS) void q4_scores_kernel(Q4View c, Q4SelectArgs a) {
   const int64_t s = blockIdx.y;
   const int b = blockIdx.y / c.H, h = blockIdx.y % c.H;
   const int t = a.t0 + blockIdx.x % a.tn, part = blockIdx.x / a.tn;
-  const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
-  constexpr int W = 2 * D / 8 / SLANES;  // 16-byte words of bounds per lane
-  const int j = threadIdx.x % SLANES;
   const int step = (int)(gridDim.x / a.tn) * (THREADS / SLANES);
-  int k = part * (THREADS / SLANES) + threadIdx.x / SLANES;
-  u32x4 x[W];
-  auto fetch = [&](int block) __attribute__((always_inline)) {
-    const u32x4* p = reinterpret_cast<const u32x4*>(
-        c.bounds + (s * nb + (block < nb ? block : nb - 1)) * 2 * D);
-#pragma unroll
-    for (int w = 0; w < W; ++w) x[w] = p[w * SLANES + j];
-  };
-  fetch(k);  // (on its way while the queries are summed)
+  const int k = part * (THREADS / SLANES) + threadIdx.x / SLANES;
+  BlockScores<D> sc(c, s);
+  sc.fetch(k);  // (on its way while the queries are summed)
   const int last_row = q4_last_row(a.tok, b, t, c.n_max);
-  if (last_row < 0 || (a.grouped && q4_grouped(c, a, b, t))) return;
-  const int last = last_row / kQ4Block;
-  __shared__ double sq[2 * D];  // q- beside lo, then q+ beside hi
-  if (threadIdx.x < D) {
-    const T* q = static_cast<const T*>(a.q.p) + b * a.q.sb + (int64_t)h * a.G * a.q.sh + t * a.q.sr;
-    double neg = 0.0, pos = 0.0;
-    for (int g = 0; g < a.G; ++g) {
-      const double v = (double)elem<T>(q + g * a.q.sh, threadIdx.x);
-      if (!(v >= 0.0)) neg += v;  // (NaN here, and so in the score)
-      if (v > 0.0) pos += v;
-    }
-    sq[threadIdx.x] = neg;
-    sq[D + threadIdx.x] = pos;
-  }
+  if (last_row < 0) return;
+  __shared__ double sq[2 * D];
+  sum_queries<T, D>(a, b, h, t, sq);
   __syncthreads();
-  double q[W][8];
-#pragma unroll
-  for (int w = 0; w < W; ++w)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q[w][i] = sq[(w * SLANES + j) * 8 + i];
-  for (; k <= last; k += step) {
-    double sum = 0.0;
-#pragma unroll
-    for (int w = 0; w < W; ++w)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sum += q[w][2 * i] * (double)__uint_as_float(x[w][i] << 16);
-        sum += q[w][2 * i + 1] * (double)__uint_as_float(x[w][i] & 0xffff0000u);
-      }
-    sum += lane_move<kSwapOnes>(sum);
-    sum += lane_move<kSwapTwos>(sum);
-    sum += lane_move<kMirror8>(sum);
-    if (j == 0) a.scores[(s * a.tn + t - a.t0) * nb + k] = score_key(sum);
-    fetch(k + step);
-  }
+  sc.queries(sq);
+  sc.run(k, step, last_row / kQ4Block, a.scores + (s * a.tn + t - a.t0) * sc.nb);
 }
 
 // The n_sel best of a row's blocks, in order.  A workgroup of W waves holds the
@@ -278,17 +293,11 @@ __global__ __launch_bounds__(THREADS) void q4_scores_kernel(Q4View c, Q4SelectAr
 // the interval that it lies in, 512 W at a time (a step or two for scores that differ; for
 // the key's 64 bits 8 at most with one wave, 6 with four, 5 with 16).  Equal keys at the border: the lowest blocks.
 // (Halving the interval instead took 6 of 9.5 us for 32 rows of 2048 blocks.)
+// keys: the scores of the n blocks that are there; out: the token's list.
 template <int W, int KPL>
-__global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs a) {
-  const int64_t s = blockIdx.y;
-  const int b = blockIdx.y / c.H, t = a.t0 + blockIdx.x;
-  const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
-  if (a.grouped && q4_grouped(c, a, b, t)) return;
+__device__ __forceinline__ void pick_blocks(const Q4SelectArgs& a, const uint64_t* keys, int n,
+                                            int32_t* out) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-  int32_t* out = a.blocks + (s * a.tok.T + t) * a.n_sel;
-  const uint64_t* keys = a.scores + (s * a.tn + blockIdx.x) * nb;
-  const int lr = q4_last_row(a.tok, b, t, c.n_max);
-  const int n = lr < 0 ? 0 : lr / kQ4Block + 1;  // blocks that are there
   __shared__ int cnt[2][W];
   __shared__ uint64_t ends[2][W];
   // a wave's keys are its KPL runs of 64 blocks
@@ -422,6 +431,80 @@ __global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs 
   for (int i = want + (int)threadIdx.x; i < a.n_sel; i += 64 * W) out[i] = -1;
 }
 
+template <int W, int KPL>
+__global__ __launch_bounds__(64 * W) void q4_pick_kernel(Q4View c, Q4SelectArgs a) {
+  const int64_t s = blockIdx.y;
+  const int b = blockIdx.y / c.H, t = a.t0 + blockIdx.x;
+  const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  const int lr = q4_last_row(a.tok, b, t, c.n_max);
+  pick_blocks<W, KPL>(a, a.scores + (s * a.tn + blockIdx.x) * nb, lr < 0 ? 0 : lr / kQ4Block + 1,
+                      a.blocks + (s * a.tok.T + t) * a.n_sel);
+}
+
+// The tokens that launch_q4_select leaves: those of whose 16 one sees more blocks than LDS
+// holds.  A sequence's are the last ones of it, padding among their 16 included.
+struct TokenRange {
+  int first, end;
+};
+__device__ __forceinline__ TokenRange q4_left_tokens(const Q4View& c, const Q4Tokens& tok, int b) {
+  constexpr int64_t kRows = kQ4SelectBlocks * kQ4Block;
+  const int cnt = tok.count ? std::min(tok.count[b], tok.T) : tok.T;
+  if (cnt <= 0 || q4_last_row(tok, b, cnt - 1, c.n_max) < kRows) return {0, 0};
+  // the first 16 whose last token there, 16 g + 15 or cnt - 1, stands at kRows or behind
+  const int64_t upto = kRows - tok.at[b] + 1;  // tokens up to it (<= cnt)
+  return {upto <= 16 ? 0 : (int)((upto - 1) / 16 * 16), std::min((cnt + 15) / 16 * 16, tok.T)};
+}
+
+// Those tokens' selection in one launch, in float64: a workgroup takes a token and key head,
+// its scores to a slot of the workspace and the choice from there, then its next ones.  What
+// is left is counted here, so that a launch costs as little as there is left of it (8 key
+// heads, 4096 tokens at row 8192 of a cache of 262144: 293 us with the launch before it, 399
+// where scores and choices had launches over all tokens).  4096 tokens over 200000 rows: 4.15
+// ms, 512 over 1000000 2.3; d = 128.
+template <typename T, int D, int KPL>
+__global__ __launch_bounds__(1024) void q4_select_rest_kernel(Q4View c, Q4SelectArgs a) {
+  constexpr int W = 16;
+  __shared__ double sq[2 * D];
+  const int lane = threadIdx.x & 63;
+  const int nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  uint64_t* slot = a.scores + (int64_t)blockIdx.x * nb;
+  int64_t item = blockIdx.x;  // of the tokens x heads left, sequence by sequence, head by head
+  int64_t before = 0;         // items of the sequences before this lane's
+  for (int b0 = 0; b0 < c.B; b0 += 64) {  // 64 sequences at a time, one per lane
+    TokenRange mine = {0, 0};
+    if (b0 + lane < c.B) mine = q4_left_tokens(c, a.tok, b0 + lane);
+    const uint64_t upto = before + wave_scan<uint64_t>((uint64_t)(mine.end - mine.first) * c.H, 0ull,
+                                                       [](uint64_t x, uint64_t y) { return x + y; });
+    for (;; item += gridDim.x) {
+      const uint64_t past = __ballot(upto > (uint64_t)item);
+      if (!past) break;  // (the same in every wave)
+      const int l = __ffsll((unsigned long long)past) - 1;
+      const int first = __builtin_amdgcn_readlane(mine.first, l);
+      const int tokens = __builtin_amdgcn_readlane(mine.end, l) - first;
+      const int64_t end = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(upto >> 32), l) << 32 |
+                                    (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)upto, l));
+      const int64_t i = item - (end - (int64_t)tokens * c.H);  // of this sequence's
+      const int b = b0 + l, h = (int)(i / tokens), t = first + (int)(i % tokens);
+      const int64_t s = (int64_t)b * c.H + h;
+      const int lr = q4_last_row(a.tok, b, t, c.n_max);
+      if (lr >= 0) {
+        BlockScores<D> sc(c, s);
+        sc.fetch(threadIdx.x / SLANES);
+        sum_queries<T, D>(a, b, h, t, sq);
+        __syncthreads();
+        sc.queries(sq);
+        sc.run(threadIdx.x / SLANES, 64 * W / SLANES, lr / kQ4Block, slot);
+      }
+      __syncthreads();  // scores, and behind the last choice
+      pick_blocks<W, KPL>(a, slot, lr < 0 ? 0 : lr / kQ4Block + 1,
+                          a.blocks + (s * a.tok.T + t) * a.n_sel);
+      __syncthreads();  // the slot is read
+    }
+    before = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(upto >> 32), 63) << 32 |
+                       (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)upto, 63));
+  }
+}
+
 // Selection for several tokens of a slice in one launch.  A workgroup takes 16 tokens:
 // their scores of every block come from the bf16 matrix instructions, the queries'
 // float64 sums split into two bf16 parts (bounds are bf16), and stay in LDS.  Such a
@@ -549,7 +632,7 @@ __global__ __launch_bounds__(64 * SW, SW == 8 ? 6 : KPL > 8 ? 4 : 8) void q4_sel
   const int most = (int)wave_max((uint32_t)(
       (there ? q4_last_row(a.tok, b, t0 + m, c.n_max) : -1) + 1));
   const int blocks = (most + kQ4Block - 1) / kQ4Block;
-  if (blocks > kQ4SelectBlocks) return;  // (left to the other launches)
+  if (blocks > kQ4SelectBlocks) return;  // (left to q4_select_rest_kernel)
 
   // The tokens' sums in parts: [k-step, part, lane] 16-byte words, lane (m, g) token m's
   // channels of words 4 i + g.  The waves share the words.
@@ -757,6 +840,19 @@ hipError_t scores_d(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <typename T, int D>
+hipError_t rest_d(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
+  const int64_t nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+  const dim3 grid((uint32_t)q4_select_slots((int64_t)c.B * c.H, nb, a.tok.T));
+  if (nb <= 16 * 64 * 8)
+    q4_select_rest_kernel<T, D, 8><<<grid, 1024, 0, st>>>(c, a);
+  else if (nb <= 16 * 64 * 16)
+    q4_select_rest_kernel<T, D, 16><<<grid, 1024, 0, st>>>(c, a);
+  else
+    q4_select_rest_kernel<T, D, 32><<<grid, 1024, 0, st>>>(c, a);
+  return hipGetLastError();
+}
+
 template <int W, int KPL>
 hipError_t pick(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {
   const dim3 grid((uint32_t)a.tn, (uint32_t)(c.B * c.H));
@@ -819,6 +915,11 @@ hipError_t launch_q4_scores(int dtype, int64_t d, const Q4View& c, const Q4Selec
 hipError_t launch_q4_select(int dtype, int64_t d, const Q4View& c, const Q4SelectArgs& a,
                             hipStream_t st) {
   Q4_BY_D(select_d, c, a, st);
+}
+
+hipError_t launch_q4_select_rest(int dtype, int64_t d, const Q4View& c, const Q4SelectArgs& a,
+                                 hipStream_t st) {
+  Q4_BY_D(rest_d, c, a, st);
 }
 
 hipError_t launch_q4_pick(const Q4View& c, const Q4SelectArgs& a, hipStream_t st) {

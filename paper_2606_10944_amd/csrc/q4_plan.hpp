@@ -81,9 +81,7 @@ inline size_t q4_attention_bytes(int64_t B, int64_t H, int64_t tiles, int64_t sp
 }
 
 // Whether a selection takes 16 tokens at a time with their scores in LDS, and whether that
-// is all of it: tokens that see more blocks than LDS holds are left to the other launches.
-// (8 key heads, 4096 tokens at row 8192 of a cache of 262144: 1029 us without, 487 with:
-// launches whose workgroups find nothing left.)
+// is all of it: tokens that see more blocks than LDS holds are left to a second launch.
 constexpr int64_t kQ4SelectBlocks = 2048;  // 16 tokens' float32 scores: 128 KiB
 inline bool q4_select_grouped(int64_t slices, int64_t T) {
   return T > 1 && slices * ((T + 15) / 16) >= 64;
@@ -92,8 +90,16 @@ inline bool q4_select_fused(int64_t slices, int64_t blocks, int64_t T) {
   return blocks <= kQ4SelectBlocks && q4_select_grouped(slices, T);
 }
 
-// Tokens whose block scores a selection holds at a time: 64 MiB of them, at least one
-// token's.
+// Workgroups of that second launch, each with a slot for the scores of a token: two per
+// compute unit, 64 MiB of slots, at least one.
+inline int64_t q4_select_slots(int64_t slices, int64_t blocks, int64_t T) {
+  const int64_t hold = ((int64_t)64 << 20) / (blocks * 8), all = slices * T;
+  const int64_t n = hold < 512 ? hold : 512;
+  return n < 1 ? 1 : (n < all ? n : all);
+}
+
+// Tokens of few whose block scores a selection holds at a time: 64 MiB of them, at least
+// one token's.
 inline int64_t q4_select_tokens(int64_t slices, int64_t blocks, int64_t T) {
   const int64_t n = ((int64_t)64 << 20) / (slices * blocks * 8);
   return n < 1 ? 1 : (n < T ? n : T);

@@ -180,6 +180,31 @@ def test_select_border_in_the_last_bit(nb, d):
         check_select_head(c, q, at, n_sel, 1, 2, got, 0)
 
 
+def test_select_over_short_sequences_of_a_large_cache_takes_few_launches():
+    """Tokens that see few blocks cost no launches for the rows that the cache could hold."""
+    from paper_2606_10944_amd import LaunchTimer
+    g = gen(33)
+    H, T, d, n = 64, 600, 32, 140000
+    c = Q4Cache(1, H, n, d, device=DEV)
+    c.bounds.copy_(torch.randn(1, H, (n + 63) // 64, 2, d, generator=g).sort(-2)[0])
+    q = randn(g, 1, H, T, d, dtype="bf16")
+    st = torch.cuda.current_stream()
+    for at in (3000, 131072 - 300):  # none and half of the tokens see more than 2048 blocks
+        with LaunchTimer(st) as lt:
+            got = thin_q4_select(q.to(DEV), c, i32([at]), 9)
+        torch.cuda.synchronize()
+        assert len(lt.records()) <= 3
+        for h in (0, 63):
+            for t in (0, 299, 300, 301, 599):
+                check_select_head_token(c, q, at, 9, 1, 2, got, h, t)
+
+
+def check_select_head_token(c, q, at, n_sel, n_sinks, n_window, got, h, t):
+    G = q.shape[1] // c.H
+    sc = ref.block_scores(q[0, h * G:(h + 1) * G, t], c.bounds[0, h].cpu()).tolist()
+    assert got[0, h, t].tolist() == ref.select(sc, at + t, n_sel, n_sinks, n_window), (h, t)
+
+
 def test_selections_of_two_threads():
     """Prompts over a large and a small cache from two host threads: each has the LDS that
     its own scores need."""

@@ -1,0 +1,19 @@
+"""The 4-bit cache's limits without a GPU."""
+import ctypes as C
+
+import pytest
+
+from paper_2606_10944_amd import _lib
+
+
+@pytest.mark.parametrize("B,H,T", [(1, 64, 600), (1, 8, 1 << 20), (4, 8, 32), (65535, 1, 2)])
+def test_a_prompts_selection_needs_a_workspace_of_few_tokens(B, H, T):
+    """Scores in LDS need none; for caches of more rows, 64 MiB (or a token's) at most,
+    whatever the number of tokens."""
+    plan, n = _lib.lib().thin_q4_select_plan, C.c_size_t(0)
+    assert plan(B, H, 131072, T, C.byref(n)) == 0 and n.value == 0
+    for rows in (131073, 1 << 20, 1 << 21):
+        assert plan(B, H, rows, T, C.byref(n)) == 0
+        nb = -(-rows // 64)
+        assert n.value % (nb * 8) == 0 and 0 < n.value <= 64 << 20
+        assert n.value == min(512, (64 << 20) // (nb * 8), B * H * T) * nb * 8
