@@ -237,3 +237,21 @@ def test_selections_of_two_threads():
     for t in threads:
         t.join()
     assert not failed
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("B", [65, 130, 256])
+def test_attention_shares_of_more_sequences_than_lanes(dtype, B):
+    """Keys shared out to workgroups over up to four sequences per lane, with nothing and
+    long caches at the lanes' ends."""
+    g = gen(40)
+    n = 4200
+    lengths = torch.randint(0, n + 1, (B,), generator=g).tolist()
+    for i, x in zip((0, 62, 63, 64, 65, 126, 127, 128, 129, 191, 192, 254, 255),
+                    (n, 0, 0, n, 1, 0, 33, 0, n, 0, 0, 32, n)):
+        if i < B:
+            lengths[i] = x
+    c = filled(g, B, 1, n, 32, lengths)
+    q = randn(g, B, 3, 2, 32, dtype=dtype)
+    at = [x - 2 for x in lengths]
+    check_attention(c, q, at, None, None, thin_q4_attention(q.to(DEV), c, i32(at)), dtype)
