@@ -255,3 +255,30 @@ def test_attention_shares_of_more_sequences_than_lanes(dtype, B):
     q = randn(g, B, 3, 2, 32, dtype=dtype)
     at = [x - 2 for x in lengths]
     check_attention(c, q, at, None, None, thin_q4_attention(q.to(DEV), c, i32(at)), dtype)
+
+
+@pytest.mark.parametrize("n_out,g_", [(64, 1), (128, 0)])
+def test_cached_rows_are_thinned(n_out, g_):
+    """Rows of the cache, read back, thinned to a part of them and attended over: the
+    coreset is that of the same rows as plain tensors, and its attention the definition's."""
+    from paper_2606_10944_amd import thin_attention, thin_compress, thin_plan
+    g = gen(50)
+    H, n, d = 2, 512, 64
+    c = filled(g, 1, H, n, d, [n])
+    k, v = thin_q4_load(c, i32([0]), n)
+    plan = thin_plan(1, H, n, d, n_out, g_)
+    u = torch.rand(max(plan["uniforms_total"], 1), generator=g).to(DEV)
+    idx = thin_compress(k, v, n_out, g_, u)
+    rows = [x.cpu() for x in (k, v)]
+    assert torch.equal(idx, thin_compress(*[x.to(DEV) for x in rows], n_out, g_, u))
+    assert idx.shape[-1] == n_out < n
+    q = randn(g, 1, H, 3, d, dtype="bf16")
+    got = thin_attention(q.to(DEV), k, v, idx).cpu().double()
+    for h in range(H):
+        i = idx[0, h].cpu().long()
+        assert i.unique().numel() == n_out and 0 <= int(i.min()) and int(i.max()) < n
+        o, A, S = ref.attention(q[0, h], rows[0][0, h, i].double(), rows[1][0, h, i].double(),
+                                torch.ones(3, n_out, dtype=torch.float64))
+        # weights rounded to bf16 (half a step each) and float32 sums, as for the cache's
+        # own kernels; the output is float32
+        assert ((got[0, h] - o).abs() <= attention_bound(o, A, S, "bf16")).all()
