@@ -81,6 +81,18 @@ def _rows(t: torch.Tensor, dev: int, name: str):
     return p, _Strides(s[0], s[1], s[2])
 
 
+def _addressable(t: torch.Tensor, strides, name: str, output: bool = False) -> None:
+    """Refuses rows that the library would for their alignment or strides."""
+    word = 16 // t.element_size()
+    bad = t.data_ptr() % 16 != 0
+    if strides is not None:
+        bad = bad or any(n > 1 and (s % word != 0 or (output and s == 0))
+                         for n, s in zip(t.shape, strides))
+    if bad:
+        raise ThinError(THIN_EINVAL, f"{name}: rows must be 16-byte aligned"
+                                     f"{' and apart' if output else ''}")
+
+
 def _ints(t: Optional[torch.Tensor], shape, dev: int, name: str):
     if t is None:
         return None
@@ -229,7 +241,9 @@ class Q4Cache:
              n_window: int = 2, O: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Outputs O [B,q_heads,T,d] of T new tokens per sequence at positions
         at[b] + t: queries Q [B,q_heads,T,d], rows K, V [B,H,T,d].  With n_sel they
-        attend to n_sel blocks of 64 rows (thin_q4_select), else to every row."""
+        attend to n_sel blocks of 64 rows (thin_q4_select), else to every row.  A step
+        that is refused has stored nothing."""
+        self._check_step(Q, n_sel, n_sinks, n_window, O, _where(stream)[0])
         if turns is not None:
             Q, K = thin_rotary(Q, at, turns, Y=K, layout=layout, amp=amp, stream=stream)
         thin_q4_store(K, V, self, at, count=count, stream=stream)
@@ -238,6 +252,21 @@ class Q4Cache:
             blocks = thin_q4_select(Q, self, at, n_sel, n_sinks=n_sinks, n_window=n_window,
                                     count=count, stream=stream)
         return thin_q4_attention(Q, self, at, count=count, blocks=blocks, O=O, stream=stream)
+
+
+    def _check_step(self, Q, n_sel, n_sinks, n_window, O, dev: int) -> None:
+        """Refuses what the selection or attention of a step would, before its rows are
+        stored."""
+        self._at(dev)
+        _, qs, Hq, T = _queries(Q, self, dev)
+        _dtype(Q, "Q")
+        _addressable(Q, qs, "Q")
+        if n_sel and not (0 <= n_sinks and 1 <= n_window and n_sinks + n_window <= n_sel <= 32768):
+            raise ThinError(THIN_EINVAL, "n_sinks >= 0, n_window >= 1 and n_sinks + n_window <= "
+                                         "n_sel <= 32768")
+        _attention_bytes(self.B, self.H, Hq, self.n_max, self.d, T, n_sel)
+        if O is not None:
+            _addressable(O, _output(O, Q, dev)[1], "O", output=True)
 
 
 def thin_q4_store(K: torch.Tensor, V: torch.Tensor, cache: Q4Cache, at: torch.Tensor, *,
@@ -302,6 +331,12 @@ def _queries(Q: torch.Tensor, cache: Q4Cache, dev: int):
     return q, qs, Hq, T
 
 
+def _output(O: torch.Tensor, Q: torch.Tensor, dev: int):
+    if O.shape != Q.shape or O.dtype != Q.dtype:
+        raise ThinError(THIN_EINVAL, "O must match Q")
+    return _rows(O, dev, "O")
+
+
 def thin_q4_select(Q: torch.Tensor, cache: Q4Cache, at: torch.Tensor, n_sel: int, *,
                    n_sinks: int = 1, n_window: int = 2, count: Optional[torch.Tensor] = None,
                    blocks: Optional[torch.Tensor] = None,
@@ -348,9 +383,7 @@ def thin_q4_attention(Q: torch.Tensor, cache: Q4Cache, at: torch.Tensor, *,
         O = _empty_like(Q, dev, stream)
         o, os_ = O.data_ptr(), None
     else:
-        if O.shape != Q.shape or O.dtype != Q.dtype:
-            raise ThinError(THIN_EINVAL, "O must match Q")
-        o, os_ = _rows(O, dev, "O")
+        o, os_ = _output(O, Q, dev)
     ws, wp, wn = _workspace(workspace, need, dev, stream)
     _check(lib().thin_q4_attention(ref, q, qs, Hq, _dtype(Q, "Q"), T, _ints(at, (B,), dev, "at"),
                                    _ints(count, (B,), dev, "count"), bp, n_sel, o, os_, wp, wn,

@@ -282,3 +282,28 @@ def test_cached_rows_are_thinned(n_out, g_):
         # weights rounded to bf16 (half a step each) and float32 sums, as for the cache's
         # own kernels; the output is float32
         assert ((got[0, h] - o).abs() <= attention_bound(o, A, S, "bf16")).all()
+
+
+def test_a_refused_step_stores_nothing():
+    """Arguments that attention or the selection would refuse are refused before the rows
+    are stored."""
+    from paper_2606_10944_amd._lib import ThinError
+    g = gen(60)
+    c = filled(g, 2, 2, 300, 64, [100, 100])
+    names = ("k_codes", "k_scales", "v_codes", "v_scales", "bounds")
+    before = [getattr(c, x).clone() for x in names]
+    q, k, v = (randn(g, 2, n, 3, 64, dtype="bf16").to(DEV) for n in (4, 2, 2))
+    at = i32([100, 100])
+    bad_q = [q[:, :3].contiguous(), q[:1], q[..., :32], q.half(), q.cpu()]
+    bad = [dict(n_sel=2), dict(n_sel=-1), dict(n_sel=40000), dict(n_sel=5, n_sinks=4),
+           dict(n_sel=5, n_window=0), dict(O=q.float()), dict(O=q[:1]), dict(O=q.cpu()),
+           dict(O=q[:, :1].expand(2, 4, 3, 64))]
+    wide = torch.zeros(2, 4, 3, 72, dtype=torch.bfloat16, device=DEV)
+    bad_q.append(wide[..., 4:68])  # not 16-byte aligned
+    bad.append(dict(O=wide[..., 4:68]))
+    for a in [(x, {}) for x in bad_q] + [(q, x) for x in bad]:
+        with pytest.raises(ThinError):
+            c.step(a[0], k, v, at, **a[1])
+        assert all(torch.equal(getattr(c, x), was) for x, was in zip(names, before)), a[1]
+    c.step(q, k, v, at, n_sel=3)
+    assert not torch.equal(c.k_codes, before[0])
