@@ -401,7 +401,7 @@ int thin_express_prefill(int32_t dtype, int64_t B, int64_t H, int64_t n, int64_t
  *   pos       (device) int32: the rows' positions [B, T] (pos_per_token != 0),
  *             or [B], the first row's, the others following it.
  *   turns     (device) float64 [rot/2]: turns per position of every pair.
- *   amp       finite.
+ *   amp       finite, as a float32 too.
  * Angles are formed in float64 and reduced to one turn before cos and sin; rows
  * are turned in float32 and rounded once.  B * T <= 2^27.
  * Errors: THIN_EINVAL, THIN_EDTYPE, THIN_EHIP.

@@ -112,7 +112,7 @@ int thin_rotary(const void* X, const int64_t* x_strides, int64_t x_heads, void* 
   if (rot < 16 || rot > d || rot % 16 != 0) return THIN_EINVAL;
   if (layout != THIN_ROTARY_HALF && layout != THIN_ROTARY_INTERLEAVED) return THIN_EINVAL;
   if (x_heads < 1 || x_heads > kMaxSlices || !valid_ints(pos, nullptr) ||
-      !turns || !aligned(turns, 8) || !isfinite(amp))
+      !turns || !aligned(turns, 8) || !isfinite((float)amp))
     return THIN_EINVAL;
   if (Y ? (y_heads < 1 || y_heads > kMaxSlices) : (y_heads != 0 || Y_out)) return THIN_EINVAL;
   thin::RotaryArgs a{};

@@ -17,3 +17,14 @@ def test_a_prompts_selection_needs_a_workspace_of_few_tokens(B, H, T):
         nb = -(-rows // 64)
         assert n.value % (nb * 8) == 0 and 0 < n.value <= 64 << 20
         assert n.value == min(512, (64 << 20) // (nb * 8), B * H * T) * nb * 8
+
+
+FAKE = C.c_void_p(0x10000)  # never dereferenced: every call below fails validation
+
+
+@pytest.mark.parametrize("amp", [3.5e38, -1e39, 1e300])
+def test_rotary_refuses_factors_that_are_no_float32(amp):
+    """Rows are turned in float32: such a factor would be infinite there."""
+    rc = _lib.lib().thin_rotary(FAKE, None, 4, FAKE, None, None, None, 0, None, None, 1, 2, 3, 64,
+                                32, 0, FAKE, 0, FAKE, amp, 0, None)
+    assert rc == _lib.THIN_EINVAL
