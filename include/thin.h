@@ -426,8 +426,8 @@ int thin_rotary(const void* X, const int64_t* x_strides, int64_t x_heads, void* 
  *                       `slow` times have it divided by factor, a linear mix
  *                       between; *amp = 0.1 ln(factor) + 1 (else 1).
  * Host-only.  turns (host) float64 [rot/2], amp (host).  THIN_EINVAL: null
- * pointers, rot not an even number >= 2 (>= 4 for BASE), base <= 1, factor < 1,
- * and for BANDS length <= 0 or slow >= fast.
+ * pointers, rot not an even number >= 2 (>= 4 for BASE), base <= 1 or (for BASE,
+ * after its rule) infinite, factor < 1, and for BANDS length <= 0 or slow >= fast.
  */
 typedef enum {
   THIN_ROTARY_PLAIN = 0,

@@ -149,6 +149,7 @@ int thin_rotary_turns(int64_t rot, double base, int32_t scaling, double factor, 
       (!(length > 0.0) || !isfinite(length) || !(slow < fast) || !isfinite(slow) || !isfinite(fast)))
     return THIN_EINVAL;
   if (scaling == THIN_ROTARY_BASE) base *= pow(factor, (double)rot / (double)(rot - 2));
+  if (!isfinite(base)) return THIN_EINVAL;
   for (int64_t i = 0; i < rot / 2; ++i) {
     double f = pow(base, -2.0 * (double)i / (double)rot) / (2.0 * M_PI);
     if (scaling == THIN_ROTARY_LINEAR) f /= factor;

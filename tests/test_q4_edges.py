@@ -28,3 +28,12 @@ def test_rotary_refuses_factors_that_are_no_float32(amp):
     rc = _lib.lib().thin_rotary(FAKE, None, 4, FAKE, None, None, None, 0, None, None, 1, 2, 3, 64,
                                 32, 0, FAKE, 0, FAKE, amp, 0, None)
     assert rc == _lib.THIN_EINVAL
+
+
+def test_turns_refuse_a_base_that_overflows():
+    """base * factor^(rot / (rot - 2)) past the float64 numbers has no table."""
+    t, a = (C.c_double * 64)(), C.c_double(0)
+    turns = _lib.lib().thin_rotary_turns
+    assert turns(64, 1e300, 2, 1e200, 0.0, 1.0, 32.0, t, C.byref(a)) == _lib.THIN_EINVAL
+    assert turns(4, 1e4, 2, 1e160, 0.0, 1.0, 32.0, t, C.byref(a)) == _lib.THIN_EINVAL
+    assert turns(64, 1e4, 2, 1e200, 0.0, 1.0, 32.0, t, C.byref(a)) == 0
