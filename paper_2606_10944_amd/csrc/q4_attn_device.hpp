@@ -93,7 +93,6 @@ __device__ __forceinline__ Slice slice_of(const Q4View& c, int64_t s) {
 template <typename T, int D>
 struct Queries {
   static constexpr int KS = D / 32, QP = Elem<T>::bytes == 2 ? 1 : 3;
-  static constexpr int N = QP * KS;  // matrix instructions for 16 keys
   bf16x8_t q[QP][KS];
   // row: this lane's query row (null: zeros); g: lane / 16
   __device__ __forceinline__ void load(const T* row, int g) {

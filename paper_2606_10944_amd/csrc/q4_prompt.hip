@@ -22,16 +22,6 @@ namespace {
 constexpr int PW = 4;    // waves
 constexpr int PK = 64;   // cached rows per tile
 
-// The schedule of a region: N times a matrix instruction, then V vector ones.
-template <int N, int V>
-__device__ __forceinline__ void interleave() {
-  if constexpr (N > 0) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
-    interleave<N - 1, V>();
-  }
-}
-
 // SPLIT: workgroups share a tile's keys and leave sums for the join.
 template <typename T, int D, int RT, bool SPLIT>
 __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnArgs a) {
@@ -198,9 +188,8 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
           for (int dt = 0; dt < D / 16; ++dt) acc[rt][dt] *= scale;
         }
       }
-      // The next tile's scores among this one's exponentials, a matrix instruction to every
-      // few of them; and whichever wave of a SIMD has products to issue goes first (754 ->
-      // 732 us by the order alone, 710 by the priority alone, 685 by both).
+      // The next tile's scores among this one's exponentials, and whichever wave of a SIMD has
+      // products to issue goes first (852 -> 800 us by the priority).
       __builtin_amdgcn_s_setprio(1);
       __builtin_amdgcn_sched_barrier(0);
       score(i ^ 1, ns);
@@ -213,9 +202,6 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
 #pragma unroll
         for (int ch = 0; ch < PK / 32; ++ch) split8<NP>(s[rt] + ch * 8, pp[rt][ch]);
       }
-      // matrix instructions of the scores, and vector ones for each: weights, keys decoded
-      constexpr int NS = PK / 16 * RT * Queries<T, D>::N;
-      interleave<NS, std::max(1, (RT * (PK / 4) * 7 / 2 + PK / 16 * KW * 4) / NS)>();
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int ch = 0; ch < PK / 32; ++ch) {
