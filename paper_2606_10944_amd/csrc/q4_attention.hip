@@ -179,8 +179,11 @@ struct Shares {
 
 // WV waves.  Without splits a workgroup takes a tile's whole keys; with them
 // workgroups share the keys and leave sums in a.part, one slot of existing rows each.
+// (bf16 lists: 128 registers hold four workgroups in a compute unit, 128 -> 123 us for 32
+// blocks of each of 509 tokens; over all rows they cost 64 -> 66 us for long caches.)
 template <typename T, int D, bool LIST, int WV>
-__global__ __launch_bounds__(64 * WV, 2) void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
+__global__ __launch_bounds__(64 * WV, Elem<T>::bytes == 2 && LIST && WV == 4 ? 4 : 2)
+void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
   // bf16 parts of the weights.  (bf16, two: 17 bits, while the sum of the weights is that of
   // the unrounded ones.  One would save nothing in one token's calls, 128 -> 115 us for 32
   // blocks of each of 509 tokens.)
