@@ -424,7 +424,9 @@ int thin_rotary(const void* X, const int64_t* x_strides, int64_t x_heads, void* 
  *   THIN_ROTARY_BANDS   pairs that turn at least `fast` times in `length`
  *                       positions keep their frequency, those that turn at most
  *                       `slow` times have it divided by factor, a linear mix
- *                       between; *amp = 0.1 ln(factor) + 1 (else 1).
+ *                       between; *amp = 0.1 ln(factor) + 1 (else 1).  A model that
+ *                       was trained with these bands and no factor takes the
+ *                       turns and 1 for amp.
  * Host-only.  turns (host) float64 [rot/2], amp (host).  THIN_EINVAL: null
  * pointers, rot not an even number >= 2 (>= 4 for BASE), base <= 1 or (for BASE,
  * after its rule) infinite, factor < 1, and for BANDS length <= 0 or slow >= fast.
@@ -443,7 +445,8 @@ int thin_rotary_turns(int64_t rot, double base, int32_t scaling, double factor, 
  * host memory, read during a call only).  A row's d channels are d/32 groups of
  * 32; a group is 32 codes of 4 bits (channel 2i in the low half of byte i: sign,
  * two exponent bits, one mantissa bit, i.e. +-{0, .5, 1, 1.5, 2, 3, 4, 6}) and one
- * scale byte s that stands for 2^(s-127).  Rows of keys and values are stored
+ * scale byte s that stands for 2^(s-127), 2 <= s <= 252 (as thin_q4_store writes
+ * it).  Rows of keys and values are stored
  * after any rotary turn.
  *   bounds  the least, then the largest stored key value of every channel over
  *           each block of THIN_Q4_BLOCK rows (the rows stored so far).

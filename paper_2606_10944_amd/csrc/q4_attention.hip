@@ -4,13 +4,13 @@
 // The kernel for few query rows: a wave takes 32 keys at a time on its own, its
 // decoded value rows in LDS, the next step's codes on their way meanwhile.
 //
-// d = 128, bf16, 8 key heads.  8 sequences of 3000 to 65536 rows, one token: 50 us for 298
-// MB, 6.0 TB/s (a stream of reads reaches 6.5), then 5 us for the join of the shared
-// tiles.  64 of 2048 blocks for 8 sequences: 11.5 + 4 us for 36 MB, latencies (a launch,
+// d = 128, bf16, 8 key heads.  8 sequences of 3000 to 65536 rows, one token: 51 us for 298
+// MB, 5.8 TB/s (a stream of reads reaches 6.5), then 5 us for the join of the shared
+// tiles.  64 of 2048 blocks for 8 sequences: 12 + 4 us for 36 MB, latencies (a launch,
 // positions, lists, codes, four steps per wave, the join's three loads in turn).  32
-// blocks for each of 509 tokens: 103 us, LDS: writing 32 decoded value rows costs a
-// compute unit 128 cycles (64 bytes each) and reading them transposed 53, of the 240 that
-// a step takes.
+// blocks for each of 509 tokens: 123 us; the vector ALU is busy two thirds of it, the
+// matrix cores a third, and of the 290 cycles that a step takes a compute unit, writing 32
+// decoded value rows to LDS costs 128 (64 bytes each) and reading them transposed 53.
 #include "q4_attn_device.hpp"
 
 namespace thin {
@@ -20,7 +20,7 @@ namespace {
 constexpr int CH = kQ4Step;
 
 // Buffers of codes of a wave: the step in work and the next (three cost registers: 8
-// sequences of up to 65536 rows 66.6 -> 68.0 us, a prompt's 1497 -> 1668).
+// sequences of up to 65536 rows 64.5 -> 66.6 us, 64 of 2048 blocks 15.6 -> 17.4).
 constexpr int PF = 2;
 
 // One wave's step: the codes of 32 keys and values.
@@ -185,8 +185,8 @@ template <typename T, int D, bool LIST, int WV>
 __global__ __launch_bounds__(64 * WV, Elem<T>::bytes == 2 && LIST && WV == 4 ? 4 : 2)
 void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
   // bf16 parts of the weights.  (bf16, two: 17 bits, while the sum of the weights is that of
-  // the unrounded ones.  One would save nothing in one token's calls, 128 -> 115 us for 32
-  // blocks of each of 509 tokens.)
+  // the unrounded ones.  One would save 1 % of one token's calls, 123 -> 110 us for 32 blocks
+  // of each of 509 tokens.)
   constexpr int NP = Elem<T>::bytes == 2 ? 2 : 3;
   using C = Codes<D>;
   __shared__ __align__(16) unsigned char lds[WV * CH * kVStride<D>];

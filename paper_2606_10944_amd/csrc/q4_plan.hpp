@@ -29,25 +29,29 @@ struct Q4AttnShape {
 
 // Few query rows per slice.  A tile's keys go to one workgroup, without a second launch to
 // join sums, up to 2048 keys, and up to 4096 where there are workgroups for most compute
-// units (d = 128, 4000 rows, one token: 256 workgroups, bf16 25.4 us against 29.5 shared
-// out, 21.6 against 23.6 with lengths of 10 to 4000; 160: 20.9, 22.7 and 20.6, 20.2; 128:
-// 20.5, 20.3 and 20.3, 17.2).  A compute unit holds one workgroup of eight waves of float32
+// units (d = 128, 4000 rows, one token: 256 workgroups, bf16 25.8 us against 30.0 shared
+// out, 22.4 against 23.7 with lengths of 10 to 4000; 160: 22.4, 23.4 and 20.4, 18.8; 128:
+// 22.4, 20.7 and 19.7, 17.1).  A compute unit holds one workgroup of eight waves of float32
 // rows of 128 (their registers), two of others: four waves where there are more (d = 128,
-// 384 workgroups over 1024 rows: float32 25.0 us with eight, 19.8 with four, bf16 15.0,
-// 14.5; over 2000 rows 35.2, 29.3 and 23.1, 21.6; d = 64, 320 over lists of 32 blocks: 13.6,
-// 14.9).
+// 384 workgroups over 1024 rows: float32 22.2 us with eight, 17.7 with four, bf16 18.6,
+// 15.0; over 2000 rows 32.4, 27.8 and 27.2, 23.1; d = 64, 320 over lists of 32 blocks: 15.6,
+// 16.6).
 // Longer keys are shared out to two workgroups of four waves per compute unit (512; 8
-// sequences of 3000 to 65536 rows, 8 key heads, d = 128, bf16: 67 us, against 85 with 256,
-// 68 with 768, 84 with 1024, the last of them run alone), those of more slices in two, so
-// that one long sequence among short ones is not left to one workgroup per head.
+// sequences of 3000 to 55000 rows, 8 key heads, d = 128, bf16: 43.7 us, against 51.6 with
+// 256, 45.9 with 768, 49.7 with 1024, the last of them run alone), those of more slices in
+// two, so that one long sequence among short ones is not left to one workgroup per head.
+// Beyond 1024 tiles, several for every compute unit, or kQ4SharedEntries sequences, four of
+// them per lane of the wave that shares them out, every tile has one workgroup (160 sequences
+// x 8 heads of 3000 to 65536 rows: 1155 us, against 1084 in two; all of 65536: 1872, 1895; of
+// 500 to 16000: 292, 287; 300 x 2 of 500 to 16000: 146, 4.6 TB/s).
 //
 // Many query rows.  The kernel that shares decoded rows pays where each compute unit has a
 // workgroup of it (16 sequences x 8 heads x 1024 rows, 256 query rows a head, 256
-// workgroups: 32 us against 42; 128 query rows, 128 workgroups: 29 against 25), or where its
-// keys are shared out.  Tiles of 16 of 8 key heads, bf16: 192 over 40000 rows 68 us against
-// 141, over 16000 42 and 64, over 4500 29 and 28; 128 over 16000 36 and 39, over 4500 27 and
-// 22, 64 over 16384 28 and 24.  Up to 4096 rows one workgroup per tile is quicker for longer:
-// 512 tiles over 4000 rows 35 against 39, 1024 57 against 51.
+// workgroups: 32 us against 43; 128 query rows, 128 workgroups: 29 against 24), or where its
+// keys are shared out.  Tiles of 16 of 8 key heads, bf16: 192 over 40000 rows 75 us against
+// 165, over 16000 44 and 73, over 4500 30 and 31; 128 over 16000 38 and 45, over 4500 28 and
+// 24, 64 over 16384 31 and 30.  Up to 4096 rows one workgroup per tile is quicker for longer:
+// 512 tiles over 4000 rows 39 against 41, 1024 65 against 54.
 inline Q4AttnShape q4_attention_shape(int64_t B, int64_t H, int64_t G, int64_t T, bool list,
                                       int64_t keys, int64_t d, bool bf16) {
   const int64_t groups = B * H * q4_row_tiles(G, T, list);

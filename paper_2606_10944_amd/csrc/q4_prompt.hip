@@ -8,11 +8,11 @@
 // once per 64 RT query rows instead of once per 16, and each operand read from LDS
 // serves RT products.
 //
-// 4096 tokens over 16384 rows, 32 heads of 128 channels, 8 key heads, bf16: 685-709 us,
-// 1.36-1.40 PFLOP/s (a library bf16 product of 8192^3 runs at 1.20).  The matrix cores alone
-// need 410 us of it (16 scaled instructions of 32 cycles and 36 of 16 per wave and tile),
-// the vector ALU 360; without the reads of the values' columns it takes 140 us less, without
-// the exponentials 120, without decoding 85.
+// 4096 tokens over 16384 rows, 32 heads of 128 channels, 8 key heads, bf16: 800 us (842 on
+// another card), 1.20 PFLOP/s, as a library bf16 product of 8192^3; float32 2.0 ms, three
+// products for one.  The matrix cores alone need 410 us of the bf16 call (68 instructions of 16
+// cycles per wave and tile), the vector ALU 475; without the reads of the values' columns it
+// takes 49 us less, without the exponentials 59, without decoding the keys 16.
 #include "q4_attn_device.hpp"
 
 namespace thin {

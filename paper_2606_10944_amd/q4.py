@@ -2,7 +2,9 @@
 and the thin_q4_* calls of include/thin.h (argument marshalling only).
 
 Tensors and the given stream live on the current device; rows are [B, heads,
-T, d] tensors of any strides with contiguous channels, 16-byte aligned.
+T, d] tensors of any strides with contiguous channels, 16-byte aligned.  No call
+is recorded by autograd, whatever its inputs require: outputs are detached.  The
+gradient of a turn is thin_rotary(..., inverse=True) of the gradient.
 """
 from __future__ import annotations
 
@@ -118,7 +120,9 @@ def thin_rotary_turns(rot: int, *, base: float = 10000.0, scaling: str = "none",
     """(turns, amp) of thin_rotary for a head whose first `rot` channels turn:
     base^(-2i/rot) / 2 pi turns per position (a float64 CPU tensor [rot/2]),
     stretched for contexts `factor` times as long as `length` by one of the rules
-    "linear", "base" and "bands" (thin_rotary_turns in include/thin.h)."""
+    "linear", "base" and "bands" (thin_rotary_turns in include/thin.h).  amp is
+    0.1 ln(factor) + 1 with "bands", else 1; models trained with the bands but
+    without that factor pass amp=1."""
     if scaling not in SCALING:
         raise ThinError(THIN_EINVAL, f"unknown scaling {scaling!r}")
     turns = torch.empty(max(int(rot) // 2, 1), dtype=torch.float64)
@@ -134,7 +138,8 @@ def thin_rotary(X: torch.Tensor, pos: torch.Tensor, turns: torch.Tensor, *,
                 out_Y: Optional[torch.Tensor] = None, stream=None):
     """Rows X [B,heads,T,d], and Y [B,heads',T,d] in the same launch, turned by
     their positions: pos int32 [B,T], or [B], the first row's.  turns float64
-    [rot/2] on the device.  inverse=True turns back (the gradient of the turn).
+    [rot/2] on the device.  inverse=True turns back: of an output's gradient, the
+    gradient of the rows (autograd does not record the call).
     out / out_Y may be X / Y themselves.  Returns out, or (out, out_Y) with Y."""
     dev, st = _where(stream)
     lay = LAYOUT.get(layout)
