@@ -415,6 +415,23 @@ int thin_rotary(const void* X, const int64_t* x_strides, int64_t x_heads, void* 
                 void* stream);
 
 /*
+ * thin_rotary with several positions per token (time, height and width of image
+ * and video tokens): pair i turns by a = 2 pi pos[b, t, axis[i]] turns[i].
+ *   pos       (device) int32 [B, T, axes], 1 <= axes <= THIN_ROTARY_MAX_AXES.
+ *   axis      (device) int32 [rot/2]: every pair's axis, in runs, in turn or in any
+ *             other order; an entry outside [0, axes) leaves its pair at position 0.
+ * Other arguments, limits and errors as thin_rotary.  With axes = 1 and axis all 0 the
+ * result is thin_rotary's for pos_per_token.
+ */
+#define THIN_ROTARY_MAX_AXES 4
+int thin_rotary_axes(const void* X, const int64_t* x_strides, int64_t x_heads, void* X_out,
+                     const int64_t* x_out_strides, const void* Y, const int64_t* y_strides,
+                     int64_t y_heads, void* Y_out, const int64_t* y_out_strides, int32_t dtype,
+                     int64_t B, int64_t T, int64_t d, int64_t rot, int32_t layout,
+                     const int32_t* pos, int32_t axes, const int32_t* axis, const double* turns,
+                     double amp, int32_t inverse, void* stream);
+
+/*
  * The table of thin_rotary: turns[i] = base^(-2i/rot) / (2 pi), i < rot/2, for
  * contexts `factor` times as long as `length` positions by one of these rules,
  *   THIN_ROTARY_PLAIN   no change (factor and length are ignored),
@@ -548,6 +565,59 @@ int thin_q4_attention(const thin_q4_cache_t* cache, const void* Q, const int64_t
                       void* stream);
 
 /*
+ * Trees of drafted tokens (speculative decoding): T <= THIN_Q4_MAX_DRAFTS drafts per
+ * sequence, draft t in cached row at[b] + t whatever its depth.  Which drafts a draft
+ * attends to is a mask of words = ceil(T/64) words of 64 bits: bit j % 64 of word j / 64 is
+ * draft j.  A step is thin_q4_tree (masks and positions), thin_rotary by these positions,
+ * thin_q4_store, thin_q4_tree_attention, and once the drafts are judged, thin_q4_keep.
+ */
+#define THIN_Q4_MAX_DRAFTS 1024
+
+/*
+ * Masks and positions of trees:
+ *   parents (device) int32 [B, T]: every draft's parent, an earlier draft; an entry that is
+ *           none (negative, or not below t) makes its draft a root.
+ *   at      (device) int32 [B]: the rows before the drafts.
+ *   seen    (device) uint64 [B, T, words]: the draft itself and its ancestors; bits from T on
+ *           are 0.
+ *   pos     (device) int32 [B, T]: at[b] + the draft's depth (roots: 0).
+ * B <= 65535.  Errors: THIN_EINVAL, THIN_EHIP.
+ */
+int thin_q4_tree(const int32_t* parents, const int32_t* at, int64_t B, int64_t T, uint64_t* seen,
+                 int32_t* pos, void* stream);
+
+/*
+ * Attention of drafts over the cache: draft t of entry b attends to the cached rows 0 ..
+ * at[b] - 1 and to row at[b] + j of every draft j < count[b] whose bit of seen[b, t] is set
+ * (its own row only if its own bit is).  Any mask is legal, not only those of thin_q4_tree:
+ * drafts that see each other both ways, or nothing.
+ *   seen    (device) uint64 [B, T, words].
+ * Rows outside the cache are not there; a draft that sees no row, or is padding, has an output
+ * row of zeros.  Everything else (types, limits, sums, workspace: thin_q4_attention_plan with
+ * n_sel = 0, errors) as thin_q4_attention; T <= THIN_Q4_MAX_DRAFTS.
+ */
+int thin_q4_tree_attention(const thin_q4_cache_t* cache, const void* Q, const int64_t* q_strides,
+                           int64_t q_heads, int32_t dtype, int64_t T, const int32_t* at,
+                           const int32_t* count, const uint64_t* seen, void* O,
+                           const int64_t* o_strides, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/*
+ * Keep an accepted path of drafts: row at[b] + i of every key head becomes what row
+ * at[b] + path[b, i] held before the call (any order; a draft may be named twice), keys and
+ * values, and the bounds of the blocks that hold rows at[b] - 1 .. are formed anew over the rows
+ * up to the last one kept, as a store of these rows forms them.
+ *   path    (device) int32 [B, P], 1 <= P <= THIN_Q4_MAX_DRAFTS.  The first entry that is
+ *           negative, or whose row or new place lies outside the cache, ends the path (at[b] <
+ *           0: at once).
+ *   end     (device) int32 [B]: at[b] + the number of rows kept, where the next tokens go.  It
+ *           overlaps neither at nor path.
+ * Rows behind the last one kept hold what they held.  Errors: THIN_EINVAL, THIN_EHIP.
+ */
+int thin_q4_keep(const thin_q4_cache_t* cache, const int32_t* at, const int32_t* path, int64_t P,
+                 int32_t* end, void* stream);
+
+/*
  * Diagnostic: out[m*16 + n] = <rows[m], rows[16 + n]> for m, n < 16, computed
  * through the MFMA row-fragment path the pair-score kernel uses.
  *   rows (device) [32, d] of `dtype`;  out (device) float32 [16, 16].
@@ -572,7 +642,7 @@ int thin_workspace_status(const void* workspace, int32_t* status, void* stream);
  * from it).  While a hook is set,
  * every kernel launch made by thin_compress, thin_compress_traced,
  * thin_compress_ex, thin_attention, thin_attention_ex, thin_express_step,
- * thin_rotary and the thin_q4_* calls is bracketed by two calls on the
+ * thin_rotary, thin_rotary_axes and the thin_q4_* calls is bracketed by two calls on the
  * calling thread:
  * hook(ctx, kernel, round, 0, stream) right before the launch is enqueued and
  * hook(ctx, kernel, round, 1, stream) right after.  The hook may enqueue
@@ -606,7 +676,9 @@ typedef enum {
   THIN_KERNEL_Q4_STORE = 13,   /* rows into the 4-bit cache               */
   THIN_KERNEL_Q4_LOAD = 14,    /* rows of the 4-bit cache                 */
   THIN_KERNEL_Q4_SELECT = 15,  /* block scores and choice                 */
-  THIN_KERNEL_Q4_ATTENTION = 16 /* attention over the 4-bit cache, joins  */
+  THIN_KERNEL_Q4_ATTENTION = 16, /* attention over the 4-bit cache, joins */
+  THIN_KERNEL_Q4_TREE = 17,    /* masks and positions of drafts           */
+  THIN_KERNEL_Q4_KEEP = 18     /* accepted drafts' rows                   */
 } thin_kernel_t;
 typedef void (*thin_launch_hook_t)(void* ctx, int32_t kernel, int32_t round, int32_t phase,
                                    void* stream);

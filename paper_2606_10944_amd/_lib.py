@@ -26,16 +26,17 @@ EXPORTS = ("thin_plan", "thin_compress", "thin_compress_static", "thin_compress_
            "thin_attention_ex", "thin_express_plan", "thin_express_create", "thin_express_step",
            "thin_express_cache", "thin_express_next", "thin_express_destroy",
            "thin_express_prefill_plan", "thin_express_prefill",
-           "thin_rotary", "thin_rotary_turns", "thin_q4_store", "thin_q4_load",
+           "thin_rotary", "thin_rotary_axes", "thin_rotary_turns", "thin_q4_store", "thin_q4_load",
            "thin_q4_select_plan", "thin_q4_select", "thin_q4_attention_plan",
-           "thin_q4_attention", "thin_selftest_gram16", "thin_status_str",
+           "thin_q4_attention", "thin_q4_tree", "thin_q4_tree_attention", "thin_q4_keep",
+           "thin_selftest_gram16", "thin_status_str",
            "thin_workspace_status", "thin_set_launch_hook")
 
 # thin_kernel_t
 KERNEL_NAMES = {0: "trace_clear", 1: "subsample", 2: "fill", 3: "vmax", 4: "scores",
                 5: "decide", 6: "attention", 7: "local", 8: "uniform", 9: "assemble",
                 10: "express", 11: "status", 12: "rotary", 13: "q4_store", 14: "q4_load",
-                15: "q4_select", 16: "q4_attention"}
+                15: "q4_select", 16: "q4_attention", 17: "q4_tree", 18: "q4_keep"}
 HALVE = {"kh": 0, "uniform": 1}  # thin_halve_t
 LaunchHook = C.CFUNCTYPE(None, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p)
 
@@ -115,6 +116,8 @@ def lib():
     F64, Q4 = C.c_double, C.POINTER(Q4CacheStruct)
     L.thin_rotary.argtypes = [P, P, I64, P, P, P, P, I64, P, P, I32, I64, I64, I64, I64, I32, P,
                               I32, P, F64, I32, P]
+    L.thin_rotary_axes.argtypes = [P, P, I64, P, P, P, P, I64, P, P, I32, I64, I64, I64, I64, I32,
+                                   P, I32, P, P, F64, I32, P]
     L.thin_rotary_turns.argtypes = [I64, F64, I32, F64, F64, F64, F64, P, C.POINTER(F64)]
     L.thin_q4_store.argtypes = [Q4, P, P, P, P, I32, I64, P, P, P]
     L.thin_q4_load.argtypes = [Q4, I64, P, P, P, I32, P]
@@ -122,6 +125,9 @@ def lib():
     L.thin_q4_select.argtypes = [Q4, P, P, I64, I32, I64, P, P, I64, I64, I64, P, P, SZ, P]
     L.thin_q4_attention_plan.argtypes = [I64, I64, I64, I64, I64, I64, I64, C.POINTER(SZ)]
     L.thin_q4_attention.argtypes = [Q4, P, P, I64, I32, I64, P, P, P, I64, P, P, P, SZ, P]
+    L.thin_q4_tree.argtypes = [P, P, I64, I64, P, P, P]
+    L.thin_q4_tree_attention.argtypes = [Q4, P, P, I64, I32, I64, P, P, P, P, P, P, SZ, P]
+    L.thin_q4_keep.argtypes = [Q4, P, P, I64, P, P]
     L.thin_selftest_gram16.argtypes = [I32, I64, P, P, P]
     L.thin_status_str.argtypes = [C.c_int]
     L.thin_status_str.restype = C.c_char_p
@@ -132,9 +138,10 @@ def lib():
               "thin_attention", "thin_attention_ex", "thin_selftest_gram16", "thin_express_plan",
               "thin_express_create", "thin_express_step", "thin_express_cache",
               "thin_express_next", "thin_express_destroy", "thin_express_prefill_plan",
-              "thin_express_prefill", "thin_workspace_status", "thin_rotary",
+              "thin_express_prefill", "thin_workspace_status", "thin_rotary", "thin_rotary_axes",
               "thin_rotary_turns", "thin_q4_store", "thin_q4_load", "thin_q4_select_plan",
-              "thin_q4_select", "thin_q4_attention_plan", "thin_q4_attention"):
+              "thin_q4_select", "thin_q4_attention_plan", "thin_q4_attention", "thin_q4_tree",
+              "thin_q4_tree_attention", "thin_q4_keep"):
         getattr(L, f).restype = C.c_int
     _lib = L
     return L

@@ -8,6 +8,8 @@
 
 using thin::observed;
 
+static_assert(THIN_Q4_MAX_DRAFTS == thin::kQ4MaxDrafts, "one bound of drafts");
+
 namespace {
 
 constexpr int64_t kMaxSlices = 65535;  // grid y
@@ -95,16 +97,55 @@ bool plan_attention(int64_t B, int64_t H, int64_t q_heads, int64_t n_max, int64_
   return true;
 }
 
-}  // namespace
+// thin_q4_attention, or with `seen` thin_q4_tree_attention.
+int attention(const thin_q4_cache_t* cache, const void* Q, const int64_t* q_strides,
+              int64_t q_heads, int32_t dtype, int64_t T, const int32_t* at, const int32_t* count,
+              const int32_t* blocks, int64_t n_sel, const uint64_t* seen, void* O,
+              const int64_t* o_strides, void* workspace, size_t workspace_bytes, void* stream) {
+  thin::Q4View c;
+  int rc = cache_view(cache, &c);
+  if (rc) return rc;
+  if (!known_dtype(dtype)) return THIN_EDTYPE;
+  AttnPlan p;
+  if (!valid_ints(at, count) || !aligned(blocks, 4) || (blocks != nullptr) != (n_sel > 0) ||
+      !plan_attention(c.B, c.H, q_heads, c.n_max, cache->d, T, n_sel, dtype == THIN_BF16, &p))
+    return THIN_EINVAL;
+  thin::Q4AttnArgs a{};
+  rc = rows_view(Q, q_strides, c.B, q_heads, T, cache->d, dtype, false, &a.q);
+  if (!rc) rc = rows_view(O, o_strides, c.B, q_heads, T, cache->d, dtype, true, &a.o);
+  if (rc) return rc;
+  if (p.bytes && (!workspace || workspace_bytes < p.bytes || !aligned16(workspace)))
+    return THIN_EWORKSPACE;
+  a.G = (int32_t)group_of(q_heads, c.H);
+  a.tok = {at, count, (int32_t)T};
+  a.blocks = blocks;
+  a.n_sel = (int32_t)n_sel;
+  a.seen = seen;
+  a.words = (int32_t)((T + 63) / 64);
+  a.shape = p.shape;
+  if (p.bytes) {
+    a.part = static_cast<float*>(workspace);
+    if (!blocks && p.shape.waves)
+      a.table = reinterpret_cast<int2*>(static_cast<char*>(workspace) + p.sums);
+  }
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e = observed(THIN_KERNEL_Q4_ATTENTION, -1, st, [&] {
+    return p.shape.waves == 0 ? thin::launch_q4_prompt(dtype, cache->d, c, a, st)
+                              : thin::launch_q4_attention(dtype, cache->d, c, a, st);
+  });
+  if (e == hipSuccess && p.shape.splits > 1)
+    e = observed(THIN_KERNEL_Q4_ATTENTION, -1, st,
+                 [&] { return thin::launch_q4_join(dtype, cache->d, c, a, st); });
+  return e == hipSuccess ? THIN_OK : THIN_EHIP;
+}
 
-extern "C" {
-
-int thin_rotary(const void* X, const int64_t* x_strides, int64_t x_heads, void* X_out,
-                const int64_t* x_out_strides, const void* Y, const int64_t* y_strides,
-                int64_t y_heads, void* Y_out, const int64_t* y_out_strides, int32_t dtype,
-                int64_t B, int64_t T, int64_t d, int64_t rot, int32_t layout, const int32_t* pos,
-                int32_t pos_per_token, const double* turns, double amp, int32_t inverse,
-                void* stream) {
+// thin_rotary, or with `axis` thin_rotary_axes.
+int rotary(const void* X, const int64_t* x_strides, int64_t x_heads, void* X_out,
+           const int64_t* x_out_strides, const void* Y, const int64_t* y_strides, int64_t y_heads,
+           void* Y_out, const int64_t* y_out_strides, int32_t dtype, int64_t B, int64_t T,
+           int64_t d, int64_t rot, int32_t layout, const int32_t* pos, int32_t pos_per_token,
+           int32_t axes, const int32_t* axis, const double* turns, double amp, int32_t inverse,
+           void* stream) {
   if (!known_dtype(dtype)) return THIN_EDTYPE;
   if (B < 1 || T < 1 || B > ((int64_t)1 << 27) || T > ((int64_t)1 << 27) ||
       B * T > ((int64_t)1 << 27) || !supported_d(d))
@@ -127,6 +168,8 @@ int thin_rotary(const void* X, const int64_t* x_strides, int64_t x_heads, void* 
   a.T = T;
   a.pos = pos;
   a.pos_per_token = pos_per_token;
+  a.axes = axes;
+  a.axis = axis;
   a.turns = turns;
   a.rot = (int32_t)rot;
   a.layout = layout;
@@ -136,6 +179,34 @@ int thin_rotary(const void* X, const int64_t* x_strides, int64_t x_heads, void* 
   const hipError_t e =
       observed(THIN_KERNEL_ROTARY, -1, st, [&] { return thin::launch_rotary(dtype, d, a, st); });
   return e == hipSuccess ? THIN_OK : THIN_EHIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+int thin_rotary(const void* X, const int64_t* x_strides, int64_t x_heads, void* X_out,
+                const int64_t* x_out_strides, const void* Y, const int64_t* y_strides,
+                int64_t y_heads, void* Y_out, const int64_t* y_out_strides, int32_t dtype,
+                int64_t B, int64_t T, int64_t d, int64_t rot, int32_t layout, const int32_t* pos,
+                int32_t pos_per_token, const double* turns, double amp, int32_t inverse,
+                void* stream) {
+  return rotary(X, x_strides, x_heads, X_out, x_out_strides, Y, y_strides, y_heads, Y_out,
+                y_out_strides, dtype, B, T, d, rot, layout, pos, pos_per_token, 0, nullptr, turns,
+                amp, inverse, stream);
+}
+
+int thin_rotary_axes(const void* X, const int64_t* x_strides, int64_t x_heads, void* X_out,
+                     const int64_t* x_out_strides, const void* Y, const int64_t* y_strides,
+                     int64_t y_heads, void* Y_out, const int64_t* y_out_strides, int32_t dtype,
+                     int64_t B, int64_t T, int64_t d, int64_t rot, int32_t layout,
+                     const int32_t* pos, int32_t axes, const int32_t* axis, const double* turns,
+                     double amp, int32_t inverse, void* stream) {
+  if (!known_dtype(dtype)) return THIN_EDTYPE;
+  if (axes < 1 || axes > THIN_ROTARY_MAX_AXES || !valid_ints(axis, nullptr)) return THIN_EINVAL;
+  return rotary(X, x_strides, x_heads, X_out, x_out_strides, Y, y_strides, y_heads, Y_out,
+                y_out_strides, dtype, B, T, d, rot, layout, pos, 1, axes, axis, turns, amp,
+                inverse, stream);
 }
 
 int thin_rotary_turns(int64_t rot, double base, int32_t scaling, double factor, double length,
@@ -279,38 +350,45 @@ int thin_q4_attention(const thin_q4_cache_t* cache, const void* Q, const int64_t
                       const int32_t* count, const int32_t* blocks, int64_t n_sel, void* O,
                       const int64_t* o_strides, void* workspace, size_t workspace_bytes,
                       void* stream) {
-  thin::Q4View c;
-  int rc = cache_view(cache, &c);
-  if (rc) return rc;
-  if (!known_dtype(dtype)) return THIN_EDTYPE;
-  AttnPlan p;
-  if (!valid_ints(at, count) || !aligned(blocks, 4) || (blocks != nullptr) != (n_sel > 0) ||
-      !plan_attention(c.B, c.H, q_heads, c.n_max, cache->d, T, n_sel, dtype == THIN_BF16, &p))
+  return attention(cache, Q, q_strides, q_heads, dtype, T, at, count, blocks, n_sel, nullptr, O,
+                   o_strides, workspace, workspace_bytes, stream);
+}
+
+int thin_q4_tree(const int32_t* parents, const int32_t* at, int64_t B, int64_t T, uint64_t* seen,
+                 int32_t* pos, void* stream) {
+  if (B < 1 || B > kMaxSlices || T < 1 || T > THIN_Q4_MAX_DRAFTS) return THIN_EINVAL;
+  if (!valid_ints(parents, nullptr) || !valid_ints(at, nullptr) || !seen || !aligned(seen, 8) ||
+      !valid_ints(pos, nullptr))
     return THIN_EINVAL;
-  thin::Q4AttnArgs a{};
-  rc = rows_view(Q, q_strides, c.B, q_heads, T, cache->d, dtype, false, &a.q);
-  if (!rc) rc = rows_view(O, o_strides, c.B, q_heads, T, cache->d, dtype, true, &a.o);
-  if (rc) return rc;
-  if (p.bytes && (!workspace || workspace_bytes < p.bytes || !aligned16(workspace)))
-    return THIN_EWORKSPACE;
-  a.G = (int32_t)group_of(q_heads, c.H);
-  a.tok = {at, count, (int32_t)T};
-  a.blocks = blocks;
-  a.n_sel = (int32_t)n_sel;
-  a.shape = p.shape;
-  if (p.bytes) {
-    a.part = static_cast<float*>(workspace);
-    if (!blocks && p.shape.waves)
-      a.table = reinterpret_cast<int2*>(static_cast<char*>(workspace) + p.sums);
-  }
   hipStream_t st = static_cast<hipStream_t>(stream);
-  hipError_t e = observed(THIN_KERNEL_Q4_ATTENTION, -1, st, [&] {
-    return p.shape.waves == 0 ? thin::launch_q4_prompt(dtype, cache->d, c, a, st)
-                              : thin::launch_q4_attention(dtype, cache->d, c, a, st);
+  const hipError_t e = observed(THIN_KERNEL_Q4_TREE, -1, st, [&] {
+    return thin::launch_q4_tree(parents, at, B, T, seen, pos, st);
   });
-  if (e == hipSuccess && p.shape.splits > 1)
-    e = observed(THIN_KERNEL_Q4_ATTENTION, -1, st,
-                 [&] { return thin::launch_q4_join(dtype, cache->d, c, a, st); });
+  return e == hipSuccess ? THIN_OK : THIN_EHIP;
+}
+
+int thin_q4_tree_attention(const thin_q4_cache_t* cache, const void* Q, const int64_t* q_strides,
+                           int64_t q_heads, int32_t dtype, int64_t T, const int32_t* at,
+                           const int32_t* count, const uint64_t* seen, void* O,
+                           const int64_t* o_strides, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  if (T > THIN_Q4_MAX_DRAFTS || !seen || !aligned(seen, 8)) return THIN_EINVAL;
+  return attention(cache, Q, q_strides, q_heads, dtype, T, at, count, nullptr, 0, seen, O,
+                   o_strides, workspace, workspace_bytes, stream);
+}
+
+int thin_q4_keep(const thin_q4_cache_t* cache, const int32_t* at, const int32_t* path, int64_t P,
+                 int32_t* end, void* stream) {
+  thin::Q4View c;
+  const int rc = cache_view(cache, &c);
+  if (rc) return rc;
+  if (P < 1 || P > THIN_Q4_MAX_DRAFTS || !valid_ints(at, nullptr) || !valid_ints(path, nullptr) ||
+      !valid_ints(end, nullptr) || end == at || end == path)
+    return THIN_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const hipError_t e = observed(THIN_KERNEL_Q4_KEEP, -1, st, [&] {
+    return thin::launch_q4_keep(cache->d, c, at, path, P, end, st);
+  });
   return e == hipSuccess ? THIN_OK : THIN_EHIP;
 }
 

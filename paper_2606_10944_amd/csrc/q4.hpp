@@ -40,6 +40,8 @@ struct RotaryArgs {
   int64_t Hx, Hy, B, T;
   const int32_t* pos;
   int32_t pos_per_token;  // pos [B, T] instead of [B] + t
+  const int32_t* axis;    // non-null: pos [B, T, axes], pair i's position that of axis[i]
+  int32_t axes;
   const double* turns;    // [rot / 2]
   int32_t rot, layout, inverse;
   float amp;
@@ -50,6 +52,14 @@ hipError_t launch_q4_store(int dtype, int64_t d, const Q4View& c, const RowsView
                            const RowsView& v, const Q4Tokens& tok, hipStream_t st);
 hipError_t launch_q4_load(int dtype, int64_t d, const Q4View& c, const int32_t* at, int64_t T,
                           void* k, void* v, hipStream_t st);
+
+// Rows at[b] + path[b, i] of every slice to rows at[b] + i, and the bounds of the blocks up to
+// the last of them; end[b]: the rows that sequence b then has.
+hipError_t launch_q4_keep(int64_t d, const Q4View& c, const int32_t* at, const int32_t* path,
+                          int64_t P, int32_t* end, hipStream_t st);
+// A tree's ancestors and positions from its parents.
+hipError_t launch_q4_tree(const int32_t* parents, const int32_t* at, int64_t B, int64_t T,
+                          uint64_t* seen, int32_t* pos, hipStream_t st);
 
 struct Q4SelectArgs {
   RowsView q;
@@ -77,6 +87,8 @@ struct Q4AttnArgs {
   Q4Tokens tok;
   const int32_t* blocks;  // null: every cached row
   int32_t n_sel;
+  const uint64_t* seen;  // a tree of drafts: [B, T, words] masks, else null
+  int32_t words;
   Q4AttnShape shape;
   // shape.splits > 1: [slot, 16, d] sums, then [slot, 2, 16] maxima and sums
   float* part;

@@ -1,5 +1,6 @@
 // Attention over the 4-bit key/value cache on gfx950: causal over every cached
-// row, or over the rows of the blocks listed for a token and key head.
+// row, over the rows of the blocks listed for a token and key head, or of a tree of
+// drafted tokens over the rows before the drafts and the drafts of its ancestors.
 //
 // The kernel for few query rows: a wave takes 32 keys at a time on its own, its
 // decoded value rows in LDS, the next step's codes on their way meanwhile.
@@ -89,21 +90,27 @@ __device__ __forceinline__ TileTokens tile_tokens(const Q4AttnArgs& a, int tile)
   return {tile * 16 / a.G, (tile * 16 + 16 < rows ? tile * 16 + 15 : rows - 1) / a.G};
 }
 
-// The last cached row that any of a tile's tokens of sequence b sees, -1 if none.
+// The last cached row that any of a tile's tokens of sequence b sees, -1 if none.  (Which
+// drafts a drafted token sees is its mask's matter: it may be any of them.)
+template <int MODE>
 __device__ __forceinline__ int tile_row(const Q4View& c, const Q4AttnArgs& a, int b, TileTokens tt) {
   const int cnt = a.tok.count ? a.tok.count[b] : a.tok.T;
+  if (MODE == kQ4Tree)
+    return cnt <= tt.first ? -1 : q4_last_row(a.tok, b, std::min(cnt, a.tok.T) - 1, c.n_max);
   return cnt <= tt.first ? -1 : q4_last_row(a.tok, b, tt.last < cnt ? tt.last : cnt - 1, c.n_max);
 }
 
 // Steps of 32 keys up to there.
+template <int MODE>
 __device__ __forceinline__ int steps_of(const Q4View& c, const Q4AttnArgs& a, int b, TileTokens tt) {
-  return (tile_row(c, a, b, tt) + CH) / CH;
+  return (tile_row<MODE>(c, a, b, tt) + CH) / CH;
 }
 
 // How the workgroups of a key head and tile share the sequences' steps.  Every
 // sequence gets workgroups by its length: a share is what a workgroup takes of one
 // sequence, the least for which the workgroups are enough.  Lane l holds sequences
 // l, l + 64, ..
+template <int MODE>
 struct Shares {
   static constexpr int N = kQ4SharedEntries / 64;
   int steps[N];  // of this lane's sequences
@@ -121,7 +128,7 @@ struct Shares {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       steps[i] = 0;
-      if (i * 64 < c.B && i * 64 + lane < c.B) steps[i] = steps_of(c, a, i * 64 + lane, tt);
+      if (i * 64 < c.B && i * 64 + lane < c.B) steps[i] = steps_of<MODE>(c, a, i * 64 + lane, tt);
       sum += steps[i];
     }
     sum = (int)wave_reduce<uint32_t>((uint32_t)sum, 0u, add);
@@ -181,9 +188,10 @@ struct Shares {
 // workgroups share the keys and leave sums in a.part, one slot of existing rows each.
 // (bf16 lists: 128 registers hold four workgroups in a compute unit, 128 -> 123 us for 32
 // blocks of each of 509 tokens; over all rows they cost 64 -> 66 us for long caches.)
-template <typename T, int D, bool LIST, int WV>
-__global__ __launch_bounds__(64 * WV, Elem<T>::bytes == 2 && LIST && WV == 4 ? 4 : 2)
+template <typename T, int D, int MODE, int WV>
+__global__ __launch_bounds__(64 * WV, Elem<T>::bytes == 2 && MODE == kQ4List && WV == 4 ? 4 : 2)
 void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
+  constexpr bool LIST = MODE == kQ4List;
   // bf16 parts of the weights.  (bf16, two: 17 bits, while the sum of the weights is that of
   // the unrounded ones.  One would save 1 % of one token's calls at d = 128, a tenth at 64 and
   // 32 (24 sequences of up to 10156 rows, 8 key heads, d = 64: 31.1 -> 27.9 us), and 123 -> 110
@@ -205,7 +213,7 @@ void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
     h = slice % c.H;
     tile = piece % gridDim.x;
     i0 = 0;
-    i1 = LIST ? a.n_sel * (kQ4Block / CH) : steps_of(c, a, b, tile_tokens(a, tile));
+    i1 = LIST ? a.n_sel * (kQ4Block / CH) : steps_of<MODE>(c, a, b, tile_tokens(a, tile));
   } else if (LIST) {
     b = blockIdx.y / c.H;
     h = blockIdx.y % c.H;
@@ -218,7 +226,7 @@ void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
     const int groups = c.B * splits;
     h = blockIdx.y;
     tile = blockIdx.x / groups;
-    const Shares sh(c, a, tile, lane);
+    const Shares<MODE> sh(c, a, tile, lane);
     // one workgroup per tile leaves the table that the join goes by
     if (h == 0 && blockIdx.x % groups == 0 && wave == 0) sh.write(c, a.table + tile * c.B, lane);
     b = sh.find(c, blockIdx.x % groups, &i0, &i1);
@@ -240,9 +248,11 @@ void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
   }
   const bool there = m < nrows;
   const int qlast = there ? q4_last_row(a.tok, b, t, c.n_max) : -1;
+  Drafts drafts;
+  if (MODE == kQ4Tree) drafts = Drafts(a, b, there ? t : a.tok.T, c.n_max);
   // the last row that any of them sees
   const int last = __builtin_amdgcn_readfirstlane(
-      LIST ? q4_last_row(a.tok, b, t, c.n_max) : tile_row(c, a, b, tile_tokens(a, tile)));
+      LIST ? q4_last_row(a.tok, b, t, c.n_max) : tile_row<MODE>(c, a, b, tile_tokens(a, tile)));
 
   // a wave's steps are i0 + wave + WV n.  LIST: lane n % 64 holds the listed block
   // of step n, for 64 steps at a time.
@@ -302,7 +312,7 @@ void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
   for (int dt = 0; dt < D / 16; ++dt) acc[dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
   unsigned char* sv = lds + wave * CH * kVStride<D>;
   // rows that every query of the tile sees need no mask
-  int all = there ? qlast : 0x7fffffff;
+  int all = there ? (MODE == kQ4Tree ? drafts.before - 1 : qlast) : 0x7fffffff;
   all = __builtin_amdgcn_readfirstlane(
       row_reduce(all, [](int x, int y) { return std::min(x, y); }));
 
@@ -327,7 +337,12 @@ void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
         *reinterpret_cast<u32x4*>(to + w8 * 16) = (u32x4){w[0], w[1], w[2], w[3]};
       }
     }
-    if (row0 + CH - 1 > all) {
+    if (MODE == kQ4Tree && row0 + CH - 1 > all) {
+      const uint32_t see = (uint32_t)drafts.window(row0) >> (4 * g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (!(see >> (j / 4 * 16 + j % 4) & 1)) sc[j] = -INFINITY;
+    } else if (row0 + CH - 1 > all) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         if (row0 + j / 4 * 16 + 4 * g + j % 4 > qlast) sc[j] = -INFINITY;
@@ -527,22 +542,26 @@ __global__ __launch_bounds__(JT) void q4_join_kernel(Q4View c, Q4AttnArgs a) {
   }
 }
 
-template <typename T, int D, bool LIST, int WV>
+template <typename T, int D, int MODE, int WV>
 hipError_t attn(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
-  const int64_t tiles = q4_row_tiles(a.G, a.tok.T, LIST);
+  const int64_t tiles = q4_row_tiles(a.G, a.tok.T, MODE == kQ4List);
   const int64_t splits = a.shape.splits;
-  const dim3 grid = LIST || splits == 1
+  const dim3 grid = MODE == kQ4List || splits == 1
                         ? dim3((uint32_t)(tiles * splits), (uint32_t)(c.B * c.H))
                         : dim3((uint32_t)(tiles * splits * c.B), (uint32_t)c.H);
-  q4_attn_kernel<T, D, LIST, WV><<<grid, 64 * WV, 0, st>>>(c, a);
+  q4_attn_kernel<T, D, MODE, WV><<<grid, 64 * WV, 0, st>>>(c, a);
   return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t attn_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
   if (a.shape.waves == 8)
-    return a.blocks ? attn<T, D, true, 8>(c, a, st) : attn<T, D, false, 8>(c, a, st);
-  return a.blocks ? attn<T, D, true, 4>(c, a, st) : attn<T, D, false, 4>(c, a, st);
+    return a.seen     ? attn<T, D, kQ4Tree, 8>(c, a, st)
+           : a.blocks ? attn<T, D, kQ4List, 8>(c, a, st)
+                      : attn<T, D, kQ4All, 8>(c, a, st);
+  return a.seen     ? attn<T, D, kQ4Tree, 4>(c, a, st)
+         : a.blocks ? attn<T, D, kQ4List, 4>(c, a, st)
+                    : attn<T, D, kQ4All, 4>(c, a, st);
 }
 
 template <typename T, int D>

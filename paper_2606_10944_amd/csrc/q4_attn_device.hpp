@@ -76,6 +76,40 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
   }
 }
 
+// Which cached rows a call's tokens attend to: every row up to their own, those of listed
+// blocks, or those before the drafts and the drafts of their masks.
+constexpr int kQ4All = 0, kQ4List = 1, kQ4Tree = 2;
+
+// What a lane's query row of a drafted tree sees: cached rows 0 .. before - 1, and row at + j
+// for the drafts j < there whose bit is set.
+struct Drafts {
+  const uint64_t* seen;
+  int before, at, there;
+  __device__ __forceinline__ Drafts() {}
+  // Token t of sequence b; t = T or a token that is not there: no row at all.
+  __device__ __forceinline__ Drafts(const Q4AttnArgs& a, int b, int t, int n_max) {
+    const int cnt = a.tok.count ? std::min(a.tok.count[b], a.tok.T) : a.tok.T;
+    const int x = a.tok.at[b];
+    at = x > n_max ? n_max : (x < -kQ4MaxDrafts ? -kQ4MaxDrafts : x);
+    there = t < cnt ? std::min(cnt, n_max - at) : 0;
+    before = t < cnt ? std::max(at, 0) : 0;
+    seen = a.seen + ((int64_t)b * a.tok.T + std::min(t, a.tok.T - 1)) * a.words;
+  }
+  // Rows row0 .. row0 + 63 (row0 >= 0): bit i is row row0 + i.
+  __device__ __forceinline__ uint64_t window(int row0) const {
+    const int off = row0 - at, j = off > 0 ? off : 0;  // the first draft among them
+    uint64_t x = 0;
+    if (j < there) {
+      x = seen[j / 64] >> (j % 64);
+      if (j % 64 != 0 && (j | 63) + 1 < there) x |= seen[j / 64 + 1] << (64 - j % 64);
+      if (there - j < 64) x &= ((uint64_t)1 << (there - j)) - 1;
+    }
+    const int old = before - row0;  // rows before the drafts
+    if (old <= 0) return x;
+    return old >= 64 ? ~(uint64_t)0 : x << old | (((uint64_t)1 << old) - 1);
+  }
+};
+
 // A slice's rows: offsets within it fit 32 bits (n_max * d / 2 <= 2^27 bytes).
 struct Slice {
   const uint8_t *kc, *ks, *vc, *vs;

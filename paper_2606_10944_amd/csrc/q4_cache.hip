@@ -1,4 +1,4 @@
-// Store, load and selection of the 4-bit key/value cache on gfx950.
+// Store, load, moves and selection of the 4-bit key/value cache on gfx950, and trees of drafts.
 //
 // A group of 32 channels with largest magnitude amax takes e = the least integer
 // in [-125, 125] with amax <= 7 * 2^e and the codes of x / 2^e rounded to nearest
@@ -54,6 +54,71 @@ __device__ __forceinline__ uint32_t encode8(float* f, uint32_t* byte) {
   return c;
 }
 
+// The bounds of a block of slice s from the least and largest values of eight channels (l * 8
+// on, l = threadIdx.x % (D / 8)) that each of a workgroup's four waves' threads holds.
+template <int D>
+__device__ __forceinline__ void write_bounds(const Q4View& c, int64_t s, int64_t block, float* mn,
+                                             float* mx) {
+  constexpr int LR = D / 8;
+  const int l = threadIdx.x % LR;
+  // over the wave's rows, then the four waves.  Halves of the wave, then its quarters,
+  // trade values so that each keeps half of them: quarter g is left with channels 2 g and
+  // 2 g + 1 of the eight.
+#pragma unroll
+  for (int n = 4; n > 1; n /= 2)
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      trade(n == 4, mn[i], mn[i + n]);
+      trade(n == 4, mx[i], mx[i + n]);
+      mn[i] = fminf(mn[i], mn[i + n]);
+      mx[i] = fmaxf(mx[i], mx[i + n]);
+    }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (LR <= 8) {
+      mn[i] = fminf(mn[i], lane_move<kTurn8>(mn[i]));
+      mx[i] = fmaxf(mx[i], lane_move<kTurn8>(mx[i]));
+    }
+    if (LR <= 4) {
+      mn[i] = fminf(mn[i], lane_move<kTurn4>(mn[i]));
+      mx[i] = fmaxf(mx[i], lane_move<kTurn4>(mx[i]));
+    }
+  }
+  __shared__ float sm[4][2][D];
+  if ((threadIdx.x & 15) < LR) {
+    const int ch = l * 8 + (threadIdx.x & 63) / 16 * 2;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      sm[threadIdx.x / 64][0][ch + i] = mn[i];
+      sm[threadIdx.x / 64][1][ch + i] = mx[i];
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < 2 * D) {
+    const int which = threadIdx.x / D, ch = threadIdx.x % D;
+    float x = sm[0][which][ch];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) x = which ? fmaxf(x, sm[w][1][ch]) : fminf(x, sm[w][0][ch]);
+    const int64_t nb = (c.n_max + kQ4Block - 1) / kQ4Block;
+    // (exact: every cached value is a bf16)
+    c.bounds[((s * nb + block) * 2 + which) * D + ch] = (uint16_t)(__float_as_uint(x) >> 16);
+  }
+}
+
+// The values of eight codes (channels 0 .. 7) into running bounds.
+__device__ __forceinline__ void take_bounds(uint32_t code, uint32_t byte, float* mn, float* mx) {
+  uint32_t w[4];
+  decode8(code, q4_scale(byte), w);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = __uint_as_float(w[i] << 16), d = __uint_as_float(w[i] & 0xffff0000u);
+    mn[2 * i] = fminf(mn[2 * i], a);
+    mx[2 * i] = fmaxf(mx[2 * i], a);
+    mn[2 * i + 1] = fminf(mn[2 * i + 1], d);
+    mx[2 * i + 1] = fmaxf(mx[2 * i + 1], d);
+  }
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS) void q4_store_kernel(Q4View c, RowsView k, RowsView v,
                                                            Q4Tokens tok) {
@@ -96,59 +161,9 @@ __global__ __launch_bounds__(THREADS) void q4_store_kernel(Q4View c, RowsView k,
       code = *reinterpret_cast<const uint32_t*>(c.k_codes + row * (D / 2) + l * 4);
       byte = c.k_scales[row * (D / 32) + l / 4];
     }
-    uint32_t w[4];
-    decode8(code, q4_scale(byte), w);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float a = __uint_as_float(w[i] << 16), d = __uint_as_float(w[i] & 0xffff0000u);
-      mn[2 * i] = fminf(mn[2 * i], a);
-      mx[2 * i] = fmaxf(mx[2 * i], a);
-      mn[2 * i + 1] = fminf(mn[2 * i + 1], d);
-      mx[2 * i + 1] = fmaxf(mx[2 * i + 1], d);
-    }
+    take_bounds(code, byte, mn, mx);
   }
-  // over the wave's rows, then the four waves.  Halves of the wave, then its quarters,
-  // trade values so that each keeps half of them: quarter g is left with channels 2 g and
-  // 2 g + 1 of the eight.
-#pragma unroll
-  for (int n = 4; n > 1; n /= 2)
-#pragma unroll
-    for (int i = 0; i < n; ++i) {
-      trade(n == 4, mn[i], mn[i + n]);
-      trade(n == 4, mx[i], mx[i + n]);
-      mn[i] = fminf(mn[i], mn[i + n]);
-      mx[i] = fmaxf(mx[i], mx[i + n]);
-    }
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if (LR <= 8) {
-      mn[i] = fminf(mn[i], lane_move<kTurn8>(mn[i]));
-      mx[i] = fmaxf(mx[i], lane_move<kTurn8>(mx[i]));
-    }
-    if (LR <= 4) {
-      mn[i] = fminf(mn[i], lane_move<kTurn4>(mn[i]));
-      mx[i] = fmaxf(mx[i], lane_move<kTurn4>(mx[i]));
-    }
-  }
-  __shared__ float sm[4][2][D];
-  if ((threadIdx.x & 15) < LR) {
-    const int ch = l * 8 + (threadIdx.x & 63) / 16 * 2;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      sm[threadIdx.x / 64][0][ch + i] = mn[i];
-      sm[threadIdx.x / 64][1][ch + i] = mx[i];
-    }
-  }
-  __syncthreads();
-  if (threadIdx.x < 2 * D) {
-    const int which = threadIdx.x / D, ch = threadIdx.x % D;
-    float x = sm[0][which][ch];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) x = which ? fmaxf(x, sm[w][1][ch]) : fminf(x, sm[w][0][ch]);
-    const int64_t nb = (c.n_max + kQ4Block - 1) / kQ4Block;
-    // (exact: every cached value is a bf16)
-    c.bounds[((s * nb + r0 / kQ4Block) * 2 + which) * D + ch] = (uint16_t)(__float_as_uint(x) >> 16);
-  }
+  write_bounds<D>(c, s, r0 / kQ4Block, mn, mx);
 }
 
 // ---------------------------------------------------------------------------
@@ -182,6 +197,144 @@ __global__ __launch_bounds__(THREADS) void q4_load_kernel(Q4View c, const int32_
       o[1] = (u32x4){w[2] << 16, w[2] & 0xffff0000u, w[3] << 16, w[3] & 0xffff0000u};
     }
   }
+}
+
+// ---------------------------------------------------------------------------
+// Keep: the rows of an accepted path of drafts move to the places behind the rows before
+// them, and the bounds of the blocks that hold these places are formed anew, as a store of
+// these rows forms them.  A workgroup takes a slice.  The rows pass through LDS whole before
+// the first is written, so a path may name rows in any order, and rows that it also writes.
+// ---------------------------------------------------------------------------
+template <int D, int CAP>
+__global__ __launch_bounds__(THREADS) void q4_keep_kernel(Q4View c, const int32_t* at_,
+                                                          const int32_t* path, int P,
+                                                          int32_t* end) {
+  constexpr int CW = D / 32;  // 16-byte words of a row's codes, and bytes of its scales
+  __shared__ u32x4 codes[2][CAP * CW];
+  __shared__ uint8_t scales[2][CAP * CW];
+  __shared__ int32_t from[CAP];
+  __shared__ int first_bad;
+  const int64_t s = blockIdx.x;
+  const int b = blockIdx.x / c.H;
+  const int64_t at = at_[b];
+  if (threadIdx.x == 0) first_bad = P;
+  __syncthreads();
+  for (int i = threadIdx.x; i < P; i += THREADS) {
+    const int32_t p = path[(int64_t)b * P + i];
+    const int64_t row = at + p;
+    from[i] = (int32_t)row;
+    if (p < 0 || at < 0 || row >= c.n_max || at + i >= c.n_max) atomicMin(&first_bad, i);
+  }
+  __syncthreads();
+  const int n = first_bad;
+  if (blockIdx.x % c.H == 0 && threadIdx.x == 0) end[b] = (int32_t)(at + n);
+  const int64_t base = s * c.n_max;
+  for (int i = threadIdx.x; i < n * CW; i += THREADS) {
+    const int64_t row = base + from[i / CW];
+    codes[0][i] = reinterpret_cast<const u32x4*>(c.k_codes + row * (D / 2))[i % CW];
+    codes[1][i] = reinterpret_cast<const u32x4*>(c.v_codes + row * (D / 2))[i % CW];
+    scales[0][i] = c.k_scales[row * CW + i % CW];
+    scales[1][i] = c.v_scales[row * CW + i % CW];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n * CW; i += THREADS) {
+    // (n * CW words in a row: the new rows lie behind one another)
+    reinterpret_cast<u32x4*>(c.k_codes + (base + at) * (D / 2))[i] = codes[0][i];
+    reinterpret_cast<u32x4*>(c.v_codes + (base + at) * (D / 2))[i] = codes[1][i];
+    c.k_scales[(base + at) * CW + i] = scales[0][i];
+    c.v_scales[(base + at) * CW + i] = scales[1][i];
+  }
+  // bounds of the blocks from the last row before the drafts to the last row kept
+  const int64_t last = at + n - 1, r0 = (at > 0 ? at - 1 : 0) / kQ4Block;
+  if (last < 0 || last >= c.n_max) return;
+  constexpr int LR = D / 8, RPP = THREADS / LR;
+  const int l = threadIdx.x % LR, rp = threadIdx.x / LR;
+  for (int64_t k = r0; k <= last / kQ4Block; ++k) {
+    float mn[8], mx[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      mn[i] = INFINITY;
+      mx[i] = -INFINITY;
+    }
+#pragma unroll
+    for (int p = 0; p < kQ4Block; p += RPP) {
+      const int64_t r = k * kQ4Block + p + rp;
+      if (r > last) continue;
+      uint32_t code, byte;
+      if (r >= at) {
+        const int i = (int)(r - at);
+        code = reinterpret_cast<const uint32_t*>(codes[0])[i * (D / 8) + l];
+        byte = scales[0][i * CW + l / 4];
+      } else {
+        code = *reinterpret_cast<const uint32_t*>(c.k_codes + (base + r) * (D / 2) + l * 4);
+        byte = c.k_scales[(base + r) * CW + l / 4];
+      }
+      take_bounds(code, byte, mn, mx);
+    }
+    __syncthreads();  // (the block before is done with the waves' bounds)
+    write_bounds<D>(c, s, k, mn, mx);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// A tree of drafts.  seen[t] has the bits of t and its ancestors, pos[t] = at + their number
+// - 1.  Parents come before their children, so a chain of ancestors runs down through the
+// words of 64 drafts.  A wave closes a word over itself by jumping from ancestor to ancestor's
+// ancestor, six times at most, and finds every draft's first ancestor below the word; then a
+// draft takes one such step per word.  A workgroup takes 256 drafts of a sequence.
+// ---------------------------------------------------------------------------
+constexpr int kTreeWords = kQ4MaxDrafts / 64;
+
+__global__ __launch_bounds__(THREADS) void q4_tree_kernel(const int32_t* parents,
+                                                          const int32_t* at, int T, uint64_t* seen,
+                                                          int32_t* pos) {
+  __shared__ uint64_t chain[kQ4MaxDrafts];  // the draft and its ancestors in its word
+  __shared__ int32_t below[kQ4MaxDrafts];   // the first one below it, -1: none
+  constexpr int RS = kTreeWords + 1;
+  __shared__ uint64_t rows[THREADS * RS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+  const int64_t b = blockIdx.y;
+  const int t0 = blockIdx.x * THREADS, t1 = std::min(T, t0 + THREADS);
+  const int words = (T + 63) / 64;
+  for (int w = wave; w * 64 < t1; w += THREADS / 64) {
+    const int t = w * 64 + lane;
+    int p = t < T ? parents[b * T + t] : -1;
+    if (p < 0 || p >= t) p = -1;
+    uint64_t bits = (uint64_t)1 << lane;
+    int jump = p >= w * 64 ? p - w * 64 : -1;  // a lane of this word
+    int up = p >= w * 64 ? -1 : p;
+    for (int i = 0; i < 6 && __any(jump >= 0); ++i) {
+      const int from = jump < 0 ? lane : jump;
+      const uint64_t more = __shfl(bits, from);
+      const int next = __shfl(jump, from), theirs = __shfl(up, from);
+      if (jump >= 0) {
+        bits |= more;
+        jump = next;
+        up = theirs;
+      }
+    }
+    chain[t] = bits;
+    below[t] = up;
+  }
+  __syncthreads();
+  const int t = t0 + threadIdx.x;
+  if (t < T) {
+    int a = t, n = 0;
+    for (int w = words - 1; w >= 0; --w) {
+      uint64_t x = 0;
+      if (a >= w * 64) {
+        x = chain[a];
+        a = below[a];
+        n += __popcll(x);
+      }
+      rows[threadIdx.x * RS + w] = x;
+    }
+    pos[b * T + t] = (int32_t)((uint32_t)at[b] + (uint32_t)n - 1u);
+  }
+  __syncthreads();
+  uint64_t* out = seen + (b * T + t0) * words;
+  for (int i = threadIdx.x; i < (t1 - t0) * words; i += THREADS)
+    out[i] = rows[i / words * RS + i % words];
 }
 
 // ---------------------------------------------------------------------------
@@ -820,6 +973,17 @@ hipError_t store_d(const Q4View& c, const RowsView& k, const RowsView& v, const 
   return hipGetLastError();
 }
 
+template <int D>
+hipError_t keep_d(const Q4View& c, const int32_t* at, const int32_t* path, int64_t P, int32_t* end,
+                  hipStream_t st) {
+  const uint32_t grid = (uint32_t)(c.B * c.H);
+  if (P <= 64)
+    q4_keep_kernel<D, 64><<<grid, THREADS, 0, st>>>(c, at, path, (int)P, end);
+  else
+    q4_keep_kernel<D, kQ4MaxDrafts><<<grid, THREADS, 0, st>>>(c, at, path, (int)P, end);
+  return hipGetLastError();
+}
+
 template <typename T, int D>
 hipError_t load_d(const Q4View& c, const int32_t* at, int64_t T_, void* k, void* v, hipStream_t st) {
   constexpr int per = THREADS / (D / 8);
@@ -905,6 +1069,20 @@ hipError_t launch_q4_store(int dtype, int64_t d, const Q4View& c, const RowsView
 hipError_t launch_q4_load(int dtype, int64_t d, const Q4View& c, const int32_t* at, int64_t T,
                           void* k, void* v, hipStream_t st) {
   Q4_BY_D(load_d, c, at, T, k, v, st);
+}
+
+hipError_t launch_q4_keep(int64_t d, const Q4View& c, const int32_t* at, const int32_t* path,
+                          int64_t P, int32_t* end, hipStream_t st) {
+  return d == 32   ? keep_d<32>(c, at, path, P, end, st)
+         : d == 64 ? keep_d<64>(c, at, path, P, end, st)
+                   : keep_d<128>(c, at, path, P, end, st);
+}
+
+hipError_t launch_q4_tree(const int32_t* parents, const int32_t* at, int64_t B, int64_t T,
+                          uint64_t* seen, int32_t* pos, hipStream_t st) {
+  const dim3 grid((uint32_t)((T + THREADS - 1) / THREADS), (uint32_t)B);
+  q4_tree_kernel<<<grid, THREADS, 0, st>>>(parents, at, (int)T, seen, pos);
+  return hipGetLastError();
 }
 
 hipError_t launch_q4_scores(int dtype, int64_t d, const Q4View& c, const Q4SelectArgs& a,

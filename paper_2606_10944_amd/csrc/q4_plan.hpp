@@ -7,6 +7,7 @@
 namespace thin {
 
 constexpr int32_t kQ4MaxTokens = 1 << 20;  // per batch entry and call
+constexpr int32_t kQ4MaxDrafts = 1024;     // drafted tokens per batch entry
 constexpr int32_t kQ4MaxGroup = 1024;      // query heads per key head
 constexpr int32_t kQ4MaxSplits = 512;      // workgroups that share one tile's keys
 constexpr int32_t kQ4SharedEntries = 256;  // batch entries whose tiles' keys are shared out

@@ -1,5 +1,6 @@
 // Attention over the 4-bit key/value cache on gfx950 for many query rows of a slice (a
-// prompt or a chunk of one): causal over every cached row.
+// prompt or a chunk of one, or a large tree of drafts): causal over every cached row, or
+// over the rows before the drafts and the drafts of each token's mask.
 //
 // A workgroup of four waves takes 64 RT query rows, RT tiles of 16 per wave, and walks
 // the cached rows 64 at a time.  Its threads bring codes to LDS once for all of them:
@@ -23,7 +24,7 @@ constexpr int PW = 4;    // waves
 constexpr int PK = 64;   // cached rows per tile
 
 // SPLIT: workgroups share a tile's keys and leave sums for the join.
-template <typename T, int D, int RT, bool SPLIT>
+template <typename T, int D, int RT, bool SPLIT, bool TREE>
 __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnArgs a) {
   constexpr bool MX = Elem<T>::bytes == 2;
   // bf16 parts of the weights, whose sum is that of the rounded ones.  (bf16, one: two take
@@ -50,7 +51,7 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
   const int cnt = a.tok.count ? std::min(a.tok.count[b], a.tok.T) : a.tok.T;
   // the last cached row that query rows up to r see
   auto seen = [&](int r) {
-    const int t = std::min(std::min(r, nrows - 1) / a.G, cnt - 1);
+    const int t = TREE ? cnt - 1 : std::min(std::min(r, nrows - 1) / a.G, cnt - 1);
     return t < 0 ? -1 : q4_last_row(a.tok, b, t, c.n_max);
   };
   const int last = __builtin_amdgcn_readfirstlane(r0 / a.G < cnt ? seen(r0 + ROWS * PW - 1) : -1);
@@ -59,6 +60,7 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
       __builtin_amdgcn_readfirstlane(w0 < nrows && w0 / a.G < cnt ? seen(w0 + ROWS - 1) : -1);
 
   int qlast[RT];
+  Drafts drafts[RT];
   int all = 0x7fffffff;  // rows up to here are seen by every query of the wave
   Queries<T, D> q[RT];
 #pragma unroll
@@ -67,7 +69,8 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
     const bool there = r < nrows;
     const int t = there ? r / a.G : 0, head = there ? r % a.G : 0;
     qlast[rt] = there ? q4_last_row(a.tok, b, t, c.n_max) : -1;
-    if (there) all = std::min(all, qlast[rt]);
+    if (TREE) drafts[rt] = Drafts(a, b, there ? t : a.tok.T, c.n_max);
+    if (there) all = std::min(all, TREE ? drafts[rt].before - 1 : qlast[rt]);
     q[rt].load(there ? static_cast<const T*>(a.q.p) + b * a.q.sb +
                            ((int64_t)h * a.G + head) * a.q.sh + t * a.q.sr
                      : nullptr,
@@ -167,10 +170,15 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
     if (row0 <= wlast) {
       if (row0 + PK - 1 > all) {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
+        for (int rt = 0; rt < RT; ++rt) {
+          uint64_t see = 0;
+          if (TREE) see = drafts[rt].window(row0) >> (4 * g);
 #pragma unroll
           for (int j = 0; j < PK / 4; ++j)
-            if (row0 + j / 4 * 16 + 4 * g + j % 4 > qlast[rt]) s[rt][j] = -INFINITY;
+            if (TREE ? !(see >> (j / 4 * 16 + j % 4) & 1)
+                     : row0 + j / 4 * 16 + 4 * g + j % 4 > qlast[rt])
+              s[rt][j] = -INFINITY;
+        }
       }
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
@@ -275,10 +283,16 @@ hipError_t prompt_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
   static_assert(16 * RT * PW == q4_prompt_rows(Elem<T>::bytes == 2), "rows of a workgroup");
   const int64_t tiles = ((int64_t)a.tok.T * a.G + 16 * RT * PW - 1) / (16 * RT * PW);
   const dim3 grid((uint32_t)(tiles * a.shape.splits), (uint32_t)(c.B * c.H));
-  if (a.shape.splits > 1)
-    q4_prompt_kernel<T, D, RT, true><<<grid, 64 * PW, 0, st>>>(c, a);
-  else
-    q4_prompt_kernel<T, D, RT, false><<<grid, 64 * PW, 0, st>>>(c, a);
+  if (a.seen) {
+    if (a.shape.splits > 1)
+      q4_prompt_kernel<T, D, RT, true, true><<<grid, 64 * PW, 0, st>>>(c, a);
+    else
+      q4_prompt_kernel<T, D, RT, false, true><<<grid, 64 * PW, 0, st>>>(c, a);
+  } else if (a.shape.splits > 1) {
+    q4_prompt_kernel<T, D, RT, true, false><<<grid, 64 * PW, 0, st>>>(c, a);
+  } else {
+    q4_prompt_kernel<T, D, RT, false, false><<<grid, 64 * PW, 0, st>>>(c, a);
+  }
   return hipGetLastError();
 }
 

@@ -8,6 +8,9 @@
 // off before the rounding to float32 (a float32 product would lose 2^-24 of a
 // position of a million: a tenth of a radian).
 //
+// With axes a pair's position is one of a token's up to four (time, height, width): the four
+// are loaded beside the table of axes and one is selected, so that no load waits for another.
+//
 // Bound by HBM: 16384 tokens x 40 heads x 128 channels, bf16, 62 us = 5.4 TB/s read and
 // written (a large copy runs at 5.1); one token of 16 sequences, 40 heads: 3.8 us, a
 // launch and the latency of positions, sines and rows.
@@ -54,8 +57,9 @@ __device__ __forceinline__ u32x4 pack<bf16_t>(const float* f) {
                  cvt_pk_bf16(f[6], f[7])};
 }
 
-// INTER: a pair is two neighbouring channels, else channels i and i + rot / 2.
-template <typename T, int D, bool INTER>
+// INTER: a pair is two neighbouring channels, else channels i and i + rot / 2.  AXES: every
+// pair has its axis' position.
+template <typename T, int D, bool INTER, bool AXES>
 __global__ __launch_bounds__(THREADS) void rotary_kernel(RotaryArgs a, int heads) {
   constexpr int P = Pairs<T>::n;
   constexpr int VT = D / (2 * P);  // threads per token
@@ -71,10 +75,24 @@ __global__ __launch_bounds__(THREADS) void rotary_kernel(RotaryArgs a, int heads
   const int c1 = INTER || !turn ? c0 + P : c0 + half;
   float cs[P], sn[P];
   if (turn) {
-    const double pos =
-        a.pos_per_token ? (double)a.pos[item] : (double)((int64_t)a.pos[b] + t);
+    double pos = 0.0;
+    int32_t at[4];
+    if constexpr (AXES) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) at[j] = a.pos[item * a.axes + (j < a.axes ? j : 0)];
+    } else {
+      pos = a.pos_per_token ? (double)a.pos[item] : (double)((int64_t)a.pos[b] + t);
+    }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
+      if constexpr (AXES) {
+        const int32_t j = a.axis[v * P + i];
+        int32_t p = 0;  // (an entry that is no axis: position 0)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (j == x && x < a.axes) p = at[x];
+        pos = (double)p;
+      }
       const double n = pos * a.turns[v * P + i];
       float s, c;
       sincospif((float)(2.0 * (n - rint(n))), &s, &c);
@@ -120,10 +138,16 @@ hipError_t launch(const RotaryArgs& a, hipStream_t st) {
   if (parts > H) parts = H;
   const int64_t heads = (H + parts - 1) / parts;
   const dim3 grid((uint32_t)tiles, (uint32_t)((H + heads - 1) / heads));
-  if (a.layout)
-    rotary_kernel<T, D, true><<<grid, THREADS, 0, st>>>(a, (int)heads);
-  else
-    rotary_kernel<T, D, false><<<grid, THREADS, 0, st>>>(a, (int)heads);
+  if (a.axis) {
+    if (a.layout)
+      rotary_kernel<T, D, true, true><<<grid, THREADS, 0, st>>>(a, (int)heads);
+    else
+      rotary_kernel<T, D, false, true><<<grid, THREADS, 0, st>>>(a, (int)heads);
+  } else if (a.layout) {
+    rotary_kernel<T, D, true, false><<<grid, THREADS, 0, st>>>(a, (int)heads);
+  } else {
+    rotary_kernel<T, D, false, false><<<grid, THREADS, 0, st>>>(a, (int)heads);
+  }
   return hipGetLastError();
 }
 

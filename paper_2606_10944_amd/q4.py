@@ -18,6 +18,7 @@ from ._lib import (THIN_BF16, THIN_EDTYPE, THIN_EINVAL, THIN_FP32, Q4CacheStruct
                    lib)
 
 BLOCK = 64  # THIN_Q4_BLOCK
+MAX_DRAFTS = 1024  # THIN_Q4_MAX_DRAFTS
 LAYOUT = {"half": 0, "interleaved": 1}
 SCALING = {"none": 0, "linear": 1, "base": 2, "bands": 3}
 
@@ -141,6 +142,24 @@ def thin_rotary(X: torch.Tensor, pos: torch.Tensor, turns: torch.Tensor, *,
     [rot/2] on the device.  inverse=True turns back: of an output's gradient, the
     gradient of the rows (autograd does not record the call).
     out / out_Y may be X / Y themselves.  Returns out, or (out, out_Y) with Y."""
+    return _rotary(X, pos, turns, None, Y, layout, amp, inverse, out, out_Y, stream)
+
+
+def thin_rotary_axes(X: torch.Tensor, pos: torch.Tensor, turns: torch.Tensor, axis: torch.Tensor,
+                     *, Y: Optional[torch.Tensor] = None, layout: str = "half", amp: float = 1.0,
+                     inverse: bool = False, out: Optional[torch.Tensor] = None,
+                     out_Y: Optional[torch.Tensor] = None, stream=None):
+    """thin_rotary with several positions per token (time, height, width): pos
+    int32 [B,T,axes], up to 4 axes, and axis int32 [rot/2] on the device, the axis
+    of every pair of channels."""
+    if pos.dim() != 3:
+        raise ThinError(THIN_EINVAL, "pos must be int32 [B,T,axes]")
+    if axis.dim() != 1 or axis.shape != turns.shape:
+        raise ThinError(THIN_EINVAL, "axis must be int32 [rot/2], as turns")
+    return _rotary(X, pos, turns, axis, Y, layout, amp, inverse, out, out_Y, stream)
+
+
+def _rotary(X, pos, turns, axis, Y, layout, amp, inverse, out, out_Y, stream):
     dev, st = _where(stream)
     lay = LAYOUT.get(layout)
     if lay is None:
@@ -151,7 +170,11 @@ def thin_rotary(X: torch.Tensor, pos: torch.Tensor, turns: torch.Tensor, *,
     if turns.dtype != torch.float64 or turns.dim() != 1 or not turns.is_contiguous():
         raise ThinError(THIN_EINVAL, "turns must be contiguous float64 [rot/2]")
     per_token = pos.dim() == 2
-    p = _ints(pos, (B, T) if per_token else (B,), dev, "pos")
+    if axis is not None:
+        axes = pos.shape[2]
+        p = _ints(pos, (B, T, axes), dev, "pos")
+    else:
+        p = _ints(pos, (B, T) if per_token else (B,), dev, "pos")
     if out is None:
         out = _empty_like(X, dev, stream)
         o, os_ = out.data_ptr(), None
@@ -177,11 +200,16 @@ def thin_rotary(X: torch.Tensor, pos: torch.Tensor, turns: torch.Tensor, *,
             oy, oys = _rows(out_Y, dev, "out_Y")
     elif out_Y is not None:
         raise ThinError(THIN_EINVAL, "out_Y without Y")
-    rc = lib().thin_rotary(x, xs, H, o, os_, y, ys, Hy, oy, oys, _dtype(X, "X"), B, T, d,
-                           2 * turns.shape[0], lay, p, per_token, _on(turns, dev, "turns"), amp,
-                           inverse, st)
+    rows = (x, xs, H, o, os_, y, ys, Hy, oy, oys, _dtype(X, "X"), B, T, d, 2 * turns.shape[0], lay,
+            p)
+    t = _on(turns, dev, "turns")
+    if axis is not None:
+        rc = lib().thin_rotary_axes(*rows, axes, _ints(axis, axis.shape, dev, "axis"), t, amp,
+                                    inverse, st)
+    else:
+        rc = lib().thin_rotary(*rows, per_token, t, amp, inverse, st)
     if rc:
-        _check(rc, "thin_rotary")
+        _check(rc, "thin_rotary" if axis is None else "thin_rotary_axes")
     return out if Y is None else (out, out_Y)
 
 
@@ -192,7 +220,8 @@ class Q4Cache:
 
     ``step`` is one decoding step or one prompt (or a chunk of it): new queries,
     keys and values, turned by their positions if `turns` is given, the rows
-    stored, and attention over the cache or over the blocks selected from it."""
+    stored, and attention over the cache or over the blocks selected from it.
+    ``draft`` is a step of a tree of drafted tokens, ``keep`` takes the accepted ones."""
 
     def __init__(self, B: int, H: int, n_max: int, d: int, *, device="cuda"):
         nb = (n_max + BLOCK - 1) // BLOCK
@@ -258,6 +287,47 @@ class Q4Cache:
                                     count=count, stream=stream)
         return thin_q4_attention(Q, self, at, count=count, blocks=blocks, O=O, stream=stream)
 
+    def draft(self, Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, at: torch.Tensor,
+              parents: Optional[torch.Tensor] = None, *, count: Optional[torch.Tensor] = None,
+              turns: Optional[torch.Tensor] = None, layout: str = "half", amp: float = 1.0,
+              tree=None, pos: Optional[torch.Tensor] = None, axis: Optional[torch.Tensor] = None,
+              O: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Outputs O [B,q_heads,T,d] of a tree of T drafted tokens behind the first at[b] rows:
+        rows K, V [B,H,T,d] are stored at at[b] + t, turned (with `turns`) by the drafts'
+        positions in the tree, and a draft attends to the rows before at[b], its ancestors and
+        itself.  parents int32 [B,T] (thin_q4_tree).  Layers of one step share a tree:
+        tree=(seen, pos) as thin_q4_tree gave them is taken in place of parents.
+        Positions of their own: pos int32 [B,T], or [B,T,axes] with the pairs' `axis`
+        (thin_rotary_axes).  keep() then takes the accepted rows.  A call that is refused has
+        stored nothing."""
+        self._check_step(Q, 0, 0, 1, O, _where(stream)[0])
+        B, T = self.B, Q.shape[2]
+        if T > MAX_DRAFTS:
+            raise ThinError(THIN_EINVAL, f"at most {MAX_DRAFTS} drafts")
+        if tree is None:
+            if parents is None or parents.shape != (B, T):
+                raise ThinError(THIN_EINVAL, "parents must be int32 [B,T]")
+            tree = thin_q4_tree(parents, at, stream=stream)
+        seen = tree[0]
+        _masks(seen, B, T, _where(stream)[0])
+        if turns is not None:
+            where = tree[1] if pos is None else pos
+            if axis is not None:
+                Q, K = thin_rotary_axes(Q, where, turns, axis, Y=K, layout=layout, amp=amp,
+                                        stream=stream)
+            else:
+                if where.shape != (B, T):
+                    raise ThinError(THIN_EINVAL, "pos must be int32 [B,T]")
+                Q, K = thin_rotary(Q, where, turns, Y=K, layout=layout, amp=amp, stream=stream)
+        elif pos is not None or axis is not None:
+            raise ThinError(THIN_EINVAL, "pos and axis need turns")
+        thin_q4_store(K, V, self, at, count=count, stream=stream)
+        return thin_q4_tree_attention(Q, self, at, seen, count=count, O=O, stream=stream)
+
+    def keep(self, at: torch.Tensor, path: torch.Tensor, *, end: Optional[torch.Tensor] = None,
+             stream=None) -> torch.Tensor:
+        """thin_q4_keep over this cache."""
+        return thin_q4_keep(self, at, path, end=end, stream=stream)
 
     def _check_step(self, Q, n_sel, n_sinks, n_window, O, dev: int) -> None:
         """Refuses what the selection or attention of a step would, before its rows are
@@ -394,3 +464,76 @@ def thin_q4_attention(Q: torch.Tensor, cache: Q4Cache, at: torch.Tensor, *,
                                    _ints(count, (B,), dev, "count"), bp, n_sel, o, os_, wp, wn,
                                    st), "thin_q4_attention")
     return O
+
+
+def thin_q4_tree(parents: torch.Tensor, at: torch.Tensor, *, seen: Optional[torch.Tensor] = None,
+                 pos: Optional[torch.Tensor] = None, stream=None):
+    """(seen, pos) of trees of drafted tokens: parents int32 [B,T], every draft's parent (an
+    earlier draft; negative: a root).  seen int64 [B,T,ceil(T/64)]: bit j % 64 of word j / 64
+    is set if draft t attends to draft j, itself and its ancestors.  pos int32 [B,T]: at[b] +
+    the draft's depth, the positions of thin_rotary."""
+    dev, st = _where(stream)
+    if parents.dim() != 2:
+        raise ThinError(THIN_EINVAL, "parents must be int32 [B,T]")
+    B, T = parents.shape
+    p, a = _ints(parents, (B, T), dev, "parents"), _ints(at, (B,), dev, "at")
+    if seen is None:
+        seen = _empty((B, T, (T + 63) // 64), torch.int64, dev, stream)
+    if pos is None:
+        pos = _empty((B, T), torch.int32, dev, stream)
+    _check(lib().thin_q4_tree(p, a, B, T, _masks(seen, B, T, dev), _ints(pos, (B, T), dev, "pos"),
+                              st), "thin_q4_tree")
+    return seen, pos
+
+
+def _masks(seen: torch.Tensor, B: int, T: int, dev: int) -> int:
+    if seen.dtype != torch.int64 or seen.shape != (B, T, (T + 63) // 64) \
+            or not seen.is_contiguous():
+        raise ThinError(THIN_EINVAL, "seen must be contiguous int64 [B,T,ceil(T/64)]")
+    return _on(seen, dev, "seen")
+
+
+def thin_q4_tree_attention(Q: torch.Tensor, cache: Q4Cache, at: torch.Tensor, seen: torch.Tensor,
+                           *, count: Optional[torch.Tensor] = None,
+                           O: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of drafts Q [B,q_heads,T,d], T <= 1024, whose rows are at[b] + t of the cache,
+    over the rows before at[b] and the drafts of their masks seen int64 [B,T,ceil(T/64)]
+    (thin_q4_tree, or any other).  Padding (t >= count[b]) and drafts that see nothing give
+    rows of zeros."""
+    dev, st = _where(stream)
+    ref = cache._at(dev)
+    q, qs, Hq, T = _queries(Q, cache, dev)
+    B, H = cache.B, cache.H
+    if T > MAX_DRAFTS:
+        raise ThinError(THIN_EINVAL, f"at most {MAX_DRAFTS} drafts")
+    need = _attention_bytes(B, H, Hq, cache.n_max, cache.d, T, 0)
+    if O is None:
+        O = _empty_like(Q, dev, stream)
+        o, os_ = O.data_ptr(), None
+    else:
+        o, os_ = _output(O, Q, dev)
+    ws, wp, wn = _workspace(workspace, need, dev, stream)
+    _check(lib().thin_q4_tree_attention(ref, q, qs, Hq, _dtype(Q, "Q"), T,
+                                        _ints(at, (B,), dev, "at"),
+                                        _ints(count, (B,), dev, "count"),
+                                        _masks(seen, B, T, dev), o, os_, wp, wn, st),
+           "thin_q4_tree_attention")
+    return O
+
+
+def thin_q4_keep(cache: Q4Cache, at: torch.Tensor, path: torch.Tensor, *,
+                 end: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Rows at[b] + path[b,i] of the cache become rows at[b] + i (path int32 [B,P], P <= 1024,
+    an accepted path of drafts, the first negative entry behind its last).  Returns end int32
+    [B], the rows that every sequence then has: the next call's `at`."""
+    dev, st = _where(stream)
+    ref = cache._at(dev)
+    if path.dim() != 2:
+        raise ThinError(THIN_EINVAL, "path must be int32 [B,P]")
+    B, P = cache.B, path.shape[1]
+    if end is None:
+        end = _empty((B,), torch.int32, dev, stream)
+    _check(lib().thin_q4_keep(ref, _ints(at, (B,), dev, "at"), _ints(path, (B, P), dev, "path"), P,
+                              _ints(end, (B,), dev, "end"), st), "thin_q4_keep")
+    return end
