@@ -254,6 +254,38 @@ int thin_attention_ex(const void* Q, const void* K, const void* V, int32_t dtype
                       void* stream);
 
 /*
+ * The gradient of thin_attention_ex (of thin_attention with logw NULL): of a scalar whose
+ * gradient with respect to O is dO, those with respect to Q, K, V and logw.  With p the
+ * probabilities of a query over its slice's coreset and g_j = <dO[s,q], V[s,I_j]>,
+ *   ds_j = p_j (g_j - sum_i p_i g_i),   dQ[s,q] = sum_j ds_j K[s,I_j] / sqrt d,
+ *   dK[s,I_j] = sum_q ds_j Q[s,q] / sqrt d,   dV[s,I_j] = sum_q p_j dO[s,q],
+ *   dlogw[s,j] = sum_q ds_j.
+ * Neither O nor any statistic of the forward is read: probabilities are formed anew.
+ *   dO      (device) [B,H,n_q,d] of out_dtype (either type, whatever dtype is).
+ *   dQ      (device) [B,H,n_q,d] of `dtype`.
+ *   dK, dV  (device) [B,H,n,d] of `dtype`: every row is written, zeros for rows that the coreset
+ *           does not list; a row listed twice gets the sum of both.
+ *   dlogw   (device, nullable) float32 [B,H,n_out], one per place of the list.
+ *   workspace (device) at least *workspace_bytes of thin_attention_backward_plan, 256-byte
+ *           aligned; contents on entry are irrelevant.  Calls that may run at the same time need
+ *           workspaces of their own.
+ * A key of log-weight -inf is not there, whatever its rows hold (its gradients are 0), nor is an
+ * entry of idx outside [0, n); a query without any key has a gradient of 0 and gives none.
+ * Outputs overlap no input and no other output.  Rows are 16-byte aligned.  Sums are in float32,
+ * in an order that depends on the sizes only: the same call gives the same bits.  bf16 rows:
+ * p and ds round to bf16 before the products with rows (not before dlogw's sum).
+ * B*H*n_q <= 2^29, B*H*n_out <= 2^25.
+ * Errors: THIN_EINVAL, THIN_EDTYPE, THIN_EWORKSPACE, THIN_EHIP.
+ */
+int thin_attention_backward_plan(int32_t dtype, int64_t B, int64_t H, int64_t n_q, int64_t n,
+                                 int64_t d, int64_t n_out, size_t* workspace_bytes);
+int thin_attention_backward(const void* Q, const void* K, const void* V, int32_t dtype, int64_t B,
+                            int64_t H, int64_t n_q, int64_t n, int64_t d, const int32_t* idx,
+                            const float* logw, int64_t n_out, const void* dO, int32_t out_dtype,
+                            void* dQ, void* dK, void* dV, float* dlogw, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
  * Thinformer decoding over an Express cache (Sec. 3-4: Alg. 1 Express with
  * Compress2 of Alg. 2 in its thin phase, Alg. 4 Thinformer, Alg. 5
  * WtdAttention), for all B*H slices in lockstep.  Point t (t = 0, 1, ...) of
@@ -641,8 +673,8 @@ int thin_workspace_status(const void* workspace, int32_t* status, void* stream);
  * of the compute contract; the library keeps no state between calls apart
  * from it).  While a hook is set,
  * every kernel launch made by thin_compress, thin_compress_traced,
- * thin_compress_ex, thin_attention, thin_attention_ex, thin_express_step,
- * thin_rotary, thin_rotary_axes and the thin_q4_* calls is bracketed by two calls on the
+ * thin_compress_ex, thin_attention, thin_attention_ex, thin_attention_backward,
+ * thin_express_step, thin_rotary, thin_rotary_axes and the thin_q4_* calls is bracketed by two calls on the
  * calling thread:
  * hook(ctx, kernel, round, 0, stream) right before the launch is enqueued and
  * hook(ctx, kernel, round, 1, stream) right after.  The hook may enqueue
@@ -678,7 +710,8 @@ typedef enum {
   THIN_KERNEL_Q4_SELECT = 15,  /* block scores and choice                 */
   THIN_KERNEL_Q4_ATTENTION = 16, /* attention over the 4-bit cache, joins */
   THIN_KERNEL_Q4_TREE = 17,    /* masks and positions of drafts           */
-  THIN_KERNEL_Q4_KEEP = 18     /* accepted drafts' rows                   */
+  THIN_KERNEL_Q4_KEEP = 18,    /* accepted drafts' rows                   */
+  THIN_KERNEL_ATTENTION_GRAD = 19 /* gradient of coreset attention, join  */
 } thin_kernel_t;
 typedef void (*thin_launch_hook_t)(void* ctx, int32_t kernel, int32_t round, int32_t phase,
                                    void* stream);

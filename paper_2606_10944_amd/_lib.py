@@ -23,7 +23,8 @@ THIN_STATUS_WAIT_EXHAUSTED = 1
 
 # Every symbol include/thin.h declares.
 EXPORTS = ("thin_plan", "thin_compress", "thin_compress_static", "thin_compress_traced", "thin_compress_ex", "thin_attention",
-           "thin_attention_ex", "thin_express_plan", "thin_express_create", "thin_express_step",
+           "thin_attention_ex", "thin_attention_backward_plan", "thin_attention_backward",
+           "thin_express_plan", "thin_express_create", "thin_express_step",
            "thin_express_cache", "thin_express_next", "thin_express_destroy",
            "thin_express_prefill_plan", "thin_express_prefill",
            "thin_rotary", "thin_rotary_axes", "thin_rotary_turns", "thin_q4_store", "thin_q4_load",
@@ -36,7 +37,8 @@ EXPORTS = ("thin_plan", "thin_compress", "thin_compress_static", "thin_compress_
 KERNEL_NAMES = {0: "trace_clear", 1: "subsample", 2: "fill", 3: "vmax", 4: "scores",
                 5: "decide", 6: "attention", 7: "local", 8: "uniform", 9: "assemble",
                 10: "express", 11: "status", 12: "rotary", 13: "q4_store", 14: "q4_load",
-                15: "q4_select", 16: "q4_attention", 17: "q4_tree", 18: "q4_keep"}
+                15: "q4_select", 16: "q4_attention", 17: "q4_tree", 18: "q4_keep",
+                19: "attention_grad"}
 HALVE = {"kh": 0, "uniform": 1}  # thin_halve_t
 LaunchHook = C.CFUNCTYPE(None, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p)
 
@@ -102,6 +104,9 @@ def lib():
                                    C.POINTER(CompressOpts), P, I64, P]
     L.thin_attention.argtypes = [P, P, P, I32, I64, I64, I64, I64, I64, P, I64, P, I32, P]
     L.thin_attention_ex.argtypes = [P, P, P, I32, I64, I64, I64, I64, I64, P, P, I64, P, I32, P]
+    L.thin_attention_backward_plan.argtypes = [I32, I64, I64, I64, I64, I64, I64, C.POINTER(SZ)]
+    L.thin_attention_backward.argtypes = [P, P, P, I32, I64, I64, I64, I64, I64, P, P, I64, P, I32,
+                                          P, P, P, P, P, SZ, P]
     L.thin_express_plan.argtypes = [I64, I64, I64, I64, I32, I64, C.POINTER(ExpressPlan)]
     L.thin_express_create.argtypes = [I32, I64, I64, I64, I64, I32, C.c_double, I32, I64, P, SZ,
                                       C.POINTER(C.c_void_p)]
@@ -135,7 +140,8 @@ def lib():
     L.thin_set_launch_hook.restype = C.c_int
     for f in ("thin_plan", "thin_compress", "thin_compress_static", "thin_compress_traced",
               "thin_compress_ex",
-              "thin_attention", "thin_attention_ex", "thin_selftest_gram16", "thin_express_plan",
+              "thin_attention", "thin_attention_ex", "thin_attention_backward_plan",
+              "thin_attention_backward", "thin_selftest_gram16", "thin_express_plan",
               "thin_express_create", "thin_express_step", "thin_express_cache",
               "thin_express_next", "thin_express_destroy", "thin_express_prefill_plan",
               "thin_express_prefill", "thin_workspace_status", "thin_rotary", "thin_rotary_axes",

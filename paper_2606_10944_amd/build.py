@@ -9,7 +9,7 @@ SO = os.path.join(HERE, "libthin.so")
 SOURCES = ["csrc/compress.hip", "csrc/attention.hip", "csrc/express.hip", "csrc/api.cpp",
            "csrc/noalloc.hip", "csrc/rotary.hip", "csrc/q4_cache.hip", "csrc/q4_attention.hip",
            "csrc/q4_prompt.hip",
-           "csrc/api_q4.cpp"]
+           "csrc/api_q4.cpp", "csrc/attention_grad.hip", "csrc/api_grad.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # no packed fp32 instructions in device code

@@ -1,0 +1,728 @@
+// The gradient of coreset attention on gfx950.  With z_qj = <q, k_j> / sqrt(d) + lw_j,
+// p = softmax_j(z) and g_qj = <do_q, v_j>:
+//   ds_qj = p_qj (g_qj - sum_i p_qi g_qi),       dlw_j = sum_q ds_qj,
+//   dq = sum_j ds_qj k_j / sqrt(d),   dk_j = sum_q ds_qj q / sqrt(d),   dv_j = sum_q p_qj do_q.
+// Probabilities are formed anew from the queries and keys; the sum p g of a row too, so
+// neither the forward's output nor its statistics are read.
+//
+// Up to 256 coreset rows (float32: 128) a workgroup holds every key of a slice, 16 or 32 per
+// wave, and walks a range of its queries, 32 at a time: one launch reads Q and dO once and
+// writes dQ, and the sums of dK and dV stay in registers.  Wider coresets take a launch that
+// owns query rows (statistics, then dQ), and the same walk per chunk of keys for dK and dV.
+// Workgroups leave their sums of dK and dV for the join, which adds them in order.
+//
+// Types.  bf16 rows: bf16 products summed in float32; p and ds round to bf16 (half a step, as
+// the gradients' own rounding) for the products over queries and over keys; a float32 dO is
+// two bf16 parts (17 bits) in g, so that dlw, a float32 sum of differences, keeps them, and
+// one in dv, which rounds to bf16 itself.  float32 rows: float32 products throughout.
+#include <math.h>
+
+#include <algorithm>
+
+#include "common.hpp"
+#include "grad.hpp"
+#include "q4_device.hpp"
+
+namespace thin {
+
+namespace {
+
+constexpr int QT = (int)kGradTile;
+constexpr float kLeast = -3.0e38f;
+constexpr double kLog2e = 1.44269504088896340736;
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+
+// Rows of D elements of T in LDS.  32 bytes past the row put rows that lanes read together on
+// different banks, in both ways of reading.
+template <typename T, int D>
+struct LdsRows {
+  static constexpr int CW = D * Elem<T>::bytes / 16;  // words per row
+  static constexpr int stride = D * Elem<T>::bytes + 32;
+};
+
+// Word v of this lane's row fragment (row m, word 4 v + g) of a tile of 16 rows.
+template <typename T, int D>
+__device__ __forceinline__ uint4 lds_word(const unsigned char* rows, int v, int m, int g) {
+  return *reinterpret_cast<const uint4*>(rows + m * LdsRows<T, D>::stride + (4 * v + g) * 16);
+}
+
+// Column 16 dt + m of rows 4 g .. 4 g + 3 and 16 + 4 g .. (of 32 rows `stride` bytes apart).
+__device__ __forceinline__ bf16x8_t lds_columns(const unsigned char* rows, int stride, int dt,
+                                                int m, int g) {
+  typedef __attribute__((address_space(3))) s16x4_t lds_t;
+  unsigned char* from =
+      const_cast<unsigned char*>(rows) + (4 * g + m / 4) * stride + dt * 32 + m % 4 * 8;
+  const s16x4_t v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)from);
+  const s16x4_t v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)(from + 16 * stride));
+  return __builtin_bit_cast(bf16x8_t,
+                            (s16x8_t)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+__device__ __forceinline__ bf16x8_t pack8(const float* a, const float* b) {
+  return __builtin_bit_cast(bf16x8_t, (u32x4){cvt_pk_bf16(a[0], a[1]), cvt_pk_bf16(a[2], a[3]),
+                                              cvt_pk_bf16(b[0], b[1]), cvt_pk_bf16(b[2], b[3])});
+}
+
+// acc (channels 16 dt + 4 g .. x a column per lane m) += rows^T w over 32 rows: w holds this
+// lane's column of rows 4 g .. 4 g + 3 (w[0]) and 16 + 4 g .. (w[1]).
+template <typename T>
+struct Weights;
+template <>
+struct Weights<bf16_t> {
+  bf16x8_t p;
+  __device__ __forceinline__ Weights(const float (*w)[4]) : p(pack8(w[0], w[1])) {}
+  __device__ __forceinline__ floatx4_t times(const unsigned char* rows, int stride, int dt, int m,
+                                             int g, floatx4_t acc) const {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_columns(rows, stride, dt, m, g), p, acc, 0,
+                                                   0, 0);
+  }
+};
+template <>
+struct Weights<float> {
+  float p[2][4];
+  __device__ __forceinline__ Weights(const float (*w)[4]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[i][j] = w[i][j];
+  }
+  __device__ __forceinline__ floatx4_t times(const unsigned char* rows, int stride, int dt, int m,
+                                             int g, floatx4_t acc) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float x = *reinterpret_cast<const float*>(rows + (16 * i + 4 * g + j) * stride +
+                                                        (16 * dt + m) * 4);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[i][j], acc, 0, 0, 0);
+      }
+    return acc;
+  }
+};
+
+// A 16-byte word of T from a row of TO (elements e .. of it), and what bf16 leaves of float32
+// (OP = 2 parts).
+template <typename T, typename TO>
+struct Parts {
+  static constexpr int n = Elem<T>::bytes == 2 && Elem<TO>::bytes == 4 ? 2 : 1;
+};
+template <typename T, typename TO>
+struct RawWord;  // as it is in memory
+template <>
+struct RawWord<bf16_t, bf16_t> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const u32x4*>(p); }
+  __device__ __forceinline__ void clear() { w = (u32x4){0, 0, 0, 0}; }
+  __device__ __forceinline__ void parts(u32x4* o) const { o[0] = w; }
+};
+template <>
+struct RawWord<float, float> {
+  u32x4 w;
+  __device__ __forceinline__ void load(const float* p) { w = *reinterpret_cast<const u32x4*>(p); }
+  __device__ __forceinline__ void clear() { w = (u32x4){0, 0, 0, 0}; }
+  __device__ __forceinline__ void parts(u32x4* o) const { o[0] = w; }
+};
+template <>
+struct RawWord<float, bf16_t> {
+  uint2 w;
+  __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void clear() { w = make_uint2(0, 0); }
+  __device__ __forceinline__ void parts(u32x4* o) const {
+    o[0] = (u32x4){w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
+  }
+};
+template <>
+struct RawWord<bf16_t, float> {
+  u32x4 w[2];
+  __device__ __forceinline__ void load(const float* p) {
+    w[0] = *reinterpret_cast<const u32x4*>(p);
+    w[1] = *reinterpret_cast<const u32x4*>(p + 4);
+  }
+  __device__ __forceinline__ void clear() { w[0] = w[1] = (u32x4){0, 0, 0, 0}; }
+  __device__ __forceinline__ void parts(u32x4* o) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a = __uint_as_float(w[i / 2][i % 2 * 2]);
+      const float b = __uint_as_float(w[i / 2][i % 2 * 2 + 1]);
+      o[0][i] = cvt_pk_bf16(a, b);
+      o[1][i] = cvt_pk_bf16(a - __uint_as_float(o[0][i] << 16),
+                            b - __uint_as_float(o[0][i] & 0xffff0000u));
+    }
+  }
+};
+
+// Four consecutive channels of a gradient.
+template <typename T>
+__device__ __forceinline__ void store4(T* p, floatx4_t o) {
+  if constexpr (Elem<T>::bytes == 2)
+    *reinterpret_cast<uint2*>(p) = make_uint2(cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]));
+  else
+    *reinterpret_cast<floatx4_t*>(p) = o;
+}
+
+// Coreset row j of slice s: its row of K and V (-1: none, or its weight is 0) and log-weight to
+// base 2.
+__device__ __forceinline__ int coreset_row(const GradArgs& a, int64_t s, int64_t j, float* bias) {
+  *bias = -INFINITY;
+  if (j >= a.n_out) return -1;
+  const int32_t r = a.idx[s * a.n_out + j];
+  const float lw = a.logw ? a.logw[s * a.n_out + j] : 0.0f;
+  if (r < 0 || r >= a.n || lw == -INFINITY) return -1;
+  *bias = lw * (float)kLog2e;
+  return r;
+}
+
+// ---------------------------------------------------------------------------
+// Keys: see above.  W waves of 16 KT keys.  ONE: every key of the slice is here.
+//
+// Lanes are l = 16 g + m.  Scores S = Q K^T by 16 queries x 16 keys: lane (m, g) holds queries
+// 4 g .. 4 g + 3 of key m, which is what the products over queries want as their second
+// operand; their first, the columns of Q and dO, come from LDS by the transposing read.  ds
+// passes through LDS, [key, query], from where every wave takes its 16 channels of dQ.
+// ---------------------------------------------------------------------------
+template <typename T, typename TO, int D, int W, int KT, bool ONE>
+__global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
+  using R = LdsRows<T, D>;
+  constexpr int NV = Frag<T, D>::NV, DT = D / 16, NK = 16 * W * KT;
+  constexpr int OP = Parts<T, TO>::n, E = 16 / Elem<T>::bytes;
+  constexpr int PLANE = QT * R::stride;
+  constexpr int IT = (QT * R::CW + 64 * W - 1) / (64 * W);  // words of a tile per thread
+  constexpr int SS = Elem<T>::bytes == 2 ? 96 : 144;        // bytes per key of ds in LDS
+  // dQ: a wave's units are (16 channels, 16 queries), 2 DT of them in all
+  constexpr int U = 2 * DT >= W ? 2 * DT / W : 1, SL = U > 1 ? U / 2 : 1;
+  __shared__ __align__(16) unsigned char tile_[2][1 + OP][PLANE];
+  __shared__ __align__(16) unsigned char ds_[ONE ? NK * SS : 16];
+  __shared__ __align__(16) float st[ONE ? W : 1][3][QT];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = lane & 15, g = lane >> 4;
+  const int part = blockIdx.x % a.shape.parts, chunk = blockIdx.x / a.shape.parts % a.shape.chunks;
+  const int64_t s = blockIdx.x / (a.shape.parts * a.shape.chunks);
+  const int64_t steps = (a.n_q + QT - 1) / QT;
+  const int64_t t0 = (int64_t)part * a.shape.run, t1 = std::min(steps, t0 + a.shape.run);
+  const T* Q = static_cast<const T*>(a.Q) + s * a.n_q * D;
+  const TO* dO = static_cast<const TO*>(a.dO) + s * a.n_q * D;
+  const T* K = static_cast<const T*>(a.K) + s * a.n * D;
+  const T* V = static_cast<const T*>(a.V) + s * a.n * D;
+
+  RawWord<T, T> rq[IT];
+  RawWord<T, TO> ro[IT];
+  auto load = [&](int64_t t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int item = i * 64 * W + (int)threadIdx.x;
+      const int64_t r = t * QT + item / R::CW;
+      if (item < QT * R::CW && t < t1 && r < a.n_q) {
+        rq[i].load(Q + r * D + item % R::CW * E);
+        ro[i].load(dO + r * D + item % R::CW * E);
+      } else {
+        rq[i].clear();
+        ro[i].clear();
+      }
+    }
+  };
+  auto put = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int item = i * 64 * W + (int)threadIdx.x;
+      if (item >= QT * R::CW) continue;
+      const int to = item / R::CW * R::stride + item % R::CW * 16;
+      u32x4 w[2];
+      rq[i].parts(w);
+      *reinterpret_cast<u32x4*>(tile_[buf][0] + to) = w[0];
+      ro[i].parts(w);
+#pragma unroll
+      for (int p = 0; p < OP; ++p) *reinterpret_cast<u32x4*>(tile_[buf][1 + p] + to) = w[p];
+    }
+  };
+  load(t0);
+
+  // this wave's keys
+  uint4 kf[KT][NV], vf[KT][NV];
+  float bias[KT];
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    const int r = coreset_row(a, s, (int64_t)chunk * NK + (wave * KT + kt) * 16 + m, &bias[kt]);
+    load_frag<T, D>(K, r, g, r >= 0, kf[kt]);
+    load_frag<T, D>(V, r, g, r >= 0, vf[kt]);
+  }
+  // columns of every key for dQ: channel 16 dt + m of keys 32 x + 4 g .. and 32 x + 16 + 4 g ..
+  float bc[Elem<T>::bytes == 4 && ONE ? SL : 1][NK / 32][2][4];
+  bf16x8_t kc[SL][NK / 32];
+  const int unit0 = wave * U;
+  const bool has_unit = unit0 < 2 * DT;
+  if (ONE && has_unit) {
+#pragma unroll
+    for (int x = 0; x < NK / 32; ++x) {
+      float f[SL][2][4];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float b;
+        const int r = coreset_row(a, s, 32 * x + i / 4 * 16 + 4 * g + i % 4, &b);
+#pragma unroll
+        for (int y = 0; y < SL; ++y)
+          f[y][i / 4][i % 4] =
+              r >= 0 ? elem<T>(K + (int64_t)r * D, 16 * (unit0 / 2 + y) + m) : 0.0f;
+      }
+#pragma unroll
+      for (int y = 0; y < SL; ++y) {
+        if constexpr (Elem<T>::bytes == 2) {
+          kc[y][x] = pack8(f[y][0], f[y][1]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) bc[y][x][i / 4][i % 4] = f[y][i / 4][i % 4];
+        }
+      }
+    }
+  }
+  put(0);
+  load(t0 + 1);
+
+  floatx4_t ak[KT][DT], av[KT][DT];
+  float aw[KT];
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    aw[kt] = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) ak[kt][dt] = av[kt][dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+  }
+  const float c2 = (float)(kLog2e / sqrt((double)D)), rd = (float)(1.0 / sqrt((double)D));
+
+  // this workgroup's share of the zeros of dK and dV, in 16-byte words, and of a step
+  const int64_t words = a.n * D / E;
+  const int64_t zs = (words + a.shape.parts - 1) / a.shape.parts;
+  int64_t z = chunk == 0 ? part * zs : words;
+  const int64_t z1 = std::min(words, z + zs);
+  const int64_t zrun = (zs + (t1 - t0) - 1) / (t1 - t0);
+  auto zeros = [&](int64_t n) __attribute__((always_inline)) {
+    const int64_t end = std::min(z1, z + n);
+    for (int64_t i = z + threadIdx.x; i < end; i += 64 * W) {
+      reinterpret_cast<u32x4*>(static_cast<T*>(a.dK) + s * a.n * D)[i] = (u32x4){0, 0, 0, 0};
+      reinterpret_cast<u32x4*>(static_cast<T*>(a.dV) + s * a.n * D)[i] = (u32x4){0, 0, 0, 0};
+    }
+    z = std::max(z, end);
+  };
+
+  // dQ of the step before from its ds
+  auto queries = [&](int64_t t) __attribute__((always_inline)) {
+    if (!has_unit) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int dt = (unit0 + u) / 2, tq = (unit0 + u) % 2;
+      floatx4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < NK / 32; ++x) {
+        if constexpr (Elem<T>::bytes == 2) {
+          o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              kc[u / 2][x], lds_columns(ds_ + 32 * x * SS, SS, tq, m, g), o, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            o = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                bc[u / 2][x][i / 4][i % 4],
+                *reinterpret_cast<const float*>(ds_ + (32 * x + i / 4 * 16 + 4 * g + i % 4) * SS +
+                                                (16 * tq + m) * 4),
+                o, 0, 0, 0);
+        }
+      }
+      const int64_t r = t * QT + 16 * tq + m;
+      if (r < a.n_q)
+        store4<T>(static_cast<T*>(a.dQ) + (s * a.n_q + r) * D + 16 * dt + 4 * g, o * rd);
+    }
+  };
+
+  __syncthreads();
+  for (int64_t t = t0; t < t1; ++t) {
+    const int buf = (int)(t - t0) & 1;
+    // scores and g: [query 16 tq + 4 g + j, key m]
+    float p[KT][2][4], gd[KT][2][4];
+#pragma unroll
+    for (int tq = 0; tq < 2; ++tq) {
+      floatx4_t zs_[KT], zg[KT];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) zs_[kt] = zg[kt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const uint4 qw = lds_word<T, D>(tile_[buf][0] + 16 * tq * R::stride, v, m, g);
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) zs_[kt] = mma_word<T>(qw, kf[kt][v], zs_[kt]);
+#pragma unroll
+        for (int o = OP - 1; o >= 0; --o) {
+          const uint4 ow = lds_word<T, D>(tile_[buf][1 + o] + 16 * tq * R::stride, v, m, g);
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt) zg[kt] = mma_word<T>(ow, vf[kt][v], zg[kt]);
+        }
+      }
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          p[kt][tq][j] = fmaf(zs_[kt][j], c2, bias[kt]);
+          gd[kt][tq][j] = zg[kt][j];
+        }
+    }
+    float f[2][4], dm[2][4];  // a row's factor and sum p g
+    if (ONE) {
+      float mw[2][4];
+      auto add = [](float x, float y) { return x + y; };
+#pragma unroll
+      for (int tq = 0; tq < 2; ++tq)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float x = p[0][tq][j];
+#pragma unroll
+          for (int kt = 1; kt < KT; ++kt) x = fmaxf(x, p[kt][tq][j]);
+          x = row_reduce(fmaxf(x, kLeast), [](float x, float y) { return fmaxf(x, y); });
+          float l = 0.0f, e = 0.0f;
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt) {
+            p[kt][tq][j] = __builtin_amdgcn_exp2f(p[kt][tq][j] - x);
+            l += p[kt][tq][j];
+            e = fmaf(p[kt][tq][j], gd[kt][tq][j], e);
+          }
+          mw[tq][j] = x;
+          f[tq][j] = row_reduce(l, add);
+          dm[tq][j] = row_reduce(e, add);
+        }
+      if (m == 0) {
+#pragma unroll
+        for (int tq = 0; tq < 2; ++tq) {
+          *reinterpret_cast<floatx4_t*>(&st[wave][0][16 * tq + 4 * g]) =
+              (floatx4_t){mw[tq][0], mw[tq][1], mw[tq][2], mw[tq][3]};
+          *reinterpret_cast<floatx4_t*>(&st[wave][1][16 * tq + 4 * g]) =
+              (floatx4_t){f[tq][0], f[tq][1], f[tq][2], f[tq][3]};
+          *reinterpret_cast<floatx4_t*>(&st[wave][2][16 * tq + 4 * g]) =
+              (floatx4_t){dm[tq][0], dm[tq][1], dm[tq][2], dm[tq][3]};
+        }
+      }
+      if (t > t0) queries(t - 1);
+      zeros(zrun);
+      __syncthreads();
+      // the waves' statistics under one maximum
+#pragma unroll
+      for (int tq = 0; tq < 2; ++tq) {
+        floatx4_t mx = *reinterpret_cast<const floatx4_t*>(&st[0][0][16 * tq + 4 * g]);
+#pragma unroll
+        for (int w = 1; w < W; ++w) {
+          const floatx4_t x = *reinterpret_cast<const floatx4_t*>(&st[w][0][16 * tq + 4 * g]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) mx[j] = fmaxf(mx[j], x[j]);
+        }
+        floatx4_t l = {0.f, 0.f, 0.f, 0.f}, e = l;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          const floatx4_t x = *reinterpret_cast<const floatx4_t*>(&st[w][0][16 * tq + 4 * g]);
+          const floatx4_t y = *reinterpret_cast<const floatx4_t*>(&st[w][1][16 * tq + 4 * g]);
+          const floatx4_t v = *reinterpret_cast<const floatx4_t*>(&st[w][2][16 * tq + 4 * g]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float k = __builtin_amdgcn_exp2f(x[j] - mx[j]);
+            l[j] = fmaf(y[j], k, l[j]);
+            e[j] = fmaf(v[j], k, e[j]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float inv = l[j] > 0.0f ? 1.0f / l[j] : 0.0f;
+          f[tq][j] = __builtin_amdgcn_exp2f(mw[tq][j] - mx[j]) * inv;
+          dm[tq][j] = e[j] * inv;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int tq = 0; tq < 2; ++tq)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int64_t r = t * QT + 16 * tq + 4 * g + j;
+          // (rows past the last: probabilities of 0)
+          const float lse = r < a.n_q ? a.stats[s * a.n_q + r] : INFINITY;
+          dm[tq][j] = r < a.n_q ? a.stats[(a.S + s) * a.n_q + r] : 0.0f;
+          f[tq][j] = 1.0f;
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt)
+            p[kt][tq][j] = __builtin_amdgcn_exp2f(p[kt][tq][j] - lse);
+        }
+      zeros(zrun);
+    }
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      float ds[2][4];
+#pragma unroll
+      for (int tq = 0; tq < 2; ++tq)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          p[kt][tq][j] *= f[tq][j];
+          ds[tq][j] = p[kt][tq][j] * (gd[kt][tq][j] - dm[tq][j]);
+          aw[kt] += ds[tq][j];
+        }
+      if (ONE) {
+        unsigned char* to = ds_ + ((wave * KT + kt) * 16 + m) * SS;
+#pragma unroll
+        for (int tq = 0; tq < 2; ++tq) {
+          if constexpr (Elem<T>::bytes == 2)
+            *reinterpret_cast<uint2*>(to + (16 * tq + 4 * g) * 2) =
+                make_uint2(cvt_pk_bf16(ds[tq][0], ds[tq][1]), cvt_pk_bf16(ds[tq][2], ds[tq][3]));
+          else
+            *reinterpret_cast<floatx4_t*>(to + (16 * tq + 4 * g) * 4) =
+                (floatx4_t){ds[tq][0], ds[tq][1], ds[tq][2], ds[tq][3]};
+        }
+      }
+      const Weights<T> wp(p[kt]), ws(ds);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        av[kt][dt] = wp.times(tile_[buf][1], R::stride, dt, m, g, av[kt][dt]);
+        ak[kt][dt] = ws.times(tile_[buf][0], R::stride, dt, m, g, ak[kt][dt]);
+      }
+    }
+    put(buf ^ 1);
+    load(t + 2);
+    __syncthreads();
+  }
+  if (ONE) queries(t1 - 1);
+  zeros(z1);
+
+  float* out = a.part + (int64_t)blockIdx.x * NK * 2 * D;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) {
+    const int key = (wave * KT + kt) * 16 + m;
+    float* o = out + (int64_t)key * 2 * D + 4 * g;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      *reinterpret_cast<floatx4_t*>(o + 16 * dt) = ak[kt][dt];
+      *reinterpret_cast<floatx4_t*>(o + D + 16 * dt) = av[kt][dt];
+    }
+    if (a.part_w) {
+      const float w = across_rows(aw[kt], true, [](float x, float y) { return x + y; });
+      if (g == 0) a.part_w[(int64_t)blockIdx.x * NK + key] = w;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Rows, for coresets wider than a workgroup holds: a wave takes 16 queries and walks the keys
+// twice, for the rows' statistics, then for dQ.  Scores S^T = K Q^T: lane (m, g) holds keys
+// 4 g .. 4 g + 3 of query m.
+// ---------------------------------------------------------------------------
+constexpr int RW = 4;  // waves
+
+template <typename T, typename TO, int D>
+__global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
+  using R = LdsRows<T, D>;
+  constexpr int NV = Frag<T, D>::NV, DT = D / 16, OP = Parts<T, TO>::n, E = 16 / Elem<T>::bytes;
+  constexpr int CK = 32;  // keys per step
+  __shared__ __align__(16) unsigned char sk[CK * R::stride], sv[CK * R::stride];
+  __shared__ float sb[CK];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
+  const int64_t blocks = (a.n_q + 16 * RW - 1) / (16 * RW);
+  const int64_t s = blockIdx.x / blocks;
+  const int64_t r = (blockIdx.x % blocks * RW + wave) * 16 + m;  // this lane's query
+  const bool there = r < a.n_q;
+  uint4 qf[NV], of[OP][NV];
+  load_frag<T, D>(static_cast<const T*>(a.Q), s * a.n_q + r, g, there, qf);
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    RawWord<T, TO> w;
+    w.clear();
+    if (there) w.load(static_cast<const TO*>(a.dO) + (s * a.n_q + r) * D + (4 * v + g) * E);
+    u32x4 x[2];
+    w.parts(x);
+#pragma unroll
+    for (int p = 0; p < OP; ++p) of[p][v] = __builtin_bit_cast(uint4, x[p]);
+  }
+  const T* K = static_cast<const T*>(a.K) + s * a.n * D;
+  const T* V = static_cast<const T*>(a.V) + s * a.n * D;
+  const float c2 = (float)(kLog2e / sqrt((double)D)), rd = (float)(1.0 / sqrt((double)D));
+  auto stage = [&](int64_t k0) __attribute__((always_inline)) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < CK * R::CW; i += 64 * RW) {
+      float b;
+      const int row = coreset_row(a, s, k0 + i / R::CW, &b);
+      u32x4 kw = {0, 0, 0, 0}, vw = kw;
+      if (row >= 0) {
+        kw = reinterpret_cast<const u32x4*>(K + (int64_t)row * D)[i % R::CW];
+        vw = reinterpret_cast<const u32x4*>(V + (int64_t)row * D)[i % R::CW];
+      }
+      const int to = i / R::CW * R::stride + i % R::CW * 16;
+      *reinterpret_cast<u32x4*>(sk + to) = kw;
+      *reinterpret_cast<u32x4*>(sv + to) = vw;
+      if (i % R::CW == 0) sb[i / R::CW] = b;
+    }
+    __syncthreads();
+  };
+  auto products = [&](float (&p)[2][4], float (&gd)[2][4]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      floatx4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        x = mma_word<T>(lds_word<T, D>(sk + 16 * kt * R::stride, v, m, g), qf[v], x);
+        const uint4 vw = lds_word<T, D>(sv + 16 * kt * R::stride, v, m, g);
+#pragma unroll
+        for (int o = OP - 1; o >= 0; --o) y = mma_word<T>(vw, of[o][v], y);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        p[kt][j] = fmaf(x[j], c2, sb[16 * kt + 4 * g + j]);
+        gd[kt][j] = y[j];
+      }
+    }
+  };
+  float mx = kLeast, l = 0.0f, e = 0.0f;
+  for (int64_t k0 = 0; k0 < a.n_out; k0 += CK) {
+    stage(k0);
+    float p[2][4], gd[2][4];
+    products(p, gd);
+    float x = mx;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x = fmaxf(x, p[i / 4][i % 4]);
+    const float k = __builtin_amdgcn_exp2f(mx - x);
+    mx = x;
+    l *= k;
+    e *= k;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float w = __builtin_amdgcn_exp2f(p[i / 4][i % 4] - mx);
+      l += w;
+      e = fmaf(w, gd[i / 4][i % 4], e);
+    }
+  }
+  auto add = [](float x, float y) { return x + y; };
+  const float top = across_rows(mx, true, [](float x, float y) { return fmaxf(x, y); });
+  const float k = __builtin_amdgcn_exp2f(mx - top);
+  l = across_rows(l * k, true, add);
+  e = across_rows(e * k, true, add);
+  // a row that no key weighs in: probabilities of 0
+  const float lse = l > 0.0f ? top + __builtin_amdgcn_logf(l) : INFINITY;
+  const float dm = l > 0.0f ? e / l : 0.0f;
+  if (there && g == 0) {
+    a.stats[s * a.n_q + r] = lse;
+    a.stats[(a.S + s) * a.n_q + r] = dm;
+  }
+  floatx4_t acc[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) acc[dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+  for (int64_t k0 = 0; k0 < a.n_out; k0 += CK) {
+    stage(k0);
+    float p[2][4], gd[2][4];
+    products(p, gd);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      p[i / 4][i % 4] =
+          __builtin_amdgcn_exp2f(p[i / 4][i % 4] - lse) * (gd[i / 4][i % 4] - dm);
+    const Weights<T> w(p);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) acc[dt] = w.times(sk, R::stride, dt, m, g, acc[dt]);
+  }
+  if (!there) return;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+    store4<T>(static_cast<T*>(a.dQ) + (s * a.n_q + r) * D + 16 * dt + 4 * g, acc[dt] * rd);
+}
+
+// ---------------------------------------------------------------------------
+// Join: a wave adds the sums of one coreset row in the order of the queries and writes its row
+// of dK and dV.  A row that the coreset lists more than once is written by its first place,
+// with the sums of all of them.
+// ---------------------------------------------------------------------------
+template <typename T, int D>
+__global__ __launch_bounds__(256) void grad_join_kernel(GradArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t w = blockIdx.x * (int64_t)4 + (threadIdx.x >> 6);
+  if (w >= a.S * a.n_out) return;
+  const int64_t s = w / a.n_out, j = w % a.n_out;
+  const int64_t NK = a.shape.keys();
+  const int32_t* idx = a.idx + s * a.n_out;
+  auto slot = [&](int64_t i, int part) {
+    return ((s * a.shape.chunks + i / NK) * a.shape.parts + part) * NK + i % NK;
+  };
+  if (a.dlogw) {
+    float x = 0.0f;
+    for (int p = lane; p < a.shape.parts; p += 64) x += a.part_w[slot(j, p)];
+#pragma unroll
+    for (int i = 32; i > 0; i /= 2) x += __shfl_xor(x, i);
+    if (lane == 0) a.dlogw[w] = x;
+  }
+  const int32_t r = idx[j];
+  if (r < 0 || r >= a.n) return;
+  constexpr int V = 2 * D / 4;  // lanes of a row of sums, four channels each
+  floatx4_t o = {0.f, 0.f, 0.f, 0.f};
+  for (int64_t i0 = 0; i0 < a.n_out; i0 += 64) {
+    uint64_t same = __ballot(i0 + lane < a.n_out && idx[i0 + lane] == r);
+    while (same) {
+      const int64_t i = i0 + __ffsll((unsigned long long)same) - 1;
+      same &= same - 1;
+      if (i < j) return;
+      if (lane < V) {
+        const float* p = a.part + slot(i, 0) * 2 * D + lane * 4;
+#pragma unroll 4
+        for (int x = 0; x < a.shape.parts; ++x)
+          o += *reinterpret_cast<const floatx4_t*>(p + x * NK * 2 * D);
+      }
+    }
+  }
+  if (lane >= V) return;
+  const bool key = lane < D / 4;
+  if (key) o *= (float)(1.0 / sqrt((double)D));
+  store4<T>(static_cast<T*>(key ? a.dK : a.dV) + (s * a.n + r) * D + lane % (D / 4) * 4, o);
+}
+
+template <typename T, typename TO, int D, int W, int KT>
+hipError_t keys_one(const GradArgs& a, hipStream_t st) {
+  const uint32_t grid = (uint32_t)(a.S * a.shape.chunks * a.shape.parts);
+  if (a.shape.one)
+    grad_keys_kernel<T, TO, D, W, KT, true><<<grid, 64 * W, 0, st>>>(a);
+  else if constexpr (W == 8)
+    grad_keys_kernel<T, TO, D, W, KT, false><<<grid, 64 * W, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, typename TO, int D>
+hipError_t keys_d(const GradArgs& a, hipStream_t st) {
+  if (a.shape.waves == 2) return keys_one<T, TO, D, 2, 1>(a, st);
+  if (a.shape.waves == 4) return keys_one<T, TO, D, 4, 1>(a, st);
+  if constexpr (Elem<T>::bytes == 2)
+    if (a.shape.tiles == 2) return keys_one<T, TO, D, 8, 2>(a, st);
+  return keys_one<T, TO, D, 8, 1>(a, st);
+}
+
+template <typename T, typename TO, int D>
+hipError_t rows_d(const GradArgs& a, hipStream_t st) {
+  const int64_t blocks = (a.n_q + 16 * RW - 1) / (16 * RW);
+  grad_rows_kernel<T, TO, D><<<(uint32_t)(a.S * blocks), 64 * RW, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int D>
+hipError_t join_d(const GradArgs& a, hipStream_t st) {
+  grad_join_kernel<T, D><<<(uint32_t)((a.S * a.n_out + 3) / 4), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Instance F<rows, gradient of the output, head dimension> of a launch.
+#define GRAD_BY_D(F, T, TO)                   \
+  return d == 32   ? F<T, TO, 32>(a, st)      \
+         : d == 64 ? F<T, TO, 64>(a, st)      \
+                   : F<T, TO, 128>(a, st)
+#define GRAD_BY_TYPES(F)                                       \
+  if (dtype == 0 && out_dtype == 0) GRAD_BY_D(F, float, float);   \
+  if (dtype == 0) GRAD_BY_D(F, float, bf16_t);                    \
+  if (out_dtype == 0) GRAD_BY_D(F, bf16_t, float);                \
+  GRAD_BY_D(F, bf16_t, bf16_t)
+
+hipError_t launch_grad_rows(int dtype, int out_dtype, int64_t d, const GradArgs& a,
+                            hipStream_t st) {
+  GRAD_BY_TYPES(rows_d);
+}
+hipError_t launch_grad_keys(int dtype, int out_dtype, int64_t d, const GradArgs& a,
+                            hipStream_t st) {
+  GRAD_BY_TYPES(keys_d);
+}
+hipError_t launch_grad_join(int dtype, int64_t d, const GradArgs& a, hipStream_t st) {
+  Q4_BY_D(join_d, a, st);
+}
+
+}  // namespace thin
