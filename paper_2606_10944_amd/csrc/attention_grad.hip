@@ -13,8 +13,8 @@
 //
 // Types.  bf16 rows: bf16 products summed in float32; p and ds round to bf16 (half a step, as
 // the gradients' own rounding) for the products over queries and over keys; a float32 dO is
-// two bf16 parts (17 bits) in g, so that dlw, a float32 sum of differences, keeps them, and
-// one in dv, which rounds to bf16 itself.  float32 rows: float32 products throughout.
+// two bf16 parts (17 bits), so that dlw, a float32 sum of differences, keeps them.  float32
+// rows: float32 products throughout.
 #include <math.h>
 
 #include <algorithm>
@@ -65,39 +65,41 @@ __device__ __forceinline__ bf16x8_t pack8(const float* a, const float* b) {
                                               cvt_pk_bf16(b[0], b[1]), cvt_pk_bf16(b[2], b[3])});
 }
 
-// acc (channels 16 dt + 4 g .. x a column per lane m) += rows^T w over 32 rows: w holds this
-// lane's column of rows 4 g .. 4 g + 3 (w[0]) and 16 + 4 g .. (w[1]).
+// Operands of a product over 32 rows: lane (m, g) holds rows 4 g .. 4 g + 3 and 16 + 4 g .. of
+// its column: of rows in LDS (column 16 dt + m), or of values it has.
 template <typename T>
-struct Weights;
+struct Column;
 template <>
-struct Weights<bf16_t> {
-  bf16x8_t p;
-  __device__ __forceinline__ Weights(const float (*w)[4]) : p(pack8(w[0], w[1])) {}
-  __device__ __forceinline__ floatx4_t times(const unsigned char* rows, int stride, int dt, int m,
-                                             int g, floatx4_t acc) const {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_columns(rows, stride, dt, m, g), p, acc, 0,
-                                                   0, 0);
+struct Column<bf16_t> {
+  bf16x8_t x;
+  __device__ __forceinline__ Column() {}
+  __device__ __forceinline__ Column(const unsigned char* rows, int stride, int dt, int m, int g)
+      : x(lds_columns(rows, stride, dt, m, g)) {}
+  __device__ __forceinline__ Column(const float (*w)[4]) : x(pack8(w[0], w[1])) {}
+  // acc (this' columns x b's) += this^T b: lane (m, g) has columns 4 g .. 4 g + 3 of this and m
+  // of b.
+  __device__ __forceinline__ floatx4_t times(const Column& b, floatx4_t acc) const {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, b.x, acc, 0, 0, 0);
   }
 };
 template <>
-struct Weights<float> {
-  float p[2][4];
-  __device__ __forceinline__ Weights(const float (*w)[4]) {
+struct Column<float> {
+  float x[8];
+  __device__ __forceinline__ Column() {}
+  __device__ __forceinline__ Column(const unsigned char* rows, int stride, int dt, int m, int g) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) p[i][j] = w[i][j];
+    for (int i = 0; i < 8; ++i)
+      x[i] = *reinterpret_cast<const float*>(rows + (i / 4 * 16 + 4 * g + i % 4) * stride +
+                                             (16 * dt + m) * 4);
   }
-  __device__ __forceinline__ floatx4_t times(const unsigned char* rows, int stride, int dt, int m,
-                                             int g, floatx4_t acc) const {
+  __device__ __forceinline__ Column(const float (*w)[4]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 8; ++i) x[i] = w[i / 4][i % 4];
+  }
+  __device__ __forceinline__ floatx4_t times(const Column& b, floatx4_t acc) const {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float x = *reinterpret_cast<const float*>(rows + (16 * i + 4 * g + j) * stride +
-                                                        (16 * dt + m) * 4);
-        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[i][j], acc, 0, 0, 0);
-      }
+    for (int i = 0; i < 8; ++i)
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], b.x[i], acc, 0, 0, 0);
     return acc;
   }
 };
@@ -192,9 +194,14 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
   constexpr int SS = Elem<T>::bytes == 2 ? 96 : 144;        // bytes per key of ds in LDS
   // dQ: a wave's units are (16 channels, 16 queries), 2 DT of them in all
   constexpr int U = 2 * DT >= W ? 2 * DT / W : 1, SL = U > 1 ? U / 2 : 1;
+  // Where registers run out, keys are read from LDS for every step: 32 keys of 128 channels per
+  // wave and those of 16 channels of every key would take 64.
+  constexpr bool KL = ONE && NK * DT >= 128 * 8;
   __shared__ __align__(16) unsigned char tile_[2][1 + OP][PLANE];
   __shared__ __align__(16) unsigned char ds_[ONE ? NK * SS : 16];
   __shared__ __align__(16) float st[ONE ? W : 1][3][QT];
+  __shared__ __align__(16) float sf[ONE ? W : 1][2][QT];  // a wave's factors, and sums p g
+  __shared__ __align__(16) unsigned char sk[KL ? NK * R::stride : 16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int m = lane & 15, g = lane >> 4;
@@ -240,20 +247,26 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
   load(t0);
 
   // this wave's keys
-  uint4 kf[KT][NV], vf[KT][NV];
+  uint4 kf[KL ? 1 : KT][NV], vf[KT][NV];
   float bias[KT];
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
-    const int r = coreset_row(a, s, (int64_t)chunk * NK + (wave * KT + kt) * 16 + m, &bias[kt]);
-    load_frag<T, D>(K, r, g, r >= 0, kf[kt]);
+    const int key = (wave * KT + kt) * 16 + m;
+    const int r = coreset_row(a, s, (int64_t)chunk * NK + key, &bias[kt]);
+    uint4* kw = kf[KL ? 0 : kt];
+    load_frag<T, D>(K, r, g, r >= 0, kw);
     load_frag<T, D>(V, r, g, r >= 0, vf[kt]);
+    if (KL) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+        *reinterpret_cast<uint4*>(sk + key * R::stride + (4 * v + g) * 16) = kw[v];
+    }
   }
   // columns of every key for dQ: channel 16 dt + m of keys 32 x + 4 g .. and 32 x + 16 + 4 g ..
-  float bc[Elem<T>::bytes == 4 && ONE ? SL : 1][NK / 32][2][4];
-  bf16x8_t kc[SL][NK / 32];
+  Column<T> kc[KL ? 1 : SL][NK / 32];
   const int unit0 = wave * U;
   const bool has_unit = unit0 < 2 * DT;
-  if (ONE && has_unit) {
+  if (ONE && !KL && has_unit) {
 #pragma unroll
     for (int x = 0; x < NK / 32; ++x) {
       float f[SL][2][4];
@@ -267,14 +280,7 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
               r >= 0 ? elem<T>(K + (int64_t)r * D, 16 * (unit0 / 2 + y) + m) : 0.0f;
       }
 #pragma unroll
-      for (int y = 0; y < SL; ++y) {
-        if constexpr (Elem<T>::bytes == 2) {
-          kc[y][x] = pack8(f[y][0], f[y][1]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) bc[y][x][i / 4][i % 4] = f[y][i / 4][i % 4];
-        }
-      }
+      for (int y = 0; y < SL; ++y) kc[y][x] = Column<T>(f[y]);
     }
   }
   put(0);
@@ -308,28 +314,27 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
   // dQ of the step before from its ds
   auto queries = [&](int64_t t) __attribute__((always_inline)) {
     if (!has_unit) return;
+    constexpr int UQ = U > 1 ? 2 : 1;  // 16-query tiles of a unit's channels
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int dt = (unit0 + u) / 2, tq = (unit0 + u) % 2;
-      floatx4_t o = {0.f, 0.f, 0.f, 0.f};
+    for (int y = 0; y < SL; ++y) {
+      const int dt = unit0 / 2 + y;
+      floatx4_t o[UQ];
+#pragma unroll
+      for (int u = 0; u < UQ; ++u) o[u] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int x = 0; x < NK / 32; ++x) {
-        if constexpr (Elem<T>::bytes == 2) {
-          o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              kc[u / 2][x], lds_columns(ds_ + 32 * x * SS, SS, tq, m, g), o, 0, 0, 0);
-        } else {
+        const Column<T> k =
+            KL ? Column<T>(sk + 32 * x * R::stride, R::stride, dt, m, g) : kc[KL ? 0 : y][x];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            o = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                bc[u / 2][x][i / 4][i % 4],
-                *reinterpret_cast<const float*>(ds_ + (32 * x + i / 4 * 16 + 4 * g + i % 4) * SS +
-                                                (16 * tq + m) * 4),
-                o, 0, 0, 0);
-        }
+        for (int u = 0; u < UQ; ++u)
+          o[u] = k.times(Column<T>(ds_ + 32 * x * SS, SS, UQ == 2 ? u : unit0 % 2, m, g), o[u]);
       }
-      const int64_t r = t * QT + 16 * tq + m;
-      if (r < a.n_q)
-        store4<T>(static_cast<T*>(a.dQ) + (s * a.n_q + r) * D + 16 * dt + 4 * g, o * rd);
+#pragma unroll
+      for (int u = 0; u < UQ; ++u) {
+        const int64_t r = t * QT + 16 * (UQ == 2 ? u : unit0 % 2) + m;
+        if (r < a.n_q)
+          store4<T>(static_cast<T*>(a.dQ) + (s * a.n_q + r) * D + 16 * dt + 4 * g, o[u] * rd);
+      }
     }
   };
 
@@ -347,7 +352,12 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
       for (int v = 0; v < NV; ++v) {
         const uint4 qw = lds_word<T, D>(tile_[buf][0] + 16 * tq * R::stride, v, m, g);
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) zs_[kt] = mma_word<T>(qw, kf[kt][v], zs_[kt]);
+        for (int kt = 0; kt < KT; ++kt)
+          zs_[kt] = mma_word<T>(
+              qw,
+              KL ? lds_word<T, D>(sk + (wave * KT + kt) * 16 * R::stride, v, m, g)
+                 : kf[KL ? 0 : kt][v],
+              zs_[kt]);
 #pragma unroll
         for (int o = OP - 1; o >= 0; --o) {
           const uint4 ow = lds_word<T, D>(tile_[buf][1 + o] + 16 * tq * R::stride, v, m, g);
@@ -400,34 +410,43 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
       if (t > t0) queries(t - 1);
       zeros(zrun);
       __syncthreads();
-      // the waves' statistics under one maximum
+      // The waves' statistics under one maximum: lane l takes row l % 32, half of the waves; then
+      // the wave's factor and sum p g of every row go to its lanes through LDS.
+      {
+        const int r = lane & 31, h = lane / 32;
+        float x[W / 2], mx = kLeast;
 #pragma unroll
-      for (int tq = 0; tq < 2; ++tq) {
-        floatx4_t mx = *reinterpret_cast<const floatx4_t*>(&st[0][0][16 * tq + 4 * g]);
-#pragma unroll
-        for (int w = 1; w < W; ++w) {
-          const floatx4_t x = *reinterpret_cast<const floatx4_t*>(&st[w][0][16 * tq + 4 * g]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) mx[j] = fmaxf(mx[j], x[j]);
+        for (int w = 0; w < W / 2; ++w) {
+          x[w] = st[2 * w + h][0][r];
+          mx = fmaxf(mx, x[w]);
         }
-        floatx4_t l = {0.f, 0.f, 0.f, 0.f}, e = l;
+        auto halves = [](float v, auto op) {
+          float u = v;
+          trade(true, v, u);
+          return op(v, u);
+        };
+        mx = halves(mx, [](float u, float v) { return fmaxf(u, v); });
+        float l = 0.0f, e = 0.0f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-          const floatx4_t x = *reinterpret_cast<const floatx4_t*>(&st[w][0][16 * tq + 4 * g]);
-          const floatx4_t y = *reinterpret_cast<const floatx4_t*>(&st[w][1][16 * tq + 4 * g]);
-          const floatx4_t v = *reinterpret_cast<const floatx4_t*>(&st[w][2][16 * tq + 4 * g]);
+        for (int w = 0; w < W / 2; ++w) {
+          const float k = __builtin_amdgcn_exp2f(x[w] - mx);
+          l = fmaf(st[2 * w + h][1][r], k, l);
+          e = fmaf(st[2 * w + h][2][r], k, e);
+        }
+        l = halves(l, add);
+        e = halves(e, add);
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        sf[wave][h][r] = (h ? e : __builtin_amdgcn_exp2f(st[wave][0][r] - mx)) * inv;
+        __builtin_amdgcn_wave_barrier();  // (a wave's own LDS operations are in order)
+#pragma unroll
+        for (int tq = 0; tq < 2; ++tq) {
+          const floatx4_t y = *reinterpret_cast<const floatx4_t*>(&sf[wave][0][16 * tq + 4 * g]);
+          const floatx4_t z = *reinterpret_cast<const floatx4_t*>(&sf[wave][1][16 * tq + 4 * g]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float k = __builtin_amdgcn_exp2f(x[j] - mx[j]);
-            l[j] = fmaf(y[j], k, l[j]);
-            e[j] = fmaf(v[j], k, e[j]);
+            f[tq][j] = y[j];
+            dm[tq][j] = z[j];
           }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float inv = l[j] > 0.0f ? 1.0f / l[j] : 0.0f;
-          f[tq][j] = __builtin_amdgcn_exp2f(mw[tq][j] - mx[j]) * inv;
-          dm[tq][j] = e[j] * inv;
         }
       }
     } else {
@@ -446,6 +465,7 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
         }
       zeros(zrun);
     }
+    Column<T> wp[KT], ws[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
       float ds[2][4];
@@ -469,12 +489,20 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
                 (floatx4_t){ds[tq][0], ds[tq][1], ds[tq][2], ds[tq][3]};
         }
       }
-      const Weights<T> wp(p[kt]), ws(ds);
+      wp[kt] = Column<T>(p[kt]);
+      ws[kt] = Column<T>(ds);
+    }
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        av[kt][dt] = wp.times(tile_[buf][1], R::stride, dt, m, g, av[kt][dt]);
-        ak[kt][dt] = ws.times(tile_[buf][0], R::stride, dt, m, g, ak[kt][dt]);
+    for (int dt = 0; dt < DT; ++dt) {
+#pragma unroll
+      for (int o = OP - 1; o >= 0; --o) {
+        const Column<T> x(tile_[buf][1 + o], R::stride, dt, m, g);
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) av[kt][dt] = x.times(wp[kt], av[kt][dt]);
       }
+      const Column<T> x(tile_[buf][0], R::stride, dt, m, g);
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) ak[kt][dt] = x.times(ws[kt], ak[kt][dt]);
     }
     put(buf ^ 1);
     load(t + 2);
@@ -611,9 +639,10 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
     for (int i = 0; i < 8; ++i)
       p[i / 4][i % 4] =
           __builtin_amdgcn_exp2f(p[i / 4][i % 4] - lse) * (gd[i / 4][i % 4] - dm);
-    const Weights<T> w(p);
+    const Column<T> w(p);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) acc[dt] = w.times(sk, R::stride, dt, m, g, acc[dt]);
+    for (int dt = 0; dt < DT; ++dt)
+      acc[dt] = Column<T>(sk, R::stride, dt, m, g).times(w, acc[dt]);
   }
   if (!there) return;
 #pragma unroll
