@@ -76,6 +76,12 @@ struct Column<bf16_t> {
   __device__ __forceinline__ Column(const unsigned char* rows, int stride, int dt, int m, int g)
       : x(lds_columns(rows, stride, dt, m, g)) {}
   __device__ __forceinline__ Column(const float (*w)[4]) : x(pack8(w[0], w[1])) {}
+  // This lane's values as part of a column in LDS: rows in a row.
+  __device__ __forceinline__ void store(unsigned char* to, int g) const {
+    const u32x4 w = __builtin_bit_cast(u32x4, x);
+    *reinterpret_cast<uint2*>(to + 8 * g) = make_uint2(w[0], w[1]);
+    *reinterpret_cast<uint2*>(to + 32 + 8 * g) = make_uint2(w[2], w[3]);
+  }
   // acc (this' columns x b's) += this^T b: lane (m, g) has columns 4 g .. 4 g + 3 of this and m
   // of b.
   __device__ __forceinline__ floatx4_t times(const Column& b, floatx4_t acc) const {
@@ -95,6 +101,10 @@ struct Column<float> {
   __device__ __forceinline__ Column(const float (*w)[4]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = w[i / 4][i % 4];
+  }
+  __device__ __forceinline__ void store(unsigned char* to, int g) const {
+    *reinterpret_cast<floatx4_t*>(to + 16 * g) = (floatx4_t){x[0], x[1], x[2], x[3]};
+    *reinterpret_cast<floatx4_t*>(to + 64 + 16 * g) = (floatx4_t){x[4], x[5], x[6], x[7]};
   }
   __device__ __forceinline__ floatx4_t times(const Column& b, floatx4_t acc) const {
 #pragma unroll
@@ -216,14 +226,17 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
 
   RawWord<T, T> rq[IT];
   RawWord<T, TO> ro[IT];
+  // (a tile's words lie behind one another: one address and 32-bit offsets)
   auto load = [&](int64_t t) __attribute__((always_inline)) {
+    const int rows = t < t1 ? (int)std::min<int64_t>(QT, a.n_q - t * QT) : 0;
+    const T* q = Q + t * QT * D;
+    const TO* o = dO + t * QT * D;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int item = i * 64 * W + (int)threadIdx.x;
-      const int64_t r = t * QT + item / R::CW;
-      if (item < QT * R::CW && t < t1 && r < a.n_q) {
-        rq[i].load(Q + r * D + item % R::CW * E);
-        ro[i].load(dO + r * D + item % R::CW * E);
+      const uint32_t item = i * 64 * W + threadIdx.x;
+      if ((int)item < rows * R::CW) {
+        rq[i].load(q + item * E);
+        ro[i].load(o + item * E);
       } else {
         rq[i].clear();
         ro[i].clear();
@@ -299,21 +312,25 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
   // this workgroup's share of the zeros of dK and dV, in 16-byte words, and of a step
   const int64_t words = a.n * D / E;
   const int64_t zs = (words + a.shape.parts - 1) / a.shape.parts;
-  int64_t z = chunk == 0 ? part * zs : words;
-  const int64_t z1 = std::min(words, z + zs);
+  const int64_t z0 = chunk == 0 ? std::min(words, part * zs) : words, z1 = std::min(words, z0 + zs);
+  int64_t z = z0;
   const int64_t zrun = (zs + (t1 - t0) - 1) / (t1 - t0);
   auto zeros = [&](int64_t n) __attribute__((always_inline)) {
     const int64_t end = std::min(z1, z + n);
-    for (int64_t i = z + threadIdx.x; i < end; i += 64 * W) {
-      reinterpret_cast<u32x4*>(static_cast<T*>(a.dK) + s * a.n * D)[i] = (u32x4){0, 0, 0, 0};
-      reinterpret_cast<u32x4*>(static_cast<T*>(a.dV) + s * a.n * D)[i] = (u32x4){0, 0, 0, 0};
+    u32x4* dk = reinterpret_cast<u32x4*>(static_cast<T*>(a.dK) + s * a.n * D);
+    u32x4* dv = reinterpret_cast<u32x4*>(static_cast<T*>(a.dV) + s * a.n * D);
+    for (; z < end; z += 64 * W) {
+      const int left = (int)std::min<int64_t>(64 * W, end - z);
+      if ((int)threadIdx.x < left) (dk + z)[threadIdx.x] = (dv + z)[threadIdx.x] = (u32x4){0, 0, 0, 0};
     }
-    z = std::max(z, end);
+    z = std::min(z, std::max(z0, end));
   };
 
   // dQ of the step before from its ds
   auto queries = [&](int64_t t) __attribute__((always_inline)) {
     if (!has_unit) return;
+    T* dQ = static_cast<T*>(a.dQ) + (s * a.n_q + t * QT) * D;
+    const int rows = (int)std::min<int64_t>(QT, a.n_q - t * QT);
     constexpr int UQ = U > 1 ? 2 : 1;  // 16-query tiles of a unit's channels
 #pragma unroll
     for (int y = 0; y < SL; ++y) {
@@ -328,12 +345,12 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
 #pragma unroll
         for (int u = 0; u < UQ; ++u)
           o[u] = k.times(Column<T>(ds_ + 32 * x * SS, SS, UQ == 2 ? u : unit0 % 2, m, g), o[u]);
+        if (KT > 1) __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int u = 0; u < UQ; ++u) {
-        const int64_t r = t * QT + 16 * (UQ == 2 ? u : unit0 % 2) + m;
-        if (r < a.n_q)
-          store4<T>(static_cast<T*>(a.dQ) + (s * a.n_q + r) * D + 16 * dt + 4 * g, o[u] * rd);
+        const int r = 16 * (UQ == 2 ? u : unit0 % 2) + m;
+        if (r < rows) store4<T>(dQ + (uint32_t)(r * D + 16 * dt + 4 * g), o[u] * rd);
       }
     }
   };
@@ -364,6 +381,7 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
 #pragma unroll
           for (int kt = 0; kt < KT; ++kt) zg[kt] = mma_word<T>(ow, vf[kt][v], zg[kt]);
         }
+        if (KT > 1) __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
@@ -373,38 +391,32 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
           gd[kt][tq][j] = zg[kt][j];
         }
     }
-    float f[2][4], dm[2][4];  // a row's factor and sum p g
     if (ONE) {
-      float mw[2][4];
       auto add = [](float x, float y) { return x + y; };
 #pragma unroll
-      for (int tq = 0; tq < 2; ++tq)
+      for (int tq = 0; tq < 2; ++tq) {
+        floatx4_t mw, l, e;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           float x = p[0][tq][j];
 #pragma unroll
           for (int kt = 1; kt < KT; ++kt) x = fmaxf(x, p[kt][tq][j]);
           x = row_reduce(fmaxf(x, kLeast), [](float x, float y) { return fmaxf(x, y); });
-          float l = 0.0f, e = 0.0f;
+          float u = 0.0f, v = 0.0f;
 #pragma unroll
           for (int kt = 0; kt < KT; ++kt) {
             p[kt][tq][j] = __builtin_amdgcn_exp2f(p[kt][tq][j] - x);
-            l += p[kt][tq][j];
-            e = fmaf(p[kt][tq][j], gd[kt][tq][j], e);
+            u += p[kt][tq][j];
+            v = fmaf(p[kt][tq][j], gd[kt][tq][j], v);
           }
-          mw[tq][j] = x;
-          f[tq][j] = row_reduce(l, add);
-          dm[tq][j] = row_reduce(e, add);
+          mw[j] = x;
+          l[j] = row_reduce(u, add);
+          e[j] = row_reduce(v, add);
         }
-      if (m == 0) {
-#pragma unroll
-        for (int tq = 0; tq < 2; ++tq) {
-          *reinterpret_cast<floatx4_t*>(&st[wave][0][16 * tq + 4 * g]) =
-              (floatx4_t){mw[tq][0], mw[tq][1], mw[tq][2], mw[tq][3]};
-          *reinterpret_cast<floatx4_t*>(&st[wave][1][16 * tq + 4 * g]) =
-              (floatx4_t){f[tq][0], f[tq][1], f[tq][2], f[tq][3]};
-          *reinterpret_cast<floatx4_t*>(&st[wave][2][16 * tq + 4 * g]) =
-              (floatx4_t){dm[tq][0], dm[tq][1], dm[tq][2], dm[tq][3]};
+        if (m == 0) {
+          *reinterpret_cast<floatx4_t*>(&st[wave][0][16 * tq + 4 * g]) = mw;
+          *reinterpret_cast<floatx4_t*>(&st[wave][1][16 * tq + 4 * g]) = l;
+          *reinterpret_cast<floatx4_t*>(&st[wave][2][16 * tq + 4 * g]) = e;
         }
       }
       if (t > t0) queries(t - 1);
@@ -438,60 +450,46 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
         sf[wave][h][r] = (h ? e : __builtin_amdgcn_exp2f(st[wave][0][r] - mx)) * inv;
         __builtin_amdgcn_wave_barrier();  // (a wave's own LDS operations are in order)
-#pragma unroll
-        for (int tq = 0; tq < 2; ++tq) {
-          const floatx4_t y = *reinterpret_cast<const floatx4_t*>(&sf[wave][0][16 * tq + 4 * g]);
-          const floatx4_t z = *reinterpret_cast<const floatx4_t*>(&sf[wave][1][16 * tq + 4 * g]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            f[tq][j] = y[j];
-            dm[tq][j] = z[j];
-          }
-        }
       }
     } else {
+      zeros(zrun);
+    }
+    // p, and ds in place of g
 #pragma unroll
-      for (int tq = 0; tq < 2; ++tq)
+    for (int tq = 0; tq < 2; ++tq) {
+      floatx4_t f = {1.f, 1.f, 1.f, 1.f}, dm;
+      if (ONE) {
+        f = *reinterpret_cast<const floatx4_t*>(&sf[wave][0][16 * tq + 4 * g]);
+        dm = *reinterpret_cast<const floatx4_t*>(&sf[wave][1][16 * tq + 4 * g]);
+      }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 4; ++j) {
+        if (!ONE) {
           const int64_t r = t * QT + 16 * tq + 4 * g + j;
           // (rows past the last: probabilities of 0)
           const float lse = r < a.n_q ? a.stats[s * a.n_q + r] : INFINITY;
-          dm[tq][j] = r < a.n_q ? a.stats[(a.S + s) * a.n_q + r] : 0.0f;
-          f[tq][j] = 1.0f;
+          dm[j] = r < a.n_q ? a.stats[(a.S + s) * a.n_q + r] : 0.0f;
 #pragma unroll
           for (int kt = 0; kt < KT; ++kt)
             p[kt][tq][j] = __builtin_amdgcn_exp2f(p[kt][tq][j] - lse);
         }
-      zeros(zrun);
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+          if (ONE) p[kt][tq][j] *= f[j];
+          gd[kt][tq][j] = p[kt][tq][j] * (gd[kt][tq][j] - dm[j]);
+          aw[kt] += gd[kt][tq][j];
+        }
+      }
     }
     Column<T> wp[KT], ws[KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      float ds[2][4];
-#pragma unroll
-      for (int tq = 0; tq < 2; ++tq)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          p[kt][tq][j] *= f[tq][j];
-          ds[tq][j] = p[kt][tq][j] * (gd[kt][tq][j] - dm[tq][j]);
-          aw[kt] += ds[tq][j];
-        }
-      if (ONE) {
-        unsigned char* to = ds_ + ((wave * KT + kt) * 16 + m) * SS;
-#pragma unroll
-        for (int tq = 0; tq < 2; ++tq) {
-          if constexpr (Elem<T>::bytes == 2)
-            *reinterpret_cast<uint2*>(to + (16 * tq + 4 * g) * 2) =
-                make_uint2(cvt_pk_bf16(ds[tq][0], ds[tq][1]), cvt_pk_bf16(ds[tq][2], ds[tq][3]));
-          else
-            *reinterpret_cast<floatx4_t*>(to + (16 * tq + 4 * g) * 4) =
-                (floatx4_t){ds[tq][0], ds[tq][1], ds[tq][2], ds[tq][3]};
-        }
-      }
       wp[kt] = Column<T>(p[kt]);
-      ws[kt] = Column<T>(ds);
+      ws[kt] = Column<T>(gd[kt]);
+      if (ONE) ws[kt].store(ds_ + ((wave * KT + kt) * 16 + m) * SS, g);
     }
+    // (one pair of columns at a time: more of them on their way cost registers that are not
+    // there)
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
@@ -503,6 +501,7 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
       const Column<T> x(tile_[buf][0], R::stride, dt, m, g);
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) ak[kt][dt] = x.times(ws[kt], ak[kt][dt]);
+      if (KT > 1) __builtin_amdgcn_sched_barrier(0);
     }
     put(buf ^ 1);
     load(t + 2);
