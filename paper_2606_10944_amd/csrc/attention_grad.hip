@@ -76,11 +76,11 @@ struct Column<bf16_t> {
   __device__ __forceinline__ Column(const unsigned char* rows, int stride, int dt, int m, int g)
       : x(lds_columns(rows, stride, dt, m, g)) {}
   __device__ __forceinline__ Column(const float (*w)[4]) : x(pack8(w[0], w[1])) {}
-  // This lane's values as part of a column in LDS: rows in a row.
-  __device__ __forceinline__ void store(unsigned char* to, int g) const {
-    const u32x4 w = __builtin_bit_cast(u32x4, x);
-    *reinterpret_cast<uint2*>(to + 8 * g) = make_uint2(w[0], w[1]);
-    *reinterpret_cast<uint2*>(to + 32 + 8 * g) = make_uint2(w[2], w[3]);
+  // The same of a row (of a column m) in LDS.
+  __device__ __forceinline__ Column(const unsigned char* row, int g) {
+    const uint2 a = *reinterpret_cast<const uint2*>(row + 8 * g);
+    const uint2 b = *reinterpret_cast<const uint2*>(row + 32 + 8 * g);
+    x = __builtin_bit_cast(bf16x8_t, (u32x4){a.x, a.y, b.x, b.y});
   }
   // acc (this' columns x b's) += this^T b: lane (m, g) has columns 4 g .. 4 g + 3 of this and m
   // of b.
@@ -102,9 +102,10 @@ struct Column<float> {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = w[i / 4][i % 4];
   }
-  __device__ __forceinline__ void store(unsigned char* to, int g) const {
-    *reinterpret_cast<floatx4_t*>(to + 16 * g) = (floatx4_t){x[0], x[1], x[2], x[3]};
-    *reinterpret_cast<floatx4_t*>(to + 64 + 16 * g) = (floatx4_t){x[4], x[5], x[6], x[7]};
+  __device__ __forceinline__ Column(const unsigned char* row, int g) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      x[i] = *reinterpret_cast<const float*>(row + (i / 4 * 16 + 4 * g + i % 4) * 4);
   }
   __device__ __forceinline__ floatx4_t times(const Column& b, floatx4_t acc) const {
 #pragma unroll
@@ -189,10 +190,11 @@ __device__ __forceinline__ int coreset_row(const GradArgs& a, int64_t s, int64_t
 // ---------------------------------------------------------------------------
 // Keys: see above.  W waves of 16 KT keys.  ONE: every key of the slice is here.
 //
-// Lanes are l = 16 g + m.  Scores S = Q K^T by 16 queries x 16 keys: lane (m, g) holds queries
-// 4 g .. 4 g + 3 of key m, which is what the products over queries want as their second
-// operand; their first, the columns of Q and dO, come from LDS by the transposing read.  ds
-// passes through LDS, [key, query], from where every wave takes its 16 channels of dQ.
+// Lanes are l = 16 g + m.  Scores S^T = K Q^T by 16 keys x 16 queries: lane (m, g) holds keys
+// 4 g .. 4 g + 3 of query m, so that a row's maximum and sums need few moves between lanes;
+// the waves' meet in LDS.  p and ds pass through LDS, [query, key]: a wave reads its own keys'
+// columns back by the transposing read for the products over queries, as it reads the columns
+// of Q and dO, and every wave reads all of ds for its 16 channels of dQ.
 // ---------------------------------------------------------------------------
 template <typename T, typename TO, int D, int W, int KT, bool ONE>
 __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
@@ -201,16 +203,15 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
   constexpr int OP = Parts<T, TO>::n, E = 16 / Elem<T>::bytes;
   constexpr int PLANE = QT * R::stride;
   constexpr int IT = (QT * R::CW + 64 * W - 1) / (64 * W);  // words of a tile per thread
-  constexpr int SS = Elem<T>::bytes == 2 ? 96 : 144;        // bytes per key of ds in LDS
+  constexpr int SS = NK * Elem<T>::bytes + 16;  // bytes per query of p and ds in LDS
   // dQ: a wave's units are (16 channels, 16 queries), 2 DT of them in all
   constexpr int U = 2 * DT >= W ? 2 * DT / W : 1, SL = U > 1 ? U / 2 : 1;
   // Where registers run out, keys are read from LDS for every step: 32 keys of 128 channels per
   // wave and those of 16 channels of every key would take 64.
   constexpr bool KL = ONE && NK * DT >= 128 * 8;
   __shared__ __align__(16) unsigned char tile_[2][1 + OP][PLANE];
-  __shared__ __align__(16) unsigned char ds_[ONE ? NK * SS : 16];
-  __shared__ __align__(16) float st[ONE ? W : 1][3][QT];
-  __shared__ __align__(16) float sf[ONE ? W : 1][2][QT];  // a wave's factors, and sums p g
+  __shared__ __align__(16) unsigned char ds_[QT * SS];
+  __shared__ float st[ONE ? W : 1][3][QT];
   __shared__ __align__(16) unsigned char sk[KL ? NK * R::stride : 16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -261,11 +262,14 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
 
   // this wave's keys
   uint4 kf[KL ? 1 : KT][NV], vf[KT][NV];
-  float bias[KT];
+  float bias[KT][4];
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
     const int key = (wave * KT + kt) * 16 + m;
-    const int r = coreset_row(a, s, (int64_t)chunk * NK + key, &bias[kt]);
+    float mine;
+    const int r = coreset_row(a, s, (int64_t)chunk * NK + key, &mine);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) bias[kt][j] = __shfl(mine, 4 * g + j);
     uint4* kw = kf[KL ? 0 : kt];
     load_frag<T, D>(K, r, g, r >= 0, kw);
     load_frag<T, D>(V, r, g, r >= 0, vf[kt]);
@@ -300,10 +304,11 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
   load(t0 + 1);
 
   floatx4_t ak[KT][DT], av[KT][DT];
-  float aw[KT];
+  float aw[KT][4];
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
-    aw[kt] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) aw[kt][j] = 0.0f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) ak[kt][dt] = av[kt][dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
   }
@@ -344,7 +349,10 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
             KL ? Column<T>(sk + 32 * x * R::stride, R::stride, dt, m, g) : kc[KL ? 0 : y][x];
 #pragma unroll
         for (int u = 0; u < UQ; ++u)
-          o[u] = k.times(Column<T>(ds_ + 32 * x * SS, SS, UQ == 2 ? u : unit0 % 2, m, g), o[u]);
+          o[u] = k.times(Column<T>(ds_ + (16 * (UQ == 2 ? u : unit0 % 2) + m) * SS +
+                                       32 * x * Elem<T>::bytes,
+                                   g),
+                         o[u]);
         if (KT > 1) __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
@@ -358,28 +366,27 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
   __syncthreads();
   for (int64_t t = t0; t < t1; ++t) {
     const int buf = (int)(t - t0) & 1;
-    // scores and g: [query 16 tq + 4 g + j, key m]
+    // scores to base 2 and g of keys 4 g + j, query 16 tq + m
     float p[KT][2][4], gd[KT][2][4];
 #pragma unroll
     for (int tq = 0; tq < 2; ++tq) {
-      floatx4_t zs_[KT], zg[KT];
+      floatx4_t x[KT], y[KT];
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) zs_[kt] = zg[kt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+      for (int kt = 0; kt < KT; ++kt) x[kt] = y[kt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const uint4 qw = lds_word<T, D>(tile_[buf][0] + 16 * tq * R::stride, v, m, g);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
-          zs_[kt] = mma_word<T>(
-              qw,
+          x[kt] = mma_word<T>(
               KL ? lds_word<T, D>(sk + (wave * KT + kt) * 16 * R::stride, v, m, g)
                  : kf[KL ? 0 : kt][v],
-              zs_[kt]);
+              qw, x[kt]);
 #pragma unroll
         for (int o = OP - 1; o >= 0; --o) {
           const uint4 ow = lds_word<T, D>(tile_[buf][1 + o] + 16 * tq * R::stride, v, m, g);
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt) zg[kt] = mma_word<T>(ow, vf[kt][v], zg[kt]);
+          for (int kt = 0; kt < KT; ++kt) y[kt] = mma_word<T>(vf[kt][v], ow, y[kt]);
         }
         if (KT > 1) __builtin_amdgcn_sched_barrier(0);
       }
@@ -387,107 +394,109 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          p[kt][tq][j] = fmaf(zs_[kt][j], c2, bias[kt]);
-          gd[kt][tq][j] = zg[kt][j];
+          p[kt][tq][j] = fmaf(x[kt][j], c2, bias[kt][j]);
+          gd[kt][tq][j] = y[kt][j];
         }
     }
+    float f[2], dm[2];  // a row's factor and sum p g
     if (ONE) {
       auto add = [](float x, float y) { return x + y; };
+      auto larger = [](float x, float y) { return fmaxf(x, y); };
 #pragma unroll
       for (int tq = 0; tq < 2; ++tq) {
-        floatx4_t mw, l, e;
+        float x = kLeast, l = 0.0f, e = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float x = p[0][tq][j];
+        for (int i = 0; i < 4 * KT; ++i) x = fmaxf(x, p[i / 4][tq][i % 4]);
+        x = across_rows(x, true, larger);
 #pragma unroll
-          for (int kt = 1; kt < KT; ++kt) x = fmaxf(x, p[kt][tq][j]);
-          x = row_reduce(fmaxf(x, kLeast), [](float x, float y) { return fmaxf(x, y); });
-          float u = 0.0f, v = 0.0f;
-#pragma unroll
-          for (int kt = 0; kt < KT; ++kt) {
-            p[kt][tq][j] = __builtin_amdgcn_exp2f(p[kt][tq][j] - x);
-            u += p[kt][tq][j];
-            v = fmaf(p[kt][tq][j], gd[kt][tq][j], v);
-          }
-          mw[j] = x;
-          l[j] = row_reduce(u, add);
-          e[j] = row_reduce(v, add);
+        for (int i = 0; i < 4 * KT; ++i) {
+          float& w = p[i / 4][tq][i % 4];
+          w = __builtin_amdgcn_exp2f(w - x);
+          l += w;
+          e = fmaf(w, gd[i / 4][tq][i % 4], e);
         }
-        if (m == 0) {
-          *reinterpret_cast<floatx4_t*>(&st[wave][0][16 * tq + 4 * g]) = mw;
-          *reinterpret_cast<floatx4_t*>(&st[wave][1][16 * tq + 4 * g]) = l;
-          *reinterpret_cast<floatx4_t*>(&st[wave][2][16 * tq + 4 * g]) = e;
+        l = across_rows(l, true, add);
+        e = across_rows(e, true, add);
+        f[tq] = x;
+        if (g == 0) {
+          st[wave][0][16 * tq + m] = x;
+          st[wave][1][16 * tq + m] = l;
+          st[wave][2][16 * tq + m] = e;
         }
       }
       if (t > t0) queries(t - 1);
       zeros(zrun);
       __syncthreads();
-      // The waves' statistics under one maximum: lane l takes row l % 32, half of the waves; then
-      // the wave's factor and sum p g of every row go to its lanes through LDS.
-      {
-        const int r = lane & 31, h = lane / 32;
-        float x[W / 2], mx = kLeast;
+      // The waves' statistics under one maximum: lane l takes row l % 32 of half of the waves,
+      // then the halves meet, and rows of 16 lanes trade the two tiles' queries.
+      const int r = lane & 31, h = lane / 32;
+      float x[W / 2], mx = kLeast, l = 0.0f, e = 0.0f;
 #pragma unroll
-        for (int w = 0; w < W / 2; ++w) {
-          x[w] = st[2 * w + h][0][r];
-          mx = fmaxf(mx, x[w]);
-        }
-        auto halves = [](float v, auto op) {
-          float u = v;
-          trade(true, v, u);
-          return op(v, u);
-        };
-        mx = halves(mx, [](float u, float v) { return fmaxf(u, v); });
-        float l = 0.0f, e = 0.0f;
-#pragma unroll
-        for (int w = 0; w < W / 2; ++w) {
-          const float k = __builtin_amdgcn_exp2f(x[w] - mx);
-          l = fmaf(st[2 * w + h][1][r], k, l);
-          e = fmaf(st[2 * w + h][2][r], k, e);
-        }
-        l = halves(l, add);
-        e = halves(e, add);
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        sf[wave][h][r] = (h ? e : __builtin_amdgcn_exp2f(st[wave][0][r] - mx)) * inv;
-        __builtin_amdgcn_wave_barrier();  // (a wave's own LDS operations are in order)
+      for (int w = 0; w < W / 2; ++w) {
+        x[w] = st[2 * w + h][0][r];
+        mx = fmaxf(mx, x[w]);
       }
+      auto halves = [](float v, auto op) {
+        float u = v;
+        trade(true, v, u);
+        return op(v, u);
+      };
+      mx = halves(mx, larger);
+#pragma unroll
+      for (int w = 0; w < W / 2; ++w) {
+        const float k = __builtin_amdgcn_exp2f(x[w] - mx);
+        l = fmaf(st[2 * w + h][1][r], k, l);
+        e = fmaf(st[2 * w + h][2][r], k, e);
+      }
+      l = halves(l, add);
+      e = halves(e, add);
+      float inv = l > 0.0f ? 1.0f / l : 0.0f, i1 = inv, m1 = mx;
+      dm[0] = dm[1] = e * inv;
+      trade(false, dm[0], dm[1]);
+      trade(false, inv, i1);
+      trade(false, mx, m1);
+      f[0] = __builtin_amdgcn_exp2f(f[0] - mx) * inv;
+      f[1] = __builtin_amdgcn_exp2f(f[1] - m1) * i1;
     } else {
+#pragma unroll
+      for (int tq = 0; tq < 2; ++tq) {
+        const int64_t r = t * QT + 16 * tq + m;
+        // (rows past the last: probabilities of 0)
+        const float lse = r < a.n_q ? a.stats[s * a.n_q + r] : INFINITY;
+        dm[tq] = r < a.n_q ? a.stats[(a.S + s) * a.n_q + r] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4 * KT; ++i)
+          p[i / 4][tq][i % 4] = __builtin_amdgcn_exp2f(p[i / 4][tq][i % 4] - lse);
+      }
       zeros(zrun);
     }
-    // p, and ds in place of g
-#pragma unroll
-    for (int tq = 0; tq < 2; ++tq) {
-      floatx4_t f = {1.f, 1.f, 1.f, 1.f}, dm;
-      if (ONE) {
-        f = *reinterpret_cast<const floatx4_t*>(&sf[wave][0][16 * tq + 4 * g]);
-        dm = *reinterpret_cast<const floatx4_t*>(&sf[wave][1][16 * tq + 4 * g]);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (!ONE) {
-          const int64_t r = t * QT + 16 * tq + 4 * g + j;
-          // (rows past the last: probabilities of 0)
-          const float lse = r < a.n_q ? a.stats[s * a.n_q + r] : INFINITY;
-          dm[j] = r < a.n_q ? a.stats[(a.S + s) * a.n_q + r] : 0.0f;
-#pragma unroll
-          for (int kt = 0; kt < KT; ++kt)
-            p[kt][tq][j] = __builtin_amdgcn_exp2f(p[kt][tq][j] - lse);
-        }
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-          if (ONE) p[kt][tq][j] *= f[j];
-          gd[kt][tq][j] = p[kt][tq][j] * (gd[kt][tq][j] - dm[j]);
-          aw[kt] += gd[kt][tq][j];
-        }
-      }
-    }
+    // p, and ds in place of g; both to LDS and back by columns, through one place
     Column<T> wp[KT], ws[KT];
+    unsigned char* mine = ds_ + (wave * KT * 16 + 4 * g) * Elem<T>::bytes + m * SS;
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      wp[kt] = Column<T>(p[kt]);
-      ws[kt] = Column<T>(gd[kt]);
-      if (ONE) ws[kt].store(ds_ + ((wave * KT + kt) * 16 + m) * SS, g);
+    for (int i = 0; i < 8 * KT; ++i) {
+      const int kt = i / 8, tq = i / 4 % 2, j = i % 4;
+      if (ONE) p[kt][tq][j] *= f[tq];
+      gd[kt][tq][j] = p[kt][tq][j] * (gd[kt][tq][j] - dm[tq]);
     }
+    if (a.part_w) {
+#pragma unroll
+      for (int i = 0; i < 8 * KT; ++i) aw[i / 8][i % 4] += gd[i / 8][i / 4 % 2][i % 4];
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * KT; ++i)
+      store4<T>(reinterpret_cast<T*>(mine + i / 2 * 16 * Elem<T>::bytes + i % 2 * 16 * SS),
+                (floatx4_t){p[i / 2][i % 2][0], p[i / 2][i % 2][1], p[i / 2][i % 2][2],
+                            p[i / 2][i % 2][3]});
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) wp[kt] = Column<T>(ds_, SS, wave * KT + kt, m, g);
+#pragma unroll
+    for (int i = 0; i < 2 * KT; ++i)
+      store4<T>(reinterpret_cast<T*>(mine + i / 2 * 16 * Elem<T>::bytes + i % 2 * 16 * SS),
+                (floatx4_t){gd[i / 2][i % 2][0], gd[i / 2][i % 2][1], gd[i / 2][i % 2][2],
+                            gd[i / 2][i % 2][3]});
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) ws[kt] = Column<T>(ds_, SS, wave * KT + kt, m, g);
     // (one pair of columns at a time: more of them on their way cost registers that are not
     // there)
 #pragma unroll
@@ -521,8 +530,11 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
       *reinterpret_cast<floatx4_t*>(o + D + 16 * dt) = av[kt][dt];
     }
     if (a.part_w) {
-      const float w = across_rows(aw[kt], true, [](float x, float y) { return x + y; });
-      if (g == 0) a.part_w[(int64_t)blockIdx.x * NK + key] = w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float w = row_reduce(aw[kt][j], [](float x, float y) { return x + y; });
+        if (m == 0) a.part_w[(int64_t)blockIdx.x * NK + key + 4 * g + j] = w;
+      }
     }
   }
 }
