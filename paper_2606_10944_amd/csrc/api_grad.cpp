@@ -38,7 +38,7 @@ int thin_attention_backward_plan(int32_t dtype, int64_t B, int64_t H, int64_t n_
   if (!workspace_bytes) return THIN_EINVAL;
   if (!known_dtype(dtype)) return THIN_EDTYPE;
   if (!valid_sizes(B, H, n_q, n, d, n_out)) return THIN_EINVAL;
-  const thin::GradShape s = thin::grad_shape(B * H, n_q, n_out, dtype == THIN_BF16);
+  const thin::GradShape s = thin::grad_shape(B * H, n_q, n_out, d, dtype == THIN_BF16);
   *workspace_bytes = thin::grad_bytes(s, B * H, n_q, d, true).all();
   return THIN_OK;
 }
@@ -54,7 +54,7 @@ int thin_attention_backward(const void* Q, const void* K, const void* V, int32_t
       !idx || !aligned(idx, 4) || !aligned(logw, 4) || !aligned(dlogw, 4))
     return THIN_EINVAL;
   thin::GradArgs a{};
-  a.shape = thin::grad_shape(B * H, n_q, n_out, dtype == THIN_BF16);
+  a.shape = thin::grad_shape(B * H, n_q, n_out, d, dtype == THIN_BF16);
   const thin::GradBytes bytes = thin::grad_bytes(a.shape, B * H, n_q, d, true);
   if (!workspace || workspace_bytes < bytes.all() || !aligned(workspace, 256))
     return THIN_EWORKSPACE;

@@ -31,6 +31,7 @@ constexpr int QT = (int)kGradTile;
 constexpr float kLeast = -3.0e38f;
 constexpr double kLog2e = 1.44269504088896340736;
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
 
@@ -115,6 +116,26 @@ struct Column<float> {
   }
 };
 
+// `bytes` bytes at p: loads past them give 0 and stores past them are dropped, without a branch,
+// so that the compiler can count a step's memory operations.  p and bytes are the wave's.
+struct Span {
+  __amdgpu_buffer_rsrc_t r;
+  __device__ __forceinline__ Span(const void* p, int bytes)
+      : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000)) {}
+  __device__ __forceinline__ u32x4 load16(uint32_t at) const {
+    return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
+  }
+  __device__ __forceinline__ u32x2 load8(uint32_t at) const {
+    return __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0);
+  }
+  __device__ __forceinline__ void store(u32x4 w, uint32_t at) const {
+    __builtin_amdgcn_raw_buffer_store_b128(w, r, at, 0, 0);
+  }
+  __device__ __forceinline__ void store(u32x2 w, uint32_t at) const {
+    __builtin_amdgcn_raw_buffer_store_b64(w, r, at, 0, 0);
+  }
+};
+
 // A 16-byte word of T from a row of TO (elements e .. of it), and what bf16 leaves of float32
 // (OP = 2 parts).
 template <typename T, typename TO>
@@ -122,38 +143,28 @@ struct Parts {
   static constexpr int n = Elem<T>::bytes == 2 && Elem<TO>::bytes == 4 ? 2 : 1;
 };
 template <typename T, typename TO>
-struct RawWord;  // as it is in memory
-template <>
-struct RawWord<bf16_t, bf16_t> {
+struct RawWord;  // as it is in memory; word `item` of a span
+template <typename T>
+struct RawWord<T, T> {
   u32x4 w;
-  __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const u32x4*>(p); }
-  __device__ __forceinline__ void clear() { w = (u32x4){0, 0, 0, 0}; }
-  __device__ __forceinline__ void parts(u32x4* o) const { o[0] = w; }
-};
-template <>
-struct RawWord<float, float> {
-  u32x4 w;
-  __device__ __forceinline__ void load(const float* p) { w = *reinterpret_cast<const u32x4*>(p); }
-  __device__ __forceinline__ void clear() { w = (u32x4){0, 0, 0, 0}; }
+  __device__ __forceinline__ void load(const Span& p, uint32_t item) { w = p.load16(item * 16); }
   __device__ __forceinline__ void parts(u32x4* o) const { o[0] = w; }
 };
 template <>
 struct RawWord<float, bf16_t> {
-  uint2 w;
-  __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const uint2*>(p); }
-  __device__ __forceinline__ void clear() { w = make_uint2(0, 0); }
+  u32x2 w;
+  __device__ __forceinline__ void load(const Span& p, uint32_t item) { w = p.load8(item * 8); }
   __device__ __forceinline__ void parts(u32x4* o) const {
-    o[0] = (u32x4){w.x << 16, w.x & 0xffff0000u, w.y << 16, w.y & 0xffff0000u};
+    o[0] = (u32x4){w[0] << 16, w[0] & 0xffff0000u, w[1] << 16, w[1] & 0xffff0000u};
   }
 };
 template <>
 struct RawWord<bf16_t, float> {
   u32x4 w[2];
-  __device__ __forceinline__ void load(const float* p) {
-    w[0] = *reinterpret_cast<const u32x4*>(p);
-    w[1] = *reinterpret_cast<const u32x4*>(p + 4);
+  __device__ __forceinline__ void load(const Span& p, uint32_t item) {
+    w[0] = p.load16(item * 32);
+    w[1] = p.load16(item * 32 + 16);
   }
-  __device__ __forceinline__ void clear() { w[0] = w[1] = (u32x4){0, 0, 0, 0}; }
   __device__ __forceinline__ void parts(u32x4* o) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -168,11 +179,25 @@ struct RawWord<bf16_t, float> {
 
 // Four consecutive channels of a gradient.
 template <typename T>
+struct Four;
+template <>
+struct Four<bf16_t> {
+  u32x2 w;
+  __device__ __forceinline__ Four() {}
+  __device__ __forceinline__ Four(floatx4_t o)
+      : w((u32x2){cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3])}) {}
+  __device__ __forceinline__ void store(bf16_t* p) const { *reinterpret_cast<u32x2*>(p) = w; }
+};
+template <>
+struct Four<float> {
+  u32x4 w;
+  __device__ __forceinline__ Four() {}
+  __device__ __forceinline__ Four(floatx4_t o) : w(__builtin_bit_cast(u32x4, o)) {}
+  __device__ __forceinline__ void store(float* p) const { *reinterpret_cast<u32x4*>(p) = w; }
+};
+template <typename T>
 __device__ __forceinline__ void store4(T* p, floatx4_t o) {
-  if constexpr (Elem<T>::bytes == 2)
-    *reinterpret_cast<uint2*>(p) = make_uint2(cvt_pk_bf16(o[0], o[1]), cvt_pk_bf16(o[2], o[3]));
-  else
-    *reinterpret_cast<floatx4_t*>(p) = o;
+  Four<T>(o).store(p);
 }
 
 // Coreset row j of slice s: its row of K and V (-1: none, or its weight is 0) and log-weight to
@@ -197,7 +222,7 @@ __device__ __forceinline__ int coreset_row(const GradArgs& a, int64_t s, int64_t
 // of Q and dO, and every wave reads all of ds for its 16 channels of dQ.
 // ---------------------------------------------------------------------------
 template <typename T, typename TO, int D, int W, int KT, bool ONE>
-__global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
+__global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(GradArgs a) {
   using R = LdsRows<T, D>;
   constexpr int NV = Frag<T, D>::NV, DT = D / 16, NK = 16 * W * KT;
   constexpr int OP = Parts<T, TO>::n, E = 16 / Elem<T>::bytes;
@@ -205,10 +230,11 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
   constexpr int IT = (QT * R::CW + 64 * W - 1) / (64 * W);  // words of a tile per thread
   constexpr int SS = NK * Elem<T>::bytes + 16;  // bytes per query of p and ds in LDS
   // dQ: a wave's units are (16 channels, 16 queries), 2 DT of them in all
-  constexpr int U = 2 * DT >= W ? 2 * DT / W : 1, SL = U > 1 ? U / 2 : 1;
+  constexpr int U = (2 * DT + W - 1) / W, SL = U > 1 ? U / 2 : 1;
   // Where registers run out, keys are read from LDS for every step: 32 keys of 128 channels per
   // wave and those of 16 channels of every key would take 64.
-  constexpr bool KL = ONE && NK * DT >= 128 * 8;
+  constexpr bool KL = ONE && (NK * DT > 128 * 8 || W > 8);
+  constexpr bool TIGHT = KT * DT >= 16;
   __shared__ __align__(16) unsigned char tile_[2][1 + OP][PLANE];
   __shared__ __align__(16) unsigned char ds_[QT * SS];
   __shared__ float st[ONE ? W : 1][3][QT];
@@ -227,28 +253,23 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
 
   RawWord<T, T> rq[IT];
   RawWord<T, TO> ro[IT];
-  // (a tile's words lie behind one another: one address and 32-bit offsets)
+  // (a tile's words lie behind one another)
+  constexpr bool EVEN = QT * R::CW % (64 * W) == 0;
   auto load = [&](int64_t t) __attribute__((always_inline)) {
     const int rows = t < t1 ? (int)std::min<int64_t>(QT, a.n_q - t * QT) : 0;
-    const T* q = Q + t * QT * D;
-    const TO* o = dO + t * QT * D;
+    const int64_t at = rows > 0 ? t * QT * D : 0;
+    const Span q(Q + at, rows * D * Elem<T>::bytes), o(dO + at, rows * D * Elem<TO>::bytes);
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const uint32_t item = i * 64 * W + threadIdx.x;
-      if ((int)item < rows * R::CW) {
-        rq[i].load(q + item * E);
-        ro[i].load(o + item * E);
-      } else {
-        rq[i].clear();
-        ro[i].clear();
-      }
+      rq[i].load(q, i * 64 * W + threadIdx.x);
+      ro[i].load(o, i * 64 * W + threadIdx.x);
     }
   };
   auto put = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
       const int item = i * 64 * W + (int)threadIdx.x;
-      if (item >= QT * R::CW) continue;
+      if (!EVEN && item >= QT * R::CW) continue;
       const int to = item / R::CW * R::stride + item % R::CW * 16;
       u32x4 w[2];
       rq[i].parts(w);
@@ -282,7 +303,7 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
   // columns of every key for dQ: channel 16 dt + m of keys 32 x + 4 g .. and 32 x + 16 + 4 g ..
   Column<T> kc[KL ? 1 : SL][NK / 32];
   const int unit0 = wave * U;
-  const bool has_unit = unit0 < 2 * DT;
+  const bool has_unit = U * W == 2 * DT || unit0 < 2 * DT;
   if (ONE && !KL && has_unit) {
 #pragma unroll
     for (int x = 0; x < NK / 32; ++x) {
@@ -314,29 +335,29 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
   }
   const float c2 = (float)(kLog2e / sqrt((double)D)), rd = (float)(1.0 / sqrt((double)D));
 
-  // this workgroup's share of the zeros of dK and dV, in 16-byte words, and of a step
+  // this workgroup's share of the zeros of dK and dV, in 16-byte words: as many in a step as the
+  // step's queries have, the rest of them behind the last step
   const int64_t words = a.n * D / E;
   const int64_t zs = (words + a.shape.parts - 1) / a.shape.parts;
-  const int64_t z0 = chunk == 0 ? std::min(words, part * zs) : words, z1 = std::min(words, z0 + zs);
-  int64_t z = z0;
-  const int64_t zrun = (zs + (t1 - t0) - 1) / (t1 - t0);
-  auto zeros = [&](int64_t n) __attribute__((always_inline)) {
-    const int64_t end = std::min(z1, z + n);
-    u32x4* dk = reinterpret_cast<u32x4*>(static_cast<T*>(a.dK) + s * a.n * D);
-    u32x4* dv = reinterpret_cast<u32x4*>(static_cast<T*>(a.dV) + s * a.n * D);
-    for (; z < end; z += 64 * W) {
-      const int left = (int)std::min<int64_t>(64 * W, end - z);
-      if ((int)threadIdx.x < left) (dk + z)[threadIdx.x] = (dv + z)[threadIdx.x] = (u32x4){0, 0, 0, 0};
+  int64_t z = chunk == 0 ? std::min(words, part * zs) : words;
+  const int64_t z1 = std::min(words, z + zs);
+  auto zeros = [&]() __attribute__((always_inline)) {
+    const int64_t at = s * a.n * D + std::min(z, z1) * E;
+    const int left = (int)std::max<int64_t>(0, std::min<int64_t>(z1 - z, IT * 64 * W)) * 16;
+    const Span k(static_cast<T*>(a.dK) + at, left), v(static_cast<T*>(a.dV) + at, left);
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      k.store((u32x4){0, 0, 0, 0}, (i * 64 * W + threadIdx.x) * 16);
+      v.store((u32x4){0, 0, 0, 0}, (i * 64 * W + threadIdx.x) * 16);
     }
-    z = std::min(z, std::max(z0, end));
+    z += IT * 64 * W;
   };
 
-  // dQ of the step before from its ds
-  auto queries = [&](int64_t t) __attribute__((always_inline)) {
+  // dQ of the step before from its ds, and its stores
+  constexpr int UQ = U > 1 ? 2 : 1;  // 16-query tiles of a unit's channels
+  Four<T> dq[SL][UQ];
+  auto queries = [&]() __attribute__((always_inline)) {
     if (!has_unit) return;
-    T* dQ = static_cast<T*>(a.dQ) + (s * a.n_q + t * QT) * D;
-    const int rows = (int)std::min<int64_t>(QT, a.n_q - t * QT);
-    constexpr int UQ = U > 1 ? 2 : 1;  // 16-query tiles of a unit's channels
 #pragma unroll
     for (int y = 0; y < SL; ++y) {
       const int dt = unit0 / 2 + y;
@@ -353,124 +374,123 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
                                        32 * x * Elem<T>::bytes,
                                    g),
                          o[u]);
-        if (KT > 1) __builtin_amdgcn_sched_barrier(0);
+        if (TIGHT) __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int u = 0; u < UQ; ++u) {
-        const int r = 16 * (UQ == 2 ? u : unit0 % 2) + m;
-        if (r < rows) store4<T>(dQ + (uint32_t)(r * D + 16 * dt + 4 * g), o[u] * rd);
-      }
+      for (int u = 0; u < UQ; ++u) dq[y][u] = Four<T>(o[u] * rd);
     }
   };
+  auto put_queries = [&](int64_t t) __attribute__((always_inline)) {
+    const int rows = has_unit && t >= t0 ? (int)std::min<int64_t>(QT, a.n_q - t * QT) : 0;
+    const Span o(static_cast<T*>(a.dQ) + (s * a.n_q + std::max(t, t0) * QT) * D,
+                 rows * D * Elem<T>::bytes);
+#pragma unroll
+    for (int y = 0; y < SL; ++y)
+#pragma unroll
+      for (int u = 0; u < UQ; ++u)
+        o.store(dq[y][u].w, (uint32_t)((16 * (UQ == 2 ? u : unit0 % 2) + m) * D +
+                                       16 * (unit0 / 2 + y) + 4 * g) *
+                                Elem<T>::bytes);
+  };
 
-  __syncthreads();
-  for (int64_t t = t0; t < t1; ++t) {
-    const int buf = (int)(t - t0) & 1;
-    // scores to base 2 and g of keys 4 g + j, query 16 tq + m
-    float p[KT][2][4], gd[KT][2][4];
+  // scores to base 2 and g of keys 4 g + j, query 16 tq + m
+  auto scores = [&](int buf, float (&p)[KT][2][4], float (&gd)[KT][2][4])
+                    __attribute__((always_inline)) {
+    floatx4_t x[KT][2], y[KT][2];
 #pragma unroll
-    for (int tq = 0; tq < 2; ++tq) {
-      floatx4_t x[KT], y[KT];
+    for (int i = 0; i < 2 * KT; ++i) x[i / 2][i % 2] = y[i / 2][i % 2] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) x[kt] = y[kt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+    for (int v = 0; v < NV; ++v) {
+      uint4 kw[KT];
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
+      for (int kt = 0; kt < KT; ++kt)
+        kw[kt] = KL ? lds_word<T, D>(sk + (wave * KT + kt) * 16 * R::stride, v, m, g)
+                    : kf[KL ? 0 : kt][v];
+#pragma unroll
+      for (int tq = 0; tq < 2; ++tq) {
         const uint4 qw = lds_word<T, D>(tile_[buf][0] + 16 * tq * R::stride, v, m, g);
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-          x[kt] = mma_word<T>(
-              KL ? lds_word<T, D>(sk + (wave * KT + kt) * 16 * R::stride, v, m, g)
-                 : kf[KL ? 0 : kt][v],
-              qw, x[kt]);
+        for (int kt = 0; kt < KT; ++kt) x[kt][tq] = mma_word<T>(kw[kt], qw, x[kt][tq]);
 #pragma unroll
         for (int o = OP - 1; o >= 0; --o) {
           const uint4 ow = lds_word<T, D>(tile_[buf][1 + o] + 16 * tq * R::stride, v, m, g);
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt) y[kt] = mma_word<T>(vf[kt][v], ow, y[kt]);
+          for (int kt = 0; kt < KT; ++kt) y[kt][tq] = mma_word<T>(vf[kt][v], ow, y[kt][tq]);
         }
-        if (KT > 1) __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          p[kt][tq][j] = fmaf(x[kt][j], c2, bias[kt][j]);
-          gd[kt][tq][j] = y[kt][j];
-        }
+      if (TIGHT) __builtin_amdgcn_sched_barrier(0);
     }
-    float f[2], dm[2];  // a row's factor and sum p g
-    if (ONE) {
-      auto add = [](float x, float y) { return x + y; };
-      auto larger = [](float x, float y) { return fmaxf(x, y); };
 #pragma unroll
-      for (int tq = 0; tq < 2; ++tq) {
-        float x = kLeast, l = 0.0f, e = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4 * KT; ++i) x = fmaxf(x, p[i / 4][tq][i % 4]);
-        x = across_rows(x, true, larger);
-#pragma unroll
-        for (int i = 0; i < 4 * KT; ++i) {
-          float& w = p[i / 4][tq][i % 4];
-          w = __builtin_amdgcn_exp2f(w - x);
-          l += w;
-          e = fmaf(w, gd[i / 4][tq][i % 4], e);
-        }
-        l = across_rows(l, true, add);
-        e = across_rows(e, true, add);
-        f[tq] = x;
-        if (g == 0) {
-          st[wave][0][16 * tq + m] = x;
-          st[wave][1][16 * tq + m] = l;
-          st[wave][2][16 * tq + m] = e;
-        }
-      }
-      if (t > t0) queries(t - 1);
-      zeros(zrun);
-      __syncthreads();
-      // The waves' statistics under one maximum: lane l takes row l % 32 of half of the waves,
-      // then the halves meet, and rows of 16 lanes trade the two tiles' queries.
-      const int r = lane & 31, h = lane / 32;
-      float x[W / 2], mx = kLeast, l = 0.0f, e = 0.0f;
-#pragma unroll
-      for (int w = 0; w < W / 2; ++w) {
-        x[w] = st[2 * w + h][0][r];
-        mx = fmaxf(mx, x[w]);
-      }
-      auto halves = [](float v, auto op) {
-        float u = v;
-        trade(true, v, u);
-        return op(v, u);
-      };
-      mx = halves(mx, larger);
-#pragma unroll
-      for (int w = 0; w < W / 2; ++w) {
-        const float k = __builtin_amdgcn_exp2f(x[w] - mx);
-        l = fmaf(st[2 * w + h][1][r], k, l);
-        e = fmaf(st[2 * w + h][2][r], k, e);
-      }
-      l = halves(l, add);
-      e = halves(e, add);
-      float inv = l > 0.0f ? 1.0f / l : 0.0f, i1 = inv, m1 = mx;
-      dm[0] = dm[1] = e * inv;
-      trade(false, dm[0], dm[1]);
-      trade(false, inv, i1);
-      trade(false, mx, m1);
-      f[0] = __builtin_amdgcn_exp2f(f[0] - mx) * inv;
-      f[1] = __builtin_amdgcn_exp2f(f[1] - m1) * i1;
-    } else {
-#pragma unroll
-      for (int tq = 0; tq < 2; ++tq) {
-        const int64_t r = t * QT + 16 * tq + m;
-        // (rows past the last: probabilities of 0)
-        const float lse = r < a.n_q ? a.stats[s * a.n_q + r] : INFINITY;
-        dm[tq] = r < a.n_q ? a.stats[(a.S + s) * a.n_q + r] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4 * KT; ++i)
-          p[i / 4][tq][i % 4] = __builtin_amdgcn_exp2f(p[i / 4][tq][i % 4] - lse);
-      }
-      zeros(zrun);
+    for (int i = 0; i < 8 * KT; ++i) {
+      const int kt = i / 8, tq = i / 4 % 2, j = i % 4;
+      p[kt][tq][j] = fmaf(x[kt][tq][j], c2, bias[kt][j]);
+      gd[kt][tq][j] = y[kt][tq][j];
     }
-    // p, and ds in place of g; both to LDS and back by columns, through one place
+  };
+  auto add = [](float x, float y) { return x + y; };
+  auto larger = [](float x, float y) { return fmaxf(x, y); };
+  // weights under the wave's own maxima (top), and the wave's statistics
+  auto local = [&](float (&p)[KT][2][4], const float (&gd)[KT][2][4], float (&top)[2])
+                   __attribute__((always_inline)) {
+#pragma unroll
+    for (int tq = 0; tq < 2; ++tq) {
+      float x = kLeast, l = 0.0f, e = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4 * KT; ++i) x = fmaxf(x, p[i / 4][tq][i % 4]);
+      x = across_rows(x, true, larger);
+#pragma unroll
+      for (int i = 0; i < 4 * KT; ++i) {
+        float& w = p[i / 4][tq][i % 4];
+        w = __builtin_amdgcn_exp2f(w - x);
+        l += w;
+        e = fmaf(w, gd[i / 4][tq][i % 4], e);
+      }
+      l = across_rows(l, true, add);
+      e = across_rows(e, true, add);
+      top[tq] = x;
+      if (g == 0) {
+        st[wave][0][16 * tq + m] = x;
+        st[wave][1][16 * tq + m] = l;
+        st[wave][2][16 * tq + m] = e;
+      }
+    }
+  };
+  // The waves' statistics under one maximum: lane l takes row l % 32 of half of the waves, then
+  // the halves meet, and rows of 16 lanes trade the two tiles' queries.
+  auto joined = [&](const float (&top)[2], float (&f)[2], float (&dm)[2])
+                    __attribute__((always_inline)) {
+    const int r = lane & 31, h = lane / 32;
+    float x[W / 2], mx = kLeast, l = 0.0f, e = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W / 2; ++w) {
+      x[w] = st[2 * w + h][0][r];
+      mx = fmaxf(mx, x[w]);
+    }
+    auto halves = [](float v, auto op) {
+      float u = v;
+      trade(true, v, u);
+      return op(v, u);
+    };
+    mx = halves(mx, larger);
+#pragma unroll
+    for (int w = 0; w < W / 2; ++w) {
+      const float k = __builtin_amdgcn_exp2f(x[w] - mx);
+      l = fmaf(st[2 * w + h][1][r], k, l);
+      e = fmaf(st[2 * w + h][2][r], k, e);
+    }
+    l = halves(l, add);
+    e = halves(e, add);
+    float inv = l > 0.0f ? 1.0f / l : 0.0f, i1 = inv, m1 = mx;
+    dm[0] = dm[1] = e * inv;
+    trade(false, dm[0], dm[1]);
+    trade(false, inv, i1);
+    trade(false, mx, m1);
+    f[0] = __builtin_amdgcn_exp2f(top[0] - mx) * inv;
+    f[1] = __builtin_amdgcn_exp2f(top[1] - m1) * i1;
+  };
+  // dK and dV of a step: p times f, ds in place of g, both through LDS by columns, in one place
+  auto keys = [&](int buf, float (&p)[KT][2][4], float (&gd)[KT][2][4], const float (&f)[2],
+                  const float (&dm)[2]) __attribute__((always_inline)) {
     Column<T> wp[KT], ws[KT];
     unsigned char* mine = ds_ + (wave * KT * 16 + 4 * g) * Elem<T>::bytes + m * SS;
 #pragma unroll
@@ -497,8 +517,8 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
                             gd[i / 2][i % 2][3]});
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) ws[kt] = Column<T>(ds_, SS, wave * KT + kt, m, g);
-    // (one pair of columns at a time: more of them on their way cost registers that are not
-    // there)
+    // (of wide waves one pair of columns at a time: more of them on their way cost registers
+    // that are not there)
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
@@ -510,14 +530,47 @@ __global__ __launch_bounds__(64 * W) void grad_keys_kernel(GradArgs a) {
       const Column<T> x(tile_[buf][0], R::stride, dt, m, g);
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) ak[kt][dt] = x.times(ws[kt], ak[kt][dt]);
-      if (KT > 1) __builtin_amdgcn_sched_barrier(0);
+      if (TIGHT) __builtin_amdgcn_sched_barrier(0);
     }
+  };
+
+  // (Memory operations end in order, stores too: a step makes a number of them that the compiler
+  // knows, so that its wait for the next tile's words is none for the stores made since.)
+  __syncthreads();
+  float p[KT][2][4], gd[KT][2][4], f[2] = {1.0f, 1.0f}, dm[2];
+  for (int64_t t = t0; t < t1; ++t) {
+    const int buf = (int)(t - t0) & 1;
+    scores(buf, p, gd);
+    if (ONE) {
+      float top[2];
+      local(p, gd, top);
+      if (t > t0) queries();
+      __syncthreads();
+      joined(top, f, dm);
+    } else {
+#pragma unroll
+      for (int tq = 0; tq < 2; ++tq) {
+        const int64_t r = t * QT + 16 * tq + m;
+        // (rows past the last: probabilities of 0)
+        const float lse = r < a.n_q ? a.stats[s * a.n_q + r] : INFINITY;
+        dm[tq] = r < a.n_q ? a.stats[(a.S + s) * a.n_q + r] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4 * KT; ++i)
+          p[i / 4][tq][i % 4] = __builtin_amdgcn_exp2f(p[i / 4][tq][i % 4] - lse);
+      }
+    }
+    if (ONE) put_queries(t - 1);
+    zeros();
+    keys(buf, p, gd, f, dm);
     put(buf ^ 1);
     load(t + 2);
     __syncthreads();
   }
-  if (ONE) queries(t1 - 1);
-  zeros(z1);
+  if (ONE) {
+    queries();
+    put_queries(t1 - 1);
+  }
+  for (int64_t i = (z1 - z + IT * 64 * W - 1) / (IT * 64 * W); i > 0; --i) zeros();
 
   float* out = a.part + (int64_t)blockIdx.x * NK * 2 * D;
 #pragma unroll
@@ -549,7 +602,7 @@ constexpr int RW = 4;  // waves
 template <typename T, typename TO, int D>
 __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   using R = LdsRows<T, D>;
-  constexpr int NV = Frag<T, D>::NV, DT = D / 16, OP = Parts<T, TO>::n, E = 16 / Elem<T>::bytes;
+  constexpr int NV = Frag<T, D>::NV, DT = D / 16, OP = Parts<T, TO>::n;
   constexpr int CK = 32;  // keys per step
   __shared__ __align__(16) unsigned char sk[CK * R::stride], sv[CK * R::stride];
   __shared__ float sb[CK];
@@ -560,11 +613,14 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   const bool there = r < a.n_q;
   uint4 qf[NV], of[OP][NV];
   load_frag<T, D>(static_cast<const T*>(a.Q), s * a.n_q + r, g, there, qf);
+  const int64_t r0 = __builtin_amdgcn_readfirstlane((int)(r - m));  // the wave's first row
+  const Span dO(static_cast<const TO*>(a.dO) + (s * a.n_q + std::min(r0, a.n_q - 1)) * D,
+                (int)std::max<int64_t>(0, std::min<int64_t>(16, a.n_q - r0)) * D *
+                    Elem<TO>::bytes);
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     RawWord<T, TO> w;
-    w.clear();
-    if (there) w.load(static_cast<const TO*>(a.dO) + (s * a.n_q + r) * D + (4 * v + g) * E);
+    w.load(dO, m * R::CW + 4 * v + g);
     u32x4 x[2];
     w.parts(x);
 #pragma unroll
@@ -724,6 +780,8 @@ hipError_t keys_d(const GradArgs& a, hipStream_t st) {
   if (a.shape.waves == 4) return keys_one<T, TO, D, 4, 1>(a, st);
   if constexpr (Elem<T>::bytes == 2)
     if (a.shape.tiles == 2) return keys_one<T, TO, D, 8, 2>(a, st);
+  if constexpr (Elem<T>::bytes == 2)
+    if (a.shape.waves == 12) return keys_one<T, TO, D, 12, 1>(a, st);
   return keys_one<T, TO, D, 8, 1>(a, st);
 }
 

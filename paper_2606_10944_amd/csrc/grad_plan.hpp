@@ -23,14 +23,18 @@ struct GradShape {
 // take half of its registers, or 16 (float32).
 constexpr int64_t grad_most_keys(bool bf16) { return bf16 ? 256 : 128; }
 
-inline GradShape grad_shape(int64_t S, int64_t n_q, int64_t n_out, bool bf16) {
+inline GradShape grad_shape(int64_t S, int64_t n_q, int64_t n_out, int64_t d, bool bf16) {
   GradShape s{};
   s.one = n_out <= grad_most_keys(bf16);
   s.waves = n_out <= 32 ? 2 : n_out <= 64 ? 4 : 8;
   s.tiles = bf16 && n_out > 128 ? 2 : 1;
+  if (bf16 && n_out > 128 && n_out <= 192 && d == 128) {
+    s.waves = 12;
+    s.tiles = 1;
+  }
   s.chunks = (int32_t)((n_out + s.keys() - 1) / s.keys());
   const int64_t steps = (n_q + kGradTile - 1) / kGradTile;
-  const int64_t slots = 256 * (8 / s.waves);
+  const int64_t slots = 256 * (s.waves > 8 ? 1 : 8 / s.waves);
   const StepSplit p = split_steps(S * s.chunks, steps, slots, 2.0, 1.0);
   s.parts = (int32_t)p.parts;
   s.run = (int32_t)p.run;

@@ -8,8 +8,8 @@ from typing import Optional
 
 import torch
 
-from ._lib import THIN_EDTYPE, THIN_EINVAL, ThinError, _check, _shape4, lib, thin_attention
-from .q4 import _dtype, _empty, _on, _where, _workspace
+from ._lib import THIN_EDTYPE, THIN_EINVAL, ThinError, _check, lib, thin_attention
+from .q4 import _dtype, _empty, _empty_like, _on, _where, _workspace
 
 
 @lru_cache(maxsize=4096)
@@ -20,12 +20,17 @@ def _bytes(dtype: int, B: int, H: int, n_q: int, n: int, d: int, n_out: int) -> 
     return need.value
 
 
-def _gradient(t: Optional[torch.Tensor], shape, dtype: torch.dtype, dev: int, stream, name: str):
-    if t is None:
-        return _empty(shape, dtype, dev, stream)
-    if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
-        raise ThinError(THIN_EINVAL, f"{name} must be contiguous {dtype} {list(shape)}")
-    return t
+def _rows4(t: torch.Tensor, dev: int, name: str) -> int:
+    """The address of contiguous rows [B,H,rows,d] on device `dev`."""
+    if t.dim() != 4 or not t.is_contiguous():
+        raise ThinError(THIN_EINVAL, f"{name} must be a contiguous [B,H,rows,d] tensor")
+    return _on(t, dev, name)
+
+
+def _gradient(t: torch.Tensor, like: torch.Tensor, dev: int, name: str) -> int:
+    if t.shape != like.shape or t.dtype != like.dtype or not t.is_contiguous():
+        raise ThinError(THIN_EINVAL, f"{name} must be contiguous {like.dtype} {list(like.shape)}")
+    return _on(t, dev, name)
 
 
 def thin_attention_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, idx: torch.Tensor,
@@ -39,39 +44,49 @@ def thin_attention_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, i
     dlogw is given).  dK and dV are [B,H,n,d], zeros in the rows that idx does not list.  The
     forward's output is not needed."""
     dev, st = _where(stream)
-    B, H, n_q, d = _shape4(Q, "Q")
-    Bk, Hk, n, dk = _shape4(K, "K")
-    if (Bk, Hk, dk) != (B, H, d) or _shape4(V, "V") != (B, H, n, d):
+    q, k, v, do = (_rows4(Q, dev, "Q"), _rows4(K, dev, "K"), _rows4(V, dev, "V"),
+                   _rows4(dO, dev, "dO"))
+    B, H, n_q, d = Q.shape
+    n = K.shape[2]
+    if K.shape != (B, H, n, d) or V.shape != K.shape:
         raise ThinError(THIN_EINVAL, "Q/K/V shapes disagree")
-    if K.dtype != Q.dtype or V.dtype != Q.dtype:
+    dt = Q.dtype
+    if K.dtype != dt or V.dtype != dt:
         raise ThinError(THIN_EDTYPE, "Q, K, V must share a dtype")
-    if _shape4(dO, "dO") != (B, H, n_q, d):
+    if dO.shape != Q.shape:
         raise ThinError(THIN_EINVAL, "dO must match Q")
-    if idx.dtype != torch.int32 or idx.dim() != 3 or idx.shape[:2] != (B, H) \
-            or not idx.is_contiguous():
+    n_out = idx.shape[-1]
+    if idx.dtype != torch.int32 or idx.shape != (B, H, n_out) or not idx.is_contiguous():
         raise ThinError(THIN_EINVAL, "idx must be contiguous int32 [B,H,n_out]")
-    n_out = idx.shape[2]
+    i = _on(idx, dev, "idx")
     w = None
     if logw is not None:
-        if logw.dtype != torch.float32 or logw.shape != (B, H, n_out) or not logw.is_contiguous():
+        if logw.dtype != torch.float32 or logw.shape != idx.shape or not logw.is_contiguous():
             raise ThinError(THIN_EINVAL, "logw must be contiguous float32 [B,H,n_out]")
         w = _on(logw, dev, "logw")
     code, out_code = _dtype(Q, "Q"), _dtype(dO, "dO")
-    ins = [_on(t, dev, name) for t, name in ((Q, "Q"), (K, "K"), (V, "V"), (idx, "idx"),
-                                             (dO, "dO"))]
     need = _bytes(code, B, H, n_q, n, d, n_out)
-    need_logw = need_logw or dlogw is not None
-    dQ = _gradient(dQ, Q.shape, Q.dtype, dev, stream, "dQ")
-    dK = _gradient(dK, K.shape, K.dtype, dev, stream, "dK")
-    dV = _gradient(dV, V.shape, V.dtype, dev, stream, "dV")
-    if need_logw:
-        dlogw = _gradient(dlogw, idx.shape, torch.float32, dev, stream, "dlogw")
+    if dQ is None:
+        dQ = _empty_like(Q, dev, stream)
+    if dK is None:
+        dK = _empty_like(K, dev, stream)
+    if dV is None:
+        dV = _empty_like(V, dev, stream)
+    g = (_gradient(dQ, Q, dev, "dQ"), _gradient(dK, K, dev, "dK"), _gradient(dV, V, dev, "dV"))
+    dw = None
+    if need_logw or dlogw is not None:
+        if dlogw is None:
+            dlogw = _empty(idx.shape, torch.float32, dev, stream)
+        elif dlogw.dtype != torch.float32 or dlogw.shape != idx.shape \
+                or not dlogw.is_contiguous():
+            raise ThinError(THIN_EINVAL, "dlogw must be contiguous float32 [B,H,n_out]")
+        dw = _on(dlogw, dev, "dlogw")
     ws, wp, wn = _workspace(workspace, need, dev, stream)
-    _check(lib().thin_attention_backward(
-        ins[0], ins[1], ins[2], code, B, H, n_q, n, d, ins[3], w, n_out, ins[4], out_code,
-        _on(dQ, dev, "dQ"), _on(dK, dev, "dK"), _on(dV, dev, "dV"),
-        _on(dlogw, dev, "dlogw") if need_logw else None, wp, wn, st), "thin_attention_backward")
-    return (dQ, dK, dV, dlogw) if need_logw else (dQ, dK, dV)
+    rc = lib().thin_attention_backward(q, k, v, code, B, H, n_q, n, d, i, w, n_out, do, out_code,
+                                       g[0], g[1], g[2], dw, wp, wn, st)
+    if rc:
+        _check(rc, "thin_attention_backward")
+    return (dQ, dK, dV) if dw is None else (dQ, dK, dV, dlogw)
 
 
 class _CoresetAttention(torch.autograd.Function):

@@ -57,8 +57,9 @@ int main() {
   const int64_t Ss[] = {1, 2, 5, 16, 64, 100, 257, 1000, 65535};
   const int64_t qs[] = {1, 31, 32, 33, 100, 1023, 4096, 16384, 65536, 1000003};
   const int64_t ks[] = {1, 16, 17, 32, 33, 64, 65, 128, 129, 192, 256, 257, 600, 5000, 300000};
-  for (int64_t S : Ss) for (int64_t q : qs) for (int64_t k : ks) for (int b = 0; b < 2; ++b) {
-    const GradShape s = grad_shape(S, q, k, b);
+  for (int64_t S : Ss) for (int64_t q : qs) for (int64_t k : ks) for (int b = 0; b < 2; ++b)
+  for (int64_t d : {32, 64, 128}) {
+    const GradShape s = grad_shape(S, q, k, d, b);
     const int64_t steps = (q + kGradTile - 1) / kGradTile;
     // every key and every step has a workgroup, none is without a step
     if (s.keys() * s.chunks < k || s.keys() * (s.chunks - 1) >= k) return 1;
