@@ -125,6 +125,9 @@ struct Span {
   __device__ __forceinline__ u32x4 load16(uint32_t at) const {
     return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0);
   }
+  __device__ __forceinline__ uint32_t load4(uint32_t at) const {
+    return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0);
+  }
   __device__ __forceinline__ u32x2 load8(uint32_t at) const {
     return __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0);
   }
@@ -265,6 +268,19 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
       ro[i].load(o, i * 64 * W + threadIdx.x);
     }
   };
+  // without ONE, the next step's statistics.  (Rows past the last have a dO of 0, and so a g, a
+  // sum p g and a ds of 0 whatever their maximum.)
+  uint32_t next[2][2];
+  auto statistics = [&](int64_t t) __attribute__((always_inline)) {
+    const int rows = t < t1 ? (int)std::min<int64_t>(QT, a.n_q - t * QT) : 0;
+    const int64_t at = s * a.n_q + (rows > 0 ? t * QT : 0);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const Span x(a.stats + k * a.S * a.n_q + at, rows * 4);
+#pragma unroll
+      for (int tq = 0; tq < 2; ++tq) next[k][tq] = x.load4((16 * tq + m) * 4);
+    }
+  };
   auto put = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
@@ -323,6 +339,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
   }
   put(0);
   load(t0 + 1);
+  if (!ONE) statistics(t0);
 
   floatx4_t ak[KT][DT], av[KT][DT];
   float aw[KT][4];
@@ -550,14 +567,13 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
     } else {
 #pragma unroll
       for (int tq = 0; tq < 2; ++tq) {
-        const int64_t r = t * QT + 16 * tq + m;
-        // (rows past the last: probabilities of 0)
-        const float lse = r < a.n_q ? a.stats[s * a.n_q + r] : INFINITY;
-        dm[tq] = r < a.n_q ? a.stats[(a.S + s) * a.n_q + r] : 0.0f;
+        const float lse = __uint_as_float(next[0][tq]);
+        dm[tq] = __uint_as_float(next[1][tq]);
 #pragma unroll
         for (int i = 0; i < 4 * KT; ++i)
           p[i / 4][tq][i % 4] = __builtin_amdgcn_exp2f(p[i / 4][tq][i % 4] - lse);
       }
+      statistics(t + 1);
     }
     if (ONE) put_queries(t - 1);
     zeros();
@@ -597,20 +613,64 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
 // twice, for the rows' statistics, then for dQ.  Scores S^T = K Q^T: lane (m, g) holds keys
 // 4 g .. 4 g + 3 of query m.
 // ---------------------------------------------------------------------------
-constexpr int RW = 4;  // waves
+constexpr int RW = 8;  // waves
 
 template <typename T, typename TO, int D>
 __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   using R = LdsRows<T, D>;
   constexpr int NV = Frag<T, D>::NV, DT = D / 16, OP = Parts<T, TO>::n;
   constexpr int CK = 32;  // keys per step
-  __shared__ __align__(16) unsigned char sk[CK * R::stride], sv[CK * R::stride];
-  __shared__ float sb[CK];
+  constexpr int IT = (CK * R::CW + 64 * RW - 1) / (64 * RW);  // words of a step per thread
+  __shared__ __align__(16) unsigned char sk[2][CK * R::stride], sv[2][CK * R::stride];
+  __shared__ float sb[2][CK];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
   const int64_t blocks = (a.n_q + 16 * RW - 1) / (16 * RW);
   const int64_t s = blockIdx.x / blocks;
   const int64_t r = (blockIdx.x % blocks * RW + wave) * 16 + m;  // this lane's query
   const bool there = r < a.n_q;
+  // A step's rows are on their way while the step before is worked on, and their numbers a step
+  // before that: a word's address waits for no load.
+  int row[IT];
+  float bias[IT], bias_next[IT];
+  u32x4 kw[IT], vw[IT];
+  const T* K = static_cast<const T*>(a.K) + s * a.n * D;
+  const T* V = static_cast<const T*>(a.V) + s * a.n * D;
+  auto number = [&](int64_t k0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < IT; ++i)
+      row[i] = coreset_row(a, s, k0 + (i * 64 * RW + (int)threadIdx.x) / R::CW, &bias_next[i]);
+  };
+  auto load = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      bias[i] = bias_next[i];
+      kw[i] = vw[i] = (u32x4){0, 0, 0, 0};
+      if (row[i] >= 0) {
+        const int64_t at = (int64_t)row[i] * R::CW + threadIdx.x % R::CW;
+        kw[i] = reinterpret_cast<const u32x4*>(K)[at];
+        vw[i] = reinterpret_cast<const u32x4*>(V)[at];
+      }
+    }
+  };
+  auto put = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int item = i * 64 * RW + (int)threadIdx.x;
+      if (item >= CK * R::CW) continue;
+      const int to = item / R::CW * R::stride + item % R::CW * 16;
+      *reinterpret_cast<u32x4*>(sk[buf] + to) = kw[i];
+      *reinterpret_cast<u32x4*>(sv[buf] + to) = vw[i];
+      if (item % R::CW == 0) sb[buf][item / R::CW] = bias[i];
+    }
+  };
+  static_assert(64 * RW % R::CW == 0, "a thread's words lie in one column");
+  const int64_t steps = (a.n_out + CK - 1) / CK;
+  // step i of 2 * steps: the keys twice
+  auto first = [&](int64_t i) { return (i < steps ? i : i - steps) * CK; };
+  number(0);
+  load();
+  number(first(1));
+
   uint4 qf[NV], of[OP][NV];
   load_frag<T, D>(static_cast<const T*>(a.Q), s * a.n_q + r, g, there, qf);
   const int64_t r0 = __builtin_amdgcn_readfirstlane((int)(r - m));  // the wave's first row
@@ -626,62 +686,55 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
 #pragma unroll
     for (int p = 0; p < OP; ++p) of[p][v] = __builtin_bit_cast(uint4, x[p]);
   }
-  const T* K = static_cast<const T*>(a.K) + s * a.n * D;
-  const T* V = static_cast<const T*>(a.V) + s * a.n * D;
   const float c2 = (float)(kLog2e / sqrt((double)D)), rd = (float)(1.0 / sqrt((double)D));
-  auto stage = [&](int64_t k0) __attribute__((always_inline)) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < CK * R::CW; i += 64 * RW) {
-      float b;
-      const int row = coreset_row(a, s, k0 + i / R::CW, &b);
-      u32x4 kw = {0, 0, 0, 0}, vw = kw;
-      if (row >= 0) {
-        kw = reinterpret_cast<const u32x4*>(K + (int64_t)row * D)[i % R::CW];
-        vw = reinterpret_cast<const u32x4*>(V + (int64_t)row * D)[i % R::CW];
-      }
-      const int to = i / R::CW * R::stride + i % R::CW * 16;
-      *reinterpret_cast<u32x4*>(sk + to) = kw;
-      *reinterpret_cast<u32x4*>(sv + to) = vw;
-      if (i % R::CW == 0) sb[i / R::CW] = b;
-    }
-    __syncthreads();
-  };
-  auto products = [&](float (&p)[2][4], float (&gd)[2][4]) __attribute__((always_inline)) {
+  auto products = [&](int buf, float (&p)[2][4], float (&gd)[2][4]) __attribute__((always_inline)) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
       floatx4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        x = mma_word<T>(lds_word<T, D>(sk + 16 * kt * R::stride, v, m, g), qf[v], x);
-        const uint4 vw = lds_word<T, D>(sv + 16 * kt * R::stride, v, m, g);
+        x = mma_word<T>(lds_word<T, D>(sk[buf] + 16 * kt * R::stride, v, m, g), qf[v], x);
+        const uint4 vw = lds_word<T, D>(sv[buf] + 16 * kt * R::stride, v, m, g);
 #pragma unroll
         for (int o = OP - 1; o >= 0; --o) y = mma_word<T>(vw, of[o][v], y);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        p[kt][j] = fmaf(x[j], c2, sb[16 * kt + 4 * g + j]);
+        p[kt][j] = fmaf(x[j], c2, sb[buf][16 * kt + 4 * g + j]);
         gd[kt][j] = y[j];
       }
     }
   };
+  put(0);
+  load();
+  number(first(2));
+  __syncthreads();
+
   float mx = kLeast, l = 0.0f, e = 0.0f;
-  for (int64_t k0 = 0; k0 < a.n_out; k0 += CK) {
-    stage(k0);
+  int64_t i = 0;
+  auto turn = [&]() __attribute__((always_inline)) {
+    put((int)(i + 1) & 1);
+    load();
+    number(first(i + 3));
+    __syncthreads();
+  };
+  for (; i < steps; ++i) {
     float p[2][4], gd[2][4];
-    products(p, gd);
+    products((int)i & 1, p, gd);
     float x = mx;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x = fmaxf(x, p[i / 4][i % 4]);
+    for (int j = 0; j < 8; ++j) x = fmaxf(x, p[j / 4][j % 4]);
     const float k = __builtin_amdgcn_exp2f(mx - x);
     mx = x;
     l *= k;
     e *= k;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float w = __builtin_amdgcn_exp2f(p[i / 4][i % 4] - mx);
+    for (int j = 0; j < 8; ++j) {
+      const float w = __builtin_amdgcn_exp2f(p[j / 4][j % 4] - mx);
       l += w;
-      e = fmaf(w, gd[i / 4][i % 4], e);
+      e = fmaf(w, gd[j / 4][j % 4], e);
     }
+    turn();
   }
   auto add = [](float x, float y) { return x + y; };
   const float top = across_rows(mx, true, [](float x, float y) { return fmaxf(x, y); });
@@ -698,18 +751,19 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   floatx4_t acc[DT];
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) acc[dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
-  for (int64_t k0 = 0; k0 < a.n_out; k0 += CK) {
-    stage(k0);
+  for (; i < 2 * steps; ++i) {
+    const int buf = (int)i & 1;
     float p[2][4], gd[2][4];
-    products(p, gd);
+    products(buf, p, gd);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      p[i / 4][i % 4] =
-          __builtin_amdgcn_exp2f(p[i / 4][i % 4] - lse) * (gd[i / 4][i % 4] - dm);
+    for (int j = 0; j < 8; ++j)
+      p[j / 4][j % 4] =
+          __builtin_amdgcn_exp2f(p[j / 4][j % 4] - lse) * (gd[j / 4][j % 4] - dm);
     const Column<T> w(p);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
-      acc[dt] = Column<T>(sk, R::stride, dt, m, g).times(w, acc[dt]);
+      acc[dt] = Column<T>(sk[buf], R::stride, dt, m, g).times(w, acc[dt]);
+    turn();
   }
   if (!there) return;
 #pragma unroll
@@ -744,17 +798,27 @@ __global__ __launch_bounds__(256) void grad_join_kernel(GradArgs a) {
   if (r < 0 || r >= a.n) return;
   constexpr int V = 2 * D / 4;  // lanes of a row of sums, four channels each
   floatx4_t o = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t i0 = 0; i0 < a.n_out; i0 += 64) {
-    uint64_t same = __ballot(i0 + lane < a.n_out && idx[i0 + lane] == r);
-    while (same) {
-      const int64_t i = i0 + __ffsll((unsigned long long)same) - 1;
-      same &= same - 1;
-      if (i < j) return;
-      if (lane < V) {
-        const float* p = a.part + slot(i, 0) * 2 * D + lane * 4;
-#pragma unroll 4
-        for (int x = 0; x < a.shape.parts; ++x)
-          o += *reinterpret_cast<const floatx4_t*>(p + x * NK * 2 * D);
+  constexpr int BATCH = 8;  // places of the list per lane at a time
+  for (int64_t i0 = 0; i0 < a.n_out; i0 += 64 * BATCH) {
+    int32_t at[BATCH];
+#pragma unroll
+    for (int x = 0; x < BATCH; ++x) {
+      const int64_t i = i0 + x * 64 + lane;
+      at[x] = idx[i < a.n_out ? i : a.n_out - 1];
+    }
+#pragma unroll
+    for (int x = 0; x < BATCH; ++x) {
+      uint64_t same = __ballot(at[x] == r && i0 + x * 64 + lane < a.n_out);
+      while (same) {
+        const int64_t i = i0 + x * 64 + __ffsll((unsigned long long)same) - 1;
+        same &= same - 1;
+        if (i < j) return;
+        if (lane < V) {
+          const float* p = a.part + slot(i, 0) * 2 * D + lane * 4;
+#pragma unroll 8
+          for (int y = 0; y < a.shape.parts; ++y)
+            o += *reinterpret_cast<const floatx4_t*>(p + y * NK * 2 * D);
+        }
       }
     }
   }

@@ -27,7 +27,7 @@ inline GradShape grad_shape(int64_t S, int64_t n_q, int64_t n_out, int64_t d, bo
   GradShape s{};
   s.one = n_out <= grad_most_keys(bf16);
   s.waves = n_out <= 32 ? 2 : n_out <= 64 ? 4 : 8;
-  s.tiles = bf16 && n_out > 128 ? 2 : 1;
+  s.tiles = bf16 && n_out > 128 && (s.one || d < 128) ? 2 : 1;
   if (bf16 && n_out > 128 && n_out <= 192 && d == 128) {
     s.waves = 12;
     s.tiles = 1;
