@@ -619,7 +619,7 @@ template <typename T, typename TO, int D>
 __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   using R = LdsRows<T, D>;
   constexpr int NV = Frag<T, D>::NV, DT = D / 16, OP = Parts<T, TO>::n;
-  constexpr int CK = 32;  // keys per step
+  constexpr int CK = 64, KT = CK / 16;  // keys per step
   constexpr int IT = (CK * R::CW + 64 * RW - 1) / (64 * RW);  // words of a step per thread
   __shared__ __align__(16) unsigned char sk[2][CK * R::stride], sv[2][CK * R::stride];
   __shared__ float sb[2][CK];
@@ -628,38 +628,45 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   const int64_t s = blockIdx.x / blocks;
   const int64_t r = (blockIdx.x % blocks * RW + wave) * 16 + m;  // this lane's query
   const bool there = r < a.n_q;
-  // A step's rows are on their way while the step before is worked on, and their numbers a step
-  // before that: a word's address waits for no load.
-  int row[IT];
-  float bias[IT], bias_next[IT];
+  // A step's rows are on their way while the step before is worked on, and their numbers and
+  // log-weights a step before that, without branches: no load waits for another.
+  int32_t at[IT];
+  float lw[IT], bias[IT];
   u32x4 kw[IT], vw[IT];
   const T* K = static_cast<const T*>(a.K) + s * a.n * D;
   const T* V = static_cast<const T*>(a.V) + s * a.n * D;
+  const int32_t* idx = a.idx + s * a.n_out;
+  const float* logw = a.logw ? a.logw + s * a.n_out : reinterpret_cast<const float*>(idx);
+  auto place = [&](int64_t k0, int i) { return k0 + (i * 64 * RW + (int)threadIdx.x) / R::CW; };
   auto number = [&](int64_t k0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < IT; ++i)
-      row[i] = coreset_row(a, s, k0 + (i * 64 * RW + (int)threadIdx.x) / R::CW, &bias_next[i]);
+    for (int i = 0; i < IT; ++i) {
+      const int64_t j = std::min(place(k0, i), a.n_out - 1);
+      at[i] = idx[j];
+      lw[i] = logw[j];
+    }
   };
-  auto load = [&]() __attribute__((always_inline)) {
+  auto load = [&](int64_t k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      bias[i] = bias_next[i];
-      kw[i] = vw[i] = (u32x4){0, 0, 0, 0};
-      if (row[i] >= 0) {
-        const int64_t at = (int64_t)row[i] * R::CW + threadIdx.x % R::CW;
-        kw[i] = reinterpret_cast<const u32x4*>(K)[at];
-        vw[i] = reinterpret_cast<const u32x4*>(V)[at];
-      }
+      const float w = a.logw ? lw[i] : 0.0f;
+      const bool is = place(k0, i) < a.n_out && at[i] >= 0 && at[i] < a.n && w != -INFINITY;
+      bias[i] = is ? w * (float)kLog2e : -INFINITY;
+      const int64_t word = (int64_t)(is ? at[i] : 0) * R::CW + threadIdx.x % R::CW;
+      kw[i] = reinterpret_cast<const u32x4*>(K)[word];
+      vw[i] = reinterpret_cast<const u32x4*>(V)[word];
     }
   };
   auto put = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
       const int item = i * 64 * RW + (int)threadIdx.x;
-      if (item >= CK * R::CW) continue;
+      if (CK * R::CW % (64 * RW) != 0 && item >= CK * R::CW) continue;
       const int to = item / R::CW * R::stride + item % R::CW * 16;
-      *reinterpret_cast<u32x4*>(sk[buf] + to) = kw[i];
-      *reinterpret_cast<u32x4*>(sv[buf] + to) = vw[i];
+      const u32x4 none = {0, 0, 0, 0};
+      const bool is = bias[i] != -INFINITY;
+      *reinterpret_cast<u32x4*>(sk[buf] + to) = is ? kw[i] : none;
+      *reinterpret_cast<u32x4*>(sv[buf] + to) = is ? vw[i] : none;
       if (item % R::CW == 0) sb[buf][item / R::CW] = bias[i];
     }
   };
@@ -668,7 +675,7 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   // step i of 2 * steps: the keys twice
   auto first = [&](int64_t i) { return (i < steps ? i : i - steps) * CK; };
   number(0);
-  load();
+  load(0);
   number(first(1));
 
   uint4 qf[NV], of[OP][NV];
@@ -687,9 +694,9 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
     for (int p = 0; p < OP; ++p) of[p][v] = __builtin_bit_cast(uint4, x[p]);
   }
   const float c2 = (float)(kLog2e / sqrt((double)D)), rd = (float)(1.0 / sqrt((double)D));
-  auto products = [&](int buf, float (&p)[2][4], float (&gd)[2][4]) __attribute__((always_inline)) {
+  auto products = [&](int buf, float (&p)[KT][4], float (&gd)[KT][4]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
+    for (int kt = 0; kt < KT; ++kt) {
       floatx4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -706,7 +713,7 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
     }
   };
   put(0);
-  load();
+  load(first(1));
   number(first(2));
   __syncthreads();
 
@@ -714,22 +721,22 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   int64_t i = 0;
   auto turn = [&]() __attribute__((always_inline)) {
     put((int)(i + 1) & 1);
-    load();
+    load(first(i + 2));
     number(first(i + 3));
     __syncthreads();
   };
   for (; i < steps; ++i) {
-    float p[2][4], gd[2][4];
+    float p[KT][4], gd[KT][4];
     products((int)i & 1, p, gd);
     float x = mx;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x = fmaxf(x, p[j / 4][j % 4]);
+    for (int j = 0; j < 4 * KT; ++j) x = fmaxf(x, p[j / 4][j % 4]);
     const float k = __builtin_amdgcn_exp2f(mx - x);
     mx = x;
     l *= k;
     e *= k;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < 4 * KT; ++j) {
       const float w = __builtin_amdgcn_exp2f(p[j / 4][j % 4] - mx);
       l += w;
       e = fmaf(w, gd[j / 4][j % 4], e);
@@ -753,16 +760,19 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   for (int dt = 0; dt < DT; ++dt) acc[dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
   for (; i < 2 * steps; ++i) {
     const int buf = (int)i & 1;
-    float p[2][4], gd[2][4];
+    float p[KT][4], gd[KT][4];
     products(buf, p, gd);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < 4 * KT; ++j)
       p[j / 4][j % 4] =
           __builtin_amdgcn_exp2f(p[j / 4][j % 4] - lse) * (gd[j / 4][j % 4] - dm);
-    const Column<T> w(p);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-      acc[dt] = Column<T>(sk[buf], R::stride, dt, m, g).times(w, acc[dt]);
+    for (int h = 0; h < KT / 2; ++h) {
+      const Column<T> w(p + 2 * h);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        acc[dt] = Column<T>(sk[buf] + 32 * h * R::stride, R::stride, dt, m, g).times(w, acc[dt]);
+    }
     turn();
   }
   if (!there) return;
