@@ -125,7 +125,9 @@ int attention(const thin_q4_cache_t* cache, const void* Q, const int64_t* q_stri
   a.shape = p.shape;
   if (p.bytes) {
     a.part = static_cast<float*>(workspace);
-    if (!blocks && p.shape.waves)
+    // (the kernel for many rows shares keys out by length for trees alone)
+    const bool several = seen && c.B > 1 && c.B <= thin::kQ4SharedEntries;
+    if (!blocks && (p.shape.waves || several))
       a.table = reinterpret_cast<int2*>(static_cast<char*>(workspace) + p.sums);
   }
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -106,84 +106,6 @@ __device__ __forceinline__ int steps_of(const Q4View& c, const Q4AttnArgs& a, in
   return (tile_row<MODE>(c, a, b, tt) + CH) / CH;
 }
 
-// How the workgroups of a key head and tile share the sequences' steps.  Every
-// sequence gets workgroups by its length: a share is what a workgroup takes of one
-// sequence, the least for which the workgroups are enough.  Lane l holds sequences
-// l, l + 64, ..
-template <int MODE>
-struct Shares {
-  static constexpr int N = kQ4SharedEntries / 64;
-  int steps[N];  // of this lane's sequences
-  int upto[N];   // shares of the sequences up to each of them
-  uint32_t share;
-
-  __device__ __forceinline__ uint32_t count(int i) const {
-    return ((uint32_t)steps[i] + share - 1) / share;
-  }
-
-  __device__ __forceinline__ Shares(const Q4View& c, const Q4AttnArgs& a, int tile, int lane) {
-    const TileTokens tt = tile_tokens(a, tile);
-    auto add = [](uint32_t x, uint32_t y) { return x + y; };
-    int sum = 0;  // (at most 2^24: 256 sequences, 2^16 steps each)
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      steps[i] = 0;
-      if (i * 64 < c.B && i * 64 + lane < c.B) steps[i] = steps_of<MODE>(c, a, i * 64 + lane, tt);
-      sum += steps[i];
-    }
-    sum = (int)wave_reduce<uint32_t>((uint32_t)sum, 0u, add);
-    // Rounded up per sequence, the shares are up to B more than the sum's: none of that is
-    // set aside at first, then quarters of B, until the workgroups are enough.  (Setting B
-    // aside at once left 32 sequences of one length half of theirs.)
-    const int groups = c.B * a.shape.splits;
-    for (int q = 0; q <= 4; ++q) {
-      const uint32_t spare = (uint32_t)(groups - c.B * q / 4);
-      const uint32_t even = ((uint32_t)sum + spare - 1) / spare;
-      share = (uint32_t)__builtin_amdgcn_readfirstlane(
-          (int)std::max(even, (uint32_t)a.shape.least));
-      uint32_t taken = 0;
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (i * 64 < c.B) taken += count(i);
-      if (wave_reduce<uint32_t>(taken, 0u, add) <= (uint32_t)groups) break;
-    }
-    int before = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      upto[i] = before;
-      if (i * 64 >= c.B) continue;
-      upto[i] += (int)wave_scan<uint32_t>(count(i), 0u, add);
-      before = __builtin_amdgcn_readlane(upto[i], 63);
-    }
-  }
-
-  // Workgroup j's sequence (-1: none is left for it) and steps i0 .. i1 - 1.
-  __device__ __forceinline__ int find(const Q4View& c, int j, int* i0, int* i1) const {
-    int b = -1;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (i * 64 >= c.B || b >= 0) continue;
-      const uint64_t past = __ballot(upto[i] > j);
-      if (!past) continue;
-      const int l = __ffsll((unsigned long long)past) - 1;
-      const int first = __builtin_amdgcn_readlane(upto[i] - (int)count(i), l);
-      *i0 = __builtin_amdgcn_readfirstlane((j - first) * (int)share);
-      const int end = __builtin_amdgcn_readlane(steps[i], l);
-      *i1 = *i0 + (int)share < end ? *i0 + (int)share : end;
-      b = i * 64 + l;
-    }
-    return b;
-  }
-
-  // The first of every sequence's workgroups and how many there are.
-  __device__ __forceinline__ void write(const Q4View& c, int2* table, int lane) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i * 64 + lane < c.B)
-        table[i * 64 + lane] = make_int2(upto[i] - (int)count(i), (int)count(i));
-  }
-};
-
 // WV waves.  Without splits a workgroup takes a tile's whole keys; with them
 // workgroups share the keys and leave sums in a.part, one slot of existing rows each.
 // (bf16 lists: 128 registers hold four workgroups in a compute unit, 128 -> 123 us for 32
@@ -226,7 +148,8 @@ void q4_attn_kernel(Q4View c, Q4AttnArgs a) {
     const int groups = c.B * splits;
     h = blockIdx.y;
     tile = blockIdx.x / groups;
-    const Shares<MODE> sh(c, a, tile, lane);
+    const TileTokens tt = tile_tokens(a, tile);
+    const Shares sh(c, a, lane, [&](int i) { return steps_of<MODE>(c, a, i, tt); });
     // one workgroup per tile leaves the table that the join goes by
     if (h == 0 && blockIdx.x % groups == 0 && wave == 0) sh.write(c, a.table + tile * c.B, lane);
     b = sh.find(c, blockIdx.x % groups, &i0, &i1);

@@ -43,10 +43,31 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
   // slice by slice; a slice's last tiles, which see the most rows, come first; the
   // workgroups that share a tile's keys side by side
   const uint32_t piece = xcd_contiguous();
-  const int slice = piece / gridDim.x, b = slice / c.H, h = slice % c.H;
-  const int splits = SPLIT ? a.shape.splits : 1, split = SPLIT ? piece % splits : 0;
-  const int tile = (int)(gridDim.x / splits) - 1 - (int)(piece % gridDim.x / splits);
+  int slice = piece / gridDim.x, b = slice / c.H, h = slice % c.H;
+  const int splits = SPLIT ? a.shape.splits : 1;
+  int split = SPLIT ? piece % splits : 0;
+  int tile = (int)(gridDim.x / splits) - 1 - (int)(piece % gridDim.x / splits);
   const int nrows = a.tok.T * a.G;
+  // a tree's keys are shared out by the sequences' lengths, if there are several: the
+  // workgroup's place among its head's and tile's, and its steps of 64 rows
+  int s0 = 0, s1 = 0;
+  const bool shared = TREE && SPLIT && a.table;
+  if (shared) {
+    const int groups = c.B * splits, first = (int)blockIdx.x / groups * (ROWS * PW);
+    tile = blockIdx.x / groups;
+    h = blockIdx.y;
+    split = blockIdx.x % groups;
+    const Shares sh(c, a, lane, [&](int i) {
+      const int there = a.tok.count ? std::min(a.tok.count[i], a.tok.T) : a.tok.T;
+      return first / a.G < there ? (q4_last_row(a.tok, i, there - 1, c.n_max) + PK) / PK : 0;
+    });
+    // (the table that the join goes by, for each 16 rows of the tile)
+    if (h == 0 && split == 0 && wave == 0)
+      for (int x = first / 16; x < (first + ROWS * PW) / 16 && x * 16 < nrows; ++x)
+        sh.write(c, a.table + x * c.B, lane);
+    b = sh.find(c, split, &s0, &s1);
+    if (b < 0) return;
+  }
   const int r0 = tile * (ROWS * PW);  // the workgroup's first query row
   const int cnt = a.tok.count ? std::min(a.tok.count[b], a.tok.T) : a.tok.T;
   // the last cached row that query rows up to r see
@@ -81,7 +102,9 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
 
   // this workgroup's share of the rows: k0 .. k1 - 1, whole tiles of them
   const int share = (last / PK + splits) / splits * PK;
-  const int k0 = split * share, k1 = SPLIT ? std::min(last + 1, k0 + share) : last + 1;
+  const int k0 = shared ? s0 * PK : split * share;
+  const int k1 = shared ? std::min(last + 1, s1 * PK)
+                        : SPLIT ? std::min(last + 1, k0 + share) : last + 1;
 
   // this thread's word of a tile: row and group
   const int srow = threadIdx.x / GR, sgr = threadIdx.x % GR;
@@ -250,8 +273,9 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
     if (r >= nrows) continue;
     if (SPLIT) {  // sums, maximum and sum of weights of the row, for the join
       const int tiles = (nrows + 15) / 16;
-      const int64_t slots = (int64_t)gridDim.y * tiles * splits;
-      const int64_t slot = ((int64_t)slice * tiles + r / 16) * splits + split;
+      const int64_t slots = (int64_t)c.B * c.H * tiles * splits;
+      const int64_t slot = shared ? ((int64_t)h * tiles + r / 16) * c.B * splits + split
+                                  : ((int64_t)slice * tiles + r / 16) * splits + split;
 #pragma unroll
       for (int dt = 0; dt < D / 16; ++dt)
         *reinterpret_cast<floatx4_t*>(a.part + (slot * 16 + m) * D + dt * 16 + 4 * g) = acc[rt][dt];
@@ -284,8 +308,10 @@ hipError_t prompt_d(const Q4View& c, const Q4AttnArgs& a, hipStream_t st) {
   const int64_t tiles = ((int64_t)a.tok.T * a.G + 16 * RT * PW - 1) / (16 * RT * PW);
   const dim3 grid((uint32_t)(tiles * a.shape.splits), (uint32_t)(c.B * c.H));
   if (a.seen) {
+    const dim3 by_length((uint32_t)(tiles * a.shape.splits * c.B), (uint32_t)c.H);
     if (a.shape.splits > 1)
-      q4_prompt_kernel<T, D, RT, true, true><<<grid, 64 * PW, 0, st>>>(c, a);
+      q4_prompt_kernel<T, D, RT, true, true>
+          <<<a.table ? by_length : grid, 64 * PW, 0, st>>>(c, a);
     else
       q4_prompt_kernel<T, D, RT, false, true><<<grid, 64 * PW, 0, st>>>(c, a);
   } else if (a.shape.splits > 1) {

@@ -197,6 +197,8 @@ TREES = [
     (64, 16, 8, 2, 130, 300, list(range(0, 160, 10)), [130] * 15 + [77]),
     (128, 1, 8, 4, 129, 5000, [4870], None),
     (64, 2, 2, 1, 1024, 4500, [3476, 0], [1024, 1000]),
+    (32, 7, 4, 4, 40, 5000, [4960, 0, -50, 700, 5000, 63, 64], [40, 40, 40, 39, 40, 0, 1]),
+    (64, 20, 2, 8, 33, 4500, [4467, *range(0, 1900, 100)], [33] * 18 + [-1, 50]),
 ]
 
 
