@@ -234,13 +234,16 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
   constexpr int SS = NK * Elem<T>::bytes + 16;  // bytes per query of p and ds in LDS
   // dQ: a wave's units are (16 channels, 16 queries), 2 DT of them in all
   constexpr int U = (2 * DT + W - 1) / W, SL = U > 1 ? U / 2 : 1;
-  // Where registers run out, keys are read from LDS for every step: 32 keys of 128 channels per
-  // wave and those of 16 channels of every key would take 64.
-  constexpr bool KL = ONE && (NK * DT > 128 * 8 || W > 8);
+  // Where registers run out, keys are read from LDS in every step: a wave's own and 16 channels
+  // of all of them would take KR.
+  constexpr int KR = 4 * NV * KT + SL * (NK / 32) * (Elem<T>::bytes == 2 ? 4 : 8);
+  constexpr bool KL = ONE && (KR > 48 || W > 8);
   constexpr bool TIGHT = KT * DT >= 16;
   __shared__ __align__(16) unsigned char tile_[2][1 + OP][PLANE];
   __shared__ __align__(16) unsigned char ds_[QT * SS];
   __shared__ float st[ONE ? W : 1][3][QT];
+  __shared__ int rows_[NK];
+  __shared__ float bias_[NK];
   __shared__ __align__(16) unsigned char sk[KL ? NK * R::stride : 16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -297,16 +300,17 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
   };
   load(t0);
 
-  // this wave's keys
+  // the rows of the workgroup's keys, then this wave's
+  for (int j = threadIdx.x; j < NK; j += 64 * W)
+    rows_[j] = coreset_row(a, s, (int64_t)chunk * NK + j, &bias_[j]);
+  __syncthreads();
   uint4 kf[KL ? 1 : KT][NV], vf[KT][NV];
   float bias[KT][4];
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) {
-    const int key = (wave * KT + kt) * 16 + m;
-    float mine;
-    const int r = coreset_row(a, s, (int64_t)chunk * NK + key, &mine);
+    const int key = (wave * KT + kt) * 16 + m, r = rows_[key];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) bias[kt][j] = __shfl(mine, 4 * g + j);
+    for (int j = 0; j < 4; ++j) bias[kt][j] = bias_[(wave * KT + kt) * 16 + 4 * g + j];
     uint4* kw = kf[KL ? 0 : kt];
     load_frag<T, D>(K, r, g, r >= 0, kw);
     load_frag<T, D>(V, r, g, r >= 0, vf[kt]);
@@ -326,12 +330,14 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
       float f[SL][2][4];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        float b;
-        const int r = coreset_row(a, s, 32 * x + i / 4 * 16 + 4 * g + i % 4, &b);
+        const int r = rows_[32 * x + i / 4 * 16 + 4 * g + i % 4];
+        // (loaded in any case: a branch would wait for every load by itself)
+        const T* row = K + (int64_t)std::max(r, 0) * D;
 #pragma unroll
-        for (int y = 0; y < SL; ++y)
-          f[y][i / 4][i % 4] =
-              r >= 0 ? elem<T>(K + (int64_t)r * D, 16 * (unit0 / 2 + y) + m) : 0.0f;
+        for (int y = 0; y < SL; ++y) {
+          const float v = elem<T>(row, 16 * (unit0 / 2 + y) + m);
+          f[y][i / 4][i % 4] = r >= 0 ? v : 0.0f;
+        }
       }
 #pragma unroll
       for (int y = 0; y < SL; ++y) kc[y][x] = Column<T>(f[y]);
@@ -416,27 +422,31 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
     floatx4_t x[KT][2], y[KT][2];
 #pragma unroll
     for (int i = 0; i < 2 * KT; ++i) x[i / 2][i % 2] = y[i / 2][i % 2] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+    // (a word of the keys serves both tiles, or, where registers are short, one after the other)
+    constexpr int QS = TIGHT ? 1 : 2;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      uint4 kw[KT];
+    for (int q0 = 0; q0 < 2; q0 += QS)
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-        kw[kt] = KL ? lds_word<T, D>(sk + (wave * KT + kt) * 16 * R::stride, v, m, g)
-                    : kf[KL ? 0 : kt][v];
+      for (int v = 0; v < NV; ++v) {
+        uint4 kw[KT];
 #pragma unroll
-      for (int tq = 0; tq < 2; ++tq) {
-        const uint4 qw = lds_word<T, D>(tile_[buf][0] + 16 * tq * R::stride, v, m, g);
+        for (int kt = 0; kt < KT; ++kt)
+          kw[kt] = KL ? lds_word<T, D>(sk + (wave * KT + kt) * 16 * R::stride, v, m, g)
+                      : kf[KL ? 0 : kt][v];
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) x[kt][tq] = mma_word<T>(kw[kt], qw, x[kt][tq]);
+        for (int tq = q0; tq < q0 + QS; ++tq) {
+          const uint4 qw = lds_word<T, D>(tile_[buf][0] + 16 * tq * R::stride, v, m, g);
 #pragma unroll
-        for (int o = OP - 1; o >= 0; --o) {
-          const uint4 ow = lds_word<T, D>(tile_[buf][1 + o] + 16 * tq * R::stride, v, m, g);
+          for (int kt = 0; kt < KT; ++kt) x[kt][tq] = mma_word<T>(kw[kt], qw, x[kt][tq]);
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt) y[kt][tq] = mma_word<T>(vf[kt][v], ow, y[kt][tq]);
+          for (int o = OP - 1; o >= 0; --o) {
+            const uint4 ow = lds_word<T, D>(tile_[buf][1 + o] + 16 * tq * R::stride, v, m, g);
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) y[kt][tq] = mma_word<T>(vf[kt][v], ow, y[kt][tq]);
+          }
         }
+        if (TIGHT) __builtin_amdgcn_sched_barrier(0);
       }
-      if (TIGHT) __builtin_amdgcn_sched_barrier(0);
-    }
 #pragma unroll
     for (int i = 0; i < 8 * KT; ++i) {
       const int kt = i / 8, tq = i / 4 % 2, j = i % 4;
