@@ -202,20 +202,22 @@ __global__ __launch_bounds__(THREADS) void q4_load_kernel(Q4View c, const int32_
 // ---------------------------------------------------------------------------
 // Keep: the rows of an accepted path of drafts move to the places behind the rows before
 // them, and the bounds of the blocks that hold these places are formed anew, as a store of
-// these rows forms them.  A workgroup takes a slice.  The rows pass through LDS whole before
-// the first is written, so a path may name rows in any order, and rows that it also writes.
+// these rows forms them.  A workgroup takes the keys or the values of a slice.  The rows pass
+// through LDS whole before the first is written, so a path may name rows in any order, and rows
+// that it also writes.
 // ---------------------------------------------------------------------------
 template <int D, int CAP>
 __global__ __launch_bounds__(THREADS) void q4_keep_kernel(Q4View c, const int32_t* at_,
                                                           const int32_t* path, int P,
                                                           int32_t* end) {
   constexpr int CW = D / 32;  // 16-byte words of a row's codes, and bytes of its scales
-  __shared__ u32x4 codes[2][CAP * CW];
-  __shared__ uint8_t scales[2][CAP * CW];
+  __shared__ u32x4 codes[CAP * CW];
+  __shared__ uint8_t scales[CAP * CW];
   __shared__ int32_t from[CAP];
   __shared__ int first_bad;
   const int64_t s = blockIdx.x;
   const int b = blockIdx.x / c.H;
+  const bool keys = blockIdx.y == 0;
   const int64_t at = at_[b];
   if (threadIdx.x == 0) first_bad = P;
   __syncthreads();
@@ -227,26 +229,25 @@ __global__ __launch_bounds__(THREADS) void q4_keep_kernel(Q4View c, const int32_
   }
   __syncthreads();
   const int n = first_bad;
-  if (blockIdx.x % c.H == 0 && threadIdx.x == 0) end[b] = (int32_t)(at + n);
+  if (keys && blockIdx.x % c.H == 0 && threadIdx.x == 0) end[b] = (int32_t)(at + n);
   const int64_t base = s * c.n_max;
+  uint8_t* cp = keys ? c.k_codes : c.v_codes;
+  uint8_t* sp = keys ? c.k_scales : c.v_scales;
+#pragma unroll 4
   for (int i = threadIdx.x; i < n * CW; i += THREADS) {
     const int64_t row = base + from[i / CW];
-    codes[0][i] = reinterpret_cast<const u32x4*>(c.k_codes + row * (D / 2))[i % CW];
-    codes[1][i] = reinterpret_cast<const u32x4*>(c.v_codes + row * (D / 2))[i % CW];
-    scales[0][i] = c.k_scales[row * CW + i % CW];
-    scales[1][i] = c.v_scales[row * CW + i % CW];
+    codes[i] = reinterpret_cast<const u32x4*>(cp + row * (D / 2))[i % CW];
+    scales[i] = sp[row * CW + i % CW];
   }
   __syncthreads();
   for (int i = threadIdx.x; i < n * CW; i += THREADS) {
     // (n * CW words in a row: the new rows lie behind one another)
-    reinterpret_cast<u32x4*>(c.k_codes + (base + at) * (D / 2))[i] = codes[0][i];
-    reinterpret_cast<u32x4*>(c.v_codes + (base + at) * (D / 2))[i] = codes[1][i];
-    c.k_scales[(base + at) * CW + i] = scales[0][i];
-    c.v_scales[(base + at) * CW + i] = scales[1][i];
+    reinterpret_cast<u32x4*>(cp + (base + at) * (D / 2))[i] = codes[i];
+    sp[(base + at) * CW + i] = scales[i];
   }
   // bounds of the blocks from the last row before the drafts to the last row kept
   const int64_t last = at + n - 1, r0 = (at > 0 ? at - 1 : 0) / kQ4Block;
-  if (last < 0 || last >= c.n_max) return;
+  if (!keys || last < 0 || last >= c.n_max) return;
   constexpr int LR = D / 8, RPP = THREADS / LR;
   const int l = threadIdx.x % LR, rp = threadIdx.x / LR;
   for (int64_t k = r0; k <= last / kQ4Block; ++k) {
@@ -263,8 +264,8 @@ __global__ __launch_bounds__(THREADS) void q4_keep_kernel(Q4View c, const int32_
       uint32_t code, byte;
       if (r >= at) {
         const int i = (int)(r - at);
-        code = reinterpret_cast<const uint32_t*>(codes[0])[i * (D / 8) + l];
-        byte = scales[0][i * CW + l / 4];
+        code = reinterpret_cast<const uint32_t*>(codes)[i * (D / 8) + l];
+        byte = scales[i * CW + l / 4];
       } else {
         code = *reinterpret_cast<const uint32_t*>(c.k_codes + (base + r) * (D / 2) + l * 4);
         byte = c.k_scales[(base + r) * CW + l / 4];
@@ -976,9 +977,11 @@ hipError_t store_d(const Q4View& c, const RowsView& k, const RowsView& v, const 
 template <int D>
 hipError_t keep_d(const Q4View& c, const int32_t* at, const int32_t* path, int64_t P, int32_t* end,
                   hipStream_t st) {
-  const uint32_t grid = (uint32_t)(c.B * c.H);
+  const dim3 grid((uint32_t)(c.B * c.H), 2);
   if (P <= 64)
     q4_keep_kernel<D, 64><<<grid, THREADS, 0, st>>>(c, at, path, (int)P, end);
+  else if (P <= 512)
+    q4_keep_kernel<D, 512><<<grid, THREADS, 0, st>>>(c, at, path, (int)P, end);
   else
     q4_keep_kernel<D, kQ4MaxDrafts><<<grid, THREADS, 0, st>>>(c, at, path, (int)P, end);
   return hipGetLastError();
