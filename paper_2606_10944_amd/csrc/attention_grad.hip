@@ -848,25 +848,43 @@ __global__ __launch_bounds__(256) void grad_join_kernel(GradArgs a) {
   store4<T>(static_cast<T*>(key ? a.dK : a.dV) + (s * a.n + r) * D + lane % (D / 4) * 4, o);
 }
 
-template <typename T, typename TO, int D, int W, int KT>
-hipError_t keys_one(const GradArgs& a, hipStream_t st) {
+template <typename T, typename TO, int D, int W, int KT, bool ONE>
+hipError_t keys_as(const GradArgs& a, hipStream_t st) {
   const uint32_t grid = (uint32_t)(a.S * a.shape.chunks * a.shape.parts);
-  if (a.shape.one)
-    grad_keys_kernel<T, TO, D, W, KT, true><<<grid, 64 * W, 0, st>>>(a);
-  else if constexpr (W == 8)
-    grad_keys_kernel<T, TO, D, W, KT, false><<<grid, 64 * W, 0, st>>>(a);
+  grad_keys_kernel<T, TO, D, W, KT, ONE><<<grid, 64 * W, 0, st>>>(a);
   return hipGetLastError();
 }
 
+// The shapes of grad_shape.
 template <typename T, typename TO, int D>
 hipError_t keys_d(const GradArgs& a, hipStream_t st) {
-  if (a.shape.waves == 2) return keys_one<T, TO, D, 2, 1>(a, st);
-  if (a.shape.waves == 4) return keys_one<T, TO, D, 4, 1>(a, st);
-  if constexpr (Elem<T>::bytes == 2)
-    if (a.shape.tiles == 2) return keys_one<T, TO, D, 8, 2>(a, st);
-  if constexpr (Elem<T>::bytes == 2)
-    if (a.shape.waves == 12) return keys_one<T, TO, D, 12, 1>(a, st);
-  return keys_one<T, TO, D, 8, 1>(a, st);
+  constexpr bool LOW = Elem<T>::bytes == 2;
+  constexpr int CHUNK = LOW && D < 128 ? 2 : 1;
+  if (!a.shape.one) return keys_as<T, TO, D, 8, CHUNK, false>(a, st);
+  const int w = a.shape.waves, t = a.shape.tiles;
+  if (w == 2 && t == 1) return keys_as<T, TO, D, 2, 1, true>(a, st);
+  if constexpr (LOW && D == 32) {
+    if (w == 2 && t == 2) return keys_as<T, TO, D, 2, 2, true>(a, st);
+    if (w == 2 && t == 4) return keys_as<T, TO, D, 2, 4, true>(a, st);
+    if (w == 4 && t == 4) return keys_as<T, TO, D, 4, 4, true>(a, st);
+  } else if constexpr (LOW && D == 64) {
+    if (w == 4 && t == 1) return keys_as<T, TO, D, 4, 1, true>(a, st);
+    if (w == 4 && t == 2) return keys_as<T, TO, D, 4, 2, true>(a, st);
+    if (w == 8 && t == 2) return keys_as<T, TO, D, 8, 2, true>(a, st);
+  } else if constexpr (LOW) {
+    if (w == 4 && t == 1) return keys_as<T, TO, D, 4, 1, true>(a, st);
+    if (w == 8 && t == 1) return keys_as<T, TO, D, 8, 1, true>(a, st);
+    if (w == 12 && t == 1) return keys_as<T, TO, D, 12, 1, true>(a, st);
+    if (w == 8 && t == 2) return keys_as<T, TO, D, 8, 2, true>(a, st);
+  } else {
+    if (w == 4 && t == 1) return keys_as<T, TO, D, 4, 1, true>(a, st);
+    if constexpr (D == 32) {
+      if (w == 4 && t == 2) return keys_as<T, TO, D, 4, 2, true>(a, st);
+    } else {
+      if (w == 8 && t == 1) return keys_as<T, TO, D, 8, 1, true>(a, st);
+    }
+  }
+  return hipErrorInvalidValue;
 }
 
 template <typename T, typename TO, int D>

@@ -19,22 +19,41 @@ struct GradShape {
   constexpr int64_t keys() const { return 16 * (int64_t)waves * tiles; }
 };
 
-// Keys that one workgroup holds at most: 32 per wave of eight (bf16), whose sums of dK and dV
-// take half of its registers, or 16 (float32).
+// Keys that one workgroup holds at most.  (Their sums of dK and dV are float32, 2 d of them per
+// key: 256 of 128 channels take half of a compute unit's registers, and float32 rows' operands
+// take twice those of bf16.)
 constexpr int64_t grad_most_keys(bool bf16) { return bf16 ? 256 : 128; }
 
+// A wave of more tiles reads a step's rows from LDS for more keys, one of fewer leaves registers
+// for a second wave beside it.  Sums of 64 registers per lane (tiles * d = 128) are best where
+// there are keys for at least two waves; us for waves x tiles, 64 slices of 8192 queries, bf16:
+//   d = 32, 64 keys 4x1 57.8, 2x2 45.7; 128 keys 8x1 107, 4x2 80.3, 2x4 70.4; 256 8x2 148, 4x4 129
+//   d = 64, 64 keys 4x1 86.0, 2x2 89.9; 128 keys 8x1 141, 4x2 116, 2x4 318; 256 8x2 191, 4x4 330
+// d = 128, 64 slices of 16384 queries: 128 keys 8x1 354, 4x2 500; 192 keys 12x1 495, 8x2 548, 4x3
+// 504; 256 keys 8x2 548, 16x1 910, 4x4 855.  float32 rows, 64 slices of 4096 queries over 128
+// keys: d = 32 8x1 135, 4x2 118; d = 64 8x1 215, 4x2 232.
 inline GradShape grad_shape(int64_t S, int64_t n_q, int64_t n_out, int64_t d, bool bf16) {
   GradShape s{};
   s.one = n_out <= grad_most_keys(bf16);
-  s.waves = n_out <= 32 ? 2 : n_out <= 64 ? 4 : 8;
-  s.tiles = bf16 && n_out > 128 && (s.one || d < 128) ? 2 : 1;
-  if (bf16 && n_out > 128 && n_out <= 192 && d == 128) {
-    s.waves = 12;
-    s.tiles = 1;
-  }
+  auto is = [&](int waves, int tiles) {
+    s.waves = waves;
+    s.tiles = tiles;
+  };
+  if (n_out <= 32)
+    is(2, 1);
+  else if (n_out <= 64)
+    d == 32 && bf16 ? is(2, 2) : is(4, 1);
+  else if (n_out <= 128)
+    d == 32 ? (bf16 ? is(2, 4) : is(4, 2)) : d == 64 && bf16 ? is(4, 2) : is(8, 1);
+  else if (s.one && d == 128 && n_out <= 192)
+    is(12, 1);
+  else if (s.one)
+    d == 32 ? is(4, 4) : is(8, 2);
+  else  // chunks
+    bf16 && d < 128 ? is(8, 2) : is(8, 1);
   s.chunks = (int32_t)((n_out + s.keys() - 1) / s.keys());
   const int64_t steps = (n_q + kGradTile - 1) / kGradTile;
-  const int64_t slots = 256 * (s.waves > 8 ? 1 : 8 / s.waves);
+  const int64_t slots = s.waves > 8 ? 256 : 256 * (8 / s.waves);
   const StepSplit p = split_steps(S * s.chunks, steps, slots, 2.0, 1.0);
   s.parts = (int32_t)p.parts;
   s.run = (int32_t)p.run;

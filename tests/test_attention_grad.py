@@ -66,7 +66,7 @@ int main() {
     if ((int64_t)s.parts * s.run < steps || (int64_t)(s.parts - 1) * s.run >= steps) return 2;
     if (s.one != (k <= grad_most_keys(b)) || (s.one && s.chunks != 1)) return 3;
     if (!s.one && s.waves != 8) return 4;
-    if (!b && s.tiles != 1) return 5;
+    if (!b && d > 32 && s.tiles != 1) return 5;
     // threads of a launch fit 32 bits where rows and keys are within the entry point's limits
     if (S * k <= (1 << 25) && S * q <= (1 << 29) &&
         S * s.chunks * s.parts * 64 * s.waves >= ((int64_t)1 << 32)) return 6;

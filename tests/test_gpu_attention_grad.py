@@ -66,7 +66,7 @@ SHAPES = [
     (1, 1, 97, 200, 192, 32), (2, 1, 160, 300, 256, 128), (1, 2, 50, 257, 257, 64),
     (1, 1, 300, 700, 333, 128), (2, 1, 64, 600, 600, 32), (1, 1, 1, 300, 300, 128),
     (1, 2, 1, 90, 40, 64), (40, 9, 40, 20, 9, 32), (1, 1, 5000, 64, 48, 64),
-    (1, 2, 2500, 400, 150, 128),
+    (1, 2, 2500, 400, 150, 128), (2, 2, 75, 300, 250, 32), (1, 2, 40, 90, 50, 32),
 ]
 TYPES = [("bf16", "bf16"), ("bf16", "fp32"), ("fp32", "fp32"), ("fp32", "bf16")]
 
