@@ -38,8 +38,13 @@ int thin_attention_backward_plan(int32_t dtype, int64_t B, int64_t H, int64_t n_
   if (!workspace_bytes) return THIN_EINVAL;
   if (!known_dtype(dtype)) return THIN_EDTYPE;
   if (!valid_sizes(B, H, n_q, n, d, n_out)) return THIN_EINVAL;
-  const thin::GradShape s = thin::grad_shape(B * H, n_q, n_out, d, dtype == THIN_BF16);
-  *workspace_bytes = thin::grad_bytes(s, B * H, n_q, d, true).all();
+  *workspace_bytes = 0;
+  for (const bool exact : {false, true}) {  // the larger of what either type of dO takes
+    const thin::GradShape s = thin::grad_shape(B * H, n_q, n_out, d, dtype == THIN_BF16,
+                                               exact && dtype == THIN_BF16);
+    const size_t n = thin::grad_bytes(s, B * H, n_q, d, true).all();
+    if (n > *workspace_bytes) *workspace_bytes = n;
+  }
   return THIN_OK;
 }
 
@@ -53,8 +58,17 @@ int thin_attention_backward(const void* Q, const void* K, const void* V, int32_t
   if (!rows(Q) || !rows(K) || !rows(V) || !rows(dO) || !rows(dQ) || !rows(dK) || !rows(dV) ||
       !idx || !aligned(idx, 4) || !aligned(logw, 4) || !aligned(dlogw, 4))
     return THIN_EINVAL;
+  const void* outs[] = {dQ, dK, dV, dlogw};
+  const void* ins[] = {Q, K, V, dO, idx, logw};
+  for (int i = 0; i < 4; ++i) {
+    for (const void* in : ins)
+      if (outs[i] && outs[i] == in) return THIN_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (outs[i] && outs[i] == outs[j]) return THIN_EINVAL;
+  }
   thin::GradArgs a{};
-  a.shape = thin::grad_shape(B * H, n_q, n_out, d, dtype == THIN_BF16);
+  a.shape = thin::grad_shape(B * H, n_q, n_out, d, dtype == THIN_BF16,
+                             dtype == THIN_BF16 && out_dtype == THIN_FP32 && dlogw);
   const thin::GradBytes bytes = thin::grad_bytes(a.shape, B * H, n_q, d, true);
   if (!workspace || workspace_bytes < bytes.all() || !aligned(workspace, 256))
     return THIN_EWORKSPACE;

@@ -13,11 +13,12 @@
 //
 // Types.  bf16 rows: bf16 products summed in float32; p and ds round to bf16 (half a step, as
 // the gradients' own rounding) for the products over queries and over keys; a float32 dO is
-// two bf16 parts (17 bits), so that dlw, a float32 sum of differences, keeps them.  float32
-// rows: float32 products throughout.
+// two bf16 parts (17 bits), or in g all three where dlw, a float32 sum of differences, is asked
+// for.  float32 rows: float32 products throughout.
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "grad.hpp"
@@ -25,9 +26,22 @@
 
 namespace thin {
 
+// float32 rows of dO of which bf16 products take all three bf16 parts.
+struct exact_t {
+  float f;
+};
+template <>
+struct Elem<exact_t> {
+  static constexpr int bytes = 4;
+};
+
 namespace {
 
-constexpr int QT = (int)kGradTile;
+// Rows of a product over rows: the bf16 instruction takes 32, of the float32 one, which takes
+// four, 16 are counted as one.
+template <typename T>
+constexpr int kUnit = Elem<T>::bytes == 2 ? 32 : 16;
+
 constexpr float kLeast = -3.0e38f;
 constexpr double kLog2e = 1.44269504088896340736;
 
@@ -66,8 +80,8 @@ __device__ __forceinline__ bf16x8_t pack8(const float* a, const float* b) {
                                               cvt_pk_bf16(b[0], b[1]), cvt_pk_bf16(b[2], b[3])});
 }
 
-// Operands of a product over 32 rows: lane (m, g) holds rows 4 g .. 4 g + 3 and 16 + 4 g .. of
-// its column: of rows in LDS (column 16 dt + m), or of values it has.
+// Operands of a product over a unit of rows: lane (m, g) holds rows 4 g .. 4 g + 3 (and of bf16
+// 16 + 4 g ..) of its column: of rows in LDS (column 16 dt + m), or of values it has.
 template <typename T>
 struct Column;
 template <>
@@ -91,26 +105,25 @@ struct Column<bf16_t> {
 };
 template <>
 struct Column<float> {
-  float x[8];
+  float x[4];
   __device__ __forceinline__ Column() {}
   __device__ __forceinline__ Column(const unsigned char* rows, int stride, int dt, int m, int g) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = *reinterpret_cast<const float*>(rows + (i / 4 * 16 + 4 * g + i % 4) * stride +
-                                             (16 * dt + m) * 4);
+    for (int i = 0; i < 4; ++i)
+      x[i] = *reinterpret_cast<const float*>(rows + (4 * g + i) * stride + (16 * dt + m) * 4);
   }
   __device__ __forceinline__ Column(const float (*w)[4]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = w[i / 4][i % 4];
+    for (int i = 0; i < 4; ++i) x[i] = w[0][i];
   }
   __device__ __forceinline__ Column(const unsigned char* row, int g) {
+    const floatx4_t a = *reinterpret_cast<const floatx4_t*>(row + 16 * g);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = *reinterpret_cast<const float*>(row + (i / 4 * 16 + 4 * g + i % 4) * 4);
+    for (int i = 0; i < 4; ++i) x[i] = a[i];
   }
   __device__ __forceinline__ floatx4_t times(const Column& b, floatx4_t acc) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 4; ++i)
       acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], b.x[i], acc, 0, 0, 0);
     return acc;
   }
@@ -139,11 +152,12 @@ struct Span {
   }
 };
 
-// A 16-byte word of T from a row of TO (elements e .. of it), and what bf16 leaves of float32
-// (OP = 2 parts).
+// A 16-byte word of T from a row of TO: one part, or the bf16 parts of float32, each the rounding
+// of what those before it leave.
 template <typename T, typename TO>
 struct Parts {
-  static constexpr int n = Elem<T>::bytes == 2 && Elem<TO>::bytes == 4 ? 2 : 1;
+  static constexpr bool mixed = Elem<T>::bytes == 2 && Elem<TO>::bytes == 4;
+  static constexpr int n = mixed ? (std::is_same<TO, exact_t>::value ? 3 : 2) : 1;
 };
 template <typename T, typename TO>
 struct RawWord;  // as it is in memory; word `item` of a span
@@ -161,8 +175,8 @@ struct RawWord<float, bf16_t> {
     o[0] = (u32x4){w[0] << 16, w[0] & 0xffff0000u, w[1] << 16, w[1] & 0xffff0000u};
   }
 };
-template <>
-struct RawWord<bf16_t, float> {
+template <int N>
+struct SplitWord {
   u32x4 w[2];
   __device__ __forceinline__ void load(const Span& p, uint32_t item) {
     w[0] = p.load16(item * 32);
@@ -171,14 +185,20 @@ struct RawWord<bf16_t, float> {
   __device__ __forceinline__ void parts(u32x4* o) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float a = __uint_as_float(w[i / 2][i % 2 * 2]);
-      const float b = __uint_as_float(w[i / 2][i % 2 * 2 + 1]);
-      o[0][i] = cvt_pk_bf16(a, b);
-      o[1][i] = cvt_pk_bf16(a - __uint_as_float(o[0][i] << 16),
-                            b - __uint_as_float(o[0][i] & 0xffff0000u));
+      float a = __uint_as_float(w[i / 2][i % 2 * 2]), b = __uint_as_float(w[i / 2][i % 2 * 2 + 1]);
+#pragma unroll
+      for (int p = 0; p < N; ++p) {
+        o[p][i] = cvt_pk_bf16(a, b);
+        a -= __uint_as_float(o[p][i] << 16);
+        b -= __uint_as_float(o[p][i] & 0xffff0000u);
+      }
     }
   }
 };
+template <>
+struct RawWord<bf16_t, float> : SplitWord<2> {};
+template <>
+struct RawWord<bf16_t, exact_t> : SplitWord<3> {};
 
 // Four consecutive channels of a gradient.
 template <typename T>
@@ -229,16 +249,22 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
   using R = LdsRows<T, D>;
   constexpr int NV = Frag<T, D>::NV, DT = D / 16, NK = 16 * W * KT;
   constexpr int OP = Parts<T, TO>::n, E = 16 / Elem<T>::bytes;
+  // queries of a step, tiles of 16 of them, and units
+  constexpr int QT = (int)grad_tile(Elem<T>::bytes == 2, W), TQ = QT / 16, UR = kUnit<T>;
+  constexpr int QU = QT / UR;
   constexpr int PLANE = QT * R::stride;
   constexpr int IT = (QT * R::CW + 64 * W - 1) / (64 * W);  // words of a tile per thread
   constexpr int SS = NK * Elem<T>::bytes + 16;  // bytes per query of p and ds in LDS
-  // dQ: a wave's units are (16 channels, 16 queries), 2 DT of them in all
-  constexpr int U = (2 * DT + W - 1) / W, SL = U > 1 ? U / 2 : 1;
+  // dQ: a wave's units are (16 channels, 16 queries), UN of them in all; of two tiles it takes
+  // both, where it has several
+  constexpr int UN = TQ * DT, U = (UN + W - 1) / W;
+  constexpr int UQ = TQ == 2 && U > 1 ? 2 : 1, SL = U / UQ;
   // Where registers run out, keys are read from LDS in every step: a wave's own and 16 channels
   // of all of them would take KR.
-  constexpr int KR = 4 * NV * KT + SL * (NK / 32) * (Elem<T>::bytes == 2 ? 4 : 8);
+  constexpr int KR = 4 * NV * KT + SL * (NK / UR) * 4;
   constexpr bool KL = ONE && (KR > 48 || W > 8);
   constexpr bool TIGHT = KT * DT >= 16;
+  static_assert(NK % UR == 0 && QT % UR == 0, "whole units of keys");
   __shared__ __align__(16) unsigned char tile_[2][1 + OP][PLANE];
   __shared__ __align__(16) unsigned char ds_[QT * SS];
   __shared__ float st[ONE ? W : 1][3][QT];
@@ -273,7 +299,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
   };
   // without ONE, the next step's statistics.  (Rows past the last have a dO of 0, and so a g, a
   // sum p g and a ds of 0 whatever their maximum.)
-  uint32_t next[2][2];
+  uint32_t next[2][TQ];
   auto statistics = [&](int64_t t) __attribute__((always_inline)) {
     const int rows = t < t1 ? (int)std::min<int64_t>(QT, a.n_q - t * QT) : 0;
     const int64_t at = s * a.n_q + (rows > 0 ? t * QT : 0);
@@ -281,7 +307,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
     for (int k = 0; k < 2; ++k) {
       const Span x(a.stats + k * a.S * a.n_q + at, rows * 4);
 #pragma unroll
-      for (int tq = 0; tq < 2; ++tq) next[k][tq] = x.load4((16 * tq + m) * 4);
+      for (int tq = 0; tq < TQ; ++tq) next[k][tq] = x.load4((16 * tq + m) * 4);
     }
   };
   auto put = [&](int buf) __attribute__((always_inline)) {
@@ -290,7 +316,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
       const int item = i * 64 * W + (int)threadIdx.x;
       if (!EVEN && item >= QT * R::CW) continue;
       const int to = item / R::CW * R::stride + item % R::CW * 16;
-      u32x4 w[2];
+      u32x4 w[3];
       rq[i].parts(w);
       *reinterpret_cast<u32x4*>(tile_[buf][0] + to) = w[0];
       ro[i].parts(w);
@@ -320,22 +346,23 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
         *reinterpret_cast<uint4*>(sk + key * R::stride + (4 * v + g) * 16) = kw[v];
     }
   }
-  // columns of every key for dQ: channel 16 dt + m of keys 32 x + 4 g .. and 32 x + 16 + 4 g ..
-  Column<T> kc[KL ? 1 : SL][NK / 32];
+  // columns of every key for dQ
+  Column<T> kc[KL ? 1 : SL][NK / UR];
   const int unit0 = wave * U;
-  const bool has_unit = U * W == 2 * DT || unit0 < 2 * DT;
+  const bool has_unit = U * W == UN || unit0 < UN;
+  const int dt0 = TQ == 2 ? unit0 / 2 : unit0;
   if (ONE && !KL && has_unit) {
 #pragma unroll
-    for (int x = 0; x < NK / 32; ++x) {
-      float f[SL][2][4];
+    for (int x = 0; x < NK / UR; ++x) {
+      float f[SL][UR / 16][4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = rows_[32 * x + i / 4 * 16 + 4 * g + i % 4];
+      for (int i = 0; i < UR / 4; ++i) {
+        const int r = rows_[UR * x + i / 4 * 16 + 4 * g + i % 4];
         // (loaded in any case: a branch would wait for every load by itself)
         const T* row = K + (int64_t)std::max(r, 0) * D;
 #pragma unroll
         for (int y = 0; y < SL; ++y) {
-          const float v = elem<T>(row, 16 * (unit0 / 2 + y) + m);
+          const float v = elem<T>(row, 16 * (dt0 + y) + m);
           f[y][i / 4][i % 4] = r >= 0 ? v : 0.0f;
         }
       }
@@ -343,6 +370,13 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
       for (int y = 0; y < SL; ++y) kc[y][x] = Column<T>(f[y]);
     }
   }
+  // whether this wave has keys at all, and the units of keys that some wave has
+  const int64_t have = a.n_out - (int64_t)chunk * NK;
+  // (not in waves of several tiles, where the branches cost registers, 69 -> 82 us for 128 keys of
+  // 32 channels, nor among twelve, most of which have keys, 488 -> 511 us for 192)
+  constexpr bool SKIP = KT == 1 && W < 12;
+  const bool active = !SKIP || wave * 16 < have;
+  const int units = !SKIP ? NK / UR : (int)std::min<int64_t>(NK / UR, (have + UR - 1) / UR);
   put(0);
   load(t0 + 1);
   if (!ONE) statistics(t0);
@@ -377,25 +411,23 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
   };
 
   // dQ of the step before from its ds, and its stores
-  constexpr int UQ = U > 1 ? 2 : 1;  // 16-query tiles of a unit's channels
   Four<T> dq[SL][UQ];
+  auto tile_of = [&](int u) { return UQ == 2 ? u : TQ == 2 ? unit0 % 2 : 0; };
   auto queries = [&]() __attribute__((always_inline)) {
     if (!has_unit) return;
 #pragma unroll
     for (int y = 0; y < SL; ++y) {
-      const int dt = unit0 / 2 + y;
       floatx4_t o[UQ];
 #pragma unroll
       for (int u = 0; u < UQ; ++u) o[u] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int x = 0; x < NK / 32; ++x) {
-        const Column<T> k =
-            KL ? Column<T>(sk + 32 * x * R::stride, R::stride, dt, m, g) : kc[KL ? 0 : y][x];
+      for (int x = 0; x < NK / UR; ++x) {
+        if (SKIP && x > 0 && x >= units) break;
+        const Column<T> k = KL ? Column<T>(sk + UR * x * R::stride, R::stride, dt0 + y, m, g)
+                               : kc[KL ? 0 : y][x];
 #pragma unroll
         for (int u = 0; u < UQ; ++u)
-          o[u] = k.times(Column<T>(ds_ + (16 * (UQ == 2 ? u : unit0 % 2) + m) * SS +
-                                       32 * x * Elem<T>::bytes,
-                                   g),
+          o[u] = k.times(Column<T>(ds_ + (16 * tile_of(u) + m) * SS + UR * x * Elem<T>::bytes, g),
                          o[u]);
         if (TIGHT) __builtin_amdgcn_sched_barrier(0);
       }
@@ -411,21 +443,21 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
     for (int y = 0; y < SL; ++y)
 #pragma unroll
       for (int u = 0; u < UQ; ++u)
-        o.store(dq[y][u].w, (uint32_t)((16 * (UQ == 2 ? u : unit0 % 2) + m) * D +
-                                       16 * (unit0 / 2 + y) + 4 * g) *
-                                Elem<T>::bytes);
+        o.store(dq[y][u].w,
+                (uint32_t)((16 * tile_of(u) + m) * D + 16 * (dt0 + y) + 4 * g) * Elem<T>::bytes);
   };
 
   // scores to base 2 and g of keys 4 g + j, query 16 tq + m
-  auto scores = [&](int buf, float (&p)[KT][2][4], float (&gd)[KT][2][4])
+  auto scores = [&](int buf, float (&p)[KT][TQ][4], float (&gd)[KT][TQ][4])
                     __attribute__((always_inline)) {
-    floatx4_t x[KT][2], y[KT][2];
+    floatx4_t x[KT][TQ], y[KT][TQ];
 #pragma unroll
-    for (int i = 0; i < 2 * KT; ++i) x[i / 2][i % 2] = y[i / 2][i % 2] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < TQ * KT; ++i)
+      x[i / TQ][i % TQ] = y[i / TQ][i % TQ] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
     // (a word of the keys serves both tiles, or, where registers are short, one after the other)
-    constexpr int QS = TIGHT ? 1 : 2;
+    constexpr int QS = TIGHT ? 1 : TQ;
 #pragma unroll
-    for (int q0 = 0; q0 < 2; q0 += QS)
+    for (int q0 = 0; q0 < TQ; q0 += QS)
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         uint4 kw[KT];
@@ -448,8 +480,8 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
         if (TIGHT) __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-    for (int i = 0; i < 8 * KT; ++i) {
-      const int kt = i / 8, tq = i / 4 % 2, j = i % 4;
+    for (int i = 0; i < 4 * TQ * KT; ++i) {
+      const int kt = i / (4 * TQ), tq = i / 4 % TQ, j = i % 4;
       p[kt][tq][j] = fmaf(x[kt][tq][j], c2, bias[kt][j]);
       gd[kt][tq][j] = y[kt][tq][j];
     }
@@ -457,10 +489,10 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
   auto add = [](float x, float y) { return x + y; };
   auto larger = [](float x, float y) { return fmaxf(x, y); };
   // weights under the wave's own maxima (top), and the wave's statistics
-  auto local = [&](float (&p)[KT][2][4], const float (&gd)[KT][2][4], float (&top)[2])
+  auto local = [&](float (&p)[KT][TQ][4], const float (&gd)[KT][TQ][4], float (&top)[TQ])
                    __attribute__((always_inline)) {
 #pragma unroll
-    for (int tq = 0; tq < 2; ++tq) {
+    for (int tq = 0; tq < TQ; ++tq) {
       float x = kLeast, l = 0.0f, e = 0.0f;
 #pragma unroll
       for (int i = 0; i < 4 * KT; ++i) x = fmaxf(x, p[i / 4][tq][i % 4]);
@@ -484,79 +516,99 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
   };
   // The waves' statistics under one maximum: lane l takes row l % 32 of half of the waves, then
   // the halves meet, and rows of 16 lanes trade the two tiles' queries.
-  auto joined = [&](const float (&top)[2], float (&f)[2], float (&dm)[2])
+  auto joined = [&](const float (&top)[TQ], float (&f)[TQ], float (&dm)[TQ])
                     __attribute__((always_inline)) {
-    const int r = lane & 31, h = lane / 32;
-    float x[W / 2], mx = kLeast, l = 0.0f, e = 0.0f;
+    if constexpr (TQ == 1) {  // (float32: every lane its own row)
+      float mx = kLeast, l = 0.0f, e = 0.0f;
 #pragma unroll
-    for (int w = 0; w < W / 2; ++w) {
-      x[w] = st[2 * w + h][0][r];
-      mx = fmaxf(mx, x[w]);
-    }
-    auto halves = [](float v, auto op) {
-      float u = v;
-      trade(true, v, u);
-      return op(v, u);
-    };
-    mx = halves(mx, larger);
+      for (int w = 0; w < W; ++w) mx = fmaxf(mx, st[w][0][m]);
 #pragma unroll
-    for (int w = 0; w < W / 2; ++w) {
-      const float k = __builtin_amdgcn_exp2f(x[w] - mx);
-      l = fmaf(st[2 * w + h][1][r], k, l);
-      e = fmaf(st[2 * w + h][2][r], k, e);
+      for (int w = 0; w < W; ++w) {
+        const float k = __builtin_amdgcn_exp2f(st[w][0][m] - mx);
+        l = fmaf(st[w][1][m], k, l);
+        e = fmaf(st[w][2][m], k, e);
+      }
+      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      dm[0] = e * inv;
+      f[0] = __builtin_amdgcn_exp2f(top[0] - mx) * inv;
+    } else {
+      const int r = lane & 31, h = lane / 32;
+      float x[W / 2], mx = kLeast, l = 0.0f, e = 0.0f;
+  #pragma unroll
+      for (int w = 0; w < W / 2; ++w) {
+        x[w] = st[2 * w + h][0][r];
+        mx = fmaxf(mx, x[w]);
+      }
+      auto halves = [](float v, auto op) {
+        float u = v;
+        trade(true, v, u);
+        return op(v, u);
+      };
+      mx = halves(mx, larger);
+  #pragma unroll
+      for (int w = 0; w < W / 2; ++w) {
+        const float k = __builtin_amdgcn_exp2f(x[w] - mx);
+        l = fmaf(st[2 * w + h][1][r], k, l);
+        e = fmaf(st[2 * w + h][2][r], k, e);
+      }
+      l = halves(l, add);
+      e = halves(e, add);
+      float inv = l > 0.0f ? 1.0f / l : 0.0f, i1 = inv, m1 = mx;
+      dm[0] = dm[1] = e * inv;
+      trade(false, dm[0], dm[1]);
+      trade(false, inv, i1);
+      trade(false, mx, m1);
+      f[0] = __builtin_amdgcn_exp2f(top[0] - mx) * inv;
+      f[1] = __builtin_amdgcn_exp2f(top[1] - m1) * i1;
     }
-    l = halves(l, add);
-    e = halves(e, add);
-    float inv = l > 0.0f ? 1.0f / l : 0.0f, i1 = inv, m1 = mx;
-    dm[0] = dm[1] = e * inv;
-    trade(false, dm[0], dm[1]);
-    trade(false, inv, i1);
-    trade(false, mx, m1);
-    f[0] = __builtin_amdgcn_exp2f(top[0] - mx) * inv;
-    f[1] = __builtin_amdgcn_exp2f(top[1] - m1) * i1;
   };
   // dK and dV of a step: p times f, ds in place of g, both through LDS by columns, in one place
-  auto keys = [&](int buf, float (&p)[KT][2][4], float (&gd)[KT][2][4], const float (&f)[2],
-                  const float (&dm)[2]) __attribute__((always_inline)) {
-    Column<T> wp[KT], ws[KT];
+  auto keys = [&](int buf, float (&p)[KT][TQ][4], float (&gd)[KT][TQ][4], const float (&f)[TQ],
+                  const float (&dm)[TQ]) __attribute__((always_inline)) {
+    Column<T> wp[KT][QU], ws[KT][QU];
     unsigned char* mine = ds_ + (wave * KT * 16 + 4 * g) * Elem<T>::bytes + m * SS;
+    auto put4 = [&](const float* v, int i) {
+      store4<T>(reinterpret_cast<T*>(mine + i / TQ * 16 * Elem<T>::bytes + i % TQ * 16 * SS),
+                (floatx4_t){v[0], v[1], v[2], v[3]});
+    };
 #pragma unroll
-    for (int i = 0; i < 8 * KT; ++i) {
-      const int kt = i / 8, tq = i / 4 % 2, j = i % 4;
+    for (int i = 0; i < 4 * TQ * KT; ++i) {
+      const int kt = i / (4 * TQ), tq = i / 4 % TQ, j = i % 4;
       if (ONE) p[kt][tq][j] *= f[tq];
       gd[kt][tq][j] = p[kt][tq][j] * (gd[kt][tq][j] - dm[tq]);
     }
     if (a.part_w) {
 #pragma unroll
-      for (int i = 0; i < 8 * KT; ++i) aw[i / 8][i % 4] += gd[i / 8][i / 4 % 2][i % 4];
+      for (int i = 0; i < 4 * TQ * KT; ++i)
+        aw[i / (4 * TQ)][i % 4] += gd[i / (4 * TQ)][i / 4 % TQ][i % 4];
     }
 #pragma unroll
-    for (int i = 0; i < 2 * KT; ++i)
-      store4<T>(reinterpret_cast<T*>(mine + i / 2 * 16 * Elem<T>::bytes + i % 2 * 16 * SS),
-                (floatx4_t){p[i / 2][i % 2][0], p[i / 2][i % 2][1], p[i / 2][i % 2][2],
-                            p[i / 2][i % 2][3]});
+    for (int i = 0; i < TQ * KT; ++i) put4(p[i / TQ][i % TQ], i);
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) wp[kt] = Column<T>(ds_, SS, wave * KT + kt, m, g);
+    for (int i = 0; i < KT * QU; ++i)
+      wp[i / QU][i % QU] = Column<T>(ds_ + i % QU * UR * SS, SS, wave * KT + i / QU, m, g);
 #pragma unroll
-    for (int i = 0; i < 2 * KT; ++i)
-      store4<T>(reinterpret_cast<T*>(mine + i / 2 * 16 * Elem<T>::bytes + i % 2 * 16 * SS),
-                (floatx4_t){gd[i / 2][i % 2][0], gd[i / 2][i % 2][1], gd[i / 2][i % 2][2],
-                            gd[i / 2][i % 2][3]});
+    for (int i = 0; i < TQ * KT; ++i) put4(gd[i / TQ][i % TQ], i);
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) ws[kt] = Column<T>(ds_, SS, wave * KT + kt, m, g);
+    for (int i = 0; i < KT * QU; ++i)
+      ws[i / QU][i % QU] = Column<T>(ds_ + i % QU * UR * SS, SS, wave * KT + i / QU, m, g);
     // (of wide waves one pair of columns at a time: more of them on their way cost registers
     // that are not there)
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
-      for (int o = OP - 1; o >= 0; --o) {
-        const Column<T> x(tile_[buf][1 + o], R::stride, dt, m, g);
+      for (int h = 0; h < QU; ++h) {
+        const int at = h * UR * R::stride;
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) av[kt][dt] = x.times(wp[kt], av[kt][dt]);
+        for (int o = std::min(OP, 2) - 1; o >= 0; --o) {  // (dV rounds to bf16: 17 bits do)
+          const Column<T> x(tile_[buf][1 + o] + at, R::stride, dt, m, g);
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt) av[kt][dt] = x.times(wp[kt][h], av[kt][dt]);
+        }
+        const Column<T> x(tile_[buf][0] + at, R::stride, dt, m, g);
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) ak[kt][dt] = x.times(ws[kt][h], ak[kt][dt]);
       }
-      const Column<T> x(tile_[buf][0], R::stride, dt, m, g);
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) ak[kt][dt] = x.times(ws[kt], ak[kt][dt]);
       if (TIGHT) __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -564,20 +616,35 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
   // (Memory operations end in order, stores too: a step makes a number of them that the compiler
   // knows, so that its wait for the next tile's words is none for the stores made since.)
   __syncthreads();
-  float p[KT][2][4], gd[KT][2][4], f[2] = {1.0f, 1.0f}, dm[2];
+  float p[KT][TQ][4], gd[KT][TQ][4], f[TQ], dm[TQ], top[TQ];
+  if (ONE && !active) {  // (a wave without keys: nothing to add, in any step)
+    for (int i = lane; i < QT; i += 64) {
+      st[wave][0][i] = kLeast;
+      st[wave][1][i] = st[wave][2][i] = 0.0f;
+    }
+    // (the ds that dQ's last unit of keys reads)
+#pragma unroll
+    for (int i = 0; i < TQ * KT; ++i)
+      store4<T>(reinterpret_cast<T*>(ds_ + (i % TQ * 16 + m) * SS +
+                                     ((wave * KT + i / TQ) * 16 + 4 * g) * Elem<T>::bytes),
+                (floatx4_t){0.f, 0.f, 0.f, 0.f});
+  }
   for (int64_t t = t0; t < t1; ++t) {
     const int buf = (int)(t - t0) & 1;
-    scores(buf, p, gd);
+    if (active) {
+      scores(buf, p, gd);
+      if (ONE) local(p, gd, top);
+    }
     if (ONE) {
-      float top[2];
-      local(p, gd, top);
       if (t > t0) queries();
       __syncthreads();
-      joined(top, f, dm);
+      if (active) joined(top, f, dm);
+      put_queries(t - 1);
     } else {
 #pragma unroll
-      for (int tq = 0; tq < 2; ++tq) {
+      for (int tq = 0; tq < TQ; ++tq) {
         const float lse = __uint_as_float(next[0][tq]);
+        f[tq] = 1.0f;
         dm[tq] = __uint_as_float(next[1][tq]);
 #pragma unroll
         for (int i = 0; i < 4 * KT; ++i)
@@ -585,9 +652,8 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
       }
       statistics(t + 1);
     }
-    if (ONE) put_queries(t - 1);
     zeros();
-    keys(buf, p, gd, f, dm);
+    if (active) keys(buf, p, gd, f, dm);
     put(buf ^ 1);
     load(t + 2);
     __syncthreads();
@@ -698,7 +764,7 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   for (int v = 0; v < NV; ++v) {
     RawWord<T, TO> w;
     w.load(dO, m * R::CW + 4 * v + g);
-    u32x4 x[2];
+    u32x4 x[3];
     w.parts(x);
 #pragma unroll
     for (int p = 0; p < OP; ++p) of[p][v] = __builtin_bit_cast(uint4, x[p]);
@@ -777,11 +843,12 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
       p[j / 4][j % 4] =
           __builtin_amdgcn_exp2f(p[j / 4][j % 4] - lse) * (gd[j / 4][j % 4] - dm);
 #pragma unroll
-    for (int h = 0; h < KT / 2; ++h) {
-      const Column<T> w(p + 2 * h);
+    for (int h = 0; h < CK / kUnit<T>; ++h) {
+      const Column<T> w(p + h * (kUnit<T> / 16));
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
-        acc[dt] = Column<T>(sk[buf] + 32 * h * R::stride, R::stride, dt, m, g).times(w, acc[dt]);
+        acc[dt] = Column<T>(sk[buf] + kUnit<T> * h * R::stride, R::stride, dt, m, g)
+                      .times(w, acc[dt]);
     }
     turn();
   }
@@ -875,7 +942,8 @@ hipError_t keys_d(const GradArgs& a, hipStream_t st) {
     if (w == 4 && t == 1) return keys_as<T, TO, D, 4, 1, true>(a, st);
     if (w == 8 && t == 1) return keys_as<T, TO, D, 8, 1, true>(a, st);
     if (w == 12 && t == 1) return keys_as<T, TO, D, 12, 1, true>(a, st);
-    if (w == 8 && t == 2) return keys_as<T, TO, D, 8, 2, true>(a, st);
+    if constexpr (!std::is_same<TO, exact_t>::value)
+      if (w == 8 && t == 2) return keys_as<T, TO, D, 8, 2, true>(a, st);
   } else {
     if (w == 4 && t == 1) return keys_as<T, TO, D, 4, 1, true>(a, st);
     if constexpr (D == 32) {
@@ -910,6 +978,7 @@ hipError_t join_d(const GradArgs& a, hipStream_t st) {
 #define GRAD_BY_TYPES(F)                                       \
   if (dtype == 0 && out_dtype == 0) GRAD_BY_D(F, float, float);   \
   if (dtype == 0) GRAD_BY_D(F, float, bf16_t);                    \
+  if (out_dtype == 0 && a.dlogw) GRAD_BY_D(F, bf16_t, exact_t);   \
   if (out_dtype == 0) GRAD_BY_D(F, bf16_t, float);                \
   GRAD_BY_D(F, bf16_t, bf16_t)
 

@@ -8,7 +8,11 @@
 
 namespace thin {
 
-constexpr int64_t kGradTile = 32;  // query rows per step of a workgroup
+// Query rows per step of a workgroup: 32, which the bf16 instruction sums over at a time; float32
+// rows of few keys 16, so that the tiles in LDS leave room for several workgroups (40 slices of
+// 14251 queries over 2 keys of 128 channels 507 -> 272 us; over 128 keys of 64 channels 16 take
+// 239 us where 32 take 214).
+constexpr int64_t grad_tile(bool bf16, int64_t waves) { return bf16 || waves > 2 ? 32 : 16; }
 
 struct GradShape {
   int32_t waves, tiles;  // of a workgroup; 16-key tiles of a wave
@@ -32,9 +36,12 @@ constexpr int64_t grad_most_keys(bool bf16) { return bf16 ? 256 : 128; }
 // d = 128, 64 slices of 16384 queries: 128 keys 8x1 354, 4x2 500; 192 keys 12x1 495, 8x2 548, 4x3
 // 504; 256 keys 8x2 548, 16x1 910, 4x4 855.  float32 rows, 64 slices of 4096 queries over 128
 // keys: d = 32 8x1 135, 4x2 118; d = 64 8x1 215, 4x2 232.
-inline GradShape grad_shape(int64_t S, int64_t n_q, int64_t n_out, int64_t d, bool bf16) {
+// exact: bf16 rows with all of a float32 dO's three parts, for which the local memory has no room
+// beside over 192 keys of 128 channels.
+inline GradShape grad_shape(int64_t S, int64_t n_q, int64_t n_out, int64_t d, bool bf16,
+                            bool exact) {
   GradShape s{};
-  s.one = n_out <= grad_most_keys(bf16);
+  s.one = n_out <= (exact && d == 128 ? 192 : grad_most_keys(bf16));
   auto is = [&](int waves, int tiles) {
     s.waves = waves;
     s.tiles = tiles;
@@ -52,7 +59,7 @@ inline GradShape grad_shape(int64_t S, int64_t n_q, int64_t n_out, int64_t d, bo
   else  // chunks
     bf16 && d < 128 ? is(8, 2) : is(8, 1);
   s.chunks = (int32_t)((n_out + s.keys() - 1) / s.keys());
-  const int64_t steps = (n_q + kGradTile - 1) / kGradTile;
+  const int64_t tile = grad_tile(bf16, s.waves), steps = (n_q + tile - 1) / tile;
   const int64_t slots = s.waves > 8 ? 256 : 256 * (8 / s.waves);
   const StepSplit p = split_steps(S * s.chunks, steps, slots, 2.0, 1.0);
   s.parts = (int32_t)p.parts;

@@ -55,7 +55,7 @@ def thin_attention_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, i
         raise ThinError(THIN_EDTYPE, "Q, K, V must share a dtype")
     if dO.shape != Q.shape:
         raise ThinError(THIN_EINVAL, "dO must match Q")
-    n_out = idx.shape[-1]
+    n_out = idx.shape[2] if idx.dim() == 3 else 0
     if idx.dtype != torch.int32 or idx.shape != (B, H, n_out) or not idx.is_contiguous():
         raise ThinError(THIN_EINVAL, "idx must be contiguous int32 [B,H,n_out]")
     i = _on(idx, dev, "idx")
@@ -99,20 +99,25 @@ class _CoresetAttention(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dO):
         Q, K, V, idx, logw = ctx.saved_tensors
+        need_logw = ctx.needs_input_grad[4]
         with torch.cuda.device(Q.device):
             g = thin_attention_backward(Q, K, V, idx, dO.contiguous(), logw=logw,
-                                        need_logw=ctx.needs_input_grad[4])
-        return g[0], g[1], g[2], None, g[3] if ctx.needs_input_grad[4] else None, None
+                                        need_logw=need_logw)
+        return g[0], g[1], g[2], None, g[3] if need_logw else None, None
 
 
 def coreset_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, idx: torch.Tensor, *,
                       logw: Optional[torch.Tensor] = None,
                       out_dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """thin_attention that autograd records, on the current stream: gradients reach Q, K, V
-    (zeros in the rows that idx does not list) and logw by thin_attention_backward.  The choice
-    of the rows, idx, has none.  Strided inputs are laid out contiguously first."""
-    idx = idx.contiguous()
-    if logw is not None:
-        logw = logw.contiguous()
-    return _CoresetAttention.apply(Q.contiguous(), K.contiguous(), V.contiguous(), idx, logw,
+    (zeros in the rows that idx does not list) and logw by thin_attention_backward, once (the
+    gradient of a gradient is refused).  The choice of the rows, idx, has none.  Strided inputs
+    are laid out contiguously first."""
+    dev, _ = _where(None)
+    for t, name in ((Q, "Q"), (K, "K"), (V, "V"), (idx, "idx"), (logw, "logw")):
+        if t is not None:
+            _on(t, dev, name)
+    _dtype(Q, "Q")
+    return _CoresetAttention.apply(Q.contiguous(), K.contiguous(), V.contiguous(),
+                                   idx.contiguous(), None if logw is None else logw.contiguous(),
                                    out_dtype)

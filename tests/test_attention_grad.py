@@ -17,8 +17,9 @@ ODD, BYTE = C.c_void_p(0x10008), C.c_void_p(0x10001)
 
 
 def call(**kw):
+    out = [C.c_void_p(0x100000 * i) for i in range(1, 4)]
     a = dict(Q=FAKE, K=FAKE, V=FAKE, dtype=1, B=2, H=3, n_q=100, n=50, d=64, idx=FAKE, logw=None,
-             n_out=20, dO=FAKE, out_dtype=0, dQ=FAKE, dK=FAKE, dV=FAKE, dlogw=None, ws=FAKE,
+             n_out=20, dO=FAKE, out_dtype=0, dQ=out[0], dK=out[1], dV=out[2], dlogw=None, ws=FAKE,
              wn=1 << 40)
     a.update(kw)
     return _lib.lib().thin_attention_backward(*a.values(), None)
@@ -28,7 +29,8 @@ def call(**kw):
     (dict(Q=None), EINVAL), (dict(K=None), EINVAL), (dict(V=ODD), EINVAL), (dict(dO=ODD), EINVAL),
     (dict(dQ=None), EINVAL), (dict(dK=ODD), EINVAL), (dict(dV=None), EINVAL),
     (dict(idx=None), EINVAL), (dict(idx=BYTE), EINVAL), (dict(logw=BYTE), EINVAL),
-    (dict(dlogw=BYTE), EINVAL), (dict(dtype=2), EDTYPE), (dict(out_dtype=-1), EDTYPE),
+    (dict(dlogw=BYTE), EINVAL), (dict(dQ=FAKE), EINVAL), (dict(dV=FAKE), EINVAL),
+    (dict(dK=C.c_void_p(0x100000)), EINVAL), (dict(dtype=2), EDTYPE), (dict(out_dtype=-1), EDTYPE),
     (dict(d=96), EINVAL), (dict(B=0), EINVAL), (dict(B=300, H=300), EINVAL), (dict(n_q=0), EINVAL),
     (dict(n=0), EINVAL), (dict(n_out=0), EINVAL), (dict(n_q=(1 << 29) // 6 + 1), EINVAL),
     (dict(n_out=(1 << 25) // 6 + 1), EINVAL), (dict(n=(1 << 30) + 1), EINVAL),
@@ -58,13 +60,13 @@ int main() {
   const int64_t qs[] = {1, 31, 32, 33, 100, 1023, 4096, 16384, 65536, 1000003};
   const int64_t ks[] = {1, 16, 17, 32, 33, 64, 65, 128, 129, 192, 256, 257, 600, 5000, 300000};
   for (int64_t S : Ss) for (int64_t q : qs) for (int64_t k : ks) for (int b = 0; b < 2; ++b)
-  for (int64_t d : {32, 64, 128}) {
-    const GradShape s = grad_shape(S, q, k, d, b);
-    const int64_t steps = (q + kGradTile - 1) / kGradTile;
+  for (int64_t d : {32, 64, 128}) for (int e = 0; e <= b; ++e) {
+    const GradShape s = grad_shape(S, q, k, d, b, e);
+    const int64_t steps = (q + grad_tile(b, s.waves) - 1) / grad_tile(b, s.waves);
     // every key and every step has a workgroup, none is without a step
     if (s.keys() * s.chunks < k || s.keys() * (s.chunks - 1) >= k) return 1;
     if ((int64_t)s.parts * s.run < steps || (int64_t)(s.parts - 1) * s.run >= steps) return 2;
-    if (s.one != (k <= grad_most_keys(b)) || (s.one && s.chunks != 1)) return 3;
+    if (s.one != (k <= (e && d == 128 ? 192 : grad_most_keys(b))) || (s.one && s.chunks != 1)) return 3;
     if (!s.one && s.waves != 8) return 4;
     if (!b && d > 32 && s.tiles != 1) return 5;
     // threads of a launch fit 32 bits where rows and keys are within the entry point's limits

@@ -377,6 +377,17 @@ def test_binding_refuses_what_does_not_fit():
     refused(THIN_EINVAL, Q, K, V, idx, dO, dlogw=logw[..., :8])
     refused(THIN_EWORKSPACE, Q, K, V, idx, dO,
             workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+    for bad in (dict(dQ=Q), dict(dQ=dO), dict(dK=K), dict(dV=K), dict(dK=V)):
+        refused(THIN_EINVAL, Q, K, V, idx, dO, **bad)
+    same = torch.empty_like(K)
+    refused(THIN_EINVAL, Q, K, V, idx, dO, dK=same, dV=same)
+    for bad in ((Q.cpu(), K, V, idx), (Q, K, V, idx.cpu())):
+        with pytest.raises(ThinError) as e:
+            coreset_attention(*bad)
+        assert e.value.status == THIN_EINVAL
+    with pytest.raises(ThinError) as e:
+        coreset_attention(Q.half(), K.half(), V.half(), idx)
+    assert e.value.status == THIN_EDTYPE
     out = torch.full_like(K, 3.0)
     got = thin_attention_backward(Q, K, V, idx, dO, logw=logw, dK=out)
     assert got[1] is out and len(got) == 3
