@@ -193,15 +193,17 @@ __global__ __launch_bounds__(64 * PW, 2) void q4_prompt_kernel(Q4View c, Q4AttnA
     if (row0 <= wlast) {
       if (row0 + PK - 1 > all) {
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          uint64_t see = 0;
-          if (TREE) see = drafts[rt].window(row0) >> (4 * g);
+        for (int rt = 0; rt < RT; ++rt)
+          if constexpr (TREE) {
+            const uint64_t see = drafts[rt].window(row0) >> (4 * g);
 #pragma unroll
-          for (int j = 0; j < PK / 4; ++j)
-            if (TREE ? !(see >> (j / 4 * 16 + j % 4) & 1)
-                     : row0 + j / 4 * 16 + 4 * g + j % 4 > qlast[rt])
-              s[rt][j] = -INFINITY;
-        }
+            for (int j = 0; j < PK / 4; ++j)
+              if (!(see >> (j / 4 * 16 + j % 4) & 1)) s[rt][j] = -INFINITY;
+          } else {
+#pragma unroll
+            for (int j = 0; j < PK / 4; ++j)
+              if (row0 + j / 4 * 16 + 4 * g + j % 4 > qlast[rt]) s[rt][j] = -INFINITY;
+          }
       }
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {

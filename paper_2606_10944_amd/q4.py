@@ -169,12 +169,12 @@ def _rotary(X, pos, turns, axis, Y, layout, amp, inverse, out, out_Y, stream):
     B, H, T, d = shape
     if turns.dtype != torch.float64 or turns.dim() != 1 or not turns.is_contiguous():
         raise ThinError(THIN_EINVAL, "turns must be contiguous float64 [rot/2]")
-    per_token = pos.dim() == 2
-    if axis is not None:
+    if axis is None:
+        per_token = pos.dim() == 2
+        p = _ints(pos, (B, T) if per_token else (B,), dev, "pos")
+    else:
         axes = pos.shape[2]
         p = _ints(pos, (B, T, axes), dev, "pos")
-    else:
-        p = _ints(pos, (B, T) if per_token else (B,), dev, "pos")
     if out is None:
         out = _empty_like(X, dev, stream)
         o, os_ = out.data_ptr(), None
@@ -200,14 +200,15 @@ def _rotary(X, pos, turns, axis, Y, layout, amp, inverse, out, out_Y, stream):
             oy, oys = _rows(out_Y, dev, "out_Y")
     elif out_Y is not None:
         raise ThinError(THIN_EINVAL, "out_Y without Y")
-    rows = (x, xs, H, o, os_, y, ys, Hy, oy, oys, _dtype(X, "X"), B, T, d, 2 * turns.shape[0], lay,
-            p)
-    t = _on(turns, dev, "turns")
-    if axis is not None:
-        rc = lib().thin_rotary_axes(*rows, axes, _ints(axis, axis.shape, dev, "axis"), t, amp,
-                                    inverse, st)
+    if axis is None:
+        rc = lib().thin_rotary(x, xs, H, o, os_, y, ys, Hy, oy, oys, _dtype(X, "X"), B, T, d,
+                               2 * turns.shape[0], lay, p, per_token, _on(turns, dev, "turns"),
+                               amp, inverse, st)
     else:
-        rc = lib().thin_rotary(*rows, per_token, t, amp, inverse, st)
+        rc = lib().thin_rotary_axes(x, xs, H, o, os_, y, ys, Hy, oy, oys, _dtype(X, "X"), B, T, d,
+                                    2 * turns.shape[0], lay, p, axes,
+                                    _ints(axis, axis.shape, dev, "axis"),
+                                    _on(turns, dev, "turns"), amp, inverse, st)
     if rc:
         _check(rc, "thin_rotary" if axis is None else "thin_rotary_axes")
     return out if Y is None else (out, out_Y)
