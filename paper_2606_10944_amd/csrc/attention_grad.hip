@@ -147,6 +147,11 @@ struct Span {
   __device__ __forceinline__ void store(u32x4 w, uint32_t at) const {
     __builtin_amdgcn_raw_buffer_store_b128(w, r, at, 0, 0);
   }
+  // (not to be kept in the caches: the zeros of dK and dV, 87 -> 76 us for 64 slices of 8192
+  // queries over 64 keys of 64 channels; dQ, whose lines several waves write, 360 -> 440 us)
+  __device__ __forceinline__ void stream(u32x4 w, uint32_t at) const {
+    __builtin_amdgcn_raw_buffer_store_b128(w, r, at, 0, 2);
+  }
   __device__ __forceinline__ void store(u32x2 w, uint32_t at) const {
     __builtin_amdgcn_raw_buffer_store_b64(w, r, at, 0, 0);
   }
@@ -404,8 +409,8 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
     const Span k(static_cast<T*>(a.dK) + at, left), v(static_cast<T*>(a.dV) + at, left);
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      k.store((u32x4){0, 0, 0, 0}, (i * 64 * W + threadIdx.x) * 16);
-      v.store((u32x4){0, 0, 0, 0}, (i * 64 * W + threadIdx.x) * 16);
+      k.stream((u32x4){0, 0, 0, 0}, (i * 64 * W + threadIdx.x) * 16);
+      v.stream((u32x4){0, 0, 0, 0}, (i * 64 * W + threadIdx.x) * 16);
     }
     z += IT * 64 * W;
   };
@@ -770,7 +775,9 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
     for (int p = 0; p < OP; ++p) of[p][v] = __builtin_bit_cast(uint4, x[p]);
   }
   const float c2 = (float)(kLog2e / sqrt((double)D)), rd = (float)(1.0 / sqrt((double)D));
-  auto products = [&](int buf, float (&p)[KT][4], float (&gd)[KT][4]) __attribute__((always_inline)) {
+  // all parts of dO for the statistics, from which dlogw is; two for dQ, which rounds to bf16
+  auto products = [&](int buf, auto parts, float (&p)[KT][4], float (&gd)[KT][4])
+                      __attribute__((always_inline)) {
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
       floatx4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
@@ -779,7 +786,7 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
         x = mma_word<T>(lds_word<T, D>(sk[buf] + 16 * kt * R::stride, v, m, g), qf[v], x);
         const uint4 vw = lds_word<T, D>(sv[buf] + 16 * kt * R::stride, v, m, g);
 #pragma unroll
-        for (int o = OP - 1; o >= 0; --o) y = mma_word<T>(vw, of[o][v], y);
+        for (int o = decltype(parts)::value - 1; o >= 0; --o) y = mma_word<T>(vw, of[o][v], y);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -803,7 +810,7 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   };
   for (; i < steps; ++i) {
     float p[KT][4], gd[KT][4];
-    products((int)i & 1, p, gd);
+    products((int)i & 1, std::integral_constant<int, OP>(), p, gd);
     float x = mx;
 #pragma unroll
     for (int j = 0; j < 4 * KT; ++j) x = fmaxf(x, p[j / 4][j % 4]);
@@ -837,7 +844,7 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   for (; i < 2 * steps; ++i) {
     const int buf = (int)i & 1;
     float p[KT][4], gd[KT][4];
-    products(buf, p, gd);
+    products(buf, std::integral_constant<int, (OP < 2 ? OP : 2)>(), p, gd);
 #pragma unroll
     for (int j = 0; j < 4 * KT; ++j)
       p[j / 4][j % 4] =
