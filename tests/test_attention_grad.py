@@ -71,7 +71,8 @@ int main() {
     if (!b && d > 32 && s.tiles != 1) return 5;
     // threads of a launch fit 32 bits where rows and keys are within the entry point's limits
     if (S * k <= (1 << 25) && S * q <= (1 << 29) &&
-        S * s.chunks * s.parts * 64 * s.waves >= ((int64_t)1 << 32)) return 6;
+        (S * s.chunks * s.parts * 64 * s.waves >= ((int64_t)1 << 32) ||
+         (s.parts >= 16 && S * k * 256 >= ((int64_t)1 << 32)))) return 6;
   }
   puts("ok");
 }
