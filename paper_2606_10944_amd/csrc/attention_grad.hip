@@ -259,7 +259,9 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
   constexpr int QU = QT / UR;
   constexpr int PLANE = QT * R::stride;
   constexpr int IT = (QT * R::CW + 64 * W - 1) / (64 * W);  // words of a tile per thread
-  constexpr int SS = NK * Elem<T>::bytes + 16;  // bytes per query of p and ds in LDS
+  // bytes per query of p and ds in LDS (bf16: 24 of padding, 0 8 16 24 32 40 took 1485 531 549 528
+  // 645 530 us at [32,32768,128], 256 keys)
+  constexpr int SS = NK * Elem<T>::bytes + (Elem<T>::bytes == 2 ? 24 : 16);
   // dQ: a wave's units are (16 channels, 16 queries), UN of them in all; of two tiles it takes
   // both, where it has several
   constexpr int UN = TQ * DT, U = (UN + W - 1) / W;

@@ -83,6 +83,17 @@ def test_gradient(B, H, n_q, n, n_out, d, dtype, out):
     assert all(torch.equal(a, b) for a, b in zip(got, again))
 
 
+@pytest.mark.parametrize("B,H,n_q,n,n_out,d", SHAPES)
+def test_gradient_without_that_of_the_weights(B, H, n_q, n, n_out, d):
+    """Products of a float32 dO with bf16 rows take fewer parts of it then."""
+    g = gen(215)
+    args = inputs(g, B, H, n_q, n, n_out, d, "bf16", "fp32", weighted=n_out % 2 == 0)
+    Q, K, V, idx, logw, dO = args
+    got = thin_attention_backward(*(to(x) for x in (Q, K, V, idx, dO)), logw=to(logw))
+    assert len(got) == 3
+    check(args, got)
+
+
 @pytest.mark.parametrize("dtype,out", [("fp32", "fp32"), ("bf16", "fp32")])
 @pytest.mark.parametrize("n_out", [7, 40, 300])
 def test_gradient_against_differences(n_out, dtype, out):
