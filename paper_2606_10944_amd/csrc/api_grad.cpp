@@ -86,13 +86,18 @@ int thin_attention_backward(const void* Q, const void* K, const void* V, int32_t
   a.n = n;
   a.n_q = n_q;
   a.n_out = n_out;
+  const int64_t row_bytes = d * (dtype == THIN_BF16 ? 2 : 4);
+  a.zeros = thin::grad_zeros(a.shape, n_q, n, row_bytes);
   char* w = static_cast<char*>(workspace);
   a.part = reinterpret_cast<float*>(w);
   if (dlogw) a.part_w = reinterpret_cast<float*>(w + bytes.part);
   a.stats = reinterpret_cast<float*>(w + bytes.part + bytes.part_w);
   hipStream_t st = static_cast<hipStream_t>(stream);
   hipError_t e = hipSuccess;
-  if (!a.shape.one)
+  if (a.zeros)
+    e = observed(THIN_KERNEL_ATTENTION_GRAD, -1, st,
+                 [&] { return thin::launch_grad_zeros(row_bytes, a, st); });
+  if (e == hipSuccess && !a.shape.one)
     e = observed(THIN_KERNEL_ATTENTION_GRAD, -1, st,
                  [&] { return thin::launch_grad_rows(dtype, out_dtype, d, a, st); });
   if (e == hipSuccess)

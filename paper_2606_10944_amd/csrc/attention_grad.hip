@@ -241,6 +241,21 @@ __device__ __forceinline__ int coreset_row(const GradArgs& a, int64_t s, int64_t
 }
 
 // ---------------------------------------------------------------------------
+// Zeros of dK and dV, where the rows are many more than the queries.
+// ---------------------------------------------------------------------------
+constexpr int ZT = 256, ZW = 8;  // threads, 16-byte words of each tensor per thread
+
+__global__ __launch_bounds__(ZT) void grad_zeros_kernel(u32x4* k, u32x4* v, int64_t words) {
+  const int64_t z = (int64_t)blockIdx.x * ZT * ZW + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < ZW; ++i)
+    if (z + i * ZT < words) {
+      k[z + i * ZT] = (u32x4){0, 0, 0, 0};
+      v[z + i * ZT] = (u32x4){0, 0, 0, 0};
+    }
+}
+
+// ---------------------------------------------------------------------------
 // Keys: see above.  W waves of 16 KT keys.  ONE: every key of the slice is here.
 //
 // Lanes are l = 16 g + m.  Scores S^T = K Q^T by 16 keys x 16 queries: lane (m, g) holds keys
@@ -403,7 +418,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
   // step's queries have, the rest of them behind the last step
   const int64_t words = a.n * D / E;
   const int64_t zs = (words + a.shape.parts - 1) / a.shape.parts;
-  int64_t z = chunk == 0 ? std::min(words, part * zs) : words;
+  int64_t z = chunk == 0 && !a.zeros ? std::min(words, part * zs) : words;
   const int64_t z1 = std::min(words, z + zs);
   auto zeros = [&]() __attribute__((always_inline)) {
     const int64_t at = s * a.n * D + std::min(z, z1) * E;
@@ -692,25 +707,35 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
 }
 
 // ---------------------------------------------------------------------------
-// Rows, for coresets wider than a workgroup holds: a wave takes 16 queries and walks the keys
-// twice, for the rows' statistics, then for dQ.  Scores S^T = K Q^T: lane (m, g) holds keys
-// 4 g .. 4 g + 3 of query m.
+// Rows, for coresets wider than a workgroup holds: SH waves take 16 queries and walk the keys
+// twice, for the rows' statistics, then for dQ; of a step's keys each takes its share, and they
+// join statistics and sums through LDS.  Scores S^T = K Q^T: lane (m, g) holds keys 4 g .. 4 g + 3
+// of query m.
+//
+// 15 slices of 2047 queries over 333 keys, d = 128, bf16 with a float32 dO: 39 us, the matrix
+// cores busy for 25 % of it, LDS 22 %, the vector ALU 29 %: the rest are a step's latencies, two
+// waves per SIMD that meet at a barrier every 64 keys.
 // ---------------------------------------------------------------------------
 constexpr int RW = 8;  // waves
 
-template <typename T, typename TO, int D>
+template <typename T, typename TO, int D, int SH>
 __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   using R = LdsRows<T, D>;
   constexpr int NV = Frag<T, D>::NV, DT = D / 16, OP = Parts<T, TO>::n;
-  constexpr int CK = 64, KT = CK / 16;  // keys per step
+  // a wave's tiles of a step's keys, and these
+  constexpr int KT = std::max(4 / SH, kUnit<T> / 16), CK = 16 * KT * SH;
   constexpr int IT = (CK * R::CW + 64 * RW - 1) / (64 * RW);  // words of a step per thread
   __shared__ __align__(16) unsigned char sk[2][CK * R::stride], sv[2][CK * R::stride];
   __shared__ float sb[2][CK];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, g = lane >> 4;
-  const int64_t blocks = (a.n_q + 16 * RW - 1) / (16 * RW);
+  __shared__ float st[SH > 1 ? RW : 1][3][16];
+  constexpr int RT = RW / SH;  // tiles of 16 queries
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = wave % SH;
+  const int64_t blocks = (a.n_q + 16 * RT - 1) / (16 * RT);
   const int64_t s = blockIdx.x / blocks;
-  const int64_t r = (blockIdx.x % blocks * RW + wave) * 16 + m;  // this lane's query
-  const bool there = r < a.n_q;
+  const int64_t r0 = (blockIdx.x % blocks * RT + wave / SH) * 16;  // the wave's first query
+  const int64_t r = r0 + m;                                        // this lane's
+  const bool there = r < a.n_q, active = r0 < a.n_q;
   // A step's rows are on their way while the step before is worked on, and their numbers and
   // log-weights a step before that, without branches: no load waits for another.
   int32_t at[IT];
@@ -763,7 +788,6 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
 
   uint4 qf[NV], of[OP][NV];
   load_frag<T, D>(static_cast<const T*>(a.Q), s * a.n_q + r, g, there, qf);
-  const int64_t r0 = __builtin_amdgcn_readfirstlane((int)(r - m));  // the wave's first row
   const Span dO(static_cast<const TO*>(a.dO) + (s * a.n_q + std::min(r0, a.n_q - 1)) * D,
                 (int)std::max<int64_t>(0, std::min<int64_t>(16, a.n_q - r0)) * D *
                     Elem<TO>::bytes);
@@ -785,14 +809,15 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
       floatx4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        x = mma_word<T>(lds_word<T, D>(sk[buf] + 16 * kt * R::stride, v, m, g), qf[v], x);
-        const uint4 vw = lds_word<T, D>(sv[buf] + 16 * kt * R::stride, v, m, g);
+        const int at = 16 * (sub * KT + kt) * R::stride;
+        x = mma_word<T>(lds_word<T, D>(sk[buf] + at, v, m, g), qf[v], x);
+        const uint4 vw = lds_word<T, D>(sv[buf] + at, v, m, g);
 #pragma unroll
         for (int o = decltype(parts)::value - 1; o >= 0; --o) y = mma_word<T>(vw, of[o][v], y);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        p[kt][j] = fmaf(x[j], c2, sb[buf][16 * kt + 4 * g + j]);
+        p[kt][j] = fmaf(x[j], c2, sb[buf][16 * (sub * KT + kt) + 4 * g + j]);
         gd[kt][j] = y[j];
       }
     }
@@ -811,32 +836,52 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
     __syncthreads();
   };
   for (; i < steps; ++i) {
-    float p[KT][4], gd[KT][4];
-    products((int)i & 1, std::integral_constant<int, OP>(), p, gd);
-    float x = mx;
+    if (active) {
+      float p[KT][4], gd[KT][4];
+      products((int)i & 1, std::integral_constant<int, OP>(), p, gd);
+      float x = mx;
 #pragma unroll
-    for (int j = 0; j < 4 * KT; ++j) x = fmaxf(x, p[j / 4][j % 4]);
-    const float k = __builtin_amdgcn_exp2f(mx - x);
-    mx = x;
-    l *= k;
-    e *= k;
+      for (int j = 0; j < 4 * KT; ++j) x = fmaxf(x, p[j / 4][j % 4]);
+      const float k = __builtin_amdgcn_exp2f(mx - x);
+      mx = x;
+      l *= k;
+      e *= k;
 #pragma unroll
-    for (int j = 0; j < 4 * KT; ++j) {
-      const float w = __builtin_amdgcn_exp2f(p[j / 4][j % 4] - mx);
-      l += w;
-      e = fmaf(w, gd[j / 4][j % 4], e);
+      for (int j = 0; j < 4 * KT; ++j) {
+        const float w = __builtin_amdgcn_exp2f(p[j / 4][j % 4] - mx);
+        l += w;
+        e = fmaf(w, gd[j / 4][j % 4], e);
+      }
     }
     turn();
   }
   auto add = [](float x, float y) { return x + y; };
-  const float top = across_rows(mx, true, [](float x, float y) { return fmaxf(x, y); });
+  float top = across_rows(mx, true, [](float x, float y) { return fmaxf(x, y); });
   const float k = __builtin_amdgcn_exp2f(mx - top);
   l = across_rows(l * k, true, add);
   e = across_rows(e * k, true, add);
+  if constexpr (SH > 1) {
+    if (g == 0) {
+      st[wave][0][m] = top;
+      st[wave][1][m] = l;
+      st[wave][2][m] = e;
+    }
+    __syncthreads();
+    const int w0 = wave - sub;
+#pragma unroll
+    for (int w = 0; w < SH; ++w) top = fmaxf(top, st[w0 + w][0][m]);
+    l = e = 0.0f;
+#pragma unroll
+    for (int w = 0; w < SH; ++w) {
+      const float k = __builtin_amdgcn_exp2f(st[w0 + w][0][m] - top);
+      l = fmaf(st[w0 + w][1][m], k, l);
+      e = fmaf(st[w0 + w][2][m], k, e);
+    }
+  }
   // a row that no key weighs in: probabilities of 0
   const float lse = l > 0.0f ? top + __builtin_amdgcn_logf(l) : INFINITY;
   const float dm = l > 0.0f ? e / l : 0.0f;
-  if (there && g == 0) {
+  if (there && g == 0 && sub == 0) {
     a.stats[s * a.n_q + r] = lse;
     a.stats[(a.S + s) * a.n_q + r] = dm;
   }
@@ -845,21 +890,38 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   for (int dt = 0; dt < DT; ++dt) acc[dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
   for (; i < 2 * steps; ++i) {
     const int buf = (int)i & 1;
-    float p[KT][4], gd[KT][4];
-    products(buf, std::integral_constant<int, (OP < 2 ? OP : 2)>(), p, gd);
+    if (active) {
+      float p[KT][4], gd[KT][4];
+      products(buf, std::integral_constant<int, (OP < 2 ? OP : 2)>(), p, gd);
 #pragma unroll
-    for (int j = 0; j < 4 * KT; ++j)
-      p[j / 4][j % 4] =
-          __builtin_amdgcn_exp2f(p[j / 4][j % 4] - lse) * (gd[j / 4][j % 4] - dm);
+      for (int j = 0; j < 4 * KT; ++j)
+        p[j / 4][j % 4] =
+            __builtin_amdgcn_exp2f(p[j / 4][j % 4] - lse) * (gd[j / 4][j % 4] - dm);
 #pragma unroll
-    for (int h = 0; h < CK / kUnit<T>; ++h) {
-      const Column<T> w(p + h * (kUnit<T> / 16));
+      for (int h = 0; h < 16 * KT / kUnit<T>; ++h) {
+        const Column<T> w(p + h * (kUnit<T> / 16));
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-        acc[dt] = Column<T>(sk[buf] + kUnit<T> * h * R::stride, R::stride, dt, m, g)
-                      .times(w, acc[dt]);
+        for (int dt = 0; dt < DT; ++dt)
+          acc[dt] = Column<T>(sk[buf] + (16 * KT * sub + kUnit<T> * h) * R::stride, R::stride, dt,
+                              m, g)
+                        .times(w, acc[dt]);
+      }
     }
     turn();
+  }
+  if constexpr (SH > 1) {  // the keys' place is free now
+    constexpr int PER = (SH - 1) * 64;
+    static_assert(RT * PER * DT * 16 <= (int)sizeof(sk), "room for the waves' sums");
+    floatx4_t* sums = reinterpret_cast<floatx4_t*>(sk[0]) + wave / SH * PER * DT;
+    if (sub > 0)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) sums[(dt * (SH - 1) + sub - 1) * 64 + lane] = acc[dt];
+    __syncthreads();
+    if (sub > 0) return;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int w = 0; w < SH - 1; ++w) acc[dt] += sums[(dt * (SH - 1) + w) * 64 + lane];
   }
   if (!there) return;
 #pragma unroll
@@ -975,8 +1037,15 @@ hipError_t keys_d(const GradArgs& a, hipStream_t st) {
 
 template <typename T, typename TO, int D>
 hipError_t rows_d(const GradArgs& a, hipStream_t st) {
-  const int64_t blocks = (a.n_q + 16 * RW - 1) / (16 * RW);
-  grad_rows_kernel<T, TO, D><<<(uint32_t)(a.S * blocks), 64 * RW, 0, st>>>(a);
+  const int share = grad_share(a.S, a.n_q);
+  const int64_t rows = 16 * RW / share;
+  const uint32_t grid = (uint32_t)(a.S * ((a.n_q + rows - 1) / rows));
+  if (share == 4)
+    grad_rows_kernel<T, TO, D, 4><<<grid, 64 * RW, 0, st>>>(a);
+  else if (share == 2)
+    grad_rows_kernel<T, TO, D, 2><<<grid, 64 * RW, 0, st>>>(a);
+  else
+    grad_rows_kernel<T, TO, D, 1><<<grid, 64 * RW, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -1003,6 +1072,12 @@ hipError_t join_d(const GradArgs& a, hipStream_t st) {
   if (out_dtype == 0) GRAD_BY_D(F, bf16_t, float);                \
   GRAD_BY_D(F, bf16_t, bf16_t)
 
+hipError_t launch_grad_zeros(int64_t row_bytes, const GradArgs& a, hipStream_t st) {
+  const int64_t words = a.S * a.n * row_bytes / 16;
+  grad_zeros_kernel<<<(uint32_t)((words + ZT * ZW - 1) / (ZT * ZW)), ZT, 0, st>>>(
+      static_cast<u32x4*>(a.dK), static_cast<u32x4*>(a.dV), words);
+  return hipGetLastError();
+}
 hipError_t launch_grad_rows(int dtype, int out_dtype, int64_t d, const GradArgs& a,
                             hipStream_t st) {
   GRAD_BY_TYPES(rows_d);

@@ -67,6 +67,25 @@ inline GradShape grad_shape(int64_t S, int64_t n_q, int64_t n_out, int64_t d, bo
   return s;
 }
 
+// Whether the zeros of dK and dV take a launch of their own (3 us and their bytes at 7 TB/s)
+// instead of the workgroups' spare time: where rows are many more than queries and a workgroup
+// would have a quarter of a megabyte to write, which takes it 3 to 6 us.  In us, without and with:
+//   24 slices of 3 queries, 16370 rows (fp32, d = 128, 17 MB per workgroup) 159, 82
+//   84 of 271, 5533 (bf16, d = 128, 0.3 MB) 75, 52; 12 of 113, 7048 (bf16, d = 64, 0.4 MB) 57, 59
+//   36 of 3451, 13941 (fp32, d = 64, 1 MB, a fourth as many queries) 79, 83
+inline bool grad_zeros(const GradShape& s, int64_t n_q, int64_t n, int64_t row_bytes) {
+  return n / 16 >= n_q && n * row_bytes * 2 / s.parts >= (1 << 18);
+}
+
+// Waves that share a tile of 16 query rows (and divide its keys) where the rows take a launch of
+// their own: as many as leave a workgroup of eight waves for each compute unit.  In us with 1, 2
+// and 4: 6 slices of 67 queries, 954 keys (fp32, d = 128) 344, 214, 152; 8 of 2048, 1024 (bf16,
+// d = 128) 109, 94, 121; 15 of 2047, 333 (the same) 79, 91, 121.
+inline int grad_share(int64_t S, int64_t n_q) {
+  auto groups = [&](int64_t tiles) { return S * ((n_q + 16 * tiles - 1) / (16 * tiles)); };
+  return groups(2) <= 256 ? 4 : groups(4) <= 256 ? 2 : 1;
+}
+
 // Bytes of the workspace: sums of dK and dV, of dlogw, and the statistics.
 struct GradBytes {
   size_t part, part_w, stats;

@@ -73,6 +73,10 @@ int main() {
     if (S * k <= (1 << 25) && S * q <= (1 << 29) &&
         (S * s.chunks * s.parts * 64 * s.waves >= ((int64_t)1 << 32) ||
          (s.parts >= 16 && S * k * 256 >= ((int64_t)1 << 32)))) return 6;
+    const int share = grad_share(S, q);
+    if (share > 1 && S * ((q + 128 / share - 1) / (128 / share)) > 256) return 7;
+    if (grad_zeros(s, q, 16 * q - 1, d * 4) || grad_zeros(s, 1, 100, d * 4)) return 8;
+    if (s.parts < 100 && !grad_zeros(s, 1, 1 << 20, d * 2)) return 9;
   }
   puts("ok");
 }

@@ -83,6 +83,31 @@ def test_gradient(B, H, n_q, n, n_out, d, dtype, out):
     assert all(torch.equal(a, b) for a, b in zip(got, again))
 
 
+@pytest.mark.parametrize("dtype,out", TYPES)
+@pytest.mark.parametrize("B,H,n_q,n,n_out,d", [
+    (33, 8, 20, 260, 257, 32), (16, 4, 200, 300, 260, 64), (32, 2, 193, 290, 288, 128),
+    (2, 1, 37, 700, 513, 128), (1, 3, 31, 400, 290, 32)])
+def test_waves_that_share_query_rows(B, H, n_q, n, n_out, d, dtype, out):
+    """One, two (twice) and four (twice) waves per tile of rows."""
+    g = gen(216)
+    args = inputs(g, B, H, n_q, n, n_out, d, dtype, out, weighted=True)
+    check(args, backward(*args))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("B,H,n_q,n,n_out,d", [
+    (1, 1, 3, 9001, 40, 128), (2, 3, 1, 16385, 1, 32), (1, 2, 7, 8003, 300, 64),
+    (1, 5, 300, 9999, 130, 128)])
+def test_many_rows_for_few_queries(B, H, n_q, n, n_out, d, dtype):
+    """Their zeros come from a launch of their own; whatever the gradients held goes."""
+    g = gen(217)
+    Q, K, V, idx, logw, dO = args = inputs(g, B, H, n_q, n, n_out, d, dtype, dtype)
+    dK, dV = (torch.full((B, H, n, d), math.nan, dtype=DT[dtype], device=DEV) for _ in range(2))
+    got = backward(*args, dK=dK, dV=dV)
+    assert got[1] is dK and got[2] is dV
+    check(args, got)
+
+
 @pytest.mark.parametrize("B,H,n_q,n,n_out,d", SHAPES)
 def test_gradient_without_that_of_the_weights(B, H, n_q, n, n_out, d):
     """Products of a float32 dO with bf16 rows take fewer parts of it then."""
