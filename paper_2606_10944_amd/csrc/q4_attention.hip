@@ -11,7 +11,9 @@
 // positions, lists, codes, four steps per wave, the join's three loads in turn).  32
 // blocks for each of 509 tokens: 123 us; the vector ALU is busy two thirds of it, the
 // matrix cores a third, and of the 290 cycles that a step takes a compute unit, writing 32
-// decoded value rows to LDS costs 128 (64 bytes each) and reading them transposed 53.
+// decoded value rows to LDS costs 128 (64 bytes each) and reading them transposed 53.  Trees of 9
+// drafts behind up to 1000 rows, 2 sequences, 16 heads over 4, d = 64, float32: 8.3 us, one launch's
+// chain of positions, codes, products, sums.
 #include "q4_attn_device.hpp"
 
 namespace thin {

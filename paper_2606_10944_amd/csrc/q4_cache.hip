@@ -205,6 +205,11 @@ __global__ __launch_bounds__(THREADS) void q4_load_kernel(Q4View c, const int32_
 // these rows forms them.  A workgroup takes the keys or the values of a slice.  The rows pass
 // through LDS whole before the first is written, so a path may name rows in any order, and rows
 // that it also writes.
+//
+// 8 x 8 slices, 7 of 64 drafts kept, d = 128: 4.8 us, a chain of the path, its rows and the
+// block's older rows.  64 x 8 slices, 500 of 1024: 22 us for 70 MB (3.2 TB/s; 28 with one workgroup
+// for keys and values); a workgroup's rows all wait for the path, and its blocks' bounds are formed
+// in turn.
 // ---------------------------------------------------------------------------
 template <int D, int CAP>
 __global__ __launch_bounds__(THREADS) void q4_keep_kernel(Q4View c, const int32_t* at_,
@@ -283,6 +288,9 @@ __global__ __launch_bounds__(THREADS) void q4_keep_kernel(Q4View c, const int32_
 // words of 64 drafts.  A wave closes a word over itself by jumping from ancestor to ancestor's
 // ancestor, six times at most, and finds every draft's first ancestor below the word; then a
 // draft takes one such step per word.  A workgroup takes 256 drafts of a sequence.
+//
+// 8 trees of 64: 2.9 us, a launch and two chains of loads; 64 of 1024: 7.2 us for 8.9 MB, six jumps
+// through LDS and up to sixteen steps up the words.
 // ---------------------------------------------------------------------------
 constexpr int kTreeWords = kQ4MaxDrafts / 64;
 

@@ -13,7 +13,8 @@
 //
 // Bound by HBM: 16384 tokens x 40 heads x 128 channels, bf16, 62 us = 5.4 TB/s read and
 // written (a large copy runs at 5.1); one token of 16 sequences, 40 heads: 3.8 us, a
-// launch and the latency of positions, sines and rows.
+// launch and the latency of positions, sines and rows.  With three axes 61.7 us (63 per call); 2047
+// tokens x 3 x 24 heads, float32, two axes, turned back, 14.0 us.
 #include "common.hpp"
 #include "q4.hpp"
 
