@@ -270,11 +270,13 @@ int thin_attention_ex(const void* Q, const void* K, const void* V, int32_t dtype
  *           aligned; contents on entry are irrelevant.  Calls that may run at the same time need
  *           workspaces of their own.
  * A key of log-weight -inf is not there, whatever its rows hold (its gradients are 0), nor is an
- * entry of idx outside [0, n); a query without any key has a gradient of 0 and gives none.
+ * entry of idx outside [0, n); a query without any key has a gradient of 0 and gives none
+ * (Q and dO are finite in this: infinities and NaN there go through every key's sums).
  * Outputs overlap no input and no other output.  Rows are 16-byte aligned.  Sums are in float32,
  * in an order that depends on the sizes only: the same call gives the same bits.  bf16 rows:
  * p and ds round to bf16 before the products with rows (not before dlogw's sum).
- * B*H*n_q <= 2^29, B*H*n_out <= 2^25.
+ * B*H*n_q <= 2^29, B*H*n_out <= 2^25, n_out <= 2^18 (every place of the list is compared with
+ * every other).
  * Errors: THIN_EINVAL, THIN_EDTYPE, THIN_EWORKSPACE, THIN_EHIP.
  */
 int thin_attention_backward_plan(int32_t dtype, int64_t B, int64_t H, int64_t n_q, int64_t n,
@@ -613,7 +615,7 @@ int thin_q4_attention(const thin_q4_cache_t* cache, const void* Q, const int64_t
  *   seen    (device) uint64 [B, T, words]: the draft itself and its ancestors; bits from T on
  *           are 0.
  *   pos     (device) int32 [B, T]: at[b] + the draft's depth (roots: 0).
- * B <= 65535.  Errors: THIN_EINVAL, THIN_EHIP.
+ * seen and pos overlap neither an input nor each other.  B <= 65535.  Errors: THIN_EINVAL, THIN_EHIP.
  */
 int thin_q4_tree(const int32_t* parents, const int32_t* at, int64_t B, int64_t T, uint64_t* seen,
                  int32_t* pos, void* stream);

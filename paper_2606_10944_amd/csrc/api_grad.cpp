@@ -14,6 +14,8 @@ constexpr int64_t kMaxSlices = 65535;
 // runtime counts in 32 bits.
 constexpr int64_t kMaxQueries = (int64_t)1 << 29;
 constexpr int64_t kMaxKeys = (int64_t)1 << 25;
+// Places of a slice's list: the join compares every one with every other (0.1 s at a million).
+constexpr int64_t kMaxList = (int64_t)1 << 18;
 constexpr int64_t kMaxRows = (int64_t)1 << 30;
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
@@ -24,7 +26,7 @@ bool known_dtype(int32_t t) { return t == THIN_FP32 || t == THIN_BF16; }
 bool valid_sizes(int64_t B, int64_t H, int64_t n_q, int64_t n, int64_t d, int64_t n_out) {
   if (B < 1 || H < 1 || B > kMaxSlices || H > kMaxSlices || B * H > kMaxSlices) return false;
   if (d != 32 && d != 64 && d != 128) return false;
-  if (n < 1 || n > kMaxRows || n_q < 1 || n_q > kMaxQueries || n_out < 1 || n_out > kMaxKeys)
+  if (n < 1 || n > kMaxRows || n_q < 1 || n_q > kMaxQueries || n_out < 1 || n_out > kMaxList)
     return false;
   return B * H * n_q <= kMaxQueries && B * H * n_out <= kMaxKeys;
 }

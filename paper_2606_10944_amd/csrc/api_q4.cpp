@@ -362,6 +362,9 @@ int thin_q4_tree(const int32_t* parents, const int32_t* at, int64_t B, int64_t T
   if (!valid_ints(parents, nullptr) || !valid_ints(at, nullptr) || !seen || !aligned(seen, 8) ||
       !valid_ints(pos, nullptr))
     return THIN_EINVAL;
+  const void* masks = seen;
+  if (masks == parents || masks == at || masks == pos || pos == parents || pos == at)
+    return THIN_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = observed(THIN_KERNEL_Q4_TREE, -1, st, [&] {
     return thin::launch_q4_tree(parents, at, B, T, seen, pos, st);

@@ -309,6 +309,8 @@ class Q4Cache:
             if parents is None or parents.shape != (B, T):
                 raise ThinError(THIN_EINVAL, "parents must be int32 [B,T]")
             tree = thin_q4_tree(parents, at, stream=stream)
+        if K.dim() != 4 or K.shape[2] != T:
+            raise ThinError(THIN_EINVAL, "K and V must have a row for every draft")
         seen = tree[0]
         _masks(seen, B, T, _where(stream)[0])
         if turns is not None:

@@ -33,7 +33,7 @@ def call(**kw):
     (dict(dK=C.c_void_p(0x100000)), EINVAL), (dict(dtype=2), EDTYPE), (dict(out_dtype=-1), EDTYPE),
     (dict(d=96), EINVAL), (dict(B=0), EINVAL), (dict(B=300, H=300), EINVAL), (dict(n_q=0), EINVAL),
     (dict(n=0), EINVAL), (dict(n_out=0), EINVAL), (dict(n_q=(1 << 29) // 6 + 1), EINVAL),
-    (dict(n_out=(1 << 25) // 6 + 1), EINVAL), (dict(n=(1 << 30) + 1), EINVAL),
+    (dict(n_out=(1 << 18) + 1), EINVAL), (dict(B=16, H=16, n_out=1 << 18), EINVAL), (dict(n=(1 << 30) + 1), EINVAL),
     (dict(B=1 << 62, H=4), EINVAL), (dict(ws=None), EWORKSPACE), (dict(ws=ODD), EWORKSPACE),
     (dict(wn=100), EWORKSPACE)])
 def test_refusals(kw, want):
@@ -48,7 +48,7 @@ def test_plan():
     assert plan(1, 2, 3, 100, 50, 64, 20, None) == EINVAL
     assert plan(5, 2, 3, 100, 50, 64, 20, C.byref(n)) == EDTYPE
     assert plan(1, 2, 3, 100, 50, 96, 20, C.byref(n)) == EINVAL
-    assert plan(1, 1, 1, 1 << 29, 1 << 30, 128, 1 << 25, C.byref(n)) == 0
+    assert plan(1, 1, 1, 1 << 29, 1 << 30, 128, 1 << 18, C.byref(n)) == 0
 
 
 PROBE = r"""

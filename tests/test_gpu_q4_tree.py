@@ -511,6 +511,8 @@ def test_binding_refuses_what_does_not_fit():
     refused(THIN_EINVAL, c.draft, q, kv, kv, at, parents, pos=pos)
     refused(THIN_EINVAL, c.draft, q, kv, kv, at, parents, turns=turns, pos=pos[:, :3])
     refused(THIN_EINVAL, c.draft, q, kv[:, :1], kv, at, parents)
+    refused(THIN_EINVAL, c.draft, q, kv[:, :, :3], kv[:, :, :3], at, parents)
+    refused(THIN_EINVAL, thin_q4_tree, parents, at, pos=parents)
     refused(THIN_EINVAL, c.draft, q, kv, kv, at, parents, O=q[:, :2])
     p3 = i32([[[0, 0, 0]] * T] * B)
     for bad in (pos, p3[:, :2], p3.long(), torch.cat([p3, p3], 2)):

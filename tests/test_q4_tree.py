@@ -32,14 +32,15 @@ def test_rotary_axes_refusals(kw, want):
 
 
 def tree(**kw):
-    a = dict(parents=FAKE, at=FAKE, B=2, T=10, seen=FAKE, pos=FAKE)
+    a = dict(parents=FAKE, at=FAKE, B=2, T=10, seen=C.c_void_p(0x20000), pos=C.c_void_p(0x30000))
     a.update(kw)
     return _lib.lib().thin_q4_tree(*a.values(), None)
 
 
 @pytest.mark.parametrize("kw", [
     dict(parents=None), dict(parents=BYTE), dict(at=None), dict(B=0), dict(B=65536), dict(T=0),
-    dict(T=1025), dict(seen=None), dict(seen=FOUR), dict(pos=None), dict(pos=BYTE)])
+    dict(T=1025), dict(seen=None), dict(seen=FOUR), dict(pos=None), dict(pos=BYTE), dict(seen=FAKE),
+    dict(pos=FAKE), dict(at=C.c_void_p(0x30000)), dict(pos=C.c_void_p(0x20000))])
 def test_tree_refusals(kw):
     assert tree(**kw) == EINVAL
 
