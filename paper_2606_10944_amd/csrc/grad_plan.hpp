@@ -36,6 +36,8 @@ constexpr int64_t grad_most_keys(bool bf16) { return bf16 ? 256 : 128; }
 // d = 128, 64 slices of 16384 queries: 128 keys 8x1 354, 4x2 500; 192 keys 12x1 495, 8x2 548, 4x3
 // 504; 256 keys 8x2 548, 16x1 910, 4x4 855.  float32 rows, 64 slices of 4096 queries over 128
 // keys: d = 32 8x1 135, 4x2 118; d = 64 8x1 215, 4x2 232.
+// Chunks, d = 128: 8 slices of 2048 queries over 1024 keys 8x1 96, 12x1 96, 8x2 121; 32 of 8192 over
+// 512 478, 497, 627; 16 of 4096 over 600 170, 164, 245.
 // exact: bf16 rows with all of a float32 dO's three parts, for which the local memory has no room
 // beside over 192 keys of 128 channels.
 inline GradShape grad_shape(int64_t S, int64_t n_q, int64_t n_out, int64_t d, bool bf16,
