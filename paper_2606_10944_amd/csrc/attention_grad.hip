@@ -54,6 +54,23 @@ constexpr int kUnit = Elem<T>::bytes == 2 ? 32 : 16;
 constexpr float kLeast = -3.0e38f;
 constexpr double kLog2e = 1.44269504088896340736;
 
+// Scores of bf16 rows are to base 2.  Those of float32 rows are not: a score of 10 would round by
+// as much again once more, where its distance from the maximum, which a weight goes by, is small.
+template <typename T>
+constexpr float kUnitScore = Elem<T>::bytes == 2 ? (float)kLog2e : 1.0f;
+template <typename T>
+__device__ __forceinline__ float weight(float x) {
+  return __builtin_amdgcn_exp2f(Elem<T>::bytes == 2 ? x : x * (float)kLog2e);
+}
+// The score of a product x.  (float32 rows: the scale's rounding would move every score alike.)
+template <typename T, int D>
+__device__ __forceinline__ float score(float x, float bias) {
+  const double c = (Elem<T>::bytes == 2 ? kLog2e : 1.0) / sqrt((double)D);
+  if constexpr (Elem<T>::bytes == 4 && D != 64)
+    bias = fmaf(x, (float)(c - (double)(float)c), bias);
+  return fmaf(x, (float)c, bias);
+}
+
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
@@ -237,15 +254,16 @@ __device__ __forceinline__ void store4(T* p, floatx4_t o) {
   Four<T>(o).store(p);
 }
 
-// Coreset row j of slice s: its row of K and V (-1: none, or its weight is 0) and log-weight to
-// base 2.
+// Coreset row j of slice s: its row of K and V (-1: none, or its weight is 0) and log-weight as
+// scores are.
+template <typename T>
 __device__ __forceinline__ int coreset_row(const GradArgs& a, int64_t s, int64_t j, float* bias) {
   *bias = -INFINITY;
   if (j >= a.n_out) return -1;
   const int32_t r = a.idx[s * a.n_out + j];
   const float lw = a.logw ? a.logw[s * a.n_out + j] : 0.0f;
   if (r < 0 || r >= a.n || lw == -INFINITY) return -1;
-  *bias = lw * (float)kLog2e;
+  *bias = lw * kUnitScore<T>;
   return r;
 }
 
@@ -328,14 +346,13 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
       ro[i].load(o, i * 64 * W + threadIdx.x);
     }
   };
-  // without ONE, the next step's statistics.  (Rows past the last have a dO of 0, and so a g, a
-  // sum p g and a ds of 0 whatever their maximum.)
-  uint32_t next[2][TQ];
+  // without ONE, the next step's statistics: maximum, 1 / sum (0 past the last row), sum p g
+  uint32_t next[3][TQ];
   auto statistics = [&](int64_t t) __attribute__((always_inline)) {
     const int rows = t < t1 ? (int)std::min<int64_t>(QT, a.n_q - t * QT) : 0;
     const int64_t at = s * a.n_q + (rows > 0 ? t * QT : 0);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < 3; ++k) {
       const Span x(a.stats + k * a.S * a.n_q + at, rows * 4);
 #pragma unroll
       for (int tq = 0; tq < TQ; ++tq) next[k][tq] = x.load4((16 * tq + m) * 4);
@@ -359,7 +376,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
 
   // the rows of the workgroup's keys, then this wave's
   for (int j = threadIdx.x; j < NK; j += 64 * W)
-    rows_[j] = coreset_row(a, s, (int64_t)chunk * NK + j, &bias_[j]);
+    rows_[j] = coreset_row<T>(a, s, (int64_t)chunk * NK + j, &bias_[j]);
   __syncthreads();
   uint4 kf[KL ? 1 : KT][NV], vf[KT][NV];
   float bias[KT][4];
@@ -421,7 +438,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) ak[kt][dt] = av[kt][dt] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
   }
-  const float c2 = (float)(kLog2e / sqrt((double)D)), rd = (float)(1.0 / sqrt((double)D));
+  const float rd = (float)(1.0 / sqrt((double)D));
 
   // this workgroup's share of the zeros of dK and dV, in 16-byte words: as many in a step as the
   // step's queries have, the rest of them behind the last step
@@ -513,7 +530,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
 #pragma unroll
     for (int i = 0; i < 4 * TQ * KT; ++i) {
       const int kt = i / (4 * TQ), tq = i / 4 % TQ, j = i % 4;
-      p[kt][tq][j] = fmaf(x[kt][tq][j], c2, bias[kt][j]);
+      p[kt][tq][j] = score<T, D>(x[kt][tq][j], bias[kt][j]);
       gd[kt][tq][j] = y[kt][tq][j];
     }
   };
@@ -531,7 +548,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
 #pragma unroll
       for (int i = 0; i < 4 * KT; ++i) {
         float& w = p[i / 4][tq][i % 4];
-        w = __builtin_amdgcn_exp2f(w - x);
+        w = weight<T>(w - x);
         l += w;
         e = fmaf(w, gd[i / 4][tq][i % 4], e);
       }
@@ -555,13 +572,13 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
       for (int w = 0; w < W; ++w) mx = fmaxf(mx, st[w][0][m]);
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        const float k = __builtin_amdgcn_exp2f(st[w][0][m] - mx);
+        const float k = weight<T>(st[w][0][m] - mx);
         l = fmaf(st[w][1][m], k, l);
         e = fmaf(st[w][2][m], k, e);
       }
       const float inv = l > 0.0f ? 1.0f / l : 0.0f;
       dm[0] = e * inv;
-      f[0] = __builtin_amdgcn_exp2f(top[0] - mx) * inv;
+      f[0] = weight<T>(top[0] - mx) * inv;
     } else {
       const int r = lane & 31, h = lane / 32;
       float x[W / 2], mx = kLeast, l = 0.0f, e = 0.0f;
@@ -578,7 +595,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
       mx = halves(mx, larger);
   #pragma unroll
       for (int w = 0; w < W / 2; ++w) {
-        const float k = __builtin_amdgcn_exp2f(x[w] - mx);
+        const float k = weight<T>(x[w] - mx);
         l = fmaf(st[2 * w + h][1][r], k, l);
         e = fmaf(st[2 * w + h][2][r], k, e);
       }
@@ -589,8 +606,8 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
       trade(false, dm[0], dm[1]);
       trade(false, inv, i1);
       trade(false, mx, m1);
-      f[0] = __builtin_amdgcn_exp2f(top[0] - mx) * inv;
-      f[1] = __builtin_amdgcn_exp2f(top[1] - m1) * i1;
+      f[0] = weight<T>(top[0] - mx) * inv;
+      f[1] = weight<T>(top[1] - m1) * i1;
     }
   };
   // dK and dV of a step: p times f, ds in place of g, both through LDS by columns, in one place
@@ -605,7 +622,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
 #pragma unroll
     for (int i = 0; i < 4 * TQ * KT; ++i) {
       const int kt = i / (4 * TQ), tq = i / 4 % TQ, j = i % 4;
-      if (ONE) p[kt][tq][j] *= f[tq];
+      p[kt][tq][j] *= f[tq];
       gd[kt][tq][j] = p[kt][tq][j] * (gd[kt][tq][j] - dm[tq]);
     }
     if (a.part_w) {
@@ -674,12 +691,13 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
     } else {
 #pragma unroll
       for (int tq = 0; tq < TQ; ++tq) {
-        const float lse = __uint_as_float(next[0][tq]);
-        f[tq] = 1.0f;
-        dm[tq] = __uint_as_float(next[1][tq]);
+        f[tq] = __uint_as_float(next[1][tq]);
+        dm[tq] = __uint_as_float(next[2][tq]);
+        // (a row past the last has scores of the log-weights alone, under no maximum)
+        const float mx = f[tq] > 0.0f ? __uint_as_float(next[0][tq]) : INFINITY;
 #pragma unroll
         for (int i = 0; i < 4 * KT; ++i)
-          p[i / 4][tq][i % 4] = __builtin_amdgcn_exp2f(p[i / 4][tq][i % 4] - lse);
+          p[i / 4][tq][i % 4] = weight<T>(p[i / 4][tq][i % 4] - mx);
       }
       statistics(t + 1);
     }
@@ -768,7 +786,7 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
     for (int i = 0; i < IT; ++i) {
       const float w = a.logw ? lw[i] : 0.0f;
       const bool is = place(k0, i) < a.n_out && at[i] >= 0 && at[i] < a.n && w != -INFINITY;
-      bias[i] = is ? w * (float)kLog2e : -INFINITY;
+      bias[i] = is ? w * kUnitScore<T> : -INFINITY;
       const int64_t word = (int64_t)(is ? at[i] : 0) * R::CW + threadIdx.x % R::CW;
       kw[i] = reinterpret_cast<const u32x4*>(K)[word];
       vw[i] = reinterpret_cast<const u32x4*>(V)[word];
@@ -809,7 +827,7 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
 #pragma unroll
     for (int p = 0; p < OP; ++p) of[p][v] = __builtin_bit_cast(uint4, x[p]);
   }
-  const float c2 = (float)(kLog2e / sqrt((double)D)), rd = (float)(1.0 / sqrt((double)D));
+  const float rd = (float)(1.0 / sqrt((double)D));
   // all parts of dO for the statistics, from which dlogw is; two for dQ, which rounds to bf16
   auto products = [&](int buf, auto parts, float (&p)[KT][4], float (&gd)[KT][4])
                       __attribute__((always_inline)) {
@@ -826,7 +844,7 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        p[kt][j] = fmaf(x[j], c2, sb[buf][16 * (sub * KT + kt) + 4 * g + j]);
+        p[kt][j] = score<T, D>(x[j], sb[buf][16 * (sub * KT + kt) + 4 * g + j]);
         gd[kt][j] = y[j];
       }
     }
@@ -851,13 +869,13 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
       float x = mx;
 #pragma unroll
       for (int j = 0; j < 4 * KT; ++j) x = fmaxf(x, p[j / 4][j % 4]);
-      const float k = __builtin_amdgcn_exp2f(mx - x);
+      const float k = weight<T>(mx - x);
       mx = x;
       l *= k;
       e *= k;
 #pragma unroll
       for (int j = 0; j < 4 * KT; ++j) {
-        const float w = __builtin_amdgcn_exp2f(p[j / 4][j % 4] - mx);
+        const float w = weight<T>(p[j / 4][j % 4] - mx);
         l += w;
         e = fmaf(w, gd[j / 4][j % 4], e);
       }
@@ -866,7 +884,7 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   }
   auto add = [](float x, float y) { return x + y; };
   float top = across_rows(mx, true, [](float x, float y) { return fmaxf(x, y); });
-  const float k = __builtin_amdgcn_exp2f(mx - top);
+  const float k = weight<T>(mx - top);
   l = across_rows(l * k, true, add);
   e = across_rows(e * k, true, add);
   if constexpr (SH > 1) {
@@ -882,17 +900,17 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
     l = e = 0.0f;
 #pragma unroll
     for (int w = 0; w < SH; ++w) {
-      const float k = __builtin_amdgcn_exp2f(st[w0 + w][0][m] - top);
+      const float k = weight<T>(st[w0 + w][0][m] - top);
       l = fmaf(st[w0 + w][1][m], k, l);
       e = fmaf(st[w0 + w][2][m], k, e);
     }
   }
-  // a row that no key weighs in: probabilities of 0
-  const float lse = l > 0.0f ? top + __builtin_amdgcn_logf(l) : INFINITY;
-  const float dm = l > 0.0f ? e / l : 0.0f;
+  // (a row that no key weighs in: probabilities of 0)
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f, dm = e * inv;
   if (there && g == 0 && sub == 0) {
-    a.stats[s * a.n_q + r] = lse;
-    a.stats[(a.S + s) * a.n_q + r] = dm;
+    a.stats[s * a.n_q + r] = top;
+    a.stats[(a.S + s) * a.n_q + r] = inv;
+    a.stats[(2 * a.S + s) * a.n_q + r] = dm;
   }
   floatx4_t acc[DT];
 #pragma unroll
@@ -905,7 +923,7 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
 #pragma unroll
       for (int j = 0; j < 4 * KT; ++j)
         p[j / 4][j % 4] =
-            __builtin_amdgcn_exp2f(p[j / 4][j % 4] - lse) * (gd[j / 4][j % 4] - dm);
+            weight<T>(p[j / 4][j % 4] - top) * inv * (gd[j / 4][j % 4] - dm);
 #pragma unroll
       for (int h = 0; h < 16 * KT / kUnit<T>; ++h) {
         const Column<T> w(p + h * (kUnit<T> / 16));

@@ -20,7 +20,7 @@ struct GradArgs {
   bool zeros;     // the zeros of dK and dV come from a launch of their own
   float* part;    // [S, chunks, parts, keys, 2, d]: sums of dK and dV
   float* part_w;  // [S, chunks, parts, keys]: of dlogw (null without)
-  float* stats;   // [2, S, n_q] where a row's statistics need a pass of their own
+  float* stats;   // [3, S, n_q] where a row's statistics need a pass of their own
 };
 // dtype of Q, K, V and the gradients; out_dtype of dO.
 hipError_t launch_grad_zeros(int64_t row_bytes, const GradArgs& a, hipStream_t st);

@@ -97,7 +97,7 @@ inline GradBytes grad_bytes(const GradShape& s, int64_t S, int64_t n_q, int64_t 
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   const size_t slots = (size_t)(S * s.chunks * s.parts * s.keys());
   return {up(slots * 2 * (size_t)d * 4), weights ? up(slots * 4) : 0,
-          s.one ? 0 : up((size_t)(S * n_q) * 8)};
+          s.one ? 0 : up((size_t)(S * n_q) * 12)};
 }
 
 }  // namespace thin

@@ -95,6 +95,17 @@ def test_waves_that_share_query_rows(B, H, n_q, n, n_out, d, dtype, out):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("n_out", [40, 300])
+def test_large_log_weights(n_out, dtype):
+    """Weights whose exponential float32 does not hold, and rows of a step that are not there."""
+    g = gen(218)
+    args = inputs(g, 1, 2, 45, 400, n_out, 64, dtype, dtype, weighted=True)
+    args[4][..., 2::5] += 200.0
+    args[4][..., 3::5] -= 200.0
+    check(args, backward(*args))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("B,H,n_q,n,n_out,d", [
     (1, 1, 3, 9001, 40, 128), (2, 3, 1, 16385, 1, 32), (1, 2, 7, 8003, 300, 64),
     (1, 5, 300, 9999, 130, 128)])
