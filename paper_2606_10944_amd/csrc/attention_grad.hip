@@ -56,6 +56,7 @@ constexpr double kLog2e = 1.44269504088896340736;
 
 // Scores of bf16 rows are to base 2.  Those of float32 rows are not: a score of 10 would round by
 // as much again once more, where its distance from the maximum, which a weight goes by, is small.
+// (64 slices of 4096 queries over 128 keys of 64 channels 219 -> 235 us for it.)
 template <typename T>
 constexpr float kUnitScore = Elem<T>::bytes == 2 ? (float)kLog2e : 1.0f;
 template <typename T>
@@ -504,10 +505,23 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
       x[i / TQ][i % TQ] = y[i / TQ][i % TQ] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
     // (a word of the keys serves both tiles, or, where registers are short, one after the other)
     constexpr int QS = TIGHT ? 1 : TQ;
+    // float32 rows' sums over many channels, or of many keys, in two halves: errors of a gradient
+    // over 532 keys of 128 channels 1.5e-6 -> 7e-7 (128 keys of 64 in one workgroup gain little
+    // and would take 239 us for 235)
+    constexpr bool HALVES = Elem<T>::bytes == 4 && QS == TQ && (!ONE || D == 128);
+    floatx4_t x0[KT][TQ], y0[KT][TQ];
 #pragma unroll
     for (int q0 = 0; q0 < TQ; q0 += QS)
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
+        if (HALVES && v == NV / 2) {
+#pragma unroll
+          for (int i = 0; i < TQ * KT; ++i) {
+            x0[i / TQ][i % TQ] = x[i / TQ][i % TQ];
+            y0[i / TQ][i % TQ] = y[i / TQ][i % TQ];
+            x[i / TQ][i % TQ] = y[i / TQ][i % TQ] = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+          }
+        }
         uint4 kw[KT];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
@@ -530,6 +544,10 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
 #pragma unroll
     for (int i = 0; i < 4 * TQ * KT; ++i) {
       const int kt = i / (4 * TQ), tq = i / 4 % TQ, j = i % 4;
+      if (HALVES) {
+        x[kt][tq][j] += x0[kt][tq][j];
+        y[kt][tq][j] += y0[kt][tq][j];
+      }
       p[kt][tq][j] = score<T, D>(x[kt][tq][j], bias[kt][j]);
       gd[kt][tq][j] = y[kt][tq][j];
     }
@@ -749,6 +767,7 @@ template <typename T, typename TO, int D, int SH>
 __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
   using R = LdsRows<T, D>;
   constexpr int NV = Frag<T, D>::NV, DT = D / 16, OP = Parts<T, TO>::n;
+  constexpr bool HALVES = Elem<T>::bytes == 4;  // (as above)
   // a wave's tiles of a step's keys, and these
   constexpr int KT = std::max(4 / SH, kUnit<T> / 16), CK = 16 * KT * SH;
   constexpr int IT = (CK * R::CW + 64 * RW - 1) / (64 * RW);  // words of a step per thread
@@ -833,14 +852,23 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
                       __attribute__((always_inline)) {
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      floatx4_t x = {0.f, 0.f, 0.f, 0.f}, y = x;
+      floatx4_t x = {0.f, 0.f, 0.f, 0.f}, y = x, x0 = x, y0 = x;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
+        if (HALVES && v == NV / 2) {
+          x0 = x;
+          y0 = y;
+          x = y = (floatx4_t){0.f, 0.f, 0.f, 0.f};
+        }
         const int at = 16 * (sub * KT + kt) * R::stride;
         x = mma_word<T>(lds_word<T, D>(sk[buf] + at, v, m, g), qf[v], x);
         const uint4 vw = lds_word<T, D>(sv[buf] + at, v, m, g);
 #pragma unroll
         for (int o = decltype(parts)::value - 1; o >= 0; --o) y = mma_word<T>(vw, of[o][v], y);
+      }
+      if (HALVES) {
+        x += x0;
+        y += y0;
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {

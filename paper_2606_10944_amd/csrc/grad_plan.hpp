@@ -35,7 +35,7 @@ constexpr int64_t grad_most_keys(bool bf16) { return bf16 ? 256 : 128; }
 //   d = 64, 64 keys 4x1 86.0, 2x2 89.9; 128 keys 8x1 141, 4x2 116, 2x4 318; 256 8x2 191, 4x4 330
 // d = 128, 64 slices of 16384 queries: 128 keys 8x1 354, 4x2 500; 192 keys 12x1 495, 8x2 548, 4x3
 // 504; 256 keys 8x2 548, 16x1 910, 4x4 855.  float32 rows, 64 slices of 4096 queries over 128
-// keys: d = 32 8x1 135, 4x2 118; d = 64 8x1 215, 4x2 232.
+// keys: d = 32 8x1 135, 4x2 118; d = 64 8x1 215, 4x2 232 (with scores to base 2).
 // Chunks, d = 128: 8 slices of 2048 queries over 1024 keys 8x1 96, 12x1 96, 8x2 121; 32 of 8192 over
 // 512 478, 497, 627; 16 of 4096 over 600 170, 164, 245.
 // exact: bf16 rows with all of a float32 dO's three parts, for which the local memory has no room
