@@ -269,9 +269,10 @@ int thin_attention_ex(const void* Q, const void* K, const void* V, int32_t dtype
  *   workspace (device) at least *workspace_bytes of thin_attention_backward_plan, 256-byte
  *           aligned; contents on entry are irrelevant.  Calls that may run at the same time need
  *           workspaces of their own.
- * A key of log-weight -inf is not there, whatever its rows hold (its gradients are 0), nor is an
- * entry of idx outside [0, n); a query without any key has a gradient of 0 and gives none
- * (Q and dO are finite in this: infinities and NaN there go through every key's sums).
+ * An entry of idx outside [0, n) is clamped to the nearest row, as in the forward: that row listed
+ * once more.  A key of log-weight -inf is not there, whatever its rows hold (its gradients are 0);
+ * a query without any key has a gradient of 0 and gives none (Q and dO are finite in this:
+ * infinities and NaN there go through every key's sums).
  * Outputs overlap no input and no other output.  Rows are 16-byte aligned.  Sums are in float32,
  * in an order that depends on the sizes only: the same call gives the same bits.  bf16 rows:
  * p and ds round to bf16 before the products with rows (not before dlogw's sum).

@@ -255,17 +255,21 @@ __device__ __forceinline__ void store4(T* p, floatx4_t o) {
   Four<T>(o).store(p);
 }
 
+// The row that an entry of the list stands for, as in the forward: the nearest one.
+__device__ __forceinline__ int32_t nearest_row(int32_t r, int64_t n) {
+  return (int32_t)std::min<int64_t>(std::max(r, 0), n - 1);
+}
+
 // Coreset row j of slice s: its row of K and V (-1: none, or its weight is 0) and log-weight as
 // scores are.
 template <typename T>
 __device__ __forceinline__ int coreset_row(const GradArgs& a, int64_t s, int64_t j, float* bias) {
   *bias = -INFINITY;
   if (j >= a.n_out) return -1;
-  const int32_t r = a.idx[s * a.n_out + j];
   const float lw = a.logw ? a.logw[s * a.n_out + j] : 0.0f;
-  if (r < 0 || r >= a.n || lw == -INFINITY) return -1;
+  if (lw == -INFINITY) return -1;
   *bias = lw * kUnitScore<T>;
-  return r;
+  return nearest_row(a.idx[s * a.n_out + j], a.n);
 }
 
 // ---------------------------------------------------------------------------
@@ -804,9 +808,9 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
       const float w = a.logw ? lw[i] : 0.0f;
-      const bool is = place(k0, i) < a.n_out && at[i] >= 0 && at[i] < a.n && w != -INFINITY;
+      const bool is = place(k0, i) < a.n_out && w != -INFINITY;
       bias[i] = is ? w * kUnitScore<T> : -INFINITY;
-      const int64_t word = (int64_t)(is ? at[i] : 0) * R::CW + threadIdx.x % R::CW;
+      const int64_t word = (int64_t)nearest_row(at[i], a.n) * R::CW + threadIdx.x % R::CW;
       kw[i] = reinterpret_cast<const u32x4*>(K)[word];
       vw[i] = reinterpret_cast<const u32x4*>(V)[word];
     }
@@ -987,8 +991,9 @@ __global__ __launch_bounds__(64 * RW) void grad_rows_kernel(GradArgs a) {
 // ---------------------------------------------------------------------------
 // Join: a wave adds the sums of one coreset row in the order of the queries and writes its row
 // of dK and dV; where there are many parts, four waves share them (64 parts of 32 rows: 8.2 us
-// with one).  A row that the coreset lists more than once is written by its first place, with
-// the sums of all of them.
+// with one).  A row that the coreset lists more than once is written by the first place whose
+// key is there, with the sums of all of them; a row whose keys are not there keeps its zeros, so
+// that a list's padding (one row, listed by every place of it) is no chain of sums.
 // ---------------------------------------------------------------------------
 template <typename T, int D, int PER>
 __global__ __launch_bounds__(256) void grad_join_kernel(GradArgs a) {
@@ -1009,8 +1014,9 @@ __global__ __launch_bounds__(256) void grad_join_kernel(GradArgs a) {
     for (int i = 32; i > 0; i /= 2) x += __shfl_xor(x, i);
     if (lane == 0) a.dlogw[w] = x;
   }
-  const int32_t r = idx[j];
-  if (r < 0 || r >= a.n) return;
+  const float* logw = a.logw ? a.logw + s * a.n_out : nullptr;
+  const int32_t r = nearest_row(idx[j], a.n);
+  if (logw && logw[j] == -INFINITY) return;
   constexpr int V = 2 * D / 4;  // lanes of a row of sums, four channels each
   floatx4_t o = {0.f, 0.f, 0.f, 0.f};
   constexpr int BATCH = 8;  // places of the list per lane at a time
@@ -1019,11 +1025,15 @@ __global__ __launch_bounds__(256) void grad_join_kernel(GradArgs a) {
 #pragma unroll
     for (int x = 0; x < BATCH; ++x) {
       const int64_t i = i0 + x * 64 + lane;
-      at[x] = idx[i < a.n_out ? i : a.n_out - 1];
+      at[x] = nearest_row(idx[i < a.n_out ? i : a.n_out - 1], a.n);
     }
 #pragma unroll
     for (int x = 0; x < BATCH; ++x) {
-      uint64_t same = __ballot(at[x] == r && i0 + x * 64 + lane < a.n_out);
+      const int64_t place = i0 + x * 64 + lane;
+      uint64_t same = __ballot(at[x] == r && place < a.n_out);
+      // (the weights of other places alone: 1024 keys' join 4 us longer with all of them)
+      if (logw && __ballot(at[x] == r && place < a.n_out && place != j))
+        same &= __ballot(logw[std::min(place, a.n_out - 1)] != -INFINITY);
       while (same) {
         const int64_t i = i0 + x * 64 + __ffsll((unsigned long long)same) - 1;
         same &= same - 1;

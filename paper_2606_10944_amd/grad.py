@@ -41,8 +41,9 @@ def thin_attention_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, i
                             workspace: Optional[torch.Tensor] = None, stream=None):
     """The gradients (dQ, dK, dV) of thin_attention(Q, K, V, idx, logw=logw) from dO, that of its
     output (float32 or bf16), with dlogw float32 [B,H,n_out] behind them when need_logw=True (or
-    dlogw is given).  dK and dV are [B,H,n,d], zeros in the rows that idx does not list.  The
-    forward's output is not needed."""
+    dlogw is given).  dK and dV are [B,H,n,d], zeros in the rows that idx does not list (entries
+    outside [0, n) list the nearest row, as in the forward).  The forward's output is not
+    needed."""
     dev, st = _where(stream)
     q, k, v, do = (_rows4(Q, dev, "Q"), _rows4(K, dev, "K"), _rows4(V, dev, "V"),
                    _rows4(dO, dev, "dO"))
