@@ -41,9 +41,9 @@ def thin_attention_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, i
                             workspace: Optional[torch.Tensor] = None, stream=None):
     """The gradients (dQ, dK, dV) of thin_attention(Q, K, V, idx, logw=logw) from dO, that of its
     output (float32 or bf16), with dlogw float32 [B,H,n_out] behind them when need_logw=True (or
-    dlogw is given).  dK and dV are [B,H,n,d], zeros in the rows that idx does not list (entries
-    outside [0, n) list the nearest row, as in the forward).  The forward's output is not
-    needed."""
+    dlogw is given).  Rows are contiguous and 16-byte aligned.  dK and dV are [B,H,n,d], zeros in
+    the rows that idx does not list (entries outside [0, n) list the nearest row, as in the
+    forward).  The forward's output is not needed."""
     dev, st = _where(stream)
     q, k, v, do = (_rows4(Q, dev, "Q"), _rows4(K, dev, "K"), _rows4(V, dev, "V"),
                    _rows4(dO, dev, "dO"))
@@ -90,6 +90,13 @@ def thin_attention_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, i
     return (dQ, dK, dV) if dw is None else (dQ, dK, dV, dlogw)
 
 
+def _laid_out(t: torch.Tensor) -> torch.Tensor:
+    """t, or a copy of it whose rows are contiguous and 16-byte aligned (a view into a flat buffer,
+    or the gradient of a concatenation, may begin anywhere)."""
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
 class _CoresetAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, Q, K, V, idx, logw, out_dtype):
@@ -102,7 +109,7 @@ class _CoresetAttention(torch.autograd.Function):
         Q, K, V, idx, logw = ctx.saved_tensors
         need_logw = ctx.needs_input_grad[4]
         with torch.cuda.device(Q.device):
-            g = thin_attention_backward(Q, K, V, idx, dO.contiguous(), logw=logw,
+            g = thin_attention_backward(Q, K, V, idx, _laid_out(dO), logw=logw,
                                         need_logw=need_logw)
         return g[0], g[1], g[2], None, g[3] if need_logw else None, None
 
@@ -113,12 +120,11 @@ def coreset_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, idx: to
     """thin_attention that autograd records, on the current stream: gradients reach Q, K, V
     (zeros in the rows that idx does not list) and logw by thin_attention_backward, once (the
     gradient of a gradient is refused).  The choice of the rows, idx, has none.  Strided inputs
-    are laid out contiguously first."""
+    are laid out contiguously first, and so are rows that are not 16-byte aligned."""
     dev, _ = _where(None)
     for t, name in ((Q, "Q"), (K, "K"), (V, "V"), (idx, "idx"), (logw, "logw")):
         if t is not None:
             _on(t, dev, name)
     _dtype(Q, "Q")
-    return _CoresetAttention.apply(Q.contiguous(), K.contiguous(), V.contiguous(),
-                                   idx.contiguous(), None if logw is None else logw.contiguous(),
-                                   out_dtype)
+    return _CoresetAttention.apply(_laid_out(Q), _laid_out(K), _laid_out(V), idx.contiguous(),
+                                   None if logw is None else logw.contiguous(), out_dtype)

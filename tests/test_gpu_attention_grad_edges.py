@@ -1,4 +1,4 @@
-"""Coreset attention and its gradient as a pair: lists that leave the rows."""
+"""Coreset attention and its gradient as a pair: lists that leave the rows, views at any offset."""
 import math
 
 import pytest
@@ -6,7 +6,7 @@ import torch
 
 import attention_grad_reference as ref
 from paper_2606_10944_amd import coreset_attention, thin_attention
-from test_gpu_attention_grad import DEV, NAMES, backward, check, gen, inputs, to
+from test_gpu_attention_grad import NAMES, backward, check, gen, inputs, to
 
 pytestmark = pytest.mark.gpu
 TYPES = [("bf16", "bf16"), ("bf16", "fp32"), ("fp32", "fp32"), ("fp32", "bf16")]
@@ -113,3 +113,51 @@ def test_keys_without_weight_hold_anything(n_out, dtype):
     got = backward(Q, K, V, idx, logw, dO)
     check((Q, K, V, near, logw, dO), got)
     assert (got[0][0, 1] == 0).all() and (got[3][0, 1] == 0).all()
+
+
+# ---------------------------------------------------------------------------
+# Views whose rows are not 16-byte aligned, through autograd
+# ---------------------------------------------------------------------------
+def at_offset(t, elements):
+    """t's values, contiguous, `elements` into a buffer of their own."""
+    flat = torch.empty(t.numel() + elements, dtype=t.dtype, device=t.device)
+    flat[elements:] = t.flatten()
+    view = flat[elements:].view(t.shape)
+    assert view.is_contiguous() and view.data_ptr() % 16 == elements * t.element_size() % 16
+    return view
+
+
+@pytest.mark.parametrize("n_out", [30, 290])
+@pytest.mark.parametrize("dtype,out", TYPES)
+def test_gradient_that_arrives_at_an_offset(n_out, dtype, out):
+    """The gradient of a concatenation is a view into that of the whole: here one element in."""
+    g = gen(303)
+    args = inputs(g, 1, 2, 45, 400, n_out, 64, dtype, out, weighted=True)
+    Q, K, V, idx, logw, dO = (to(x) for x in args)
+    leaves = [x.requires_grad_() for x in (Q, K, V, logw)]
+    O = coreset_attention(Q, K, V, idx, logw=logw, out_dtype=dO.dtype)
+    one = torch.ones(1, dtype=dO.dtype, device=dO.device)
+    torch.cat((one, O.flatten())).backward(torch.cat((one, dO.flatten())))
+    for x, want in zip(leaves, backward(*args)):
+        assert torch.equal(x.grad, want)
+    check(args, [x.grad for x in leaves])
+
+
+@pytest.mark.parametrize("n_out", [30, 290])
+@pytest.mark.parametrize("dtype,offset", [("bf16", 1), ("bf16", 2), ("bf16", 4), ("fp32", 1),
+                                          ("fp32", 2), ("fp32", 3)])
+def test_rows_at_an_offset(n_out, dtype, offset):
+    """Queries, keys and values out of flat buffers: the output and gradients of aligned ones."""
+    g = gen(304)
+    args = inputs(g, 1, 2, 45, 400, n_out, 64, dtype, dtype, weighted=True)
+    Q, K, V, idx, logw, dO = (to(x) for x in args)
+    want = coreset_attention(Q, K, V, idx, logw=logw)
+    leaves = [at_offset(x, offset).requires_grad_() for x in (Q, K, V)] \
+        + [logw.clone().requires_grad_()]
+    O = coreset_attention(*leaves[:3], idx, logw=leaves[3])
+    assert torch.equal(O, want)
+    O.backward(dO.float())
+    exact = args[:5] + (args[5].float(),)
+    for x, grad in zip(leaves, backward(*exact)):
+        assert torch.equal(x.grad, grad)
+    check(exact, [x.grad for x in leaves])
