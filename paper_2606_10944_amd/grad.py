@@ -8,7 +8,7 @@ from typing import Optional
 
 import torch
 
-from ._lib import THIN_EDTYPE, THIN_EINVAL, ThinError, _check, lib, thin_attention
+from ._lib import THIN_EDTYPE, THIN_EINVAL, ThinError, _check, _shape4, lib, thin_attention
 from .q4 import _dtype, _empty, _empty_like, _on, _where, _workspace
 
 
@@ -120,11 +120,18 @@ def coreset_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, idx: to
     """thin_attention that autograd records, on the current stream: gradients reach Q, K, V
     (zeros in the rows that idx does not list) and logw by thin_attention_backward, once (the
     gradient of a gradient is refused).  The choice of the rows, idx, has none.  Strided inputs
-    are laid out contiguously first, and so are rows that are not 16-byte aligned."""
+    are laid out contiguously first, and so are rows that are not 16-byte aligned.  Where a
+    gradient is asked for, sizes that thin_attention_backward does not take are refused here."""
     dev, _ = _where(None)
     for t, name in ((Q, "Q"), (K, "K"), (V, "V"), (idx, "idx"), (logw, "logw")):
         if t is not None:
             _on(t, dev, name)
-    _dtype(Q, "Q")
-    return _CoresetAttention.apply(_laid_out(Q), _laid_out(K), _laid_out(V), idx.contiguous(),
-                                   None if logw is None else logw.contiguous(), out_dtype)
+    code = _dtype(Q, "Q")
+    recorded = torch.is_grad_enabled() and any(
+        t is not None and t.requires_grad for t in (Q, K, V, logw))
+    Q, K, V, idx = _laid_out(Q), _laid_out(K), _laid_out(V), idx.contiguous()
+    if recorded:
+        B, H, n_q, d = _shape4(Q, "Q")
+        _bytes(code, B, H, n_q, _shape4(K, "K")[2], d, idx.shape[2] if idx.dim() == 3 else 0)
+    return _CoresetAttention.apply(Q, K, V, idx, None if logw is None else logw.contiguous(),
+                                   out_dtype)

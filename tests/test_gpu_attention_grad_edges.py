@@ -1,12 +1,13 @@
-"""Coreset attention and its gradient as a pair: lists that leave the rows, views at any offset."""
+"""Coreset attention and its gradient as a pair: lists that leave the rows, views at any offset,
+sizes that one of them has not."""
 import math
 
 import pytest
 import torch
 
 import attention_grad_reference as ref
-from paper_2606_10944_amd import coreset_attention, thin_attention
-from test_gpu_attention_grad import NAMES, backward, check, gen, inputs, to
+from paper_2606_10944_amd import THIN_EINVAL, ThinError, coreset_attention, thin_attention
+from test_gpu_attention_grad import DEV, NAMES, backward, check, gen, inputs, to
 
 pytestmark = pytest.mark.gpu
 TYPES = [("bf16", "bf16"), ("bf16", "fp32"), ("fp32", "fp32"), ("fp32", "bf16")]
@@ -161,3 +162,34 @@ def test_rows_at_an_offset(n_out, dtype, offset):
     for x, grad in zip(leaves, backward(*exact)):
         assert torch.equal(x.grad, grad)
     check(exact, [x.grad for x in leaves])
+
+
+# ---------------------------------------------------------------------------
+# Sizes that the output has and its gradient has not
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("H,n_out", [(1, (1 << 18) + 1), (256, (1 << 17) + 1)])
+@pytest.mark.parametrize("which", ["Q", "K", "V", "logw"])
+def test_sizes_without_a_gradient_are_refused_at_once(H, n_out, which):
+    g = gen(305)
+    x = {k: torch.randn(1, H, 2, 32, generator=g).to(DEV) for k in "QKV"}
+    x["logw"] = torch.zeros(1, H, n_out, device=DEV)
+    idx = torch.zeros(1, H, n_out, dtype=torch.int32, device=DEV)
+    x[which].requires_grad_()
+    with pytest.raises(ThinError) as e:
+        coreset_attention(x["Q"], x["K"], x["V"], idx, logw=x["logw"])
+    assert e.value.status == THIN_EINVAL
+
+
+def test_sizes_without_a_gradient_have_an_output():
+    """Nothing is recorded where nothing asks for a gradient: one row, listed 2^18 + 1 times."""
+    g = gen(306)
+    n_out = (1 << 18) + 1
+    Q, K, V = (torch.randn(1, 1, r, 32, generator=g).to(DEV) for r in (3, 1, 1))
+    idx = torch.zeros(1, 1, n_out, dtype=torch.int32, device=DEV)
+    leaf = Q.clone().requires_grad_()
+    with torch.no_grad():
+        a = coreset_attention(leaf, K, V, idx)
+    for O in (a, coreset_attention(Q, K, V, idx)):
+        # equal weights: sums of n_out terms over their number, each off by n_out 2^-24 at most
+        assert ((O - V).abs() <= 2 * n_out * 2.0 ** -24 * V.abs()).all()
+        assert not O.requires_grad
