@@ -1,11 +1,12 @@
 """Coreset attention and its gradient as a pair: lists that leave the rows, views at any offset,
-sizes that one of them has not."""
+sizes that one of them has not, and launch shapes beside those of the other tests."""
 import math
 
 import pytest
 import torch
 
 import attention_grad_reference as ref
+import test_gpu_attention_grad as grad
 from paper_2606_10944_amd import THIN_EINVAL, ThinError, coreset_attention, thin_attention
 from test_gpu_attention_grad import DEV, NAMES, backward, check, gen, inputs, to
 
@@ -193,3 +194,27 @@ def test_sizes_without_a_gradient_have_an_output():
         # equal weights: sums of n_out terms over their number, each off by n_out 2^-24 at most
         assert ((O - V).abs() <= 2 * n_out * 2.0 ** -24 * V.abs()).all()
         assert not O.requires_grad
+
+
+# ---------------------------------------------------------------------------
+# Launch shapes
+# ---------------------------------------------------------------------------
+SHAPES = [
+    # B, H, n_q, n, n_out, d: 65 to 128 keys of 32 channels, four waves per row of the join
+    (1, 2, 70, 200, 65, 32), (2, 1, 97, 150, 100, 32), (1, 1, 33, 128, 128, 32),
+    (1, 1, 5000, 64, 48, 32),
+    # one wave and two waves per tile of rows
+    (33, 8, 20, 260, 257, 32), (33, 8, 20, 260, 257, 64), (33, 8, 20, 260, 257, 128),
+    (16, 4, 200, 300, 260, 32), (16, 4, 200, 300, 260, 64), (32, 2, 193, 290, 288, 128),
+]
+
+
+@pytest.mark.parametrize("dtype,out", TYPES)
+@pytest.mark.parametrize("B,H,n_q,n,n_out,d", SHAPES)
+def test_gradient(B, H, n_q, n, n_out, d, dtype, out):
+    grad.test_gradient(B, H, n_q, n, n_out, d, dtype, out)
+
+
+@pytest.mark.parametrize("B,H,n_q,n,n_out,d", SHAPES)
+def test_gradient_without_that_of_the_weights(B, H, n_q, n, n_out, d):
+    grad.test_gradient_without_that_of_the_weights(B, H, n_q, n, n_out, d)
