@@ -645,6 +645,8 @@ int thin_q4_tree_attention(const thin_q4_cache_t* cache, const void* Q, const in
  *   path    (device) int32 [B, P], 1 <= P <= THIN_Q4_MAX_DRAFTS.  The first entry that is
  *           negative, or whose row or new place lies outside the cache, ends the path (at[b] <
  *           0: at once).
+ *           A draft that was padding when the drafts were stored (t >= count[b]) has no row of
+ *           its own: a path that names it keeps whatever the cache held there.
  *   end     (device) int32 [B]: at[b] + the number of rows kept, where the next tokens go.  It
  *           overlaps neither at nor path.
  * Rows behind the last one kept hold what they held.  Errors: THIN_EINVAL, THIN_EHIP.

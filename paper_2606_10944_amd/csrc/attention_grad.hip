@@ -5,20 +5,28 @@
 // Probabilities are formed anew from the queries and keys; the sum p g of a row too, so
 // neither the forward's output nor its statistics are read.
 //
-// Up to 256 coreset rows (float32: 128) a workgroup holds every key of a slice, 16 or 32 per
-// wave, and walks a range of its queries, 32 at a time: one launch reads Q and dO once and
-// writes dQ, and the sums of dK and dV stay in registers.  Wider coresets take a launch that
-// owns query rows (statistics, then dQ), and the same walk per chunk of keys for dK and dV.
+// Up to 256 coreset rows (float32: 128; bf16 with all of a float32 dO: 192 of 128 channels) a
+// workgroup holds every key of a slice, 16 to 64 per wave, and walks a range of its queries, 32 at
+// a time (16 of float32 rows over up to 32 keys): one launch reads Q and dO once and writes dQ,
+// and the sums of dK and dV stay in registers.  Wider coresets take a launch that owns query rows
+// (statistics, then dQ), and the same walk per chunk of keys for dK and dV.
 // Workgroups leave their sums of dK and dV for the join, which adds them in order.  Rows off the
 // coreset are zeros that the walk writes beside its own work, or a launch of their own.
 //
-// 64 slices of 16384 queries over 192 keys, d = 128, bf16: 460 to 500 us, 555 TFLOP/s at 10 d per
-// (query, key), 2.9 TB/s; the walk takes 445 of it, the join 16.  The matrix cores are busy for
-// 20 % of the walk, the vector ALU 34 %, LDS 50 % (a fifth of that conflicts): without the traffic
-// with HBM it takes 284 us of 360 (128 keys), without that and the products 200, which the row
-// statistics' way through LDS, that of p and ds, and three barriers per 32 queries are.
-// Over 128 keys 350 us; 32 slices of 32768 over 256 keys 530.  The smallest calls are two dependent
-// launches, 6 + 5 us, behind 14 us of host time.
+// 64 slices of 16384 queries over 192 keys, d = 128, bf16: 470 to 500 us, 550 TFLOP/s at 10 d per
+// (query, key), 2.9 TB/s; the walk takes 450 of it, the join 16.  The matrix cores are busy for
+// 26 % of the cycles that the walk's waves live, the vector ALU 42 %, LDS 50 % (conflicts 1 %):
+// a wave owns 16 keys alone, so twelve of them read Q and dO from LDS, by rows and by columns, for
+// few products each, and 8 of the 12 have units of dQ.  Without the traffic with HBM it takes 284
+// us of 360 (128 keys), without that and the products 200: the row statistics' way through LDS,
+// that of p and ds, and two barriers per 32 queries.  Over 128 keys 350 us; 32 slices of 32768 over
+// 256 keys 520.  float32 rows over 512 keys (16 slices of 2048) 345 us, the matrix cores busy for 75
+// and 78 % of the two large launches, which form scores and g three times.  The smallest calls are
+// two dependent launches, 6 + 5 us, behind 14 us of host time.
+//
+// Registers.  Waves of 32 and 64 keys leave some in scratch: bytes per lane for dO of bf16, of
+// float32, and of float32 with dlogw: d = 32 2 x 4 0, 40, 40, 4 x 4 68, 84, 80; d = 64 8 x 2 36, 20,
+// 28; d = 128 8 x 2 8, 48.  The other shapes that were measured there are slower (see grad_shape).
 //
 // Types.  bf16 rows: bf16 products summed in float32; p and ds round to bf16 (half a step, as
 // the gradients' own rounding) for the products over queries and over keys; a float32 dO is
@@ -500,7 +508,7 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
                 (uint32_t)((16 * tile_of(u) + m) * D + 16 * (dt0 + y) + 4 * g) * Elem<T>::bytes);
   };
 
-  // scores to base 2 and g of keys 4 g + j, query 16 tq + m
+  // scores (of bf16 rows to base 2, of float32 to e) and g of keys 4 g + j, query 16 tq + m
   auto scores = [&](int buf, float (&p)[KT][TQ][4], float (&gd)[KT][TQ][4])
                     __attribute__((always_inline)) {
     floatx4_t x[KT][TQ], y[KT][TQ];
@@ -762,8 +770,10 @@ __global__ __launch_bounds__(64 * W, W > 8 ? W / 4 : 2) void grad_keys_kernel(Gr
 // of query m.
 //
 // 15 slices of 2047 queries over 333 keys, d = 128, bf16 with a float32 dO: 39 us, the matrix
-// cores busy for 25 % of it, LDS 22 %, the vector ALU 29 %: the rest are a step's latencies, two
-// waves per SIMD that meet at a barrier every 64 keys.
+// cores busy for 30 % of the waves' cycles, LDS 27 %, the vector ALU 37 %: the rest are a step's
+// latencies, two waves per SIMD that meet at a barrier every 64 keys.  About half of it is the
+// second pass, which forms scores and g again: up to a few hundred keys they could stay in
+// registers between the passes, which has not been tried.
 // ---------------------------------------------------------------------------
 constexpr int RW = 8;  // waves
 

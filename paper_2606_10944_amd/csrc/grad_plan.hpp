@@ -11,7 +11,8 @@ namespace thin {
 // Query rows per step of a workgroup: 32, which the bf16 instruction sums over at a time; float32
 // rows of few keys 16, so that the tiles in LDS leave room for several workgroups (40 slices of
 // 14251 queries over 2 keys of 128 channels 507 -> 272 us; over 128 keys of 64 channels 16 take
-// 239 us where 32 take 214).
+// 239 us where 32 take 214; not measured at 33 to 64 keys of 128 channels, where 32 queries take
+// 115,200 bytes and leave one workgroup per compute unit, 16 slices of 4096 over 48 keys 78 us).
 constexpr int64_t grad_tile(bool bf16, int64_t waves) { return bf16 || waves > 2 ? 32 : 16; }
 
 struct GradShape {
@@ -62,6 +63,9 @@ inline GradShape grad_shape(int64_t S, int64_t n_q, int64_t n_out, int64_t d, bo
     bf16 && d < 128 ? is(8, 2) : is(8, 1);
   s.chunks = (int32_t)((n_out + s.keys() - 1) / s.keys());
   const int64_t tile = grad_tile(bf16, s.waves), steps = (n_q + tile - 1) / tile;
+  // (By waves alone.  At 128 channels LDS holds fewer: of float32 rows or a float32 dO two
+  // workgroups of two waves instead of four, of float32 rows one of four waves instead of two; the
+  // others wait for these.)
   const int64_t slots = s.waves > 8 ? 256 : 256 * (8 / s.waves);
   const StepSplit p = split_steps(S * s.chunks, steps, slots, 2.0, 1.0);
   s.parts = (int32_t)p.parts;

@@ -207,9 +207,9 @@ __global__ __launch_bounds__(THREADS) void q4_load_kernel(Q4View c, const int32_
 // that it also writes.
 //
 // 8 x 8 slices, 7 of 64 drafts kept, d = 128: 4.8 us, a chain of the path, its rows and the
-// block's older rows.  64 x 8 slices, 500 of 1024: 22 us for 70 MB (3.2 TB/s; 28 with one workgroup
-// for keys and values); a workgroup's rows all wait for the path, and its blocks' bounds are formed
-// in turn.
+// block's older rows.  64 x 8 slices, 500 of 1024: 21 us for 70 MB (3.3 TB/s; 28 with one workgroup
+// for keys and values), 24 where other caches were worked on in between; a workgroup's rows all
+// wait for the path, and its blocks' bounds are formed in turn, two barriers each.
 // ---------------------------------------------------------------------------
 template <int D, int CAP>
 __global__ __launch_bounds__(THREADS) void q4_keep_kernel(Q4View c, const int32_t* at_,

@@ -18,8 +18,11 @@
 // Trees: the tiles of rows before the drafts need no mask; the drafts' own tiles take a bit of a
 // word each.  Several trees share out their keys by the sequences' lengths, as the kernel for few
 // rows does.  8 trees of 64 drafts behind 3000 to 65536 rows, the same heads: 320 us and 11 for the
-// join (482 shared out by the longest), 0.79 PFLOP/s; 1021 drafts behind 16384 rows 261 and 13.6.
-// The matrix cores are busy for 35 to 40 % of it.  Plain prompts keep the code they had.
+// join (482 shared out by the longest), 0.78 PFLOP/s; 1021 drafts behind 16384 rows 261 and 13.5;
+// float32 798 and 581 us in all.  Of the first the matrix cores are busy for 43 % of the waves'
+// cycles, the vector ALU 47 %; a share ends with its sequence, so the longest take 153 steps where
+// an even share of all sequences' steps would be 134, a seventh less.  Plain prompts keep the code
+// they had.
 #include "q4_attn_device.hpp"
 
 namespace thin {

@@ -119,7 +119,8 @@ def coreset_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, idx: to
                       out_dtype: torch.dtype = torch.float32) -> torch.Tensor:
     """thin_attention that autograd records, on the current stream: gradients reach Q, K, V
     (zeros in the rows that idx does not list) and logw by thin_attention_backward, once (the
-    gradient of a gradient is refused).  The choice of the rows, idx, has none.  Strided inputs
+    gradient of a gradient is refused).  The choice of the rows, idx, has none.  A step that is
+    captured into a graph calls thin_attention and thin_attention_backward itself.  Strided inputs
     are laid out contiguously first, and so are rows that are not 16-byte aligned.  Where a
     gradient is asked for, sizes that thin_attention_backward does not take are refused here."""
     dev, _ = _where(None)

@@ -528,8 +528,9 @@ def thin_q4_tree_attention(Q: torch.Tensor, cache: Q4Cache, at: torch.Tensor, se
 def thin_q4_keep(cache: Q4Cache, at: torch.Tensor, path: torch.Tensor, *,
                  end: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Rows at[b] + path[b,i] of the cache become rows at[b] + i (path int32 [B,P], P <= 1024,
-    an accepted path of drafts, the first negative entry behind its last).  Returns end int32
-    [B], the rows that every sequence then has: the next call's `at`."""
+    an accepted path of drafts, the first negative entry behind its last; padding, drafts t >=
+    count[b], is not for a path: its rows were never stored).  Returns end int32 [B], the rows
+    that every sequence then has: the next call's `at`."""
     dev, st = _where(stream)
     ref = cache._at(dev)
     if path.dim() != 2:
